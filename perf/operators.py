@@ -291,7 +291,7 @@ def _prepare_list(case, g):
     if case["kind"] == "clip":
         if not case["active"]:
             s["max_norm"] *= 4
-        s["clipped"] = [torch.empty_like(x) for x in s["grads"]]
+        s["clipped"] = [torch.zeros_like(x) for x in s["grads"]]
     if case["kind"] == "adam":
         (_, total, places), = s["groups"]
         s["param"] = _flat(total, places, TYPES[case["param"]], randn(0.02))
