@@ -693,6 +693,155 @@ int dora_step_rewards(const float* cost, const int32_t* removals, const int32_t*
                       int32_t n_blocks, int32_t batch, int32_t depth, int32_t n0, float a,
                       float* reward, float* ret, dora_stream_t stream);
 
+/*
+ * The policy update (App. D.2: clipped PPO; Table 4: Adam): from a rollout's
+ * actions to changed weights.  The entries below take 16- and 32-bit floats,
+ * named by: */
+enum dora_dtype { DORA_BF16 = 0, DORA_F16 = 1, DORA_F32 = 2 };
+
+/*
+ * dora_policy_loss -- the clipped policy loss of categorical actions, with KL
+ * and entropy terms, and its gradient with respect to the logits, in one
+ * launch.  For row r with legal logits z (the first n_r of the row), action a,
+ * l = z_a - log sum_j exp z_j, rho = exp(l - old_logp), x = ref_logp - l,
+ * p = softmax(z), H = -sum_j p_j log p_j:
+ *   row_loss = w [ -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *                  + kl_coef (exp x - 1 - x) - entropy_coef H ],
+ *   grad_j   = g (1(j = a) - p_j) + w entropy_coef p_j (log p_j + H),
+ *   g        = w [ -rho A (rho A <= clip(rho) A) + kl_coef (1 - exp x) ].
+ * logits     [rows, ld] of `dtype` (dora_dtype), ld >= classes >= 1, aligned to
+ *            its elements (rows may start at any alignment).
+ * legal      nullable int32 [rows]: n_r, the legal actions come first (the
+ *            budget grid's feasible counts do); logits past them are not read.
+ *            NULL = classes.
+ * actions    int32 [rows]; a negative one means that the row has none.
+ * old_logp   fp32 [rows], the log-probability when the action was taken;
+ * ref_logp   nullable fp32 [rows], under the reference policy (required when
+ *            kl_coef != 0; with it NULL the KL term is 0);
+ * advantages fp32 [rows]; weights nullable fp32 [rows] (NULL = 1): w, e.g. one
+ *            over the number of actions, 0 for padding.
+ * A row without an action or of weight 0 takes no part: its logits are not
+ * read, its outputs and gradient are 0.  An action at or past n_r, or n_r
+ * outside [0, classes], gives NaN outputs and gradients for the row (and NaN
+ * totals) and DORA_ERR_DEVICE_BAD_COUNT.  Logits of -inf are actions of
+ * probability 0; NaN, +inf, or a row of -inf alone make the row NaN.
+ * clip_low in [0, 1], clip_high >= 0.
+ * logp       out fp32 [rows]: l.  entropy nullable out fp32 [rows]: H.
+ * row_loss   nullable out fp32 [rows].
+ * grad       nullable out [rows, ld] of `dtype`: columns [0, classes) are
+ *            written, 0 past n_r; grad == logits is allowed.
+ * totals     nullable out fp32 [6], sums over the rows that take part: row_loss;
+ *            w times the clipped policy term, the KL term and H; the weight of
+ *            the rows whose gradient the clipping removed; the weight.
+ * workspace  dora_policy_workspace_size() bytes, 256-byte aligned, zero-filled
+ *            once after allocation; needed with totals only.  Calls that share
+ *            it are ordered on one stream.
+ * Statistics and gradients are computed in fp32 and rounded once; the totals
+ * are summed in a fixed order (same inputs, same bits).
+ */
+size_t dora_policy_workspace_size(void);
+int dora_policy_loss(const void* logits, int32_t dtype, int32_t rows, int32_t classes, int64_t ld,
+                     const int32_t* legal, const int32_t* actions, const float* old_logp,
+                     const float* ref_logp, const float* advantages, const float* weights,
+                     float clip_low, float clip_high, float kl_coef, float entropy_coef,
+                     float* logp, float* entropy, float* row_loss, void* grad, float* totals,
+                     void* workspace, size_t workspace_bytes, int32_t* status,
+                     dora_stream_t stream);
+
+/*
+ * dora_pl_policy_loss -- the same loss of each image's ordered removal
+ * sequence, l its Plackett-Luce log-probability (dora_pl_logprob; scores, cu,
+ * k, order as there), and its gradient with respect to the scores, in one
+ * launch.  old_logp, ref_logp, advantages, weights, the coefficients, logp,
+ * row_loss, totals and the workspace as in dora_policy_loss, per image; no
+ * entropy term (totals[3] is 0).  grad nullable fp32 [t_cap]: every row of
+ * every image is written (CLS rows 0).  An image with k = 0 (its gate is
+ * closed) or weight 0 takes no part.  Device errors as in dora_pl_logprob: a
+ * repeated or out-of-range entry makes the image NaN.  l is summed in fp64, so
+ * that the ratio of a long sequence keeps its digits.
+ */
+int dora_pl_policy_loss(const float* scores, const int32_t* cu, int32_t batch, int32_t t_cap,
+                        const int32_t* k, const int32_t* order, int32_t k_cap,
+                        const float* old_logp, const float* ref_logp, const float* advantages,
+                        const float* weights, float clip_low, float clip_high, float kl_coef,
+                        float* logp, float* row_loss, float* grad, float* totals, void* workspace,
+                        size_t workspace_bytes, int32_t* status, dora_stream_t stream);
+
+/*
+ * A list of tensors that are updated together.  dora_param (host): one
+ * contiguous tensor of n elements, its gradient (grad_dtype), and, nullable,
+ *   clipped     where dora_clip_grads writes (grad_dtype; NULL = in place);
+ *   param, exp_avg, exp_avg_sq   weights (param_dtype) and fp32 moments of
+ *               dora_adam_step, all three or none;
+ *   copy        bf16 [n]: the updated weights, rounded (what a forward in bf16
+ *               reads when param is an fp32 master).
+ * Pointers are aligned to their elements; 16-byte alignment is faster.  No two
+ * tensors overlap.
+ * dora_param_list_prepare writes the list into `data` (device,
+ * dora_param_list_size bytes, 256-byte aligned) and fills the host handle
+ * *list, which the calls below take; done once for a set of buffers.  The
+ * list's memory also holds the calls' partial sums: calls on one list are
+ * ordered on one stream.  dora_param_list_size is 0 for arguments that prepare
+ * refuses.
+ */
+typedef struct dora_param {
+  const void* grad;
+  void* clipped;
+  void* param;
+  float* exp_avg;
+  float* exp_avg_sq;
+  dora_bf16* copy;
+  int64_t n;
+  int32_t grad_dtype;
+  int32_t param_dtype;
+} dora_param;
+typedef struct dora_param_list {
+  void* data;
+  int64_t elements;
+  int32_t count;
+  int32_t spans;
+  int32_t has_params;   /* 1: every tensor has param, exp_avg and exp_avg_sq */
+} dora_param_list;
+size_t dora_param_list_size(const dora_param* params, int32_t count);
+int dora_param_list_prepare(const dora_param* params, int32_t count, void* data, size_t bytes,
+                            dora_param_list* list, dora_stream_t stream);
+
+/*
+ * dora_grad_norm -- norm fp32 [2] (device): norm[0] = the 2-norm N over all
+ * gradients of the list, norm[1] = min(1, max_norm / N) (1 when N is 0 or not
+ * finite).  max_norm >= 0 (infinity: no clipping).  Squares are summed without
+ * overflow or underflow for any finite gradients, in a fixed order.
+ */
+int dora_grad_norm(const dora_param_list* list, float max_norm, float* norm, dora_stream_t stream);
+
+/*
+ * dora_clip_grads -- dora_grad_norm, then every gradient times norm[1] (fp32
+ * product, one rounding), in place or into the tensor's `clipped`.  A norm that
+ * is not finite leaves the values as they are (`clipped` receives them).
+ */
+int dora_clip_grads(const dora_param_list* list, float max_norm, float* norm,
+                    dora_stream_t stream);
+
+/*
+ * dora_adam_step -- one Adam step on every tensor of the list, fp32
+ * arithmetic: with d = f grad, t the number of this step,
+ *   exp_avg    m <- beta1 m + (1 - beta1) d
+ *   exp_avg_sq v <- beta2 v + (1 - beta2) d^2
+ *   param      p <- p (1 - lr weight_decay)
+ *                   - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * clip nullable: the norm fp32 [2] of dora_grad_norm; f = clip[1], and a norm
+ * that is not finite skips the step (nothing changes, t does not advance).
+ * NULL: f = 1.  state: device, dora_adam_state_size() bytes, 16-byte aligned,
+ * zero-filled before the first step or set by dora_adam_init; its first 8 bytes
+ * are the int64 number of steps taken, and it counts on the device, so a
+ * captured step may be replayed.
+ * dora_adam_init -- the state after `step` steps with these betas (to resume).
+ */
+size_t dora_adam_state_size(void);
+int dora_adam_init(void* state, int64_t step, double beta1, double beta2, dora_stream_t stream);
+int dora_adam_step(const dora_param_list* list, void* state, double lr, double beta1, double beta2,
+                   double eps, double weight_decay, const float* clip, dora_stream_t stream);
+
 /* Synchronises the current device and copies the status word at `status_dev`
  * (a device int32, e.g. dora_workspace_status(ws)) to *code.  Test/debug
  * only: it blocks the host. */

@@ -637,3 +637,101 @@ def step_rewards(costs: np.ndarray, removals: np.ndarray, blocks, depth: int, n0
         prev = costs[j]
     return out
 
+
+
+def clipped_terms(logp: np.ndarray, old: np.ndarray, adv: np.ndarray, ref, low: float,
+                  high: float) -> tuple:
+    """(policy term, KL term, whether the clipping removed the gradient,
+    d policy / d logp, d KL / d logp) of actions: the clipped surrogate
+    -min(rho A, clip(rho, 1 - low, 1 + high) A), rho = exp(logp - old), and
+    exp x - 1 - x with x = ref - logp (0 without a reference)."""
+    rho = np.exp(logp - old)
+    cut = np.clip(rho, 1 - low, 1 + high) * adv
+    plain = rho * adv
+    clipped = plain > cut
+    if ref is None:
+        kl, dkl = np.zeros_like(logp), np.zeros_like(logp)
+    else:
+        kl, dkl = np.expm1(ref - logp) - (ref - logp), -np.expm1(ref - logp)
+    return -np.where(clipped, cut, plain), kl, clipped, -np.where(clipped, 0.0, plain), dkl
+
+
+def policy_loss(logits: np.ndarray, actions, old, adv, ref=None, weights=None, legal=None,
+                low: float = 0.2, high: float = 0.2, kl_coef: float = 0.0,
+                entropy_coef: float = 0.0) -> dict:
+    """Clipped policy loss of categorical actions, row by row, with its gradient
+    with respect to the logits: w [policy + kl_coef KL - entropy_coef H] over
+    the first legal[r] logits; rows with a negative action or weight 0 take no
+    part (everything 0)."""
+    rows, classes = logits.shape
+    out = {"logp": np.zeros(rows), "entropy": np.zeros(rows), "row_loss": np.zeros(rows),
+           "grad": np.zeros((rows, classes)), "totals": np.zeros(6)}
+    for r in range(rows):
+        w = 1.0 if weights is None else float(weights[r])
+        if actions[r] < 0 or w == 0:
+            continue
+        n = classes if legal is None else int(legal[r])
+        z = np.asarray(logits[r, :n], dtype=np.float64)
+        with np.errstate(divide="ignore"):
+            lq = z - _logsumexp(z)
+        p = np.exp(lq)
+        plogp = np.where(p > 0, p * np.where(p > 0, lq, 0.0), 0.0)
+        h = -plogp.sum()
+        lp = np.array([lq[actions[r]]])
+        pol, kl, clipped, dpol, dkl = clipped_terms(
+            lp, np.array([old[r]], dtype=np.float64), np.array([adv[r]], dtype=np.float64),
+            None if ref is None else np.array([ref[r]], dtype=np.float64), low, high)
+        g = w * (dpol[0] + kl_coef * dkl[0])
+        d = -g * p + w * entropy_coef * (plogp + p * h)
+        d[actions[r]] += g
+        out["logp"][r], out["entropy"][r] = lp[0], h
+        out["row_loss"][r] = w * (pol[0] + kl_coef * kl[0] - entropy_coef * h)
+        out["grad"][r, :n] = d
+        out["totals"] += [out["row_loss"][r], w * pol[0], w * kl[0], w * h, w * clipped[0], w]
+    return out
+
+
+def pl_policy_loss(scores: np.ndarray, cu, k, order, old, adv, ref=None, weights=None,
+                   low: float = 0.2, high: float = 0.2, kl_coef: float = 0.0) -> dict:
+    """policy_loss of each image's ordered removal sequence (pl_logprob), with
+    its gradient with respect to the scores; k = 0 takes no part."""
+    b = len(cu) - 1
+    out = {"logp": np.zeros(b), "row_loss": np.zeros(b), "grad": np.zeros(len(scores)),
+           "totals": np.zeros(6)}
+    for i in range(b):
+        w = 1.0 if weights is None else float(weights[i])
+        if k[i] == 0 or w == 0:
+            continue
+        s = np.asarray(scores[cu[i] + 1:cu[i + 1]], dtype=np.float64)
+        seq = order[i, :k[i]]
+        lp = np.array([pl_logprob(s, seq)])
+        pol, kl, clipped, dpol, dkl = clipped_terms(
+            lp, np.array([old[i]], dtype=np.float64), np.array([adv[i]], dtype=np.float64),
+            None if ref is None else np.array([ref[i]], dtype=np.float64), low, high)
+        g = w * (dpol[0] + kl_coef * dkl[0])
+        out["logp"][i] = lp[0]
+        out["row_loss"][i] = w * (pol[0] + kl_coef * kl[0])
+        out["grad"][cu[i] + 1:cu[i + 1]] = g * pl_logprob_grad(s, seq)
+        out["totals"] += [out["row_loss"][i], w * pol[0], w * kl[0], 0.0, w * clipped[0], w]
+    return out
+
+
+def grad_norm(grads: list, max_norm: float) -> tuple:
+    """(2-norm over all tensors, min(1, max_norm / norm)); the factor is 1 for a
+    norm that is 0 or not finite."""
+    peak = max([float(np.max(np.abs(g))) for g in grads if g.size] + [0.0])
+    if peak == 0 or not np.isfinite(peak):
+        return peak, 1.0
+    norm = peak * math.sqrt(sum(float(np.sum((g.astype(np.float64) / peak) ** 2)) for g in grads))
+    return norm, min(1.0, max_norm / norm)
+
+
+def adam_step(p: np.ndarray, m: np.ndarray, v: np.ndarray, grad: np.ndarray, step: int, lr: float,
+              beta1: float, beta2: float, eps: float, decay: float, factor: float = 1.0) -> tuple:
+    """(p, m, v) after Adam step number ``step`` (from 1) on factor * grad, with
+    decoupled weight decay."""
+    d = factor * grad
+    m = beta1 * m + (1 - beta1) * d
+    v = beta2 * v + (1 - beta2) * d * d
+    mh, vh = m / (1 - beta1 ** step), v / (1 - beta2 ** step)
+    return p * (1 - lr * decay) - lr * mh / (np.sqrt(vh) + eps), m, v

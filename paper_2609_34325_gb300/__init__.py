@@ -26,6 +26,9 @@ __all__ = [
     "alloc_actor_workspace", "dora_pruned_block_actor", "dora_patch_embed",
     "dora_classifier_head", "dora_classifier_head_lc1", "dora_fold_layerscale",
     "dora_pl_sample", "dora_pl_logprob", "dora_branch", "dora_kd_cost", "dora_step_rewards",
+    "dora_policy_loss", "dora_pl_policy_loss", "dora_policy_workspace_size",
+    "alloc_policy_workspace", "ParamList", "dora_grad_norm", "dora_clip_grads",
+    "dora_adam_step", "dora_adam_init", "alloc_adam_state",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -38,6 +41,8 @@ NOALLOC_SCRATCH_BYTES = 32 << 20
 _Tensor = torch.Tensor
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _vp, _i32, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+_i64, _f64 = ctypes.c_int64, ctypes.c_double
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # enum dora_dtype
 _SIGS = {
     "dora_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "dora_version": (ctypes.c_int, []),
@@ -98,6 +103,20 @@ _SIGS = {
                                                _vp, _vp, _vp, _vp, _vp, _sz, _vp, _i32, _vp, _vp,
                                                _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
                                                _vp]),
+    "dora_policy_workspace_size": (_sz, []),
+    "dora_policy_loss": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                        _f32, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                        _vp, _vp]),
+    "dora_pl_policy_loss": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp,
+                                           _vp, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _sz,
+                                           _vp, _vp]),
+    "dora_param_list_size": (_sz, [_vp, _i32]),
+    "dora_param_list_prepare": (ctypes.c_int, [_vp, _i32, _vp, _sz, _vp, _vp]),
+    "dora_grad_norm": (ctypes.c_int, [_vp, _f32, _vp, _vp]),
+    "dora_clip_grads": (ctypes.c_int, [_vp, _f32, _vp, _vp]),
+    "dora_adam_state_size": (_sz, []),
+    "dora_adam_init": (ctypes.c_int, [_vp, _i64, _f64, _f64, _vp]),
+    "dora_adam_step": (ctypes.c_int, [_vp, _vp, _f64, _f64, _f64, _f64, _f64, _vp, _vp]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -855,3 +874,222 @@ def dora_step_rewards(cost, removals, blocks, depth, n0, a, reward, ret=None, st
         _check(code, "dora_step_rewards")
     return reward
 
+
+
+# ---------------------------------------------------------------------------
+# the policy update: clipped losses, gradient norm and clipping, Adam
+# ---------------------------------------------------------------------------
+
+def dora_policy_workspace_size() -> int:
+    return int(load_library().dora_policy_workspace_size())
+
+
+def alloc_policy_workspace(device=None) -> torch.Tensor:
+    """Zero-filled workspace of the policy losses; any number of rows."""
+    return torch.zeros(dora_policy_workspace_size(), dtype=torch.uint8, device=device or "cuda")
+
+
+def _rows(n, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must have {n} entries")
+
+
+def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None, grad=None,
+                     classes=None, legal=None, ref_logp=None, weights=None, clip_low=0.2,
+                     clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, entropy=None, row_loss=None,
+                     totals=None, status=None, stream=None):
+    """Clipped policy loss of categorical actions and d loss / d logits.
+
+    logits [R, ld] (bf16, fp16 or fp32; rows contiguous, any row stride), of
+    which the first ``classes`` columns count (all by default) and, with
+    ``legal`` (int32 [R]), the first legal[r] of row r.  ``grad`` (like logits,
+    or logits itself) receives the gradient; logp, entropy and row_loss fp32
+    [R]; totals fp32 [6] (sums of the loss, the policy, KL and entropy terms,
+    the clipped weight and the weight; needs ``workspace``)."""
+    dt = _DTYPES.get(logits.dtype) if isinstance(logits, _Tensor) and logits.is_cuda else None
+    if dt is None or logits.dim() != 2:
+        raise TypeError("logits must be a 2-D CUDA tensor of bf16, fp16 or fp32")
+    rows, cols = logits.shape
+    ld = logits.stride(0) if rows > 1 else cols
+    if (cols > 1 and logits.stride(1) != 1) or ld < cols:
+        raise TypeError("the rows of logits must be contiguous and not overlap")
+    classes = cols if classes is None else int(classes)
+    if not 1 <= classes <= cols:
+        raise ValueError("classes must be in [1, logits.shape[1]]")
+    if grad is not None and grad is not logits and not (
+            isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
+            grad.shape == logits.shape and grad.stride() == logits.stride()):
+        raise TypeError("grad must be like logits: device, type, shape and strides")
+    if not (actions.numel() == old_logp.numel() == advantages.numel() == logp.numel() == rows):
+        raise ValueError("actions, old_logp, advantages and logp must have one entry per row")
+    _rows(rows, legal=legal, ref_logp=ref_logp, weights=weights, entropy=entropy,
+          row_loss=row_loss)
+    if totals is not None and totals.numel() < 6:
+        raise ValueError("totals must hold 6 floats")
+    code = load_library().dora_policy_loss(
+        logits.data_ptr(), dt, rows, classes, ld, _opt(legal, _I32, "legal"),
+        _arg(actions, _I32, "actions"), _arg(old_logp, _F32, "old_logp"),
+        _opt(ref_logp, _F32, "ref_logp"), _arg(advantages, _F32, "advantages"),
+        _opt(weights, _F32, "weights"), clip_low, clip_high, kl_coef, entropy_coef,
+        _arg(logp, _F32, "logp"), _opt(entropy, _F32, "entropy"),
+        _opt(row_loss, _F32, "row_loss"), None if grad is None else grad.data_ptr(),
+        _opt(totals, _F32, "totals"), _opt(workspace, _U8, "workspace"),
+        0 if workspace is None else workspace.numel(), _opt(status, _I32, "status"),
+        _stream(stream))
+    if code:
+        _check(code, "dora_policy_loss")
+    return logp
+
+
+def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, workspace=None,
+                        grad=None, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
+                        kl_coef=0.0, row_loss=None, totals=None, status=None, stream=None):
+    """Clipped policy loss of the ordered removal sequences ``order`` (int32 [B,
+    k_cap], the first k[i] entries of image i) and d loss / d scores (``grad``,
+    row-aligned); the other arguments per image as in dora_policy_loss."""
+    s, c, kp = _arg(scores, _F32, "scores"), _arg(cu, _I32, "cu"), _arg(k, _I32, "k")
+    o, b = _arg(order, _I32, "order"), cu.numel() - 1
+    if order.dim() != 2 or order.size(0) != b:
+        raise ValueError("order must be [B, k_cap]")
+    if not (k.numel() == old_logp.numel() == advantages.numel() == logp.numel() == b):
+        raise ValueError("k, old_logp, advantages and logp must have one entry per image")
+    _rows(b, ref_logp=ref_logp, weights=weights, row_loss=row_loss)
+    if grad is not None and grad.numel() != scores.numel():
+        raise ValueError("grad must match scores")
+    if totals is not None and totals.numel() < 6:
+        raise ValueError("totals must hold 6 floats")
+    code = load_library().dora_pl_policy_loss(
+        s, c, b, scores.numel(), kp, o, order.size(1), _arg(old_logp, _F32, "old_logp"),
+        _opt(ref_logp, _F32, "ref_logp"), _arg(advantages, _F32, "advantages"),
+        _opt(weights, _F32, "weights"), clip_low, clip_high, kl_coef, _arg(logp, _F32, "logp"),
+        _opt(row_loss, _F32, "row_loss"), _opt(grad, _F32, "grad"), _opt(totals, _F32, "totals"),
+        _opt(workspace, _U8, "workspace"), 0 if workspace is None else workspace.numel(),
+        _opt(status, _I32, "status"), _stream(stream))
+    if code:
+        _check(code, "dora_pl_policy_loss")
+    return logp
+
+
+class _ParamC(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("grad", "clipped", "param", "exp_avg", "exp_avg_sq", "copy")] + [
+        ("n", _i64), ("grad_dtype", _i32), ("param_dtype", _i32)]
+
+
+class _ParamListC(ctypes.Structure):
+    _fields_ = [("data", _vp), ("elements", _i64), ("count", _i32), ("spans", _i32),
+                ("has_params", _i32)]
+
+
+class ParamList:
+    """Tensors that are updated together, laid out on the device once
+    (dora_param_list_prepare): gradients (bf16, fp16 or fp32, contiguous) and,
+    each a list of as many tensors or None, ``clipped`` (where dora_clip_grads
+    writes; None: in place), ``params`` with ``exp_avg`` and ``exp_avg_sq``
+    (fp32), and bf16 ``copies`` of the updated weights.  The tensors are kept
+    alive here; make a new list when any of them moves.  Calls on one list are
+    ordered on one stream."""
+
+    def __init__(self, grads, params=None, exp_avg=None, exp_avg_sq=None, copies=None,
+                 clipped=None, stream=None):
+        self.grads = list(grads)
+        n = len(self.grads)
+        if n == 0:
+            raise ValueError("a list needs at least one tensor")
+        if (params is None) != (exp_avg is None) or (params is None) != (exp_avg_sq is None):
+            raise ValueError("params, exp_avg and exp_avg_sq are given together")
+        if copies is not None and params is None:
+            raise ValueError("copies need params")
+        more = {"clipped": clipped, "params": params, "exp_avg": exp_avg,
+                "exp_avg_sq": exp_avg_sq, "copies": copies}
+        for name, ts in more.items():
+            ts = [None] * n if ts is None else list(ts)
+            if len(ts) != n:
+                raise ValueError(f"{name} must have as many tensors as grads")
+            setattr(self, name, ts)
+        c = (_ParamC * n)()
+        for i, g in enumerate(self.grads):
+            p = self.params[i]
+            for name, t, dtypes in (("grads", g, _DTYPES), ("clipped", self.clipped[i], (g.dtype,)),
+                                    ("params", p, _DTYPES), ("exp_avg", self.exp_avg[i], (_F32,)),
+                                    ("exp_avg_sq", self.exp_avg_sq[i], (_F32,)),
+                                    ("copies", self.copies[i], (_BF16,))):
+                if t is None and more.get(name, grads) is None:
+                    continue
+                if not isinstance(t, _Tensor) or not t.is_cuda or t.dtype not in dtypes or \
+                        not t.is_contiguous():
+                    raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor of "
+                                    f"{', '.join(map(str, dtypes))}")
+                if t.numel() != g.numel() or t.device != self.grads[0].device:
+                    raise ValueError(f"{name}[{i}] must match grads[{i}] in size and device")
+            c[i] = _ParamC(_ptr(g), _ptr(self.clipped[i]), _ptr(p), _ptr(self.exp_avg[i]),
+                           _ptr(self.exp_avg_sq[i]), _ptr(self.copies[i]), g.numel(),
+                           _DTYPES[g.dtype], 2 if p is None else _DTYPES[p.dtype])
+        size = int(load_library().dora_param_list_size(c, n))
+        self.data = torch.empty(size, dtype=torch.uint8, device=self.grads[0].device)
+        self.c = _ParamListC()
+        self.ref = ctypes.byref(self.c)
+        _check(load_library().dora_param_list_prepare(c, n, _ptr(self.data), size, self.ref,
+                                                      _stream(stream)), "dora_param_list_prepare")
+
+
+def _list(plist):
+    if not isinstance(plist, ParamList):
+        raise TypeError("a ParamList is required")
+    return plist.ref
+
+
+def dora_grad_norm(plist, max_norm, norm, stream=None):
+    """norm (fp32 [2]): the 2-norm over all gradients of the list and the factor
+    min(1, max_norm / norm) (1 when the norm is not finite)."""
+    n = _arg(norm, _F32, "norm")
+    if norm.numel() < 2:
+        raise ValueError("norm must hold 2 floats")
+    code = load_library().dora_grad_norm(_list(plist), max_norm, n, _stream(stream))
+    if code:
+        _check(code, "dora_grad_norm")
+    return norm
+
+
+def dora_clip_grads(plist, max_norm, norm, stream=None):
+    """dora_grad_norm, then the gradients times the factor: in place, or into the
+    list's ``clipped``."""
+    n = _arg(norm, _F32, "norm")
+    if norm.numel() < 2:
+        raise ValueError("norm must hold 2 floats")
+    code = load_library().dora_clip_grads(_list(plist), max_norm, n, _stream(stream))
+    if code:
+        _check(code, "dora_clip_grads")
+    return norm
+
+
+def dora_adam_init(state, step=0, beta1=0.9, beta2=0.999, stream=None):
+    """The Adam state (uint8) after ``step`` steps with these betas."""
+    s = _arg(state, _U8, "state")
+    if state.numel() < int(load_library().dora_adam_state_size()):
+        raise ValueError("state is too small")
+    _check(load_library().dora_adam_init(s, int(step), float(beta1), float(beta2),
+                                         _stream(stream)), "dora_adam_init")
+    return state
+
+
+def alloc_adam_state(device=None, step=0, beta1=0.9, beta2=0.999, stream=None) -> torch.Tensor:
+    """Device state of dora_adam_step; ``state[:8].view(torch.int64)`` is the
+    number of steps taken."""
+    n = int(load_library().dora_adam_state_size())
+    return dora_adam_init(torch.empty(n, dtype=torch.uint8, device=device or "cuda"), step, beta1,
+                          beta2, stream)
+
+
+def dora_adam_step(plist, state, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0,
+                   clip=None, stream=None):
+    """One Adam step (decoupled weight decay) on every tensor of the list; with
+    ``clip``, the norm of dora_grad_norm, on the clipped gradients, and no step
+    at all when that norm is not finite."""
+    s = _arg(state, _U8, "state")
+    if state.numel() < 64 or (clip is not None and clip.numel() < 2):
+        raise ValueError("state must hold dora_adam_state_size() bytes and clip 2 floats")
+    code = load_library().dora_adam_step(_list(plist), s, lr, beta1, beta2, eps, weight_decay,
+                                         _opt(clip, _F32, "clip"), _stream(stream))
+    if code:
+        _check(code, "dora_adam_step")
