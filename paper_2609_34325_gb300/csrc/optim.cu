@@ -13,6 +13,7 @@
 
 #include "dora.h"
 #include "dora_ptx.cuh"
+#include "granule.cuh"
 #include "token_ops.cuh"
 
 namespace dora {
@@ -105,72 +106,6 @@ __device__ __forceinline__ void for_pieces(const List& list, int span, F f) {
   }
 }
 
-// 16 bytes of elements of T.
-template <typename T>
-struct Granule;
-template <>
-struct Granule<float> {
-  static constexpr int kElems = 4;
-  static __device__ __forceinline__ void unpack(uint4 q, float* v) {
-    v[0] = __uint_as_float(q.x);
-    v[1] = __uint_as_float(q.y);
-    v[2] = __uint_as_float(q.z);
-    v[3] = __uint_as_float(q.w);
-  }
-  static __device__ __forceinline__ uint4 pack(const float* v) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                      __float_as_uint(v[3]));
-  }
-};
-template <>
-struct Granule<__nv_bfloat16> {
-  static constexpr int kElems = 8;
-  static __device__ __forceinline__ void unpack(uint4 q, float* v) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  }
-  static __device__ __forceinline__ uint32_t pair(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  static __device__ __forceinline__ uint4 pack(const float* v) {
-    return make_uint4(pair(v[0], v[1]), pair(v[2], v[3]), pair(v[4], v[5]), pair(v[6], v[7]));
-  }
-};
-template <>
-struct Granule<__half> {
-  static constexpr int kElems = 8;
-  static __device__ __forceinline__ void unpack(uint4 q, float* v) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    }
-  }
-  static __device__ __forceinline__ uint32_t pair(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  static __device__ __forceinline__ uint4 pack(const float* v) {
-    return make_uint4(pair(v[0], v[1]), pair(v[2], v[3]), pair(v[4], v[5]), pair(v[6], v[7]));
-  }
-};
-
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_float(float v, float* to) { *to = v; }
-__device__ __forceinline__ void from_float(float v, __half* to) { *to = __float2half_rn(v); }
-__device__ __forceinline__ void from_float(float v, __nv_bfloat16* to) {
-  *to = __float2bfloat16_rn(v);
-}
-
 // Elements before the first 16-byte boundary (at most n).
 template <typename T>
 __device__ __forceinline__ int64_t head_of(const T* p, int64_t n) {
@@ -197,7 +132,7 @@ __device__ __forceinline__ double squares(const float (&v)[N]) {
   a += b;
   if (a > kSquaresLow && a < kSquaresHigh) return a;
   double t = 0.;
-#pragma unroll 1
+#pragma unroll
   for (int i = 0; i < N; ++i) t += static_cast<double>(v[i]) * v[i];
   return t;
 }
@@ -367,20 +302,89 @@ __device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamStep& s, f
   *p = fmaf(*p, a.keep, -(s.step_size * *m) / fmaf(sqrtf(*v), s.root_scale, a.eps));
 }
 
+// Four elements of T at an address that is a multiple of their size.
+template <typename T>
+struct Quad {                             // bf16, fp16
+  uint2 q;
+  __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void unpack(float* v) const {
+    float w[8];
+    Granule<T>::unpack(make_uint4(q.x, q.y, 0u, 0u), w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = w[k];
+  }
+  static __device__ __forceinline__ void store(const float* v, T* p) {
+    *reinterpret_cast<uint2*>(p) =
+        make_uint2(Granule<T>::pair(v[0], v[1]), Granule<T>::pair(v[2], v[3]));
+  }
+};
+template <>
+struct Quad<float> {
+  uint4 q;
+  __device__ __forceinline__ void load(const float* p) { q = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void unpack(float* v) const { Granule<float>::unpack(q, v); }
+  static __device__ __forceinline__ void store(const float* v, float* p) {
+    *reinterpret_cast<uint4*>(p) = Granule<float>::pack(v);
+  }
+};
+template <typename T>
+__device__ __forceinline__ bool quads(const T* p) {
+  return (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0;
+}
+
 template <typename P, typename G>
 __device__ __forceinline__ void piece_adam(const AdamArgs& a, const AdamStep& s, const Entry& e,
                                            int64_t from, int64_t n) {
+  constexpr int kInFlight = 2;
   P* p = static_cast<P*>(e.param) + from;
   const G* g = static_cast<const G*>(e.grad) + from;
   float *m = e.m + from, *v = e.v + from;
-  uint16_t* c = e.copy != nullptr ? e.copy + from : nullptr;
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
+  __nv_bfloat16* c =
+      e.copy != nullptr ? reinterpret_cast<__nv_bfloat16*>(e.copy) + from : nullptr;
+  int64_t done = 0;
+  if (quads(p) && quads(g) && quads(m) && quads(v) && (c == nullptr || quads(c))) {
+    const int64_t groups = n / 4;
+    done = groups * 4;
+    for (int64_t i = threadIdx.x; i < groups; i += kInFlight * kThreads) {
+      Quad<P> qp[kInFlight];
+      Quad<G> qg[kInFlight];
+      Quad<float> qm[kInFlight], qv[kInFlight];
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) {
+        const int64_t at = 4 * (i + u * kThreads);
+        if (at < done) {
+          qg[u].load(g + at);
+          qp[u].load(p + at);
+          qm[u].load(m + at);
+          qv[u].load(v + at);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) {
+        const int64_t at = 4 * (i + u * kThreads);
+        if (at < done) {
+          float fp[4], fg[4], fm[4], fv[4];
+          qp[u].unpack(fp);
+          qg[u].unpack(fg);
+          qm[u].unpack(fm);
+          qv[u].unpack(fv);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) adam_one(a, s, fg[k], fp + k, fm + k, fv + k);
+          Quad<P>::store(fp, p + at);
+          Quad<float>::store(fm, m + at);
+          Quad<float>::store(fv, v + at);
+          if (c != nullptr) Quad<__nv_bfloat16>::store(fp, c + at);
+        }
+      }
+    }
+  }
+  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) {
     float pi = to_float(p[i]), mi = m[i], vi = v[i];
     adam_one(a, s, to_float(g[i]), &pi, &mi, &vi);
     from_float(pi, p + i);
     m[i] = mi;
     v[i] = vi;
-    if (c != nullptr) c[i] = __bfloat16_as_ushort(__float2bfloat16_rn(pi));
+    if (c != nullptr) from_float(pi, c + i);
   }
 }
 

@@ -21,6 +21,7 @@
 
 #include "dora.h"
 #include "dora_ptx.cuh"
+#include "granule.cuh"
 #include "token_ops.cuh"
 
 namespace dora {
@@ -54,8 +55,22 @@ struct Actions {
 };
 
 // Sums over a thread's rows: loss, policy term, KL, entropy, clipped weight, weight.
+// Each is a pair of fp32 values, the second what the first lost (Knuth's two-sum):
+// fp64 additions, six a row in one thread, would cost its warp more than the row.
 struct Sums {
-  double v[kTerms] = {0., 0., 0., 0., 0., 0.};
+  float v[kTerms], lost[kTerms];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kTerms; ++i) v[i] = lost[i] = 0.f;
+  }
+  __device__ __forceinline__ void add(int i, float x) {
+    const float t = v[i] + x, b = t - v[i];
+    lost[i] += (v[i] - (t - b)) + (x - b);
+    v[i] = t;
+  }
+  __device__ __forceinline__ double get(int i) const {
+    return static_cast<double>(v[i]) + lost[i];
+  }
 };
 
 // One row's loss from l - q, x = q_ref - l and the entropy h; returns g.  A NaN
@@ -80,12 +95,12 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   row *= w;
   *loss = row;
   if (sums == nullptr) return g * w;
-  sums->v[0] += row;
-  sums->v[1] += static_cast<double>(w) * surrogate;
-  sums->v[2] += static_cast<double>(w) * kl;
-  sums->v[3] += static_cast<double>(w) * h;
-  sums->v[4] += inside ? 0.f : w;
-  sums->v[5] += w;
+  sums->add(0, row);
+  sums->add(1, w * surrogate);
+  sums->add(2, w * kl);
+  sums->add(3, w * h);
+  sums->add(4, inside ? 0.f : w);
+  sums->add(5, w);
   return g * w;
 }
 
@@ -98,7 +113,7 @@ __device__ __forceinline__ void finish_totals(const Actions& p, const Sums& sums
   Workspace* ws = p.ws;
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) ws->partial[blockIdx.x][i] = sums.v[i];
+    for (int i = 0; i < kTerms; ++i) ws->partial[blockIdx.x][i] = sums.get(i);
     __threadfence();
     last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
   }
@@ -117,27 +132,6 @@ __device__ __forceinline__ void finish_totals(const Actions& p, const Sums& sums
   if (threadIdx.x == 0) ws->ticket = 0;
 }
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_float(float v, float* to) { *to = v; }
-__device__ __forceinline__ void from_float(float v, __half* to) { *to = __float2half_rn(v); }
-__device__ __forceinline__ void from_float(float v, __nv_bfloat16* to) {
-  *to = __float2bfloat16_rn(v);
-}
-
-__device__ __forceinline__ float block_max(float v, float* scratch) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = scratch[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) v = fmaxf(v, scratch[w]);
-  return v;
-}
-
 template <typename F>
 __device__ __forceinline__ F block_sum(F v, F* scratch) {
 #pragma unroll
@@ -152,10 +146,14 @@ __device__ __forceinline__ F block_sum(F v, F* scratch) {
 }
 
 // ---------------------------------------------------------------------------
-// Categorical actions: one CTA walks the rows; a row is read for its maximum,
-// for its sums s = sum e^{z - m} and t = sum e^{z - m} (z - m), and for the
-// gradient:  p_j = e^{z_j - m} / s,  H = log s - t / s,
+// Categorical actions.  A row is read once into registers, as 16-byte granules,
+// by the lanes of a warp, a CTA or a cluster of CTAs; from there come its maximum
+// m, its sums s = sum e^{z - m} and t = sum e^{z - m} (z - m), and the gradient:
+//   p_j = e^{z_j - m} / s,  H = log s - t / s,
 //   d loss / d z_j = g (1(j = a) - p_j) + w c p_j (log p_j + H).
+// Rows start at any alignment: granules are aligned in memory, `mis` elements of
+// the first belong to what lies before the row, and a granule that is not wholly
+// inside is loaded and stored by its elements.
 // ---------------------------------------------------------------------------
 template <typename T>
 struct Rows {
@@ -169,67 +167,449 @@ struct Rows {
   int32_t* status;
 };
 
+// A row's scalars, loaded while the row before is worked on.
+struct RowIn {
+  int action, n;
+  float w, old_logp, adv, ref;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) policy_loss_kernel(Rows<T> r, Actions p) {
-  __shared__ float scratch[kThreads / 32];
+__device__ __forceinline__ RowIn row_in(const Rows<T>& r, const Actions& p, int row) {
+  RowIn in = {-1, 0, 0.f, 0.f, 0.f, 0.f};
+  if (row < r.rows) {
+    in.action = r.actions[row];
+    in.w = p.weights != nullptr ? p.weights[row] : 1.f;
+    in.n = r.legal != nullptr ? r.legal[row] : r.classes;
+    in.old_logp = p.old_logp[row];
+    in.adv = p.advantages[row];
+    in.ref = p.ref_logp != nullptr ? p.ref_logp[row] : 0.f;
+  }
+  return in;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// e^d for a difference d <= 0 of logits.
+__device__ __forceinline__ float exp_of(float d) { return ex2(d * kLog2e); }
+
+constexpr float kFloor = -200.f;          // below it e^d is 0: keeps 0 * inf out of e^d * d
+
+template <typename T>
+struct RowPtr {
+  static constexpr int kE = Granule<T>::kElems;
+  const T* z;                             // the row's first element
+  int mis;                                // elements of its first granule before it
+  __device__ __forceinline__ explicit RowPtr(const T* p)
+      : z(p), mis(static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {}
+
+  // Granule i of the row, elements outside [0, n) as -inf.
+  __device__ __forceinline__ uint4 load(int i, int n) const {
+    const int c = i * kE - mis;
+    if (c >= 0 && c + kE <= n) return *reinterpret_cast<const uint4*>(z + c);
+    constexpr uint32_t kNone = Granule<T>::kNegInfWord;
+    uint4 q = make_uint4(kNone, kNone, kNone, kNone);
+    if (c < n) {
+      float v[kE];
+      Granule<T>::unpack(q, v);
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        if (c + e >= 0 && c + e < n) v[e] = to_float(z[c + e]);
+      q = Granule<T>::pack(v);            // exact: the values come from T
+    }
+    return q;
+  }
+  // Values of granule i into the row at `to` of `classes` elements, 0 from n on.
+  __device__ __forceinline__ void store(T* to, bool aligned, int i, int n, int classes,
+                                        float* v) const {
+    const int c = i * kE - mis;
+    if (c >= classes) return;
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      if (c + e >= n) v[e] = 0.f;
+    if (aligned && c >= 0 && c + kE <= classes) {
+      *reinterpret_cast<uint4*>(to + c) = Granule<T>::pack(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        if (c + e >= 0 && c + e < classes) from_float(v[e], to + c + e);
+    }
+  }
+};
+
+// Sums of e^{z - m} and e^{z - m} (z - m) over one granule.  An m of -inf (nothing
+// but -inf so far) counts as 0, so that its terms are 0 and not NaN.
+template <typename T>
+__device__ __forceinline__ void add_exps(uint4 q, float m, float* s, float* t) {
+  constexpr int kE = Granule<T>::kElems;
+  float v[kE];
+  Granule<T>::unpack(q, v);
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const float d = v[e] - m, x = exp_of(d);
+    *s += x;
+    *t = fmaf(x, fmaxf(d, kFloor), *t);
+  }
+}
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// What the gradient of a row needs.
+struct RowGrad {
+  float m, a, b, g;                       // d loss / d z = e^{z - m} (a + b (z - m)) + g 1(j = a)
+  int granule, element;                   // of the action
+};
+
+template <typename T>
+__device__ __forceinline__ void grad_granule(uint4 q, const RowGrad& k, int i, float* v) {
+  constexpr int kE = Granule<T>::kElems;
+  Granule<T>::unpack(q, v);
+  if (k.b == 0.f) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = exp_of(v[e] - k.m) * k.a;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const float d = v[e] - k.m;
+      v[e] = exp_of(d) * fmaf(k.b, fmaxf(d, kFloor), k.a);
+    }
+  }
+  if (i == k.granule) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      if (e == k.element) v[e] += k.g;
+  }
+}
+
+// The row's outputs and what its gradient needs, from m, s, t and the action's logit;
+// `leader` writes and counts.
+template <typename T>
+__device__ __forceinline__ RowGrad finish_row(const Rows<T>& r, const Actions& p, const RowIn& in,
+                                              int row, float za, float m, float s, float t,
+                                              int mis, bool leader, Sums* sums) {
+  constexpr int kE = Granule<T>::kElems;
+  const float ls = logf(s), inv = 1.f / s, h = ls - t * inv;
+  const float lp = (za - m) - ls;
+  float loss;
+  const float g = row_terms(p, lp - in.old_logp, in.ref - lp, in.adv, in.w, h, &loss,
+                            leader ? sums : nullptr);
+  if (leader) {
+    p.logp[row] = lp;
+    if (r.entropy != nullptr) r.entropy[row] = h;
+    if (p.row_loss != nullptr) p.row_loss[row] = loss;
+  }
+  const float cw = in.w * p.entropy_coef;
+  return RowGrad{m, (cw * (h - ls) - g) * inv, cw * inv, g, (in.action + mis) / kE,
+                 (in.action + mis) % kE};
+}
+
+// A row that takes no part (0) or is not valid (NaN).
+template <typename T>
+__device__ __forceinline__ void fill_row(const Rows<T>& r, const Actions& p, int row, float fill,
+                                         Sums* sums) {
+  if (fill != 0.f) {
+    record_status(r.status, DORA_ERR_DEVICE_BAD_COUNT);
+    for (int i = 0; i < kTerms; ++i) sums->add(i, fill);
+  }
+  p.logp[row] = fill;
+  if (r.entropy != nullptr) r.entropy[row] = fill;
+  if (p.row_loss != nullptr) p.row_loss[row] = fill;
+}
+
+__device__ __forceinline__ bool same_alignment(const void* a, const void* b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
+}
+
+// The CTA's sums are those of its first `holders` times `stride` threads.
+template <int kStride, int kBlock>
+__device__ __forceinline__ void gather_sums(const Actions& p, Sums* sums) {
+  if (p.totals == nullptr || kBlock == kStride) return;
+  __shared__ double all[kBlock / kStride][kTerms];
+  if (threadIdx.x % kStride == 0)
+#pragma unroll
+    for (int i = 0; i < kTerms; ++i) all[threadIdx.x / kStride][i] = sums->get(i);
+  __syncthreads();
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int i = 0; i < kTerms; ++i) {
+      double t = 0.;
+      for (int k = 0; k < kBlock / kStride; ++k) t += all[k][i];
+      sums->v[i] = static_cast<float>(t);
+      sums->lost[i] = static_cast<float>(t - sums->v[i]);
+    }
+}
+
+// Short rows: kLanes lanes of a warp hold one, kHeld granules each.
+template <typename T, int kLanes, int kHeld>
+__global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Actions p) {
+  constexpr int kRowsPerCta = kThreads / kLanes;
   pdl_wait();
+  const int lane = threadIdx.x % kLanes;
+  const int step = gridDim.x * kRowsPerCta;
   Sums sums;
-  for (int row = blockIdx.x; row < r.rows; row += gridDim.x) {
-    const T* z = r.logits + row * r.ld;
+  sums.clear();
+  // the loop is the same for all groups of a warp: shuffles need every lane
+  const int first = blockIdx.x * kRowsPerCta + (threadIdx.x / 32) * (32 / kLanes);
+  int row = first + (threadIdx.x % 32) / kLanes;
+  RowIn in = row_in(r, p, row);
+  for (int base = first; base < r.rows; base += step, row += step) {
+    const bool exists = row < r.rows;
+    const bool takes = exists && in.action >= 0 && in.w != 0.f;
+    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
+    const int n = takes && !bad ? in.n : 0;
+    const RowPtr<T> z(r.logits + (exists ? row : 0) * r.ld);
+    const float za = n > 0 ? to_float(z.z[in.action]) : 0.f;
+    uint4 q[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) q[i] = z.load(lane + i * kLanes, n);
+    const RowIn next = row_in(r, p, row + step);
+    float m = -INFINITY, s = 0.f, t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) m = fmaxf(m, Granule<T>::largest(q[i]));
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1)
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) add_exps<T>(q[i], m, &s, &t);
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, off);
+      t += __shfl_xor_sync(0xffffffffu, t, off);
+    }
+    __syncwarp();                         // every lane has read its logits: grad may be logits
+    if (exists) {
+      T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
+      const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+      if (n > 0) {
+        const RowGrad k = finish_row(r, p, in, row, za, m, s, t, z.mis, lane == 0, &sums);
+        if (dz != nullptr)
+#pragma unroll
+          for (int i = 0; i < kHeld; ++i) {
+            float v[Granule<T>::kElems];
+            grad_granule<T>(q[i], k, lane + i * kLanes, v);
+            z.store(dz, aligned, lane + i * kLanes, n, r.classes, v);
+          }
+      } else {
+        const float fill = bad ? NAN : 0.f;
+        if (lane == 0) fill_row(r, p, row, fill, &sums);
+        if (dz != nullptr)
+#pragma unroll
+          for (int i = 0; i < kHeld; ++i) {
+            float v[Granule<T>::kElems];
+#pragma unroll
+            for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
+            z.store(dz, aligned, lane + i * kLanes, r.classes, r.classes, v);
+          }
+      }
+    }
+    in = next;
+  }
+  gather_sums<kLanes, kThreads>(p, &sums);
+  finish_totals(p, sums);
+}
+
+// (m, s, t) of a part of a row; parts are brought to a common m exactly as often as
+// they are joined.
+struct Part {
+  float m, s, t, pad;
+};
+
+// Every warp's part goes to every CTA of the cluster, and every warp joins them all:
+// one barrier a row.  `slots` alternate from row to row, so that a warp that is a
+// row ahead writes where nobody reads.
+template <int kWarps, int kCtas>
+__device__ __forceinline__ Part join_parts(Part mine, Part* slots) {
+  constexpr int kParts = kWarps * kCtas;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (kCtas == 1) {
+    if (lane == 0) slots[warp] = mine;
+    __syncthreads();
+  } else {
+    if (lane < kCtas) {
+      const uint32_t local = smem_u32(slots + cluster_ctarank() * kWarps + warp);
+      asm volatile(
+          "{\n\t.reg .b32 ra;\n\t"
+          "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+          "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(local),
+          "r"(lane), "f"(mine.m), "f"(mine.s), "f"(mine.t), "f"(0.f)
+          : "memory");
+    }
+    cluster_sync();
+  }
+  constexpr int kPer = (kParts + 31) / 32;
+  Part h[kPer];
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = lane + 32 * i;
+    h[i] = at < kParts ? slots[at] : Part{-INFINITY, 0.f, 0.f, 0.f};
+    m = fmaxf(m, h[i].m);
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (h[i].m != -INFINITY || h[i].s != 0.f) {             // a NaN sum is taken along
+      const float d = h[i].m - m, x = exp_of(d);
+      s = fmaf(h[i].s, x, s);
+      t = fmaf(fmaf(h[i].s, fmaxf(d, kFloor), h[i].t), x, t);
+    }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, off);
+    t += __shfl_xor_sync(0xffffffffu, t, off);
+  }
+  return Part{m, s, t, 0.f};
+}
+
+// Longer rows: kCtas CTAs (a cluster when there are several) hold one.
+template <typename T, int kBlock, int kHeld, int kCtas>
+__global__ void __launch_bounds__(kBlock, kHeld > 4 ? 2 : (kBlock > 128 ? 3 : 10))
+    policy_block_kernel(Rows<T> r, Actions p) {
+  constexpr int kWarps = kBlock / 32;
+  __shared__ Sums sums;                   // thread 0's: registers are for the row
+  __shared__ Part slots[2][kWarps * kCtas];
+  pdl_wait();
+  const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int step = gridDim.x / kCtas;
+  const int g0 = rank * kBlock * kHeld + threadIdx.x;
+  const bool leader = rank == 0 && threadIdx.x == 0;
+  int parity = 0;
+  if (threadIdx.x == 0) sums.clear();
+  int row = blockIdx.x / kCtas;
+  RowIn in = row_in(r, p, row);
+  for (; row < r.rows; row += step) {
+    const RowIn next = row_in(r, p, row + step);
+    const bool takes = in.action >= 0 && in.w != 0.f;
+    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
+    const RowPtr<T> z(r.logits + row * r.ld);
     T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
-    const int action = r.actions[row];
-    const float w = p.weights != nullptr ? p.weights[row] : 1.f;
-    const int n = r.legal != nullptr ? r.legal[row] : r.classes;
-    const bool takes = action >= 0 && w != 0.f;
-    const bool bad = takes && (n < 0 || n > r.classes || action >= n);
-    if (!takes || bad) {
-      const float fill = bad ? NAN : 0.f;
-      if (threadIdx.x == 0) {
-        if (bad) record_status(r.status, DORA_ERR_DEVICE_BAD_COUNT);
-        p.logp[row] = fill;
-        if (r.entropy != nullptr) r.entropy[row] = fill;
-        if (p.row_loss != nullptr) p.row_loss[row] = fill;
-        for (int i = 0; i < kTerms; ++i) sums.v[i] += fill;
+    const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+    if (takes && !bad) {
+      const float za = to_float(z.z[in.action]);
+      uint4 q[kHeld];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) q[i] = z.load(g0 + i * kBlock, in.n);
+      Part part = {-INFINITY, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) part.m = fmaxf(part.m, Granule<T>::largest(q[i]));
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1)
+        part.m = fmaxf(part.m, __shfl_xor_sync(0xffffffffu, part.m, off));
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) add_exps<T>(q[i], base_of(part.m), &part.s, &part.t);
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) {
+        part.s += __shfl_xor_sync(0xffffffffu, part.s, off);
+        part.t += __shfl_xor_sync(0xffffffffu, part.t, off);
       }
+      // after its barrier every logit of the row has been read: grad may be logits
+      part = join_parts<kWarps, kCtas>(part, slots[parity]);
+      parity ^= 1;
+      const RowGrad k =
+          finish_row(r, p, in, row, za, part.m, part.s, part.t, z.mis, leader, &sums);
       if (dz != nullptr)
-        for (int j = threadIdx.x; j < r.classes; j += kThreads) from_float(fill, dz + j);
-      continue;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+          float v[Granule<T>::kElems];
+          grad_granule<T>(q[i], k, g0 + i * kBlock, v);
+          z.store(dz, aligned, g0 + i * kBlock, in.n, r.classes, v);
+        }
+    } else {
+      const float fill = bad ? NAN : 0.f;
+      if (leader) fill_row(r, p, row, fill, &sums);
+      if (dz != nullptr)
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+          float v[Granule<T>::kElems];
+#pragma unroll
+          for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
+          z.store(dz, aligned, g0 + i * kBlock, r.classes, r.classes, v);
+        }
     }
-    float m = -INFINITY;
-    for (int j = threadIdx.x; j < n; j += kThreads) m = fmaxf(m, to_float(z[j]));
-    m = block_max(m, scratch);
-    float s = 0.f, t = 0.f;
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-      const float d = to_float(z[j]) - m;
-      const float e = expf(d);
-      s += e;
-      t = fmaf(e, fmaxf(d, -200.f), t);   // e = 0 at -inf: no 0 * inf
-    }
-    s = block_sum(s, scratch);
-    t = block_sum(t, scratch);
-    const float za = to_float(z[action]);
-    const float ls = logf(s), h = ls - t / s;
-    const float lp = (za - m) - ls;
-    const float x = p.ref_logp != nullptr ? p.ref_logp[row] - lp : 0.f;
-    float loss;
-    const float g = row_terms(p, lp - p.old_logp[row], x, p.advantages[row], w, h, &loss,
-                              threadIdx.x == 0 ? &sums : nullptr);
-    if (threadIdx.x == 0) {
-      p.logp[row] = lp;
-      if (r.entropy != nullptr) r.entropy[row] = h;
-      if (p.row_loss != nullptr) p.row_loss[row] = loss;
-    }
-    if (dz == nullptr) continue;
-    __syncthreads();                      // the action's logit is read before it is overwritten
-    const float cw = w * p.entropy_coef, a = (cw * (h - ls) - g) / s, b = cw / s;
-    for (int j = threadIdx.x; j < r.classes; j += kThreads) {
-      float v = 0.f;
-      if (j < n) {
-        const float d = to_float(z[j]) - m;
-        v = expf(d) * fmaf(b, fmaxf(d, -200.f), a);
-        if (j == action) v += g;
+    in = next;
+  }
+  finish_totals(p, sums);
+}
+
+// Rows longer than the registers of a cluster: the same, but the row is read a second
+// time (from L2, where the clusters' rows fit) for its gradient.
+constexpr int kLongBlock = 512, kLongCtas = 8, kLongStep = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, Actions p) {
+  constexpr int kWarps = kLongBlock / 32, kStride = kLongBlock * kLongCtas;
+  __shared__ Part slots[2][kWarps * kLongCtas];
+  __shared__ Sums sums;
+  pdl_wait();
+  const int rank = static_cast<int>(cluster_ctarank());
+  const int step = gridDim.x / kLongCtas;
+  const int g0 = rank * kLongBlock + threadIdx.x;
+  const bool leader = rank == 0 && threadIdx.x == 0;
+  int parity = 0;
+  if (threadIdx.x == 0) sums.clear();
+  for (int row = blockIdx.x / kLongCtas; row < r.rows; row += step) {
+    const RowIn in = row_in(r, p, row);
+    const bool takes = in.action >= 0 && in.w != 0.f;
+    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
+    const RowPtr<T> z(r.logits + row * r.ld);
+    T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
+    const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+    const int granules = (r.classes + z.mis + Granule<T>::kElems - 1) / Granule<T>::kElems;
+    if (takes && !bad) {
+      const float za = to_float(z.z[in.action]);
+      Part part = {-INFINITY, 0.f, 0.f, 0.f};
+      for (int i = g0; i < granules; i += kStride * kLongStep) {
+        uint4 q[kLongStep];
+#pragma unroll
+        for (int u = 0; u < kLongStep; ++u) q[u] = z.load(i + u * kStride, in.n);
+        float m = part.m;
+#pragma unroll
+        for (int u = 0; u < kLongStep; ++u) m = fmaxf(m, Granule<T>::largest(q[u]));
+        if (m > part.m && part.s != 0.f) {
+          const float d = part.m - m, x = exp_of(d);
+          part.t = fmaf(part.s, fmaxf(d, kFloor), part.t) * x;
+          part.s *= x;
+        }
+        part.m = m;
+#pragma unroll
+        for (int u = 0; u < kLongStep; ++u) add_exps<T>(q[u], base_of(m), &part.s, &part.t);
       }
-      from_float(v, dz + j);
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) {
+        const Part o = {__shfl_xor_sync(0xffffffffu, part.m, off),
+                        __shfl_xor_sync(0xffffffffu, part.s, off),
+                        __shfl_xor_sync(0xffffffffu, part.t, off), 0.f};
+        const float m = fmaxf(part.m, o.m), c = base_of(m);
+        const float da = part.m - c, db = o.m - c, xa = exp_of(da), xb = exp_of(db);
+        part.t = fmaf(part.s, fmaxf(da, kFloor), part.t) * xa +
+                 fmaf(o.s, fmaxf(db, kFloor), o.t) * xb;
+        part.s = part.s * xa + o.s * xb;
+        part.m = m;
+      }
+      part = join_parts<kWarps, kLongCtas>(part, slots[parity]);
+      parity ^= 1;
+      const RowGrad k =
+          finish_row(r, p, in, row, za, part.m, part.s, part.t, z.mis, leader, &sums);
+      if (dz != nullptr)
+        for (int i = g0; i < granules; i += kStride) {
+          float v[Granule<T>::kElems];
+          grad_granule<T>(z.load(i, in.n), k, i, v);
+          z.store(dz, aligned, i, in.n, r.classes, v);
+        }
+    } else {
+      const float fill = bad ? NAN : 0.f;
+      if (leader) fill_row(r, p, row, fill, &sums);
+      if (dz != nullptr)
+        for (int i = g0; i < granules; i += kStride) {
+          float v[Granule<T>::kElems];
+#pragma unroll
+          for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
+          z.store(dz, aligned, i, r.classes, r.classes, v);
+        }
     }
   }
   finish_totals(p, sums);
@@ -298,6 +678,7 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
   __shared__ int bad;
   pdl_wait();
   Sums sums;
+  sums.clear();
   for (int img = blockIdx.x; img < q.batch; img += gridDim.x) {
     const int lo = q.cu[img], hi = q.cu[img + 1];
     int n = hi - lo - 1, k = q.k[img];
@@ -334,7 +715,7 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
         if (takes) record_status(q.status, DORA_ERR_DEVICE_BAD_COUNT);
         p.logp[img] = fill;
         if (p.row_loss != nullptr) p.row_loss[img] = fill;
-        for (int i = 0; i < kTerms; ++i) sums.v[i] += fill;
+        for (int i = 0; i < kTerms; ++i) sums.add(i, fill);
       }
       if (q.grad != nullptr && inside)
         for (int r = lo + threadIdx.x; r < hi; r += kThreads) q.grad[r] = fill;
@@ -439,14 +820,79 @@ int grid_for(int rows, int per_sm) {
   return ctas < policy::kMaxCtas ? ctas : policy::kMaxCtas;
 }
 
+// A dependent launch of clusters of `ctas` CTAs.
+template <typename T>
+int launch_rows(void (*kern)(policy::Rows<T>, policy::Actions), int grid, int block, int ctas,
+                cudaStream_t stream, const policy::Rows<T>& r, const policy::Actions& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (ctas > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = ctas;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  if (pdl_enabled()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return launched(cudaLaunchKernelEx(&cfg, kern, r, p));
+}
+
+template <typename T, int kHeld>
+int launch_blocks(int ctas, cudaStream_t stream, const policy::Rows<T>& r,
+                  const policy::Actions& p) {
+  const int clusters = grid_for(r.rows, kHeld > 4 ? 2 : 3);   // CTAs that an SM holds
+  const int grid = ctas * (clusters * ctas > num_sms() * (kHeld > 4 ? 2 : 3)
+                               ? num_sms() * (kHeld > 4 ? 2 : 3) / ctas
+                               : clusters);
+  switch (ctas) {
+    case 1: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 1>, grid, 512, 1, stream, r, p);
+    case 2: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 2>, grid, 512, 2, stream, r, p);
+    case 4: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 4>, grid, 512, 4, stream, r, p);
+    default: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 8>, grid, 512, 8, stream, r, p);
+  }
+}
+
 template <typename T>
 int launch_policy(const void* logits, void* grad, int64_t ld, int rows, int classes,
                   const int32_t* legal, const int32_t* actions, float* entropy, int32_t* status,
                   const policy::Actions& p, cudaStream_t stream) {
-  policy::Rows<T> r = {static_cast<const T*>(logits), static_cast<T*>(grad), ld, rows, classes,
-                       legal, actions, entropy, status};
-  return launched(launch_pdl(policy::policy_loss_kernel<T>, dim3(grid_for(rows, 8)),
-                             dim3(policy::kThreads), 0, stream, r, p));
+  const policy::Rows<T> r = {static_cast<const T*>(logits), static_cast<T*>(grad), ld, rows,
+                             classes, legal, actions, entropy, status};
+  constexpr int kE = Granule<T>::kElems;
+  // granules that a row can touch: one more where rows may start inside one
+  const bool aligned = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && ld % kE == 0;
+  const int64_t need = (static_cast<int64_t>(classes) + (aligned ? 0 : kE - 1) + kE - 1) / kE;
+  if (need <= 8)
+    return launch_rows(policy::policy_warp_kernel<T, 8, 1>, grid_for((rows + 31) / 32, 8), 256, 1,
+                       stream, r, p);
+  if (need <= 32)
+    return launch_rows(policy::policy_warp_kernel<T, 8, 4>, grid_for((rows + 31) / 32, 8), 256, 1,
+                       stream, r, p);
+  if (need <= 128)
+    return launch_rows(policy::policy_warp_kernel<T, 32, 4>, grid_for((rows + 7) / 8, 8), 256, 1,
+                       stream, r, p);
+  if (need <= 512)
+    return launch_rows(policy::policy_block_kernel<T, 128, 4, 1>, grid_for(rows, 12), 128, 1,
+                       stream, r, p);
+  if (need > 512 * 8 * 8)
+    return launch_rows(policy::policy_long_kernel<T>,
+                       policy::kLongCtas * grid_for(rows, 1) > num_sms() * 2
+                           ? num_sms() * 2 / policy::kLongCtas * policy::kLongCtas
+                           : policy::kLongCtas * rows,
+                       policy::kLongBlock, policy::kLongCtas, stream, r, p);
+  int ctas = 1;
+  while (need > 512 * 8 * ctas) ctas *= 2;
+  while (ctas < 8 && rows * ctas * 2 <= num_sms()) ctas *= 2;   // few rows: more SMs a row
+  return need <= 512 * 4 * ctas ? launch_blocks<T, 4>(ctas, stream, r, p)
+                                : launch_blocks<T, 8>(ctas, stream, r, p);
 }
 }  // namespace
 
