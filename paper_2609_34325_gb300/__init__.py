@@ -889,10 +889,12 @@ def alloc_policy_workspace(device=None) -> torch.Tensor:
     return torch.zeros(dora_policy_workspace_size(), dtype=torch.uint8, device=device or "cuda")
 
 
-def _rows(n, **tensors):
-    for name, t in tensors.items():
+def _entries(n, tensors, totals):
+    for t in tensors:
         if t is not None and t.numel() != n:
-            raise ValueError(f"{name} must have {n} entries")
+            raise ValueError("every per-action tensor must have one entry per row (per image)")
+    if totals is not None and totals.numel() < 6:
+        raise ValueError("totals must hold 6 floats")
 
 
 def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None, grad=None,
@@ -910,7 +912,7 @@ def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None
     dt = _DTYPES.get(logits.dtype) if isinstance(logits, _Tensor) and logits.is_cuda else None
     if dt is None or logits.dim() != 2:
         raise TypeError("logits must be a 2-D CUDA tensor of bf16, fp16 or fp32")
-    rows, cols = logits.shape
+    rows, cols = logits.size(0), logits.size(1)
     ld = logits.stride(0) if rows > 1 else cols
     if (cols > 1 and logits.stride(1) != 1) or ld < cols:
         raise TypeError("the rows of logits must be contiguous and not overlap")
@@ -919,14 +921,11 @@ def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None
         raise ValueError("classes must be in [1, logits.shape[1]]")
     if grad is not None and grad is not logits and not (
             isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
-            grad.shape == logits.shape and grad.stride() == logits.stride()):
+            grad.dim() == 2 and grad.size(0) == rows and grad.size(1) == cols and
+            (grad.stride(0) == ld or rows <= 1) and (grad.stride(1) == 1 or cols == 1)):
         raise TypeError("grad must be like logits: device, type, shape and strides")
-    if not (actions.numel() == old_logp.numel() == advantages.numel() == logp.numel() == rows):
-        raise ValueError("actions, old_logp, advantages and logp must have one entry per row")
-    _rows(rows, legal=legal, ref_logp=ref_logp, weights=weights, entropy=entropy,
-          row_loss=row_loss)
-    if totals is not None and totals.numel() < 6:
-        raise ValueError("totals must hold 6 floats")
+    _entries(rows, (actions, old_logp, advantages, logp, legal, ref_logp, weights, entropy,
+                    row_loss), totals)
     code = load_library().dora_policy_loss(
         logits.data_ptr(), dt, rows, classes, ld, _opt(legal, _I32, "legal"),
         _arg(actions, _I32, "actions"), _arg(old_logp, _F32, "old_logp"),
@@ -952,13 +951,9 @@ def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, worksp
     o, b = _arg(order, _I32, "order"), cu.numel() - 1
     if order.dim() != 2 or order.size(0) != b:
         raise ValueError("order must be [B, k_cap]")
-    if not (k.numel() == old_logp.numel() == advantages.numel() == logp.numel() == b):
-        raise ValueError("k, old_logp, advantages and logp must have one entry per image")
-    _rows(b, ref_logp=ref_logp, weights=weights, row_loss=row_loss)
+    _entries(b, (k, old_logp, advantages, logp, ref_logp, weights, row_loss), totals)
     if grad is not None and grad.numel() != scores.numel():
         raise ValueError("grad must match scores")
-    if totals is not None and totals.numel() < 6:
-        raise ValueError("totals must hold 6 floats")
     code = load_library().dora_pl_policy_loss(
         s, c, b, scores.numel(), kp, o, order.size(1), _arg(old_logp, _F32, "old_logp"),
         _opt(ref_logp, _F32, "ref_logp"), _arg(advantages, _F32, "advantages"),

@@ -4,7 +4,10 @@
 //
 // The list lives on the device: one entry per tensor, and the tensors cut into
 // units of kUnit elements that are dealt out evenly as spans of consecutive
-// units, whatever the tensors' sizes.  A CTA walks its spans, piece by piece.
+// units, whatever the tensors' sizes.  A CTA walks its span, piece by piece.  To
+// begin a tensor costs a CTA about as long as kBegin units take (its entry, then its
+// first values: two round trips to memory), and counts as that many: a hundred
+// vectors in a row would otherwise be one CTA's, while the others wait for it.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -21,7 +24,9 @@ namespace optim {
 
 constexpr int kThreads = 256;
 constexpr int kUnit = 1024;               // elements
-constexpr int kMaxSpans = 152 * 8;
+constexpr int kBegin = 6;                 // units
+constexpr int kCtasPerSm = 4;             // resident, by their registers
+constexpr int kMaxSpans = 152 * kCtasPerSm;   // a span a CTA, all at once
 constexpr int kFill = 48;                 // entries written by one launch, passed by value
 
 struct Entry {
@@ -31,15 +36,16 @@ struct Entry {
   float *m, *v;
   uint16_t* copy;                         // nullable, bf16
   int64_t n;
-  int64_t first_unit;
+  int64_t first_unit;                     // of its elements; kBegin units before belong to it
   int32_t grad_type, param_type;
 };
 
-// Units [unit, unit_end) of the whole list, starting in tensor `tensor`.
+// Units [unit, unit_end) of the whole list, from tensor `tensor` to `last_tensor`,
+// with those tensors' entries, so that a CTA reads where to begin in one load.
 struct Span {
   int64_t unit, unit_end;
-  int32_t tensor, pad;
-  Entry first;                            // the entry of that tensor
+  int32_t tensor, last_tensor;
+  Entry first, last;
 };
 
 struct Header {
@@ -66,7 +72,17 @@ __global__ void fill_entries_kernel(Header* header, Entry* entries, int first, i
   if (threadIdx.x < count) entries[first + threadIdx.x] = args.e[threadIdx.x];
 }
 
-__device__ __forceinline__ int64_t units_of(int64_t n) { return (n + kUnit - 1) / kUnit; }
+// The last tensor that starts at or before a unit (the one that holds it: tensors
+// without elements start where the next one does).
+__device__ __forceinline__ int tensor_of(const List& list, int64_t unit) {
+  int lo = 0, hi = list.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    const Entry& e = list.entries[mid];
+    if (e.first_unit - (e.n > 0 ? kBegin : 0) <= unit) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
 
 __global__ void fill_spans_kernel(List list, int64_t units) {
   pdl_wait();
@@ -75,129 +91,195 @@ __global__ void fill_spans_kernel(List list, int64_t units) {
   Span s;
   s.unit = units * b / list.n_spans;
   s.unit_end = units * (b + 1) / list.n_spans;
-  int lo = 0, hi = list.count - 1;        // the last tensor that starts at or before the unit
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (list.entries[mid].first_unit <= s.unit) lo = mid; else hi = mid - 1;
-  }
-  s.tensor = lo;
-  s.pad = 0;
-  s.first = list.entries[lo];
+  s.tensor = tensor_of(list, s.unit);
+  s.last_tensor = s.unit_end > s.unit ? tensor_of(list, s.unit_end - 1) : s.tensor;
+  s.first = list.entries[s.tensor];
+  s.last = list.entries[s.last_tensor];
   list.spans[b] = s;
 }
 
-// f(entry, first element, elements) for every piece of the span.
-template <typename F>
+// f(entry, first element, elements) for every piece of the span, from its first to
+// its last tensor, or the other way round.  The entry stays in memory, and a piece
+// has at most kPiece elements, counted in 32 bits: both leave registers to the data.
+constexpr int kPiece = 1 << 28;
+
+template <bool kForward, typename F>
 __device__ __forceinline__ void for_pieces(const List& list, int span, F f) {
-  const Span& s = list.spans[span];
-  int64_t unit = s.unit;
-  const int64_t end = s.unit_end;
+  const Span* s = list.spans + span;
+  const int64_t unit = s->unit, end = s->unit_end;
   if (unit >= end) return;
-  int tensor = s.tensor;
-  Entry e = s.first;
+  int tensor = kForward ? s->tensor : s->last_tensor;
+  const int stop = kForward ? s->last_tensor : s->tensor;
+  const Entry* e = kForward ? &s->first : &s->last;
   while (true) {
-    const int64_t from = (unit - e.first_unit) * kUnit;
-    const int64_t last = (end - e.first_unit) * kUnit;
-    const int64_t to = last < e.n ? last : e.n;
-    if (to > from) f(e, from, to - from);
-    unit = e.first_unit + units_of(e.n);
-    if (unit >= end || ++tensor >= list.count) return;
-    e = list.entries[tensor];
+    const int64_t n = e->n, first_unit = e->first_unit;
+    int64_t from = unit > first_unit ? (unit - first_unit) * kUnit : 0;
+    int64_t to = (end - first_unit) * kUnit;
+    to = to < n ? to : n;
+    while (to > from) {
+      const int some = to - from < kPiece ? static_cast<int>(to - from) : kPiece;
+      f(*e, kForward ? from : to - some, some);
+      if (kForward) from += some; else to -= some;
+    }
+    if (tensor == stop) return;
+    tensor += kForward ? 1 : -1;
+    e = list.entries + tensor;
   }
 }
 
+// A tensor's type is looked at where its values are unpacked or packed, not by a
+// loop for each type: the loads in flight are the same for all, and one loop leaves
+// them their registers (three types times three in Adam's took 255, or spilled).
+__device__ __forceinline__ int size_of(int type) { return type == DORA_F32 ? 4 : 2; }
+__device__ __forceinline__ const char* at_elem(const void* p, int type, int64_t i) {
+  return static_cast<const char*>(p) + i * size_of(type);
+}
+__device__ __forceinline__ char* at_elem(void* p, int type, int64_t i) {
+  return static_cast<char*>(p) + i * size_of(type);
+}
+__device__ __forceinline__ float load_one(const void* p, int type, int i) {
+  if (type == DORA_F32) return static_cast<const float*>(p)[i];
+  if (type == DORA_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return to_float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_one(float v, void* p, int type, int i) {
+  if (type == DORA_F32) static_cast<float*>(p)[i] = v;
+  else if (type == DORA_BF16) from_float(v, static_cast<__nv_bfloat16*>(p) + i);
+  else from_float(v, static_cast<__half*>(p) + i);
+}
+
 // Elements before the first 16-byte boundary (at most n).
-template <typename T>
-__device__ __forceinline__ int64_t head_of(const T* p, int64_t n) {
-  const int64_t h = ((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / sizeof(T);
+__device__ __forceinline__ int head_of(const void* p, int type, int n) {
+  const int h = static_cast<int>((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) /
+                size_of(type);
   return h < n ? h : n;
 }
 
 // ---------------------------------------------------------------------------
 // Norm.  Squares are summed in 32 bits over the elements that a thread has at
-// hand at once and carried on in 64, so the result does not depend on the list's
-// length; a 32-bit sum that left the middle of its range (gradients above about
-// 1e18 or below 1e-18) is taken again in 64 bits.
+// hand at once; the sums are carried on in pairs of fp32 values, the second what
+// the first lost (Knuth's two-sum: six additions where an fp64 one takes the warp
+// 16 cycles or more), and joined in 64 bits.  A sum out of the middle of the
+// range (gradients above about 1e11 or below 1e-16) is taken again in 64 bits.
 // ---------------------------------------------------------------------------
-constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e37f;
+constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e25f;
 
-template <int N>
-__device__ __forceinline__ double squares(const float (&v)[N]) {
-  float a = 0.f, b = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    a = fmaf(v[i], v[i], a);
-    if (i + 1 < N) b = fmaf(v[i + 1], v[i + 1], b);
+struct SumOfSquares {
+  float sum, lost;
+  double wide;
+  __device__ __forceinline__ bool add(float x) {         // false: out of range
+    if (!(x > kSquaresLow && x < kSquaresHigh)) return false;
+    const float t = sum + x, b = t - sum;
+    lost += (sum - (t - b)) + (x - b);
+    sum = t;
+    return true;
   }
-  a += b;
-  if (a > kSquaresLow && a < kSquaresHigh) return a;
-  double t = 0.;
+  __device__ __forceinline__ void add_one(float v) {
+    if (!add(v * v)) wide += static_cast<double>(v) * v;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void add_squares(uint4 q, float* a, float* b) {
+  float v[Granule<T>::kElems];
+  Granule<T>::unpack(q, v);
 #pragma unroll
-  for (int i = 0; i < N; ++i) t += static_cast<double>(v[i]) * v[i];
-  return t;
+  for (int k = 0; k < Granule<T>::kElems; k += 2) {
+    *a = fmaf(v[k], v[k], *a);
+    *b = fmaf(v[k + 1], v[k + 1], *b);
+  }
 }
 
 template <typename T>
-__device__ __forceinline__ double piece_squares(const T* p, int64_t n) {
-  constexpr int kE = Granule<T>::kElems, kInFlight = 4;
-  double acc = 0.;
-  const int64_t head = head_of(p, n);
-  const int64_t granules = (n - head) / kE, tail = head + granules * kE;
-  if (threadIdx.x < head) {
-    const float v[1] = {to_float(p[threadIdx.x])};
-    acc += squares(v);
-  }
-  if (tail + threadIdx.x < n) {
-    const float v[1] = {to_float(p[tail + threadIdx.x])};
-    acc += squares(v);
-  }
-  const uint4* g = reinterpret_cast<const uint4*>(p + head);
-  for (int64_t i = threadIdx.x; i < granules; i += kInFlight * kThreads) {
+__device__ __forceinline__ double wide_squares(uint4 q) {
+  float v[Granule<T>::kElems];
+  Granule<T>::unpack(q, v);
+  double t = 0.;
+#pragma unroll
+  for (int k = 0; k < Granule<T>::kElems; ++k) t += static_cast<double>(v[k]) * v[k];
+  return t;
+}
+
+__device__ __forceinline__ void piece_squares(const void* p, int type, int n, SumOfSquares* acc) {
+  constexpr int kInFlight = 8;
+  const int elems = 16 / size_of(type);
+  const int head = head_of(p, type, n);
+  const int granules = (n - head) / elems, tail = head + granules * elems;
+  if (threadIdx.x < head) acc->add_one(load_one(p, type, threadIdx.x));
+  if (tail + threadIdx.x < n) acc->add_one(load_one(p, type, tail + threadIdx.x));
+  const uint4* g = reinterpret_cast<const uint4*>(at_elem(p, type, head));
+  for (int i = threadIdx.x; i < granules; i += kInFlight * kThreads) {
     uint4 q[kInFlight];
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u)
-      q[u] = i + u * kThreads < granules ? __ldg(g + i + u * kThreads) : make_uint4(0, 0, 0, 0);
-    uint32_t any = 0;
-    float v[kInFlight * kE];
+      q[u] = i + u * kThreads < granules ? g[i + u * kThreads] : make_uint4(0, 0, 0, 0);
+    float a = 0.f, b = 0.f;
+    if (type == DORA_F32) {
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      any |= q[u].x | q[u].y | q[u].z | q[u].w;
-      Granule<T>::unpack(q[u], v + u * kE);
+      for (int u = 0; u < kInFlight; ++u) add_squares<float>(q[u], &a, &b);
+    } else if (type == DORA_BF16) {
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) add_squares<__nv_bfloat16>(q[u], &a, &b);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) add_squares<__half>(q[u], &a, &b);
     }
-    if (any != 0) acc += squares(v);
+    if (!acc->add(a + b)) {
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u)
+        if ((q[u].x | q[u].y | q[u].z | q[u].w) != 0)
+          acc->wide += type == DORA_F32    ? wide_squares<float>(q[u])
+                       : type == DORA_BF16 ? wide_squares<__nv_bfloat16>(q[u])
+                                           : wide_squares<__half>(q[u]);
+    }
   }
-  return acc;
 }
 
+// Sum over the block, for the threads of its first warp.
 __device__ __forceinline__ double block_sum(double v, double* scratch) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  __syncthreads();
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = scratch[0];
+  v = threadIdx.x < kThreads / 32 ? scratch[threadIdx.x] : 0.;
 #pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) v += scratch[w];
+  for (int off = kThreads / 64; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
+
+// The same of what the threads summed: fp32 within a warp (a few roundings of values
+// that are in the middle of the range), 64 bits from there on.
+__device__ __forceinline__ double block_sum(const SumOfSquares& mine, double* scratch) {
+  float f = mine.sum + mine.lost;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) f += __shfl_xor_sync(0xffffffffu, f, off);
+  double v = f;
+  if (__any_sync(0xffffffffu, mine.wide != 0.)) {
+    v = mine.wide;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    v += f;
+  }
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = threadIdx.x < kThreads / 32 ? scratch[threadIdx.x] : 0.;
+#pragma unroll
+  for (int off = kThreads / 64; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
   return v;
 }
 
 // out[0] = the norm, out[1] = min(1, max_norm / norm), 1 for a norm that is not finite; the CTA that is last adds
 // the spans' sums in their order.
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
     grad_norm_kernel(List list, float max_norm, float* __restrict__ out) {
   __shared__ double scratch[kThreads / 32];
   __shared__ bool last;
   pdl_wait();
-  double acc = 0.;
-  for_pieces(list, blockIdx.x, [&](const Entry& e, int64_t from, int64_t n) {
-    if (e.grad_type == DORA_F32)
-      acc += piece_squares(static_cast<const float*>(e.grad) + from, n);
-    else if (e.grad_type == DORA_BF16)
-      acc += piece_squares(static_cast<const __nv_bfloat16*>(e.grad) + from, n);
-    else
-      acc += piece_squares(static_cast<const __half*>(e.grad) + from, n);
+  SumOfSquares mine = {0.f, 0.f, 0.};
+  for_pieces<true>(list, blockIdx.x, [&](const Entry& e, int64_t from, int n) {
+    piece_squares(at_elem(e.grad, e.grad_type, from), e.grad_type, n, &mine);
   });
-  acc = block_sum(acc, scratch);
+  const double acc = block_sum(mine, scratch);
   if (threadIdx.x == 0) {
     list.header->partial[blockIdx.x] = acc;
     __threadfence();
@@ -211,62 +293,66 @@ __global__ void __launch_bounds__(kThreads)
     t += __ldcg(&list.header->partial[b]);
   t = block_sum(t, scratch);
   if (threadIdx.x == 0) {
-    const float norm = static_cast<float>(sqrt(t));
+    // fp64 square roots are long; most sums have one in fp32
+    const float norm = t > kSquaresLow && t < kSquaresHigh ? sqrtf(static_cast<float>(t))
+                                                           : static_cast<float>(sqrt(t));
     out[0] = norm;
-    out[1] = isfinite(norm) && norm > max_norm ? static_cast<float>(max_norm / sqrt(t)) : 1.f;
+    out[1] = isfinite(norm) && norm > max_norm ? max_norm / norm : 1.f;
     list.header->ticket = 0;
   }
 }
 
 // ---------------------------------------------------------------------------
-// Clipping.  A norm that is not finite leaves the gradients as they are.
+// Clipping.  A norm that is not finite leaves the gradients as they are.  Spans
+// are walked from their ends, which the norm has read last and L2 may still hold.
 // ---------------------------------------------------------------------------
 template <typename T>
-__device__ __forceinline__ void piece_scale(const T* p, T* y, int64_t n, float f) {
-  constexpr int kE = Granule<T>::kElems, kInFlight = 4;
+__device__ __forceinline__ uint4 scaled(uint4 q, float f) {
+  float v[Granule<T>::kElems];
+  Granule<T>::unpack(q, v);
+#pragma unroll
+  for (int k = 0; k < Granule<T>::kElems; ++k) v[k] *= f;
+  return Granule<T>::pack(v);
+}
+
+__device__ __forceinline__ void piece_scale(const void* p, void* y, int type, int n, float f) {
+  constexpr int kInFlight = 8;
   if ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(y)) & 15u) {
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) from_float(to_float(p[i]) * f, y + i);
+    for (int i = threadIdx.x; i < n; i += kThreads) store_one(load_one(p, type, i) * f, y, type, i);
     return;
   }
-  const int64_t head = head_of(p, n);
-  const int64_t granules = (n - head) / kE, tail = head + granules * kE;
-  if (threadIdx.x < head) from_float(to_float(p[threadIdx.x]) * f, y + threadIdx.x);
+  const int elems = 16 / size_of(type);
+  const int head = head_of(p, type, n);
+  const int granules = (n - head) / elems, tail = head + granules * elems;
+  if (threadIdx.x < head)
+    store_one(load_one(p, type, threadIdx.x) * f, y, type, threadIdx.x);
   if (tail + threadIdx.x < n)
-    from_float(to_float(p[tail + threadIdx.x]) * f, y + tail + threadIdx.x);
-  const uint4* g = reinterpret_cast<const uint4*>(p + head);
-  uint4* o = reinterpret_cast<uint4*>(y + head);
-  for (int64_t i = threadIdx.x; i < granules; i += kInFlight * kThreads) {
+    store_one(load_one(p, type, tail + threadIdx.x) * f, y, type, tail + threadIdx.x);
+  const uint4* g = reinterpret_cast<const uint4*>(at_elem(p, type, head));
+  uint4* o = reinterpret_cast<uint4*>(at_elem(y, type, head));
+  for (int i = granules - 1 - static_cast<int>(threadIdx.x); i >= 0; i -= kInFlight * kThreads) {
     uint4 q[kInFlight];
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u)
-      if (i + u * kThreads < granules) q[u] = g[i + u * kThreads];
+      if (i >= u * kThreads) q[u] = g[i - u * kThreads];
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u)
-      if (i + u * kThreads < granules) {
-        float v[kE];
-        Granule<T>::unpack(q[u], v);
-#pragma unroll
-        for (int k = 0; k < kE; ++k) v[k] *= f;
-        o[i + u * kThreads] = Granule<T>::pack(v);
-      }
+      if (i >= u * kThreads)
+        o[i - u * kThreads] = type == DORA_F32    ? scaled<float>(q[u], f)
+                              : type == DORA_BF16 ? scaled<__nv_bfloat16>(q[u], f)
+                                                  : scaled<__half>(q[u], f);
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
     scale_grads_kernel(List list, const float* __restrict__ norm) {
   pdl_wait();
   const float f = isfinite(norm[0]) ? norm[1] : 1.f;
-  for_pieces(list, blockIdx.x, [&](const Entry& e, int64_t from, int64_t n) {
+  for_pieces<false>(list, blockIdx.x, [&](const Entry& e, int64_t from, int n) {
     void* to = e.clipped != nullptr ? e.clipped : const_cast<void*>(e.grad);
     if (to == e.grad && f == 1.f) return;
-    if (e.grad_type == DORA_F32)
-      piece_scale(static_cast<const float*>(e.grad) + from, static_cast<float*>(to) + from, n, f);
-    else if (e.grad_type == DORA_BF16)
-      piece_scale(static_cast<const __nv_bfloat16*>(e.grad) + from,
-                  static_cast<__nv_bfloat16*>(to) + from, n, f);
-    else
-      piece_scale(static_cast<const __half*>(e.grad) + from, static_cast<__half*>(to) + from, n,
-                  f);
+    piece_scale(at_elem(e.grad, e.grad_type, from), at_elem(to, e.grad_type, from), e.grad_type, n,
+                f);
   });
 }
 
@@ -302,101 +388,89 @@ __device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamStep& s, f
   *p = fmaf(*p, a.keep, -(s.step_size * *m) / fmaf(sqrtf(*v), s.root_scale, a.eps));
 }
 
-// Four elements of T at an address that is a multiple of their size.
+// Four elements at an address that is a multiple of their size: 16 bytes of fp32, 8
+// (in x and y) of the others.
+__device__ __forceinline__ uint4 load_quad(const void* p, int type, int i) {
+  if (type == DORA_F32) return static_cast<const uint4*>(p)[i];
+  const uint2 q = static_cast<const uint2*>(p)[i];
+  return make_uint4(q.x, q.y, 0u, 0u);
+}
 template <typename T>
-struct Quad {                             // bf16, fp16
-  uint2 q;
-  __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void unpack(float* v) const {
-    float w[8];
-    Granule<T>::unpack(make_uint4(q.x, q.y, 0u, 0u), w);
+__device__ __forceinline__ void unpack_half_granule(uint4 q, float* v) {
+  float w[Granule<T>::kElems];
+  Granule<T>::unpack(q, w);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = w[k];
-  }
-  static __device__ __forceinline__ void store(const float* v, T* p) {
-    *reinterpret_cast<uint2*>(p) =
-        make_uint2(Granule<T>::pair(v[0], v[1]), Granule<T>::pair(v[2], v[3]));
-  }
-};
-template <>
-struct Quad<float> {
-  uint4 q;
-  __device__ __forceinline__ void load(const float* p) { q = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void unpack(float* v) const { Granule<float>::unpack(q, v); }
-  static __device__ __forceinline__ void store(const float* v, float* p) {
-    *reinterpret_cast<uint4*>(p) = Granule<float>::pack(v);
-  }
-};
+  for (int k = 0; k < 4; ++k) v[k] = w[k];
+}
+__device__ __forceinline__ void unpack_quad(uint4 q, int type, float* v) {
+  if (type == DORA_F32) Granule<float>::unpack(q, v);
+  else if (type == DORA_BF16) unpack_half_granule<__nv_bfloat16>(q, v);
+  else unpack_half_granule<__half>(q, v);
+}
 template <typename T>
-__device__ __forceinline__ bool quads(const T* p) {
-  return (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0;
+__device__ __forceinline__ uint2 pack_half_granule(const float* v) {
+  return make_uint2(Granule<T>::pair(v[0], v[1]), Granule<T>::pair(v[2], v[3]));
+}
+__device__ __forceinline__ void store_quad(const float* v, void* p, int type, int i) {
+  if (type == DORA_F32) static_cast<uint4*>(p)[i] = Granule<float>::pack(v);
+  else static_cast<uint2*>(p)[i] = type == DORA_BF16 ? pack_half_granule<__nv_bfloat16>(v)
+                                                     : pack_half_granule<__half>(v);
+}
+__device__ __forceinline__ bool has_quads(const void* p, int type) {
+  return (reinterpret_cast<uintptr_t>(p) & (4 * size_of(type) - 1)) == 0;
 }
 
-template <typename P, typename G>
 __device__ __forceinline__ void piece_adam(const AdamArgs& a, const AdamStep& s, const Entry& e,
-                                           int64_t from, int64_t n) {
+                                           int64_t from, int n) {
   constexpr int kInFlight = 2;
-  P* p = static_cast<P*>(e.param) + from;
-  const G* g = static_cast<const G*>(e.grad) + from;
+  const int gt = e.grad_type, pt = e.param_type;
+  const void* g = at_elem(e.grad, gt, from);
+  void* p = at_elem(e.param, pt, from);
   float *m = e.m + from, *v = e.v + from;
-  __nv_bfloat16* c =
-      e.copy != nullptr ? reinterpret_cast<__nv_bfloat16*>(e.copy) + from : nullptr;
-  int64_t done = 0;
-  if (quads(p) && quads(g) && quads(m) && quads(v) && (c == nullptr || quads(c))) {
-    const int64_t groups = n / 4;
-    done = groups * 4;
-    for (int64_t i = threadIdx.x; i < groups; i += kInFlight * kThreads) {
-      Quad<P> qp[kInFlight];
-      Quad<G> qg[kInFlight];
-      Quad<float> qm[kInFlight], qv[kInFlight];
+  void* c = e.copy != nullptr ? e.copy + from : nullptr;
+  int done = 0;
+  if (has_quads(p, pt) && has_quads(g, gt) && has_quads(m, DORA_F32) && has_quads(v, DORA_F32) &&
+      has_quads(c, DORA_BF16)) {
+    const int quads = n / 4;
+    done = quads * 4;
+    for (int i = quads - 1 - static_cast<int>(threadIdx.x); i >= 0; i -= kInFlight * kThreads) {
+      uint4 qp[kInFlight], qg[kInFlight], qm[kInFlight], qv[kInFlight];
 #pragma unroll
-      for (int u = 0; u < kInFlight; ++u) {
-        const int64_t at = 4 * (i + u * kThreads);
-        if (at < done) {
-          qg[u].load(g + at);
-          qp[u].load(p + at);
-          qm[u].load(m + at);
-          qv[u].load(v + at);
+      for (int u = 0; u < kInFlight; ++u)
+        if (i >= u * kThreads) {
+          qg[u] = load_quad(g, gt, i - u * kThreads);
+          qp[u] = load_quad(p, pt, i - u * kThreads);
+          qm[u] = load_quad(m, DORA_F32, i - u * kThreads);
+          qv[u] = load_quad(v, DORA_F32, i - u * kThreads);
         }
-      }
 #pragma unroll
-      for (int u = 0; u < kInFlight; ++u) {
-        const int64_t at = 4 * (i + u * kThreads);
-        if (at < done) {
+      for (int u = 0; u < kInFlight; ++u)
+        if (i >= u * kThreads) {
           float fp[4], fg[4], fm[4], fv[4];
-          qp[u].unpack(fp);
-          qg[u].unpack(fg);
-          qm[u].unpack(fm);
-          qv[u].unpack(fv);
+          unpack_quad(qp[u], pt, fp);
+          unpack_quad(qg[u], gt, fg);
+          unpack_quad(qm[u], DORA_F32, fm);
+          unpack_quad(qv[u], DORA_F32, fv);
 #pragma unroll
           for (int k = 0; k < 4; ++k) adam_one(a, s, fg[k], fp + k, fm + k, fv + k);
-          Quad<P>::store(fp, p + at);
-          Quad<float>::store(fm, m + at);
-          Quad<float>::store(fv, v + at);
-          if (c != nullptr) Quad<__nv_bfloat16>::store(fp, c + at);
+          store_quad(fp, p, pt, i - u * kThreads);
+          store_quad(fm, m, DORA_F32, i - u * kThreads);
+          store_quad(fv, v, DORA_F32, i - u * kThreads);
+          if (c != nullptr) store_quad(fp, c, DORA_BF16, i - u * kThreads);
         }
-      }
     }
   }
-  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) {
-    float pi = to_float(p[i]), mi = m[i], vi = v[i];
-    adam_one(a, s, to_float(g[i]), &pi, &mi, &vi);
-    from_float(pi, p + i);
+  for (int i = done + threadIdx.x; i < n; i += kThreads) {
+    float pi = load_one(p, pt, i), mi = m[i], vi = v[i];
+    adam_one(a, s, load_one(g, gt, i), &pi, &mi, &vi);
+    store_one(pi, p, pt, i);
     m[i] = mi;
     v[i] = vi;
-    if (c != nullptr) from_float(pi, c + i);
+    if (c != nullptr) store_one(pi, c, DORA_BF16, i);
   }
 }
 
-template <typename P>
-__device__ __forceinline__ void piece_adam_of(const AdamArgs& a, const AdamStep& s, const Entry& e,
-                                              int64_t from, int64_t n) {
-  if (e.grad_type == DORA_F32) piece_adam<P, float>(a, s, e, from, n);
-  else if (e.grad_type == DORA_BF16) piece_adam<P, __nv_bfloat16>(a, s, e, from, n);
-  else piece_adam<P, __half>(a, s, e, from, n);
-}
-
-__global__ void __launch_bounds__(kThreads) adam_step_kernel(List list, AdamArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) adam_step_kernel(List list, AdamArgs a) {
   pdl_wait();
   const AdamState st = *a.state;
   AdamStep s = {1.f, 0.f, 0.f};
@@ -410,10 +484,8 @@ __global__ void __launch_bounds__(kThreads) adam_step_kernel(List list, AdamArgs
   s.step_size = a.lr / static_cast<float>(1. - p1);
   s.root_scale = 1.f / sqrtf(static_cast<float>(1. - p2));
   if (!skip)
-    for_pieces(list, blockIdx.x, [&](const Entry& e, int64_t from, int64_t n) {
-      if (e.param_type == DORA_F32) piece_adam_of<float>(a, s, e, from, n);
-      else if (e.param_type == DORA_BF16) piece_adam_of<__nv_bfloat16>(a, s, e, from, n);
-      else piece_adam_of<__half>(a, s, e, from, n);
+    for_pieces<false>(list, blockIdx.x, [&](const Entry& e, int64_t from, int n) {
+      piece_adam(a, s, e, from, n);
     });
   __syncthreads();                        // every thread of the CTA has read the state
   if (threadIdx.x == 0) {
@@ -456,6 +528,11 @@ bool aligned_to(const void* p, int32_t dtype) {
 
 bool known_type(int32_t t) { return t >= DORA_BF16 && t <= DORA_F32; }
 
+// A tensor's units, with those that count for its begin.
+int64_t units_of(int64_t n) {
+  return n > 0 ? optim::kBegin + (n + optim::kUnit - 1) / optim::kUnit : 0;
+}
+
 // Checks the tensors and counts their units; -1 when one is not valid.
 int64_t count_units(const dora_param* params, int32_t count, int64_t* elements, bool* has_params) {
   int64_t units = 0;
@@ -474,7 +551,7 @@ int64_t count_units(const dora_param* params, int32_t count, int64_t* elements, 
                        !aligned_to(t.exp_avg, DORA_F32) || !aligned_to(t.exp_avg_sq, DORA_F32) ||
                        !aligned_to(t.copy, DORA_BF16)))
       return -1;
-    units += (t.n + optim::kUnit - 1) / optim::kUnit;
+    units += units_of(t.n);
     *elements += t.n;
   }
   return units;
@@ -530,15 +607,16 @@ int dora_param_list_prepare(const dora_param* params, int32_t count, void* data,
   if (e != DORA_OK) return e;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   const optim::List l = layout(data, count, spans_for(units));
-  int64_t first_unit = 0;
+  int64_t unit = 0;
   for (int32_t first = 0; first < count; first += optim::kFill) {
     const int some = count - first < optim::kFill ? count - first : optim::kFill;
     optim::FillArgs args = {};
     for (int i = 0; i < some; ++i) {
       const dora_param& t = params[first + i];
       args.e[i] = optim::Entry{t.grad, t.clipped, t.param, t.exp_avg, t.exp_avg_sq, t.copy, t.n,
-                               first_unit, t.grad_dtype, t.param_dtype};
-      first_unit += (t.n + optim::kUnit - 1) / optim::kUnit;
+                               unit + (t.n > 0 ? optim::kBegin : 0), t.grad_dtype,
+                               t.param_dtype};
+      unit += units_of(t.n);
     }
     const int rc = launched(launch_pdl(optim::fill_entries_kernel, dim3(1), dim3(optim::kFill), 0,
                                        stream, l.header, l.entries, first, some, args));
