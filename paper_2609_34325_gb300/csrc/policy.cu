@@ -35,10 +35,29 @@ constexpr int kThreads = 256;
 constexpr int kMaxVisual = 2048;          // visual tokens per image held in shared memory
 constexpr int kPerThread = kMaxVisual / kThreads;
 
+// A sum as a pair of fp32 values, the second what the first lost (Knuth's two-sum).
+// Six fp32 additions where fp64 has one: fp64 sums over the rows took the kernel on
+// short rows four times as long as the rows (65536 x 96 fp32: 17 us without, 61 with).
+struct Pair {
+  float v, lost;
+  __device__ __forceinline__ void add(float x) {
+    const float t = v + x, b = t - v;
+    lost += (v - (t - b)) + (x - b);
+    v = t;
+  }
+  __device__ __forceinline__ void add(Pair o) {
+    add(o.v);
+    lost += o.lost;
+  }
+};
+__device__ __forceinline__ Pair shfl_xor(Pair p, int off) {
+  return {__shfl_xor_sync(0xffffffffu, p.v, off), __shfl_xor_sync(0xffffffffu, p.lost, off)};
+}
+
 struct Workspace {
   unsigned ticket;                        // CTAs done; zero between calls
   unsigned pad[63];
-  double partial[kMaxCtas][kTerms];
+  Pair partial[kTerms][kMaxCtas];
 };
 
 // What both losses take per action, and the terms' coefficients.
@@ -55,22 +74,13 @@ struct Actions {
 };
 
 // Sums over a thread's rows: loss, policy term, KL, entropy, clipped weight, weight.
-// Each is a pair of fp32 values, the second what the first lost (Knuth's two-sum):
-// fp64 additions, six a row in one thread, would cost its warp more than the row.
 struct Sums {
-  float v[kTerms], lost[kTerms];
+  Pair v[kTerms];
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) v[i] = lost[i] = 0.f;
+    for (int i = 0; i < kTerms; ++i) v[i] = Pair{0.f, 0.f};
   }
-  __device__ __forceinline__ void add(int i, float x) {
-    const float t = v[i] + x, b = t - v[i];
-    lost[i] += (v[i] - (t - b)) + (x - b);
-    v[i] = t;
-  }
-  __device__ __forceinline__ double get(int i) const {
-    return static_cast<double>(v[i]) + lost[i];
-  }
+  __device__ __forceinline__ void add(int i, float x) { v[i].add(x); }
 };
 
 // One row's loss from l - q, x = q_ref - l and the entropy h; returns g.  A NaN
@@ -109,11 +119,17 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
 // depend on which one that is, and leaves the ticket at zero for the next call.
 __device__ __forceinline__ void finish_totals(const Actions& p, const Sums& sums) {
   if (p.totals == nullptr) return;
+  if (gridDim.x == 1) {
+    if (threadIdx.x == 0)
+#pragma unroll
+      for (int i = 0; i < kTerms; ++i) p.totals[i] = sums.v[i].v + sums.v[i].lost;
+    return;
+  }
   __shared__ bool last;
   Workspace* ws = p.ws;
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) ws->partial[blockIdx.x][i] = sums.get(i);
+    for (int i = 0; i < kTerms; ++i) ws->partial[i][blockIdx.x] = sums.v[i];
     __threadfence();
     last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
   }
@@ -122,12 +138,14 @@ __device__ __forceinline__ void finish_totals(const Actions& p, const Sums& sums
   __threadfence();
   const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   for (int i = threadIdx.x >> 5; i < kTerms; i += warps) {
-    double t = 0.;
-    for (int c = lane; c < static_cast<int>(gridDim.x); c += 32)
-      t += __ldcg(&ws->partial[c][i]);
+    Pair t = {0.f, 0.f};
+    for (int c = lane; c < static_cast<int>(gridDim.x); c += 32) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(&ws->partial[i][c]));
+      t.add(Pair{x.x, x.y});
+    }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-    if (lane == 0) p.totals[i] = static_cast<float>(t);
+    for (int off = 16; off > 0; off >>= 1) t.add(shfl_xor(t, off));
+    if (lane == 0) p.totals[i] = t.v + t.lost;
   }
   if (threadIdx.x == 0) ws->ticket = 0;
 }
@@ -221,6 +239,19 @@ struct RowPtr {
       q = Granule<T>::pack(v);            // exact: the values come from T
     }
     return q;
+  }
+  // kHeld granules from i on, kStep apart.
+  template <int kHeld, int kStep>
+  __device__ __forceinline__ void load_all(int i, int n, uint4* q) const {
+    const int c = i * kE - mis;
+    if (c >= 0 && c + ((kHeld - 1) * kStep + 1) * kE <= n) {
+      const uint4* g = reinterpret_cast<const uint4*>(z + c);
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) q[u] = g[u * kStep];
+    } else {
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) q[u] = load(i + u * kStep, n);
+    }
   }
   // Values of granule i into the row at `to` of `classes` elements, 0 from n on.
   __device__ __forceinline__ void store(T* to, bool aligned, int i, int n, int classes,
@@ -322,23 +353,36 @@ __device__ __forceinline__ bool same_alignment(const void* a, const void* b) {
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// The CTA's sums are those of its first `holders` times `stride` threads.
-template <int kStride, int kBlock>
+// Thread 0 gets the sums of all threads that are a multiple of kStride (the others'
+// are zero).
+template <int kStride>
 __device__ __forceinline__ void gather_sums(const Actions& p, Sums* sums) {
-  if (p.totals == nullptr || kBlock == kStride) return;
-  __shared__ double all[kBlock / kStride][kTerms];
-  if (threadIdx.x % kStride == 0)
+  if (p.totals == nullptr) return;
+  __shared__ Pair all[kTerms][kThreads / 32];
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) all[threadIdx.x / kStride][i] = sums->get(i);
+  for (int i = 0; i < kTerms; ++i) {
+    Pair t = sums->v[i];
+#pragma unroll
+    for (int off = 16; off >= kStride; off >>= 1) t.add(shfl_xor(t, off));
+    if ((threadIdx.x & 31) == 0) all[i][threadIdx.x >> 5] = t;
+  }
   __syncthreads();
-  if (threadIdx.x == 0)
+  if (threadIdx.x < 32) {                 // lane: warp (low bits) of terms 0..3, then of 4, 5
+    static_assert(kThreads / 32 == 8 && kTerms == 6, "eight warps in groups of eight lanes");
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) {
-      double t = 0.;
-      for (int k = 0; k < kBlock / kStride; ++k) t += all[k][i];
-      sums->v[i] = static_cast<float>(t);
-      sums->lost[i] = static_cast<float>(t - sums->v[i]);
+    for (int half = 0; half < 2; ++half) {
+      const int i = 4 * half + (threadIdx.x >> 3);
+      Pair t = i < kTerms ? all[i][threadIdx.x & 7] : Pair{0.f, 0.f};
+#pragma unroll
+      for (int off = 4; off > 0; off >>= 1) t.add(shfl_xor(t, off));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const Pair o = {__shfl_sync(0xffffffffu, t.v, 8 * k),
+                        __shfl_sync(0xffffffffu, t.lost, 8 * k)};
+        if (4 * half + k < kTerms) sums->v[4 * half + k] = o;
+      }
     }
+  }
 }
 
 // Short rows: kLanes lanes of a warp hold one, kHeld granules each.
@@ -362,8 +406,7 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
     const RowPtr<T> z(r.logits + (exists ? row : 0) * r.ld);
     const float za = n > 0 ? to_float(z.z[in.action]) : 0.f;
     uint4 q[kHeld];
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) q[i] = z.load(lane + i * kLanes, n);
+    z.template load_all<kHeld, kLanes>(lane, n, q);
     const RowIn next = row_in(r, p, row + step);
     float m = -INFINITY, s = 0.f, t = 0.f;
 #pragma unroll
@@ -406,7 +449,7 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
     }
     in = next;
   }
-  gather_sums<kLanes, kThreads>(p, &sums);
+  gather_sums<kLanes>(p, &sums);
   finish_totals(p, sums);
 }
 
@@ -491,8 +534,7 @@ __global__ void __launch_bounds__(kBlock, kHeld > 4 ? 2 : (kBlock > 128 ? 3 : 10
     if (takes && !bad) {
       const float za = to_float(z.z[in.action]);
       uint4 q[kHeld];
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) q[i] = z.load(g0 + i * kBlock, in.n);
+      z.template load_all<kHeld, kBlock>(g0, in.n, q);
       Part part = {-INFINITY, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kHeld; ++i) part.m = fmaxf(part.m, Granule<T>::largest(q[i]));
@@ -511,13 +553,25 @@ __global__ void __launch_bounds__(kBlock, kHeld > 4 ? 2 : (kBlock > 128 ? 3 : 10
       parity ^= 1;
       const RowGrad k =
           finish_row(r, p, in, row, za, part.m, part.s, part.t, z.mis, leader, &sums);
-      if (dz != nullptr)
+      if (dz != nullptr) {
+        const int c = g0 * Granule<T>::kElems - z.mis;
+        if (aligned && c >= 0 && c + ((kHeld - 1) * kBlock + 1) * Granule<T>::kElems <= in.n) {
+          uint4* to = reinterpret_cast<uint4*>(dz + c);
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-          float v[Granule<T>::kElems];
-          grad_granule<T>(q[i], k, g0 + i * kBlock, v);
-          z.store(dz, aligned, g0 + i * kBlock, in.n, r.classes, v);
+          for (int i = 0; i < kHeld; ++i) {
+            float v[Granule<T>::kElems];
+            grad_granule<T>(q[i], k, g0 + i * kBlock, v);
+            to[i * kBlock] = Granule<T>::pack(v);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kHeld; ++i) {
+            float v[Granule<T>::kElems];
+            grad_granule<T>(q[i], k, g0 + i * kBlock, v);
+            z.store(dz, aligned, g0 + i * kBlock, in.n, r.classes, v);
+          }
         }
+      }
     } else {
       const float fill = bad ? NAN : 0.f;
       if (leader) fill_row(r, p, row, fill, &sums);
@@ -564,8 +618,7 @@ __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, A
       Part part = {-INFINITY, 0.f, 0.f, 0.f};
       for (int i = g0; i < granules; i += kStride * kLongStep) {
         uint4 q[kLongStep];
-#pragma unroll
-        for (int u = 0; u < kLongStep; ++u) q[u] = z.load(i + u * kStride, in.n);
+        z.template load_all<kLongStep, kStride>(i, in.n, q);
         float m = part.m;
 #pragma unroll
         for (int u = 0; u < kLongStep; ++u) m = fmaxf(m, Granule<T>::largest(q[u]));
