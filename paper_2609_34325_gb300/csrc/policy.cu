@@ -19,6 +19,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "dora.h"
 #include "dora_ptx.cuh"
 #include "granule.cuh"
@@ -28,7 +30,6 @@ namespace dora {
 namespace policy {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTerms = 6;                 // sums over the rows, in the order of `totals`
 constexpr int kMaxCtas = 152 * 16;        // partial sums that the workspace holds
 constexpr int kThreads = 256;
@@ -73,21 +74,23 @@ struct Actions {
   Workspace* ws;                          // used with totals
 };
 
-// Sums over a thread's rows: loss, policy term, KL, entropy, clipped weight, weight.
-struct Sums {
-  Pair v[kTerms];
-  __device__ __forceinline__ void clear() {
+// The terms that a row adds to the totals: loss, policy term, KL, entropy, clipped
+// weight, weight.  They are counted by six lanes, each its own.
+struct Terms {
+  float v[kTerms];
+  __device__ __forceinline__ float of(int lane) const {
+    float x = v[0];
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) v[i] = Pair{0.f, 0.f};
+    for (int i = 1; i < kTerms; ++i) x = lane == i ? v[i] : x;
+    return lane < kTerms ? x : 0.f;
   }
-  __device__ __forceinline__ void add(int i, float x) { v[i].add(x); }
 };
+__device__ __forceinline__ Terms all_terms(float x) { return {{x, x, x, x, x, x}}; }
 
 // One row's loss from l - q, x = q_ref - l and the entropy h; returns g.  A NaN
-// ratio is left to spread (comparisons, no fmin).  `sums` of the one thread that
-// counts the row, null for the others.
+// ratio is left to spread (comparisons, no fmin).
 __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, float x, float adv,
-                                           float w, float h, float* loss, Sums* sums) {
+                                           float w, float h, Terms* terms) {
   const float ratio = expf(log_ratio);
   const float lo = 1.f - p.clip_low, hi = 1.f + p.clip_high;
   const float cut = (ratio < lo ? lo : (ratio > hi ? hi : ratio)) * adv;
@@ -102,36 +105,29 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   }
   float row = fmaf(p.kl_coef, kl, surrogate);
   if (p.entropy_coef != 0.f) row = fmaf(-p.entropy_coef, h, row);
-  row *= w;
-  *loss = row;
-  if (sums == nullptr) return g * w;
-  sums->add(0, row);
-  sums->add(1, w * surrogate);
-  sums->add(2, w * kl);
-  sums->add(3, w * h);
-  sums->add(4, inside ? 0.f : w);
-  sums->add(5, w);
+  *terms = Terms{{w * row, w * surrogate, w * kl, w * h, inside ? 0.f : w, w}};
   return g * w;
 }
 
-// The CTA's sums (held by thread 0) go to its place in the workspace; the CTA that
-// is last adds all of them in the order of the CTAs, so that the totals do not
-// depend on which one that is, and leaves the ticket at zero for the next call.
-__device__ __forceinline__ void finish_totals(const Actions& p, const Sums& sums) {
+// The totals.  Lanes i < kTerms of a CTA's first warp hold its sum of term i.  It goes
+// to the CTA's place in the workspace; the CTA that is last adds all of them in the
+// order of the CTAs, so that the totals do not depend on which one that is, and leaves
+// the ticket at zero for the next call.
+__device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   if (p.totals == nullptr) return;
   if (gridDim.x == 1) {
-    if (threadIdx.x == 0)
-#pragma unroll
-      for (int i = 0; i < kTerms; ++i) p.totals[i] = sums.v[i].v + sums.v[i].lost;
+    if (threadIdx.x < kTerms) p.totals[threadIdx.x] = sum.v + sum.lost;
     return;
   }
   __shared__ bool last;
   Workspace* ws = p.ws;
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int i = 0; i < kTerms; ++i) ws->partial[i][blockIdx.x] = sums.v[i];
-    __threadfence();
-    last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+  if (threadIdx.x < 32) {
+    if (threadIdx.x < kTerms) {
+      ws->partial[threadIdx.x][blockIdx.x] = sum;
+      __threadfence();
+    }
+    __syncwarp();
+    if (threadIdx.x == 0) last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
   }
   __syncthreads();
   if (!last) return;
@@ -164,11 +160,14 @@ __device__ __forceinline__ F block_sum(F v, F* scratch) {
 }
 
 // ---------------------------------------------------------------------------
-// Categorical actions.  A row is read once into registers, as 16-byte granules,
-// by the lanes of a warp, a CTA or a cluster of CTAs; from there come its maximum
-// m, its sums s = sum e^{z - m} and t = sum e^{z - m} (z - m), and the gradient:
-//   p_j = e^{z_j - m} / s,  H = log s - t / s,
-//   d loss / d z_j = g (1(j = a) - p_j) + w c p_j (log p_j + H).
+// Categorical actions.  A row is read once, as 16-byte granules, by a group of lanes,
+// a CTA or a cluster of CTAs; from there come its sums and its gradient.  With m the
+// largest logit, d_j = z_j - m and e_j = e^{d_j} (the difference first: the largest has
+// e = 1 to the last bit, and an action that is certain log-probability and gradient 0):
+//   s = sum e_j,  t = sum e_j d_j,
+//   l = (z_a - m) - ln s,  H = ln s - t / s,  p_j = e_j / s,
+//   d loss / d z_j = g (1(j = a) - p_j) + w c_H p_j (log p_j + H)
+//                  = e_j (a + b d_j) + g 1(j = a).
 // Rows start at any alignment: granules are aligned in memory, `mis` elements of
 // the first belong to what lies before the row, and a granule that is not wholly
 // inside is loaded and stored by its elements.
@@ -185,24 +184,34 @@ struct Rows {
   int32_t* status;
 };
 
-// A row's scalars, loaded while the row before is worked on.
-struct RowIn {
+// Whether a row takes part, and how many of its logits are legal (-1: not valid).
+struct RowUse {
   int action, n;
-  float w, old_logp, adv, ref;
+  bool takes;
 };
 
 template <typename T>
-__device__ __forceinline__ RowIn row_in(const Rows<T>& r, const Actions& p, int row) {
-  RowIn in = {-1, 0, 0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ RowUse row_use(const Rows<T>& r, const Actions& p, int row) {
+  RowUse u = {-1, 0, false};
   if (row < r.rows) {
-    in.action = r.actions[row];
-    in.w = p.weights != nullptr ? p.weights[row] : 1.f;
-    in.n = r.legal != nullptr ? r.legal[row] : r.classes;
-    in.old_logp = p.old_logp[row];
-    in.adv = p.advantages[row];
-    in.ref = p.ref_logp != nullptr ? p.ref_logp[row] : 0.f;
+    u.action = r.actions[row];
+    const float w = p.weights != nullptr ? p.weights[row] : 1.f;
+    u.n = r.legal != nullptr ? r.legal[row] : r.classes;
+    u.takes = u.action >= 0 && w != 0.f;
+    if (u.n < 0 || u.n > r.classes || u.action >= u.n) u.n = -1;
   }
-  return in;
+  return u;
+}
+__device__ __forceinline__ bool computed(const RowUse& u) { return u.takes && u.n > 0; }
+
+// The other scalars of a row that takes part.
+struct RowIn {
+  float w, old_logp, adv, ref;
+};
+__device__ __forceinline__ RowIn row_in(const Actions& p, int row, int rows) {
+  if (row >= rows) return {0.f, 0.f, 0.f, 0.f};
+  return {p.weights != nullptr ? p.weights[row] : 1.f, p.old_logp[row], p.advantages[row],
+          p.ref_logp != nullptr ? p.ref_logp[row] : 0.f};
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -211,58 +220,52 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// e^d for a difference d <= 0 of logits.
-__device__ __forceinline__ float exp_of(float d) { return ex2(d * kLog2e); }
+constexpr float kFloor = -1e30f;          // e^kFloor is 0: keeps 0 * inf out of e d
 
-constexpr float kFloor = -200.f;          // below it e^d is 0: keeps 0 * inf out of e^d * d
-
+// A row's granules.  [whole_lo, whole_hi): those that lie wholly in its first n
+// elements.
 template <typename T>
 struct RowPtr {
   static constexpr int kE = Granule<T>::kElems;
   const T* z;                             // the row's first element
   int mis;                                // elements of its first granule before it
-  __device__ __forceinline__ explicit RowPtr(const T* p)
-      : z(p), mis(static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {}
-
-  // Granule i of the row, elements outside [0, n) as -inf.
-  __device__ __forceinline__ uint4 load(int i, int n) const {
-    const int c = i * kE - mis;
-    if (c >= 0 && c + kE <= n) return *reinterpret_cast<const uint4*>(z + c);
-    constexpr uint32_t kNone = Granule<T>::kNegInfWord;
-    uint4 q = make_uint4(kNone, kNone, kNone, kNone);
-    if (c < n) {
-      float v[kE];
-      Granule<T>::unpack(q, v);
-#pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (c + e >= 0 && c + e < n) v[e] = to_float(z[c + e]);
-      q = Granule<T>::pack(v);            // exact: the values come from T
-    }
-    return q;
+  int whole_lo, whole_hi;
+  __device__ __forceinline__ RowPtr(const T* p, int n)
+      : z(p), mis(static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {
+    whole_lo = mis > 0 ? 1 : 0;
+    whole_hi = (n + mis) / kE;
   }
-  // kHeld granules from i on, kStep apart.
-  template <int kHeld, int kStep>
-  __device__ __forceinline__ void load_all(int i, int n, uint4* q) const {
-    const int c = i * kE - mis;
-    if (c >= 0 && c + ((kHeld - 1) * kStep + 1) * kE <= n) {
-      const uint4* g = reinterpret_cast<const uint4*>(z + c);
-#pragma unroll
-      for (int u = 0; u < kHeld; ++u) q[u] = g[u * kStep];
-    } else {
-#pragma unroll
-      for (int u = 0; u < kHeld; ++u) q[u] = load(i + u * kStep, n);
-    }
+  __device__ __forceinline__ bool whole(int i) const { return i >= whole_lo && i < whole_hi; }
+  __device__ __forceinline__ int granules(int classes) const {
+    return (classes + mis + kE - 1) / kE;
   }
-  // Values of granule i into the row at `to` of `classes` elements, 0 from n on.
-  __device__ __forceinline__ void store(T* to, bool aligned, int i, int n, int classes,
-                                        float* v) const {
+  __device__ __forceinline__ const uint4* at(int i) const {
+    return reinterpret_cast<const uint4*>(z - mis) + i;
+  }
+  // The granules of a row that starts like this one.
+  __device__ __forceinline__ uint4* as_granules(T* to) const {
+    return reinterpret_cast<uint4*>(to - mis);
+  }
+  // Granule i of the row by its elements, those outside [0, n) as -inf.
+  __device__ __forceinline__ uint4 load_part(int i, int n) const {
     const int c = i * kE - mis;
-    if (c >= classes) return;
+    float v[kE];
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      v[e] = c + e >= 0 && c + e < n ? to_float(z[c + e]) : -INFINITY;
+    return Granule<T>::pack(v);           // exact: the values come from T
+  }
+  // Granule i into the row at `to` of `classes` elements, 0 from n on.
+  __device__ __forceinline__ void store_part(T* to, bool aligned, int i, int n, int classes,
+                                             uint4 q) const {
+    const int c = i * kE - mis;
+    float v[kE];
+    Granule<T>::unpack(q, v);
 #pragma unroll
     for (int e = 0; e < kE; ++e)
       if (c + e >= n) v[e] = 0.f;
     if (aligned && c >= 0 && c + kE <= classes) {
-      *reinterpret_cast<uint4*>(to + c) = Granule<T>::pack(v);
+      *reinterpret_cast<uint4*>(to + c) = Granule<T>::pack(v);   // exact: values of T
     } else {
 #pragma unroll
       for (int e = 0; e < kE; ++e)
@@ -271,118 +274,185 @@ struct RowPtr {
   }
 };
 
-// Sums of e^{z - m} and e^{z - m} (z - m) over one granule.  An m of -inf (nothing
-// but -inf so far) counts as 0, so that its terms are 0 and not NaN.
+// The elements of a granule less m: 16-bit ones by mixed additions, without a
+// conversion before.
 template <typename T>
-__device__ __forceinline__ void add_exps(uint4 q, float m, float* s, float* t) {
-  constexpr int kE = Granule<T>::kElems;
-  float v[kE];
-  Granule<T>::unpack(q, v);
+__device__ __forceinline__ void differences(uint4 q, float minus_m, float* d);
+template <>
+__device__ __forceinline__ void differences<float>(uint4 q, float minus_m, float* d) {
+  Granule<float>::unpack(q, d);
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    const float d = v[e] - m, x = exp_of(d);
-    *s += x;
-    *t = fmaf(x, fmaxf(d, kFloor), *t);
-  }
+  for (int e = 0; e < 4; e += 2)
+    f2_unpack(f2_add(f2_pack(d[e], d[e + 1]), f2_pack(minus_m, minus_m)), d[e], d[e + 1]);
 }
+template <>
+__device__ __forceinline__ void differences<__nv_bfloat16>(uint4 q, float minus_m, float* d) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "mov.b32 {lo, hi}, %2;\n\t"
+        "add.f32.bf16 %0, lo, %3;\n\t"
+        "add.f32.bf16 %1, hi, %3;\n\t}"
+        : "=f"(d[2 * e]), "=f"(d[2 * e + 1])
+        : "r"(w[e]), "f"(minus_m));
+}
+template <>
+__device__ __forceinline__ void differences<__half>(uint4 q, float minus_m, float* d) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "mov.b32 {lo, hi}, %2;\n\t"
+        "add.f32.f16 %0, lo, %3;\n\t"
+        "add.f32.f16 %1, hi, %3;\n\t}"
+        : "=f"(d[2 * e]), "=f"(d[2 * e + 1])
+        : "r"(w[e]), "f"(minus_m));
+}
+
+// e^d of two differences.
+__device__ __forceinline__ uint64_t exps_of(float d0, float d1) {
+  float x0, x1;
+  f2_unpack(f2_mul(f2_pack(d0, d1), f2_pack(kLog2e, kLog2e)), x0, x1);
+  return f2_pack(ex2(x0), ex2(x1));
+}
+
+// An m of -inf (nothing but -inf so far) counts as 0: its terms are 0 and not NaN.
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ float warp_max(float v, int lanes) {
+  for (int off = lanes / 2; off > 0; off >>= 1)
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v, int lanes) {
+  for (int off = lanes / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
+
+// (m, s, t) of a part of a row, and the action's logit where it is known.
+// Stored 16 bytes at once, also into other CTAs' shared memory: aligned to them.
+struct alignas(16) Part {
+  float m, s, t, za;
+};
+static_assert(sizeof(Part) == 16 && alignof(Part) == 16, "one 16-byte store");
+
+// Adds a part to sums whose largest logit is m.
+__device__ __forceinline__ void add_part(const Part& h, float m, float* s, float* t) {
+  if (h.m == -INFINITY && h.s == 0.f) return;             // a NaN sum is taken along
+  const float d = h.m - m, x = ex2(d * kLog2e);
+  *s = fmaf(h.s, x, *s);
+  *t = fmaf(fmaf(h.s, fmaxf(d, kFloor), h.t), x, *t);
+}
+
+// A thread's running sums, in pairs: what it has is brought to the new largest logit,
+// then the new granules are added.
+struct RowSum {
+  float m;
+  uint64_t s, t;
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    s = t = 0;
+  }
+  template <typename T, int kN>
+  __device__ __forceinline__ void add(const uint4 (&q)[kN]) {
+    constexpr int kE = Granule<T>::kElems;
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < kN; ++u) top = fmaxf(top, Granule<T>::largest(q[u]));
+    const float base = base_of(top), d0 = fmaxf(m - base, kFloor), x0 = ex2(d0 * kLog2e);
+    const uint64_t x = f2_pack(x0, x0);
+    t = f2_mul(f2_fma(s, f2_pack(d0, d0), t), x);
+    s = f2_mul(s, x);
+    m = top;
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      float d[kE];
+      differences<T>(q[u], -base, d);
+#pragma unroll
+      for (int e = 0; e < kE; e += 2) {
+        const uint64_t p = exps_of(d[e], d[e + 1]);
+        s = f2_add(s, p);
+        t = f2_fma(p, f2_pack(fmaxf(d[e], kFloor), fmaxf(d[e + 1], kFloor)), t);
+      }
+    }
+  }
+  // The sums of `lanes` lanes, in all of them.
+  __device__ __forceinline__ Part over(int lanes) const {
+    float s0, s1, t0, t1;
+    f2_unpack(s, s0, s1);
+    f2_unpack(t, t0, t1);
+    const float top = warp_max(m, lanes);
+    const float d = fmaxf(m - base_of(top), kFloor), x = ex2(d * kLog2e);
+    const float sum = s0 + s1;
+    return {top, warp_sum(sum * x, lanes), warp_sum(fmaf(sum, d, t0 + t1) * x, lanes), 0.f};
+  }
+};
 
 // What the gradient of a row needs.
 struct RowGrad {
-  float m, a, b, g;                       // d loss / d z = e^{z - m} (a + b (z - m)) + g 1(j = a)
-  int granule, element;                   // of the action
+  float m, a, b, at_action;               // e^{z - m} (a + b (z - m)); the action's own
 };
 
-template <typename T>
-__device__ __forceinline__ void grad_granule(uint4 q, const RowGrad& k, int i, float* v) {
+template <typename T, bool kEntropy>
+__device__ __forceinline__ uint4 grad_granule(uint4 q, const RowGrad& k) {
   constexpr int kE = Granule<T>::kElems;
-  Granule<T>::unpack(q, v);
-  if (k.b == 0.f) {
+  float d[kE];
+  differences<T>(q, -k.m, d);
+  const uint64_t a = f2_pack(k.a, k.a), b = f2_pack(k.b, k.b);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = exp_of(v[e] - k.m) * k.a;
-  } else {
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const float d = v[e] - k.m;
-      v[e] = exp_of(d) * fmaf(k.b, fmaxf(d, kFloor), k.a);
-    }
+  for (int e = 0; e < kE; e += 2) {
+    const uint64_t p = exps_of(d[e], d[e + 1]);
+    const uint64_t f =
+        kEntropy ? f2_fma(f2_pack(fmaxf(d[e], kFloor), fmaxf(d[e + 1], kFloor)), b, a) : a;
+    f2_unpack(f2_mul(p, f), d[e], d[e + 1]);
   }
-  if (i == k.granule) {
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (e == k.element) v[e] += k.g;
-  }
+  return Granule<T>::pack(d);
+}
+template <typename T>
+__device__ __forceinline__ uint4 grad_granule(uint4 q, const RowGrad& k) {
+  return k.b == 0.f ? grad_granule<T, false>(q, k) : grad_granule<T, true>(q, k);
 }
 
-// The row's outputs and what its gradient needs, from m, s, t and the action's logit;
-// `leader` writes and counts.
+// The row's outputs, its terms and what its gradient needs, from the row's sums and
+// the action's logit; `leader` writes.
 template <typename T>
 __device__ __forceinline__ RowGrad finish_row(const Rows<T>& r, const Actions& p, const RowIn& in,
-                                              int row, float za, float m, float s, float t,
-                                              int mis, bool leader, Sums* sums) {
-  constexpr int kE = Granule<T>::kElems;
-  const float ls = logf(s), inv = 1.f / s, h = ls - t * inv;
-  const float lp = (za - m) - ls;
-  float loss;
-  const float g = row_terms(p, lp - in.old_logp, in.ref - lp, in.adv, in.w, h, &loss,
-                            leader ? sums : nullptr);
+                                              int row, float za, const Part& x, bool leader,
+                                              Terms* terms) {
+  const float ls = logf(x.s), inv = 1.f / x.s, h = fmaf(-x.t, inv, ls);
+  const float da = za - x.m, lp = da - ls;
+  const float g = row_terms(p, lp - in.old_logp, in.ref - lp, in.adv, in.w, h, terms);
   if (leader) {
     p.logp[row] = lp;
     if (r.entropy != nullptr) r.entropy[row] = h;
-    if (p.row_loss != nullptr) p.row_loss[row] = loss;
+    if (p.row_loss != nullptr) p.row_loss[row] = terms->v[0];
   }
   const float cw = in.w * p.entropy_coef;
-  return RowGrad{m, (cw * (h - ls) - g) * inv, cw * inv, g, (in.action + mis) / kE,
-                 (in.action + mis) % kE};
+  const float a = (cw * (h - ls) - g) * inv, b = cw * inv;
+  return RowGrad{x.m, a, b, fmaf(ex2(da * kLog2e), fmaf(b, fmaxf(da, kFloor), a), g)};
 }
 
-// A row that takes no part (0) or is not valid (NaN).
+// The outputs of a row that takes no part (0) or is not valid (NaN).
 template <typename T>
-__device__ __forceinline__ void fill_row(const Rows<T>& r, const Actions& p, int row, float fill,
-                                         Sums* sums) {
-  if (fill != 0.f) {
-    record_status(r.status, DORA_ERR_DEVICE_BAD_COUNT);
-    for (int i = 0; i < kTerms; ++i) sums->add(i, fill);
-  }
+__device__ __forceinline__ void fill_row(const Rows<T>& r, const Actions& p, int row, float fill) {
+  if (fill != 0.f) record_status(r.status, DORA_ERR_DEVICE_BAD_COUNT);
   p.logp[row] = fill;
   if (r.entropy != nullptr) r.entropy[row] = fill;
   if (p.row_loss != nullptr) p.row_loss[row] = fill;
 }
 
-__device__ __forceinline__ bool same_alignment(const void* a, const void* b) {
-  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
+template <typename T>
+__device__ __forceinline__ void fill_granule(const RowPtr<T>& z, T* dz, bool aligned, int i,
+                                             int classes, float fill) {
+  float v[Granule<T>::kElems];
+#pragma unroll
+  for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
+  z.store_part(dz, aligned, i, classes, classes, Granule<T>::pack(v));
 }
 
-// Thread 0 gets the sums of all threads that are a multiple of kStride (the others'
-// are zero).
-template <int kStride>
-__device__ __forceinline__ void gather_sums(const Actions& p, Sums* sums) {
-  if (p.totals == nullptr) return;
-  __shared__ Pair all[kTerms][kThreads / 32];
-#pragma unroll
-  for (int i = 0; i < kTerms; ++i) {
-    Pair t = sums->v[i];
-#pragma unroll
-    for (int off = 16; off >= kStride; off >>= 1) t.add(shfl_xor(t, off));
-    if ((threadIdx.x & 31) == 0) all[i][threadIdx.x >> 5] = t;
-  }
-  __syncthreads();
-  if (threadIdx.x < 32) {                 // lane: warp (low bits) of terms 0..3, then of 4, 5
-    static_assert(kThreads / 32 == 8 && kTerms == 6, "eight warps in groups of eight lanes");
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int i = 4 * half + (threadIdx.x >> 3);
-      Pair t = i < kTerms ? all[i][threadIdx.x & 7] : Pair{0.f, 0.f};
-#pragma unroll
-      for (int off = 4; off > 0; off >>= 1) t.add(shfl_xor(t, off));
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const Pair o = {__shfl_sync(0xffffffffu, t.v, 8 * k),
-                        __shfl_sync(0xffffffffu, t.lost, 8 * k)};
-        if (4 * half + k < kTerms) sums->v[4 * half + k] = o;
-      }
-    }
-  }
+__device__ __forceinline__ bool same_alignment(const void* a, const void* b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
 // Short rows: kLanes lanes of a warp hold one, kHeld granules each.
@@ -392,96 +462,93 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
   pdl_wait();
   const int lane = threadIdx.x % kLanes;
   const int step = gridDim.x * kRowsPerCta;
-  Sums sums;
-  sums.clear();
+  Pair sum = {0.f, 0.f};
   // the loop is the same for all groups of a warp: shuffles need every lane
   const int first = blockIdx.x * kRowsPerCta + (threadIdx.x / 32) * (32 / kLanes);
   int row = first + (threadIdx.x % 32) / kLanes;
-  RowIn in = row_in(r, p, row);
+  RowUse use = row_use(r, p, row);
   for (int base = first; base < r.rows; base += step, row += step) {
-    const bool exists = row < r.rows;
-    const bool takes = exists && in.action >= 0 && in.w != 0.f;
-    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
-    const int n = takes && !bad ? in.n : 0;
-    const RowPtr<T> z(r.logits + (exists ? row : 0) * r.ld);
-    const float za = n > 0 ? to_float(z.z[in.action]) : 0.f;
+    const bool exists = row < r.rows, live = computed(use);
+    const int n = live ? use.n : 0;
+    const RowPtr<T> z(r.logits + (exists ? row : 0) * r.ld, n);
     uint4 q[kHeld];
-    z.template load_all<kHeld, kLanes>(lane, n, q);
-    const RowIn next = row_in(r, p, row + step);
-    float m = -INFINITY, s = 0.f, t = 0.f;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) m = fmaxf(m, Granule<T>::largest(q[i]));
-#pragma unroll
-    for (int off = kLanes / 2; off > 0; off >>= 1)
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) add_exps<T>(q[i], m, &s, &t);
-#pragma unroll
-    for (int off = kLanes / 2; off > 0; off >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, off);
-      t += __shfl_xor_sync(0xffffffffu, t, off);
+    for (int u = 0; u < kHeld; ++u) {
+      const int i = lane + u * kLanes;
+      if (z.whole(i)) q[u] = *z.at(i);
+      else q[u] = z.load_part(i, n);
     }
+    RowIn in = {0.f, 0.f, 0.f, 0.f};
+    float za = 0.f;
+    if (live) {
+      in = row_in(p, row, r.rows);
+      za = to_float(z.z[use.action]);
+    }
+    const RowUse next = row_use(r, p, row + step);
+    RowSum x;
+    x.clear();
+    x.add<T>(q);
+    const Part part = x.over(kLanes);
     __syncwarp();                         // every lane has read its logits: grad may be logits
     if (exists) {
       T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
       const bool aligned = dz != nullptr && same_alignment(dz, z.z);
-      if (n > 0) {
-        const RowGrad k = finish_row(r, p, in, row, za, m, s, t, z.mis, lane == 0, &sums);
-        if (dz != nullptr)
+      const int end = z.granules(r.classes);
+      if (live) {
+        Terms terms;
+        const RowGrad k = finish_row(r, p, in, row, za, part, lane == 0, &terms);
+        sum.add(terms.of(lane));
+        if (dz != nullptr) {
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i) {
-            float v[Granule<T>::kElems];
-            grad_granule<T>(q[i], k, lane + i * kLanes, v);
-            z.store(dz, aligned, lane + i * kLanes, n, r.classes, v);
+          for (int u = 0; u < kHeld; ++u) {
+            const int i = lane + u * kLanes;
+            if (i >= end) continue;
+            const uint4 v = grad_granule<T>(q[u], k);
+            if (aligned && z.whole(i)) *(z.as_granules(dz) + i) = v;
+            else z.store_part(dz, aligned, i, n, r.classes, v);
           }
+          // the lane that has stored the action's granule
+          if (((use.action + z.mis) / z.kE) % kLanes == lane)
+            from_float(k.at_action, dz + use.action);
+        }
       } else {
-        const float fill = bad ? NAN : 0.f;
-        if (lane == 0) fill_row(r, p, row, fill, &sums);
+        const float fill = use.takes ? NAN : 0.f;
+        if (lane == 0) fill_row(r, p, row, fill);
+        sum.add(all_terms(fill).of(lane));
         if (dz != nullptr)
-#pragma unroll
-          for (int i = 0; i < kHeld; ++i) {
-            float v[Granule<T>::kElems];
-#pragma unroll
-            for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
-            z.store(dz, aligned, lane + i * kLanes, r.classes, r.classes, v);
-          }
+          for (int i = lane; i < end; i += kLanes) fill_granule(z, dz, aligned, i, r.classes, fill);
       }
     }
-    in = next;
+    use = next;
   }
-  gather_sums<kLanes>(p, &sums);
-  finish_totals(p, sums);
+  if (p.totals == nullptr) return;
+  // lane i of every group holds its term i: groups of a warp, then warps
+  __shared__ Pair all[kThreads / 32][kTerms];
+#pragma unroll
+  for (int off = 16; off >= kLanes; off >>= 1) sum.add(shfl_xor(sum, off));
+  if ((threadIdx.x & 31) < kTerms) all[threadIdx.x >> 5][threadIdx.x & 31] = sum;
+  __syncthreads();
+  if (threadIdx.x < kTerms)
+#pragma unroll
+    for (int k = 1; k < kThreads / 32; ++k) sum.add(all[k][threadIdx.x]);
+  finish_totals(p, sum);
 }
 
-// (m, s, t) of a part of a row; parts are brought to a common m exactly as often as
-// they are joined.
-struct Part {
-  float m, s, t, pad;
-};
+// A part into the place `slot` of CTA `cta` of the cluster.
+__device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(smem_u32(slot)),
+      "r"(cta), "f"(x.m), "f"(x.s), "f"(x.t), "f"(x.za)
+      : "memory");
+}
 
-// Every warp's part goes to every CTA of the cluster, and every warp joins them all:
-// one barrier a row.  `slots` alternate from row to row, so that a warp that is a
-// row ahead writes where nobody reads.
-template <int kWarps, int kCtas>
-__device__ __forceinline__ Part join_parts(Part mine, Part* slots) {
-  constexpr int kParts = kWarps * kCtas;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (kCtas == 1) {
-    if (lane == 0) slots[warp] = mine;
-    __syncthreads();
-  } else {
-    if (lane < kCtas) {
-      const uint32_t local = smem_u32(slots + cluster_ctarank() * kWarps + warp);
-      asm volatile(
-          "{\n\t.reg .b32 ra;\n\t"
-          "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
-          "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(local),
-          "r"(lane), "f"(mine.m), "f"(mine.s), "f"(mine.t), "f"(0.f)
-          : "memory");
-    }
-    cluster_sync();
-  }
+// The row's sums from its kParts parts, in every lane of a warp.
+template <int kParts>
+__device__ __forceinline__ Part join_parts(const Part* slots) {
   constexpr int kPer = (kParts + 31) / 32;
+  const int lane = threadIdx.x & 31;
   Part h[kPer];
   float m = -INFINITY;
 #pragma unroll
@@ -490,182 +557,322 @@ __device__ __forceinline__ Part join_parts(Part mine, Part* slots) {
     h[i] = at < kParts ? slots[at] : Part{-INFINITY, 0.f, 0.f, 0.f};
     m = fmaxf(m, h[i].m);
   }
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  m = warp_max(m, 32);
   float s = 0.f, t = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    if (h[i].m != -INFINITY || h[i].s != 0.f) {             // a NaN sum is taken along
-      const float d = h[i].m - m, x = exp_of(d);
-      s = fmaf(h[i].s, x, s);
-      t = fmaf(fmaf(h[i].s, fmaxf(d, kFloor), h[i].t), x, t);
-    }
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, off);
-    t += __shfl_xor_sync(0xffffffffu, t, off);
-  }
-  return Part{m, s, t, 0.f};
+  for (int i = 0; i < kPer; ++i) add_part(h[i], m, &s, &t);
+  return Part{m, warp_sum(s, 32), warp_sum(t, 32), slots[0].za};
 }
 
-// Longer rows: kCtas CTAs (a cluster when there are several) hold one.
-template <typename T, int kBlock, int kHeld, int kCtas>
-__global__ void __launch_bounds__(kBlock, kHeld > 4 ? 2 : (kBlock > 128 ? 3 : 10))
-    policy_block_kernel(Rows<T> r, Actions p) {
-  constexpr int kWarps = kBlock / 32;
-  __shared__ Sums sums;                   // thread 0's: registers are for the row
-  __shared__ Part slots[2][kWarps * kCtas];
-  pdl_wait();
+// Longer rows: kCtas CTAs (a cluster when there are several) hold one, an equal part
+// each, in a ring of kStages stages of shared memory.  Three kinds of warps, so that
+// nothing waits for a row's one reduction: while it is on its way the next row is
+// being summed, and the one after it loaded.
+//   warp 1          fills the stages: one bulk copy of a row's whole granules;
+//   warps 2..       sum their granules of row i (one read of the stage, kept in
+//                   registers for the maximum and the exponentials), send the parts
+//                   to every CTA of the cluster, then write the gradient of row i - 1;
+//   warp 0          joins the parts of row i, finishes its scalars and hands the
+//                   gradient's coefficients to its CTA.
+// Parts have four places: a warp sends those of row i + 4 after its CTA has joined
+// row i + 2, hence after every CTA's sums of row i + 2, which follow that CTA's
+// coefficients of row i and with them its last look at the parts of row i.
+template <typename T, int kSumWarps, int kCtas, int kStages, int kPerSm>
+__global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
+    policy_ring_kernel(Rows<T> r, Actions p) {
+  constexpr int kHeld = 8, kSum = kSumWarps * 32, kStage = kSum * kHeld;
+  constexpr int kParts = kSumWarps * kCtas;
+  extern __shared__ __align__(128) uint4 ring[];
+  __shared__ Part slots[4][kParts];
+  __shared__ RowGrad grads[2];
+  __shared__ uint64_t full[kStages], empty[kStages], joined[4], ready[2];
+  __shared__ int abort;
   const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int step = gridDim.x / kCtas;
-  const int g0 = rank * kBlock * kHeld + threadIdx.x;
-  const bool leader = rank == 0 && threadIdx.x == 0;
-  int parity = 0;
-  if (threadIdx.x == 0) sums.clear();
-  int row = blockIdx.x / kCtas;
-  RowIn in = row_in(r, p, row);
-  for (; row < r.rows; row += step) {
-    const RowIn next = row_in(r, p, row + step);
-    const bool takes = in.action >= 0 && in.w != 0.f;
-    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
-    const RowPtr<T> z(r.logits + row * r.ld);
-    T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
-    const bool aligned = dz != nullptr && same_alignment(dz, z.z);
-    if (takes && !bad) {
-      const float za = to_float(z.z[in.action]);
-      uint4 q[kHeld];
-      z.template load_all<kHeld, kBlock>(g0, in.n, q);
-      Part part = {-INFINITY, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) part.m = fmaxf(part.m, Granule<T>::largest(q[i]));
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1)
-        part.m = fmaxf(part.m, __shfl_xor_sync(0xffffffffu, part.m, off));
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) add_exps<T>(q[i], base_of(part.m), &part.s, &part.t);
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) {
-        part.s += __shfl_xor_sync(0xffffffffu, part.s, off);
-        part.t += __shfl_xor_sync(0xffffffffu, part.t, off);
-      }
-      // after its barrier every logit of the row has been read: grad may be logits
-      part = join_parts<kWarps, kCtas>(part, slots[parity]);
-      parity ^= 1;
-      const RowGrad k =
-          finish_row(r, p, in, row, za, part.m, part.s, part.t, z.mis, leader, &sums);
-      if (dz != nullptr) {
-        const int c = g0 * Granule<T>::kElems - z.mis;
-        if (aligned && c >= 0 && c + ((kHeld - 1) * kBlock + 1) * Granule<T>::kElems <= in.n) {
-          uint4* to = reinterpret_cast<uint4*>(dz + c);
-#pragma unroll
-          for (int i = 0; i < kHeld; ++i) {
-            float v[Granule<T>::kElems];
-            grad_granule<T>(q[i], k, g0 + i * kBlock, v);
-            to[i * kBlock] = Granule<T>::pack(v);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kHeld; ++i) {
-            float v[Granule<T>::kElems];
-            grad_granule<T>(q[i], k, g0 + i * kBlock, v);
-            z.store(dz, aligned, g0 + i * kBlock, in.n, r.classes, v);
-          }
-        }
-      }
-    } else {
-      const float fill = bad ? NAN : 0.f;
-      if (leader) fill_row(r, p, row, fill, &sums);
-      if (dz != nullptr)
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-          float v[Granule<T>::kElems];
-#pragma unroll
-          for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
-          z.store(dz, aligned, g0 + i * kBlock, r.classes, r.classes, v);
-        }
+  const int step = gridDim.x / kCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    abort = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], kSumWarps);
     }
-    in = next;
+    for (int s = 0; s < 4; ++s) mbar_init(&joined[s], kParts);
+    for (int s = 0; s < 2; ++s) mbar_init(&ready[s], 1);
+    fence_barrier_init();
   }
-  finish_totals(p, sums);
+  if (kCtas > 1) cluster_sync();          // the others' barriers are there to be written
+  else __syncthreads();
+  pdl_wait();
+
+  // granules [lo, hi) of a row are this CTA's
+  auto bounds = [&](const RowPtr<T>& z, int* lo, int* hi) {
+    const int all = z.granules(r.classes), per = (all + kCtas - 1) / kCtas;
+    *lo = min(rank * per, all);
+    *hi = min(*lo + per, all);
+  };
+  // a wait that ran out is reported, and what follows computed from what is there
+  auto wait = [&](uint64_t* bar, int phase) {
+    if (!mbar_wait(bar, phase & 1, &abort)) record_status(r.status, DORA_ERR_TIMEOUT);
+  };
+  Pair sum = {0.f, 0.f};
+  int row = blockIdx.x / kCtas;
+  int stage = 0, lap = 0, count = 0;      // of the rows that are computed
+  RowUse use = row_use(r, p, row);
+
+  if (warp == 1) {
+    if (lane == 0) {
+      for (; row < r.rows; row += step) {
+        const RowUse next = row_use(r, p, row + step);
+        if (computed(use)) {
+          const RowPtr<T> z(r.logits + row * r.ld, use.n);
+          int lo, hi;
+          bounds(z, &lo, &hi);
+          const int from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
+          if (lap > 0) wait(&empty[stage], lap - 1);
+          if (to > from) {
+            mbar_arrive_expect_tx(&full[stage], (to - from) * 16);
+            bulk_load(ring + stage * kStage + (from - lo), z.at(from), (to - from) * 16,
+                      &full[stage]);
+          } else {
+            mbar_arrive(&full[stage]);
+          }
+          if (++stage == kStages) {
+            stage = 0;
+            ++lap;
+          }
+        }
+        use = next;
+      }
+      if (abort)                          // no copy may land after the CTA is gone
+        for (int s = 0; s < kStages; ++s)
+          mbar_wait_limited(&full[s], (s < stage ? lap : lap - 1) & 1, kWaitLimitNs / 8);
+    }
+  } else if (warp == 0) {
+    const bool leader = rank == 0 && lane == 0;
+    RowIn in = row_in(p, row, r.rows);
+    for (; row < r.rows; row += step) {
+      const RowUse next = row_use(r, p, row + step);
+      const RowIn next_in = row_in(p, row + step, r.rows);
+      if (computed(use)) {
+        const int slot = count & 3;
+        if (kCtas == 1) {
+          wait(&joined[slot], count >> 2);
+        } else if (!mbar_wait_cluster(&joined[slot], (count >> 2) & 1, &abort)) {
+          record_status(r.status, DORA_ERR_TIMEOUT);
+        }
+        __syncwarp();
+        const Part x = join_parts<kParts>(slots[slot]);
+        Terms terms;
+        const RowGrad k = finish_row(r, p, in, row, x.za, x, leader, &terms);
+        if (lane == 0) {
+          grads[count & 1] = k;
+          mbar_arrive(&ready[count & 1]);
+        }
+        if (rank == 0) sum.add(terms.of(lane));
+        ++count;
+      } else {
+        const float fill = use.takes ? NAN : 0.f;
+        if (leader) fill_row(r, p, row, fill);
+        if (rank == 0) sum.add(all_terms(fill).of(lane));
+      }
+      use = next;
+      in = next_in;
+    }
+  } else {
+    const int me = threadIdx.x - 64;
+    // the row whose gradient is due
+    int due = -1, due_stage = 0, due_count = 0;
+    RowUse due_use = {-1, 0, false};
+    auto gradient = [&]() {
+      const RowPtr<T> z(r.logits + due * r.ld, due_use.n);
+      T* dz = r.grad != nullptr ? r.grad + due * r.ld : nullptr;
+      const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+      int lo, hi;
+      bounds(z, &lo, &hi);
+      if (computed(due_use)) {
+        const int n = due_use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
+        const uint4* held = ring + due_stage * kStage - lo;
+        wait(&ready[due_count & 1], due_count >> 1);
+        if (dz != nullptr) {
+          const RowGrad k = grads[due_count & 1];
+          int i = from + me;
+          if (aligned) {
+            uint4* out = z.as_granules(dz);
+            if (k.b == 0.f) {
+#pragma unroll 2
+              for (; i < to; i += kSum) out[i] = grad_granule<T, false>(held[i], k);
+            } else {
+#pragma unroll 2
+              for (; i < to; i += kSum) out[i] = grad_granule<T, true>(held[i], k);
+            }
+          } else {
+            for (; i < to; i += kSum)
+              z.store_part(dz, false, i, n, r.classes, grad_granule<T>(held[i], k));
+          }
+          // the granules that are not whole, and what lies past the legal logits
+          if (me == 0 && lo < from)
+            z.store_part(dz, aligned, lo, n, r.classes, grad_granule<T>(z.load_part(lo, n), k));
+          for (i = max(from, to) + me; i < hi; i += kSum)
+            z.store_part(dz, aligned, i, n, r.classes, grad_granule<T>(z.load_part(i, n), k));
+          // the thread that has stored the action's granule
+          const int ia = (due_use.action + z.mis) / z.kE;
+          const int owner = ia < from ? 0 : (ia - (ia < to ? from : max(from, to))) & (kSum - 1);
+          if (ia >= lo && ia < hi && owner == me) from_float(k.at_action, dz + due_use.action);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[due_stage]);
+      } else if (dz != nullptr) {
+        const float fill = due_use.takes ? NAN : 0.f;
+        for (int i = lo + me; i < hi; i += kSum)
+          fill_granule(z, dz, aligned, i, r.classes, fill);
+      }
+    };
+    // The action's logit goes with the first warp's part: read before any CTA can write
+    // the row's gradient, which may lie over its logits.  It and the row's scalars are
+    // on their way a row and two rows ahead.
+    auto action_logit = [&](int at, const RowUse& u) {
+      return warp == 2 && computed(u) ? to_float(r.logits[at * r.ld + u.action]) : 0.f;
+    };
+    RowUse next = row_use(r, p, row + step);
+    float za = action_logit(row, use);
+    for (; row < r.rows; row += step) {
+      const RowUse after = row_use(r, p, row + 2 * step);
+      const float next_za = action_logit(row + step, next);
+      int at_stage = 0, at_count = 0;
+      if (computed(use)) {
+        const RowPtr<T> z(r.logits + row * r.ld, use.n);
+        int lo, hi;
+        bounds(z, &lo, &hi);
+        const int n = use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
+        const uint4* held = ring + stage * kStage - lo;
+        RowSum x;
+        x.clear();
+        // the granules that are not whole: the row's first and the last with legal logits
+        if (me == 0 && lo < from) {
+          const uint4 q[1] = {z.load_part(lo, n)};
+          x.add<T>(q);
+        }
+        if (me == 1 && to >= from && to < hi && to >= z.whole_lo) {
+          const uint4 q[1] = {z.load_part(to, n)};
+          x.add<T>(q);
+        }
+        wait(&full[stage], lap);
+        int i = from + me;
+        for (; i + 3 * kSum < to; i += 4 * kSum) {
+          const uint4 q[4] = {held[i], held[i + kSum], held[i + 2 * kSum], held[i + 3 * kSum]};
+          x.add<T>(q);
+        }
+        for (; i < to; i += kSum) {
+          const uint4 q[1] = {held[i]};
+          x.add<T>(q);
+        }
+        Part part = x.over(32);
+        part.za = za;
+        const int slot = count & 3;
+        Part* at = &slots[slot][rank * kSumWarps + warp - 2];
+        if (kCtas == 1) {
+          if (lane == 0) {
+            *at = part;
+            mbar_arrive(&joined[slot]);
+          }
+        } else if (lane < kCtas) {
+          store_part_remote(part, at, lane);
+          mbar_arrive_remote(&joined[slot], lane);
+        }
+        at_stage = stage;
+        at_count = count++;
+        if (++stage == kStages) {
+          stage = 0;
+          ++lap;
+        }
+      }
+      if (due >= 0) gradient();
+      due = row;
+      due_use = use;
+      due_stage = at_stage;
+      due_count = at_count;
+      use = next;
+      next = after;
+      za = next_za;
+    }
+    if (due >= 0) gradient();
+  }
+  __syncwarp();
+  if (kCtas > 1) cluster_sync();          // nobody leaves while parts may be on their way to it
+  finish_totals(p, sum);
 }
 
-// Rows longer than the registers of a cluster: the same, but the row is read a second
-// time (from L2, where the clusters' rows fit) for its gradient.
+// Rows longer than a cluster's registers: the same without the ring; a row is read a
+// second time (from L2, where the clusters' rows fit) for its gradient.
 constexpr int kLongBlock = 512, kLongCtas = 8, kLongStep = 4;
 
 template <typename T>
 __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, Actions p) {
   constexpr int kWarps = kLongBlock / 32, kStride = kLongBlock * kLongCtas;
   __shared__ Part slots[2][kWarps * kLongCtas];
-  __shared__ Sums sums;
+  cluster_sync();                         // the others' shared memory is there to be written
   pdl_wait();
   const int rank = static_cast<int>(cluster_ctarank());
   const int step = gridDim.x / kLongCtas;
   const int g0 = rank * kLongBlock + threadIdx.x;
   const bool leader = rank == 0 && threadIdx.x == 0;
   int parity = 0;
-  if (threadIdx.x == 0) sums.clear();
+  Pair sum = {0.f, 0.f};
   for (int row = blockIdx.x / kLongCtas; row < r.rows; row += step) {
-    const RowIn in = row_in(r, p, row);
-    const bool takes = in.action >= 0 && in.w != 0.f;
-    const bool bad = takes && (in.n < 0 || in.n > r.classes || in.action >= in.n);
-    const RowPtr<T> z(r.logits + row * r.ld);
+    const RowUse use = row_use(r, p, row);
+    const RowPtr<T> z(r.logits + row * r.ld, use.n);
     T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
     const bool aligned = dz != nullptr && same_alignment(dz, z.z);
-    const int granules = (r.classes + z.mis + Granule<T>::kElems - 1) / Granule<T>::kElems;
-    if (takes && !bad) {
-      const float za = to_float(z.z[in.action]);
-      Part part = {-INFINITY, 0.f, 0.f, 0.f};
-      for (int i = g0; i < granules; i += kStride * kLongStep) {
+    const int end = z.granules(r.classes);
+    if (computed(use)) {
+      const int n = use.n;
+      const RowIn in = row_in(p, row, r.rows);
+      const float za = to_float(z.z[use.action]);
+      RowSum x;
+      x.clear();
+      for (int i = g0; i < end; i += kStride * kLongStep) {
         uint4 q[kLongStep];
-        z.template load_all<kLongStep, kStride>(i, in.n, q);
-        float m = part.m;
 #pragma unroll
-        for (int u = 0; u < kLongStep; ++u) m = fmaxf(m, Granule<T>::largest(q[u]));
-        if (m > part.m && part.s != 0.f) {
-          const float d = part.m - m, x = exp_of(d);
-          part.t = fmaf(part.s, fmaxf(d, kFloor), part.t) * x;
-          part.s *= x;
+        for (int u = 0; u < kLongStep; ++u) {
+          const int at = i + u * kStride;
+          if (z.whole(at)) q[u] = *z.at(at);
+          else q[u] = z.load_part(at, n);
         }
-        part.m = m;
-#pragma unroll
-        for (int u = 0; u < kLongStep; ++u) add_exps<T>(q[u], base_of(m), &part.s, &part.t);
+        x.add<T>(q);
       }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) {
-        const Part o = {__shfl_xor_sync(0xffffffffu, part.m, off),
-                        __shfl_xor_sync(0xffffffffu, part.s, off),
-                        __shfl_xor_sync(0xffffffffu, part.t, off), 0.f};
-        const float m = fmaxf(part.m, o.m), c = base_of(m);
-        const float da = part.m - c, db = o.m - c, xa = exp_of(da), xb = exp_of(db);
-        part.t = fmaf(part.s, fmaxf(da, kFloor), part.t) * xa +
-                 fmaf(o.s, fmaxf(db, kFloor), o.t) * xb;
-        part.s = part.s * xa + o.s * xb;
-        part.m = m;
-      }
-      part = join_parts<kWarps, kLongCtas>(part, slots[parity]);
+      Part part = x.over(32);
+      // every warp's part goes to every CTA; places alternate from row to row, so that a
+      // warp that is a row ahead writes where nobody reads
+      if ((threadIdx.x & 31) < kLongCtas)
+        store_part_remote(part, slots[parity] + rank * kWarps + (threadIdx.x >> 5),
+                          threadIdx.x & 31);
+      // after this barrier every logit of the row has been read: grad may be logits
+      cluster_sync();
+      part = join_parts<kWarps * kLongCtas>(slots[parity]);
       parity ^= 1;
-      const RowGrad k =
-          finish_row(r, p, in, row, za, part.m, part.s, part.t, z.mis, leader, &sums);
-      if (dz != nullptr)
-        for (int i = g0; i < granules; i += kStride) {
-          float v[Granule<T>::kElems];
-          grad_granule<T>(z.load(i, in.n), k, i, v);
-          z.store(dz, aligned, i, in.n, r.classes, v);
+      Terms terms;
+      const RowGrad k = finish_row(r, p, in, row, za, part, leader, &terms);
+      if (rank == 0) sum.add(terms.of(threadIdx.x));
+      if (dz != nullptr) {
+        for (int i = g0; i < end; i += kStride) {
+          if (aligned && z.whole(i))
+            *(z.as_granules(dz) + i) = grad_granule<T>(*z.at(i), k);
+          else
+            z.store_part(dz, aligned, i, n, r.classes,
+                         grad_granule<T>(z.whole(i) ? *z.at(i) : z.load_part(i, n), k));
         }
+        // the thread that has stored the action's granule
+        if (((use.action + z.mis) / z.kE) % kStride == g0)
+          from_float(k.at_action, dz + use.action);
+      }
     } else {
-      const float fill = bad ? NAN : 0.f;
-      if (leader) fill_row(r, p, row, fill, &sums);
+      const float fill = use.takes ? NAN : 0.f;
+      if (leader) fill_row(r, p, row, fill);
+      if (rank == 0) sum.add(all_terms(fill).of(threadIdx.x));
       if (dz != nullptr)
-        for (int i = g0; i < granules; i += kStride) {
-          float v[Granule<T>::kElems];
-#pragma unroll
-          for (int e = 0; e < Granule<T>::kElems; ++e) v[e] = fill;
-          z.store(dz, aligned, i, r.classes, r.classes, v);
-        }
+        for (int i = g0; i < end; i += kStride) fill_granule(z, dz, aligned, i, r.classes, fill);
     }
   }
-  finish_totals(p, sums);
+  finish_totals(p, sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -730,8 +937,7 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
   __shared__ double dpart[kThreads / 32];
   __shared__ int bad;
   pdl_wait();
-  Sums sums;
-  sums.clear();
+  Pair sum = {0.f, 0.f};
   for (int img = blockIdx.x; img < q.batch; img += gridDim.x) {
     const int lo = q.cu[img], hi = q.cu[img + 1];
     int n = hi - lo - 1, k = q.k[img];
@@ -768,8 +974,8 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
         if (takes) record_status(q.status, DORA_ERR_DEVICE_BAD_COUNT);
         p.logp[img] = fill;
         if (p.row_loss != nullptr) p.row_loss[img] = fill;
-        for (int i = 0; i < kTerms; ++i) sums.add(i, fill);
       }
+      sum.add(all_terms(fill).of(threadIdx.x));
       if (q.grad != nullptr && inside)
         for (int r = lo + threadIdx.x; r < hi; r += kThreads) q.grad[r] = fill;
       continue;
@@ -820,12 +1026,13 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
     }
     lp = block_sum(lp, dpart);            // its barriers publish `upto`
     const float x = p.ref_logp != nullptr ? static_cast<float>(p.ref_logp[img] - lp) : 0.f;
-    float loss;
+    Terms terms;
     const float g = row_terms(p, static_cast<float>(lp - p.old_logp[img]), x, p.advantages[img], w,
-                              0.f, &loss, threadIdx.x == 0 ? &sums : nullptr);
+                              0.f, &terms);
+    sum.add(terms.of(threadIdx.x));
     if (threadIdx.x == 0) {
       p.logp[img] = static_cast<float>(lp);
-      if (p.row_loss != nullptr) p.row_loss[img] = loss;
+      if (p.row_loss != nullptr) p.row_loss[img] = terms.v[0];
     }
     if (q.grad == nullptr) continue;
     if (threadIdx.x == 0) q.grad[lo] = 0.f;                                 // CLS
@@ -835,7 +1042,7 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
       q.grad[lo + 1 + j] = g * ((u > 0 ? 1.f : 0.f) - a.s * expf(s[j] + a.m));
     }
   }
-  finish_totals(p, sums);
+  finish_totals(p, sum);
 }
 
 }  // namespace policy
@@ -851,6 +1058,7 @@ int device_or_error() {
   return DORA_OK;
 }
 int launched(cudaError_t e) { return e == cudaSuccess ? DORA_OK : DORA_ERR_CUDA; }
+constexpr int kMaxDevices = 64;
 
 // The pointers are looked at when there are rows at all: an empty batch has none.
 int check_actions(const policy::Actions& p, int rows, size_t workspace_bytes) {
@@ -873,13 +1081,17 @@ int grid_for(int rows, int per_sm) {
   return ctas < policy::kMaxCtas ? ctas : policy::kMaxCtas;
 }
 
-// A dependent launch of clusters of `ctas` CTAs.
 template <typename T>
-int launch_rows(void (*kern)(policy::Rows<T>, policy::Actions), int grid, int block, int ctas,
+using RowsKernel = void (*)(policy::Rows<T>, policy::Actions);
+
+// A dependent launch of `teams` clusters of `ctas` CTAs (or as many as fit at once).
+template <typename T>
+int launch_rows(RowsKernel<T> kern, int teams, int block, int ctas, size_t smem,
                 cudaStream_t stream, const policy::Rows<T>& r, const policy::Actions& p) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = dim3(teams * ctas);
   cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   int n = 0;
@@ -898,19 +1110,47 @@ int launch_rows(void (*kern)(policy::Rows<T>, policy::Actions), int grid, int bl
   return launched(cudaLaunchKernelEx(&cfg, kern, r, p));
 }
 
-template <typename T, int kHeld>
-int launch_blocks(int ctas, cudaStream_t stream, const policy::Rows<T>& r,
-                  const policy::Actions& p) {
-  const int clusters = grid_for(r.rows, kHeld > 4 ? 2 : 3);   // CTAs that an SM holds
-  const int grid = ctas * (clusters * ctas > num_sms() * (kHeld > 4 ? 2 : 3)
-                               ? num_sms() * (kHeld > 4 ? 2 : 3) / ctas
-                               : clusters);
-  switch (ctas) {
-    case 1: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 1>, grid, 512, 1, stream, r, p);
-    case 2: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 2>, grid, 512, 2, stream, r, p);
-    case 4: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 4>, grid, 512, 4, stream, r, p);
-    default: return launch_rows(policy::policy_block_kernel<T, 512, kHeld, 8>, grid, 512, 8, stream, r, p);
-  }
+// How many clusters of this kernel the device holds at once; asked once a device.
+// A cluster's CTAs come from one group of SMs, so that these are fewer than the SMs
+// divided by the CTAs, and a grid of more would run the rest after the others' end.
+template <typename T>
+int resident_clusters(RowsKernel<T> kern, int block, int ctas, size_t smem,
+                      std::atomic<int>* cache) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  int n = cache[dev].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) return 0;
+  cache[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// kPerSm CTAs an SM; the grid is what is resident at once.
+template <typename T, int kSumWarps, int kCtas, int kPerSm>
+int launch_ring(cudaStream_t stream, const policy::Rows<T>& r, const policy::Actions& p) {
+  constexpr int kStages = 3;
+  const RowsKernel<T> kern = policy::policy_ring_kernel<T, kSumWarps, kCtas, kStages, kPerSm>;
+  constexpr size_t smem = static_cast<size_t>(kStages) * kSumWarps * 32 * 8 * 16;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(smem));
+  if (e != cudaSuccess) return launched(e);
+  static std::atomic<int> cache[kMaxDevices];
+  const int most = kCtas == 1 ? num_sms() * kPerSm
+                              : resident_clusters<T>(kern, kSumWarps * 32 + 64, kCtas, smem, cache);
+  if (most < 1) return DORA_ERR_CUDA;
+  return launch_rows<T>(kern, r.rows < most ? r.rows : most, kSumWarps * 32 + 64, kCtas, smem,
+                        stream, r, p);
 }
 
 template <typename T>
@@ -924,28 +1164,31 @@ int launch_policy(const void* logits, void* grad, int64_t ld, int rows, int clas
   const bool aligned = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && ld % kE == 0;
   const int64_t need = (static_cast<int64_t>(classes) + (aligned ? 0 : kE - 1) + kE - 1) / kE;
   if (need <= 8)
-    return launch_rows(policy::policy_warp_kernel<T, 8, 1>, grid_for((rows + 31) / 32, 8), 256, 1,
-                       stream, r, p);
+    return launch_rows<T>(policy::policy_warp_kernel<T, 8, 1>, grid_for((rows + 31) / 32, 8), 256,
+                          1, 0, stream, r, p);
   if (need <= 32)
-    return launch_rows(policy::policy_warp_kernel<T, 8, 4>, grid_for((rows + 31) / 32, 8), 256, 1,
-                       stream, r, p);
+    return launch_rows<T>(policy::policy_warp_kernel<T, 8, 4>, grid_for((rows + 31) / 32, 8), 256,
+                          1, 0, stream, r, p);
   if (need <= 128)
-    return launch_rows(policy::policy_warp_kernel<T, 32, 4>, grid_for((rows + 7) / 8, 8), 256, 1,
-                       stream, r, p);
-  if (need <= 512)
-    return launch_rows(policy::policy_block_kernel<T, 128, 4, 1>, grid_for(rows, 12), 128, 1,
-                       stream, r, p);
-  if (need > 512 * 8 * 8)
-    return launch_rows(policy::policy_long_kernel<T>,
-                       policy::kLongCtas * grid_for(rows, 1) > num_sms() * 2
-                           ? num_sms() * 2 / policy::kLongCtas * policy::kLongCtas
-                           : policy::kLongCtas * rows,
-                       policy::kLongBlock, policy::kLongCtas, stream, r, p);
+    return launch_rows<T>(policy::policy_warp_kernel<T, 32, 4>, grid_for((rows + 7) / 8, 8), 256,
+                          1, 0, stream, r, p);
+  if (need > 4096 * 8) {
+    static std::atomic<int> cache[kMaxDevices];
+    const int most = resident_clusters<T>(policy::policy_long_kernel<T>, policy::kLongBlock,
+                                          policy::kLongCtas, 0, cache);
+    if (most < 1) return DORA_ERR_CUDA;
+    return launch_rows<T>(policy::policy_long_kernel<T>, rows < most ? rows : most,
+                          policy::kLongBlock, policy::kLongCtas, 0, stream, r, p);
+  }
   int ctas = 1;
-  while (need > 512 * 8 * ctas) ctas *= 2;
-  while (ctas < 8 && rows * ctas * 2 <= num_sms()) ctas *= 2;   // few rows: more SMs a row
-  return need <= 512 * 4 * ctas ? launch_blocks<T, 4>(ctas, stream, r, p)
-                                : launch_blocks<T, 8>(ctas, stream, r, p);
+  while (need > 4096 * ctas) ctas *= 2;
+  while (ctas < 8 && need > 1024 && rows * ctas * 2 <= num_sms()) ctas *= 2;   // few rows
+  if (ctas == 8) return launch_ring<T, 16, 8, 1>(stream, r, p);
+  if (ctas == 4) return launch_ring<T, 16, 4, 1>(stream, r, p);
+  if (ctas == 2) return launch_ring<T, 16, 2, 1>(stream, r, p);
+  if (need > 2048) return launch_ring<T, 16, 1, 1>(stream, r, p);
+  if (need > 1024) return launch_ring<T, 8, 1, 2>(stream, r, p);
+  return launch_ring<T, 4, 1, 4>(stream, r, p);
 }
 }  // namespace
 
@@ -960,7 +1203,7 @@ int dora_policy_loss(const void* logits, int32_t dtype, int32_t rows, int32_t cl
                      float* logp, float* entropy, float* row_loss, void* grad, float* totals,
                      void* workspace, size_t workspace_bytes, int32_t* status,
                      dora_stream_t stream_) {
-  if (rows < 0 || classes < 1 || ld < classes || dtype < DORA_BF16 || dtype > DORA_F32)
+  if (rows < 0 || rows > (1 << 30) || classes < 1 || ld < classes || dtype < DORA_BF16 || dtype > DORA_F32)
     return DORA_ERR_INVALID_ARG;
   if (rows > 0 && (logits == nullptr || actions == nullptr)) return DORA_ERR_INVALID_ARG;
   const uintptr_t size_mask = dtype == DORA_F32 ? 3u : 1u;
