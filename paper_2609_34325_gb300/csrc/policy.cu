@@ -223,17 +223,18 @@ __device__ __forceinline__ float ex2(float x) {
 constexpr float kFloor = -1e30f;          // e^kFloor is 0: keeps 0 * inf out of e d
 
 // A row's granules.  [whole_lo, whole_hi): those that lie wholly in its first n
-// elements.
+// elements; [0, some_hi): those that hold some of them.
 template <typename T>
 struct RowPtr {
   static constexpr int kE = Granule<T>::kElems;
   const T* z;                             // the row's first element
   int mis;                                // elements of its first granule before it
-  int whole_lo, whole_hi;
+  int whole_lo, whole_hi, some_hi;
   __device__ __forceinline__ RowPtr(const T* p, int n)
       : z(p), mis(static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {
     whole_lo = mis > 0 ? 1 : 0;
     whole_hi = (n + mis) / kE;
+    some_hi = (n + mis + kE - 1) / kE;
   }
   __device__ __forceinline__ bool whole(int i) const { return i >= whole_lo && i < whole_hi; }
   __device__ __forceinline__ int granules(int classes) const {
@@ -254,6 +255,16 @@ struct RowPtr {
     for (int e = 0; e < kE; ++e)
       v[e] = c + e >= 0 && c + e < n ? to_float(z[c + e]) : -INFINITY;
     return Granule<T>::pack(v);           // exact: the values come from T
+  }
+  // The same of a granule that is at hand.
+  __device__ __forceinline__ uint4 only_row(uint4 q, int i, int n) const {
+    const int c = i * kE - mis;
+    float v[kE];
+    Granule<T>::unpack(q, v);
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      if (c + e < 0 || c + e >= n) v[e] = -INFINITY;
+    return Granule<T>::pack(v);
   }
   // Granule i into the row at `to` of `classes` elements, 0 from n on.
   __device__ __forceinline__ void store_part(T* to, bool aligned, int i, int n, int classes,
@@ -603,6 +614,14 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
   else __syncthreads();
   pdl_wait();
 
+  // The copied granules [from, to) of this CTA's [lo, hi): all that hold some of the
+  // row's legal logits, and with them a few of its neighbours' (looked at by nobody),
+  // but nothing before the first row's or past the last one's logits.
+  const T* last = r.logits + (r.rows - 1) * r.ld + r.classes;
+  auto copied = [&](const RowPtr<T>& z, int row, int lo, int hi, int* from, int* to) {
+    *from = max(lo, row == 0 ? z.whole_lo : 0);
+    *to = min(hi, z.z - z.mis + z.some_hi * z.kE <= last ? z.some_hi : z.whole_hi);
+  };
   // granules [lo, hi) of a row are this CTA's
   auto bounds = [&](const RowPtr<T>& z, int* lo, int* hi) {
     const int all = z.granules(r.classes), per = (all + kCtas - 1) / kCtas;
@@ -626,7 +645,8 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
           const RowPtr<T> z(r.logits + row * r.ld, use.n);
           int lo, hi;
           bounds(z, &lo, &hi);
-          const int from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
+          int from, to;
+          copied(z, row, lo, hi, &from, &to);
           if (lap > 0) wait(&empty[stage], lap - 1);
           if (to > from) {
             mbar_arrive_expect_tx(&full[stage], (to - from) * 16);
@@ -679,6 +699,12 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
     }
   } else {
     const int me = threadIdx.x - 64;
+    // Whether thread 0 has to see to the row's first granule (the row starts inside it),
+    // thread 1 to its last with legal logits (they end inside it).
+    auto is_part = [me](const RowPtr<T>& z, int lo, int hi) {
+      if (me == 0) return lo == 0 && z.whole_lo > 0;
+      return z.whole_hi < z.some_hi && z.whole_hi >= max(lo, z.whole_lo) && z.whole_hi < hi;
+    };
     // the row whose gradient is due
     int due = -1, due_stage = 0, due_count = 0;
     RowUse due_use = {-1, 0, false};
@@ -691,6 +717,8 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       if (computed(due_use)) {
         const int n = due_use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
         const uint4* held = ring + due_stage * kStage - lo;
+        int held_lo, held_hi;
+        copied(z, due, lo, hi, &held_lo, &held_hi);
         wait(&ready[due_count & 1], due_count >> 1);
         if (dz != nullptr) {
           const RowGrad k = grads[due_count & 1];
@@ -708,14 +736,17 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
             for (; i < to; i += kSum)
               z.store_part(dz, false, i, n, r.classes, grad_granule<T>(held[i], k));
           }
-          // the granules that are not whole, and what lies past the legal logits
-          if (me == 0 && lo < from)
-            z.store_part(dz, aligned, lo, n, r.classes, grad_granule<T>(z.load_part(lo, n), k));
-          for (i = max(from, to) + me; i < hi; i += kSum)
-            z.store_part(dz, aligned, i, n, r.classes, grad_granule<T>(z.load_part(i, n), k));
+          // the granules that are not whole (threads 0 and 1), and those past the legal logits
+          i = me == 0 ? 0 : z.whole_hi;
+          if (me < 2 && is_part(z, lo, hi))
+            z.store_part(dz, aligned, i, n, r.classes,
+                         grad_granule<T>(i >= held_lo && i < held_hi ? held[i]
+                                                                     : z.load_part(i, n), k));
+          for (i = max(lo, z.some_hi) + me; i < hi; i += kSum)
+            fill_granule(z, dz, aligned, i, r.classes, 0.f);
           // the thread that has stored the action's granule
           const int ia = (due_use.action + z.mis) / z.kE;
-          const int owner = ia < from ? 0 : (ia - (ia < to ? from : max(from, to))) & (kSum - 1);
+          const int owner = ia < z.whole_lo ? 0 : ia < z.whole_hi ? (ia - from) & (kSum - 1) : 1;
           if (ia >= lo && ia < hi && owner == me) from_float(k.at_action, dz + due_use.action);
         }
         __syncwarp();
@@ -746,15 +777,8 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
         const uint4* held = ring + stage * kStage - lo;
         RowSum x;
         x.clear();
-        // the granules that are not whole: the row's first and the last with legal logits
-        if (me == 0 && lo < from) {
-          const uint4 q[1] = {z.load_part(lo, n)};
-          x.add<T>(q);
-        }
-        if (me == 1 && to >= from && to < hi && to >= z.whole_lo) {
-          const uint4 q[1] = {z.load_part(to, n)};
-          x.add<T>(q);
-        }
+        int held_lo, held_hi;
+        copied(z, row, lo, hi, &held_lo, &held_hi);
         wait(&full[stage], lap);
         int i = from + me;
         for (; i + 3 * kSum < to; i += 4 * kSum) {
@@ -763,6 +787,12 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
         }
         for (; i < to; i += kSum) {
           const uint4 q[1] = {held[i]};
+          x.add<T>(q);
+        }
+        if (me < 2 && is_part(z, lo, hi)) {
+          i = me == 0 ? 0 : z.whole_hi;
+          const uint4 q[1] = {i >= held_lo && i < held_hi ? z.only_row(held[i], i, n)
+                                                          : z.load_part(i, n)};
           x.add<T>(q);
         }
         Part part = x.over(32);
