@@ -184,23 +184,32 @@ struct Rows {
   int32_t* status;
 };
 
+// A row's action, weight and legal logits as they are loaded, a row or two ahead:
+// nothing is made of them before their row's turn, so that no warp waits for them.
+struct RowAhead {
+  int action, n;
+  float w;
+};
+template <typename T>
+__device__ __forceinline__ RowAhead row_ahead(const Rows<T>& r, const Actions& p, int row) {
+  RowAhead a = {-1, 0, 1.f};
+  if (row < r.rows) {
+    a.action = r.actions[row];
+    a.n = r.legal != nullptr ? r.legal[row] : r.classes;
+    if (p.weights != nullptr) a.w = p.weights[row];
+  }
+  return a;
+}
+
 // Whether a row takes part, and how many of its logits are legal (-1: not valid).
 struct RowUse {
   int action, n;
   bool takes;
 };
-
 template <typename T>
-__device__ __forceinline__ RowUse row_use(const Rows<T>& r, const Actions& p, int row) {
-  RowUse u = {-1, 0, false};
-  if (row < r.rows) {
-    u.action = r.actions[row];
-    const float w = p.weights != nullptr ? p.weights[row] : 1.f;
-    u.n = r.legal != nullptr ? r.legal[row] : r.classes;
-    u.takes = u.action >= 0 && w != 0.f;
-    if (u.n < 0 || u.n > r.classes || u.action >= u.n) u.n = -1;
-  }
-  return u;
+__device__ __forceinline__ RowUse row_use(const Rows<T>& r, const RowAhead& a) {
+  const bool valid = a.n >= 0 && a.n <= r.classes && a.action < a.n;
+  return {a.action, valid ? a.n : -1, a.action >= 0 && a.w != 0.f};
 }
 __device__ __forceinline__ bool computed(const RowUse& u) { return u.takes && u.n > 0; }
 
@@ -477,8 +486,9 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
   // the loop is the same for all groups of a warp: shuffles need every lane
   const int first = blockIdx.x * kRowsPerCta + (threadIdx.x / 32) * (32 / kLanes);
   int row = first + (threadIdx.x % 32) / kLanes;
-  RowUse use = row_use(r, p, row);
+  RowAhead next = row_ahead(r, p, row);
   for (int base = first; base < r.rows; base += step, row += step) {
+    const RowUse use = row_use(r, next);
     const bool exists = row < r.rows, live = computed(use);
     const int n = live ? use.n : 0;
     const RowPtr<T> z(r.logits + (exists ? row : 0) * r.ld, n);
@@ -495,7 +505,7 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
       in = row_in(p, row, r.rows);
       za = to_float(z.z[use.action]);
     }
-    const RowUse next = row_use(r, p, row + step);
+    next = row_ahead(r, p, row + step);
     RowSum x;
     x.clear();
     x.add<T>(q);
@@ -530,7 +540,6 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
           for (int i = lane; i < end; i += kLanes) fill_granule(z, dz, aligned, i, r.classes, fill);
       }
     }
-    use = next;
   }
   if (p.totals == nullptr) return;
   // lane i of every group holds its term i: groups of a warp, then warps
@@ -635,12 +644,13 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
   Pair sum = {0.f, 0.f};
   int row = blockIdx.x / kCtas;
   int stage = 0, lap = 0, count = 0;      // of the rows that are computed
-  RowUse use = row_use(r, p, row);
+  RowAhead next = row_ahead(r, p, row);
 
   if (warp == 1) {
     if (lane == 0) {
       for (; row < r.rows; row += step) {
-        const RowUse next = row_use(r, p, row + step);
+        const RowUse use = row_use(r, next);
+        next = row_ahead(r, p, row + step);
         if (computed(use)) {
           const RowPtr<T> z(r.logits + row * r.ld, use.n);
           int lo, hi;
@@ -660,7 +670,6 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
             ++lap;
           }
         }
-        use = next;
       }
       if (abort)                          // no copy may land after the CTA is gone
         for (int s = 0; s < kStages; ++s)
@@ -670,7 +679,8 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
     const bool leader = rank == 0 && lane == 0;
     RowIn in = row_in(p, row, r.rows);
     for (; row < r.rows; row += step) {
-      const RowUse next = row_use(r, p, row + step);
+      const RowUse use = row_use(r, next);
+      next = row_ahead(r, p, row + step);
       const RowIn next_in = row_in(p, row + step, r.rows);
       if (computed(use)) {
         const int slot = count & 3;
@@ -694,7 +704,6 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
         if (leader) fill_row(r, p, row, fill);
         if (rank == 0) sum.add(all_terms(fill).of(lane));
       }
-      use = next;
       in = next_in;
     }
   } else {
@@ -704,6 +713,12 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
     auto is_part = [me](const RowPtr<T>& z, int lo, int hi) {
       if (me == 0) return lo == 0 && z.whole_lo > 0;
       return z.whole_hi < z.some_hi && z.whole_hi >= max(lo, z.whole_lo) && z.whole_hi < hi;
+    };
+    auto part_of = [&](const RowPtr<T>& z, int row, int lo, int hi, int i, int n,
+                       const uint4* held) {
+      int from, to;
+      copied(z, row, lo, hi, &from, &to);
+      return i >= from && i < to ? z.only_row(held[i], i, n) : z.load_part(i, n);
     };
     // the row whose gradient is due
     int due = -1, due_stage = 0, due_count = 0;
@@ -717,8 +732,6 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       if (computed(due_use)) {
         const int n = due_use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
         const uint4* held = ring + due_stage * kStage - lo;
-        int held_lo, held_hi;
-        copied(z, due, lo, hi, &held_lo, &held_hi);
         wait(&ready[due_count & 1], due_count >> 1);
         if (dz != nullptr) {
           const RowGrad k = grads[due_count & 1];
@@ -740,8 +753,7 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
           i = me == 0 ? 0 : z.whole_hi;
           if (me < 2 && is_part(z, lo, hi))
             z.store_part(dz, aligned, i, n, r.classes,
-                         grad_granule<T>(i >= held_lo && i < held_hi ? held[i]
-                                                                     : z.load_part(i, n), k));
+                         grad_granule<T>(part_of(z, due, lo, hi, i, n, held), k));
           for (i = max(lo, z.some_hi) + me; i < hi; i += kSum)
             fill_granule(z, dz, aligned, i, r.classes, 0.f);
           // the thread that has stored the action's granule
@@ -761,13 +773,18 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
     // the row's gradient, which may lie over its logits.  It and the row's scalars are
     // on their way a row and two rows ahead.
     auto action_logit = [&](int at, const RowUse& u) {
-      return warp == 2 && computed(u) ? to_float(r.logits[at * r.ld + u.action]) : 0.f;
+      T z;
+      from_float(0.f, &z);
+      if (warp == 2 && computed(u)) z = r.logits[at * r.ld + u.action];
+      return z;
     };
-    RowUse next = row_use(r, p, row + step);
-    float za = action_logit(row, use);
+    RowUse use = row_use(r, next);
+    next = row_ahead(r, p, row + step);
+    T za = action_logit(row, use);
     for (; row < r.rows; row += step) {
-      const RowUse after = row_use(r, p, row + 2 * step);
-      const float next_za = action_logit(row + step, next);
+      const RowUse next_use = row_use(r, next);
+      next = row_ahead(r, p, row + 2 * step);
+      const T next_za = action_logit(row + step, next_use);
       int at_stage = 0, at_count = 0;
       if (computed(use)) {
         const RowPtr<T> z(r.logits + row * r.ld, use.n);
@@ -777,8 +794,6 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
         const uint4* held = ring + stage * kStage - lo;
         RowSum x;
         x.clear();
-        int held_lo, held_hi;
-        copied(z, row, lo, hi, &held_lo, &held_hi);
         wait(&full[stage], lap);
         int i = from + me;
         for (; i + 3 * kSum < to; i += 4 * kSum) {
@@ -791,12 +806,11 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
         }
         if (me < 2 && is_part(z, lo, hi)) {
           i = me == 0 ? 0 : z.whole_hi;
-          const uint4 q[1] = {i >= held_lo && i < held_hi ? z.only_row(held[i], i, n)
-                                                          : z.load_part(i, n)};
+          const uint4 q[1] = {part_of(z, row, lo, hi, i, n, held)};
           x.add<T>(q);
         }
         Part part = x.over(32);
-        part.za = za;
+        part.za = to_float(za);
         const int slot = count & 3;
         Part* at = &slots[slot][rank * kSumWarps + warp - 2];
         if (kCtas == 1) {
@@ -820,8 +834,7 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       due_use = use;
       due_stage = at_stage;
       due_count = at_count;
-      use = next;
-      next = after;
+      use = next_use;
       za = next_za;
     }
     if (due >= 0) gradient();
@@ -848,7 +861,7 @@ __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, A
   int parity = 0;
   Pair sum = {0.f, 0.f};
   for (int row = blockIdx.x / kLongCtas; row < r.rows; row += step) {
-    const RowUse use = row_use(r, p, row);
+    const RowUse use = row_use(r, row_ahead(r, p, row));
     const RowPtr<T> z(r.logits + row * r.ld, use.n);
     T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
     const bool aligned = dz != nullptr && same_alignment(dz, z.z);
