@@ -34,7 +34,6 @@ constexpr int kTerms = 6;                 // sums over the rows, in the order of
 constexpr int kMaxCtas = 152 * 16;        // partial sums that the workspace holds
 constexpr int kThreads = 256;
 constexpr int kMaxVisual = 2048;          // visual tokens per image held in shared memory
-constexpr int kPerThread = kMaxVisual / kThreads;
 
 // A sum as a pair of fp32 values, the second what the first lost (Knuth's two-sum).
 // Six fp32 additions where fp64 has one: fp64 sums over the rows took the kernel on
@@ -144,19 +143,6 @@ __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
     if (lane == 0) p.totals[i] = t.v + t.lost;
   }
   if (threadIdx.x == 0) ws->ticket = 0;
-}
-
-template <typename F>
-__device__ __forceinline__ F block_sum(F v, F* scratch) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = scratch[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) v += scratch[w];
-  return v;
 }
 
 // ---------------------------------------------------------------------------
@@ -919,46 +905,64 @@ __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, A
 }
 
 // ---------------------------------------------------------------------------
-// Ordered removals.  (m, s) stands for m + log s; sums of exponentials are only
-// ever added, so that nothing cancels whatever the range of the scores.
+// Ordered removals.  With M the image's largest score, e_j = e^{s_j - M}, and
+//   S_t = sum of e over the tokens not removed before step t   (suffix sums)
+//   Q_t = sum_{u <= t} 1 / S_u                                 (prefix sums)
+//   l = sum_t (s_{i_t} - M) - ln S_t,
+//   d l / d s_j = 1(j removed) - e_j Q_{u_j}, u_j its step, k for a token that stays:
+// both scans only add, and cost one exponential a token.  Scores that lie further
+// apart than kRange would underflow: such an image's sums are kept as pairs (m, s) for
+// s e^m, each with a maximum of its own, at two exponentials an addition.
+//
+// One CTA an image, a thread an equal run of steps; the removal order, one
+// round trip after another, is what an image takes (256 images of 197 tokens, 60
+// removed, 9 us; 1024 of 577, 120 removed, 13 us), so the CTAs are small and all of
+// a batch are resident at once.
 // ---------------------------------------------------------------------------
-struct Lse {
+constexpr int kSeqThreads = 128, kSeqWarps = kSeqThreads / 32, kSeqPerSm = 8;
+constexpr float kRange = 80.f;            // e^-kRange and its reciprocal are far from fp32's ends
+
+struct Scaled {                           // s e^m
   float m, s;
 };
-__device__ __forceinline__ Lse lse_merge(Lse a, Lse b) {
+__device__ __forceinline__ Scaled plus(Scaled a, Scaled b) {
   if (a.s == 0.f) return b;
   if (b.s == 0.f) return a;
   const float m = fmaxf(a.m, b.m);
   return {m, a.s * expf(a.m - m) + b.s * expf(b.m - m)};
 }
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ float zero(float) { return 0.f; }
+__device__ __forceinline__ Scaled zero(Scaled) { return {-INFINITY, 0.f}; }
+__device__ __forceinline__ float from_lane(float v, int lane) {
+  return __shfl_sync(0xffffffffu, v, lane);
+}
+__device__ __forceinline__ Scaled from_lane(Scaled v, int lane) {
+  return {__shfl_sync(0xffffffffu, v.m, lane), __shfl_sync(0xffffffffu, v.s, lane)};
+}
+// e^{s - M}, its reciprocal's like, its logarithm less M, and e^{s - M} times a sum.
+__device__ __forceinline__ float term_of(float s, float m, float) { return expf(s - m); }
+__device__ __forceinline__ Scaled term_of(float s, float m, Scaled) { return {s - m, 1.f}; }
+__device__ __forceinline__ float inverse(float v) { return 1.f / v; }
+__device__ __forceinline__ Scaled inverse(Scaled v) { return {-v.m, 1.f / v.s}; }
+__device__ __forceinline__ float log_of(float d, float v) { return d - logf(v); }
+__device__ __forceinline__ float log_of(float d, Scaled v) { return (d - v.m) - logf(v.s); }
+__device__ __forceinline__ float times_exp(float d, float v) { return expf(d) * v; }
+__device__ __forceinline__ float times_exp(float d, Scaled v) { return expf(d + v.m) * v.s; }
 
-// Inclusive scan over the block's threads of one pair each, from thread 0 on
-// (forward) or from the last one back; returns the exclusive value (what the
-// threads before, or after, hold together).
-template <bool kForward>
-__device__ __forceinline__ Lse block_scan(Lse v, Lse* scratch) {
-  constexpr int kWarps = kThreads / 32;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Lse inc = v;
+// Sum of the lanes before (kForward) or after each lane of the warp; `all` the warp's.
+template <bool kForward, typename V>
+__device__ __forceinline__ V warp_scan(V v, V* all) {
+  const int lane = threadIdx.x & 31;
+  V inc = v;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const Lse o = kForward ? Lse{__shfl_up_sync(0xffffffffu, inc.m, off),
-                                 __shfl_up_sync(0xffffffffu, inc.s, off)}
-                           : Lse{__shfl_down_sync(0xffffffffu, inc.m, off),
-                                 __shfl_down_sync(0xffffffffu, inc.s, off)};
-    if (kForward ? lane >= off : lane + off < 32) inc = lse_merge(o, inc);
+    const V o = from_lane(inc, kForward ? lane - off : lane + off);
+    if (kForward ? lane >= off : lane + off < 32) inc = plus(o, inc);
   }
-  __syncthreads();
-  if (lane == (kForward ? 31 : 0)) scratch[warp] = inc;
-  Lse before = kForward ? Lse{__shfl_up_sync(0xffffffffu, inc.m, 1),
-                              __shfl_up_sync(0xffffffffu, inc.s, 1)}
-                        : Lse{__shfl_down_sync(0xffffffffu, inc.m, 1),
-                              __shfl_down_sync(0xffffffffu, inc.s, 1)};
-  if (lane == (kForward ? 0 : 31)) before = Lse{-INFINITY, 0.f};
-  __syncthreads();
-  for (int i = 0; i < kWarps; ++i)
-    if (kForward ? i < warp : i > warp) before = lse_merge(before, scratch[i]);
-  return before;
+  *all = from_lane(inc, kForward ? 31 : 0);
+  const V before = from_lane(inc, kForward ? lane - 1 : lane + 1);
+  return lane == (kForward ? 0 : 31) ? zero(v) : before;
 }
 
 struct Sequences {
@@ -972,22 +976,92 @@ struct Sequences {
   int32_t* status;
 };
 
-__global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, Actions p) {
-  __shared__ float s[kMaxVisual];
-  __shared__ int32_t pos[kMaxVisual];     // 1 + the step that removes j, 0 if kept
-  __shared__ Lse upto[kMaxVisual];        // sum over u <= t of exp(-L_u)
-  __shared__ Lse part[kThreads / 32];
-  __shared__ double dpart[kThreads / 32];
-  __shared__ int bad;
+struct SequenceShared {
+  float s[kMaxVisual];                    // s_j - M
+  unsigned short step[kMaxVisual];        // 1 + the step that removes j, 0 if kept
+  Scaled sums[kMaxVisual];                // S_t, then Q_t (fp32: the first half)
+  Scaled part[3][kSeqWarps];
+  Pair lp[kSeqWarps];
+  float hi[kSeqWarps], lo[kSeqWarps];
+  int bad;
+};
+
+// An image's log-probability (in every thread); Q_t in h->sums.
+template <typename V>
+__device__ __forceinline__ Pair sequence_sums(SequenceShared* h, const int32_t* seq, int n, int k) {
+  V* sums = reinterpret_cast<V*>(h->sums);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (k + kSeqThreads - 1) / kSeqThreads;
+  const int c0 = min(static_cast<int>(threadIdx.x) * per, k), c1 = min(c0 + per, k);
+  const V none = zero(V());
+  V rest = none, own = none, all;
+  for (int j = threadIdx.x; j < n; j += kSeqThreads)
+    if (h->step[j] == 0) rest = plus(rest, term_of(h->s[j], 0.f, V()));
+  for (int t = c0; t < c1; ++t) own = plus(own, term_of(h->s[seq[t]], 0.f, V()));
+  warp_scan<true>(rest, &all);
+  V* part = reinterpret_cast<V*>(h->part);
+  if (lane == 0) part[warp] = all;
+  V acc = warp_scan<false>(own, &all);
+  if (lane == 0) part[kSeqWarps + warp] = all;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSeqWarps; ++w) {
+    acc = plus(acc, part[w]);
+    if (w > warp) acc = plus(acc, part[kSeqWarps + w]);
+  }
+  Pair lp = {0.f, 0.f};
+  V inv = none;
+  for (int t = c1 - 1; t >= c0; --t) {
+    const float d = h->s[seq[t]];
+    acc = plus(acc, term_of(d, 0.f, V()));
+    sums[t] = acc;
+    lp.add(log_of(d, acc));
+    inv = plus(inv, inverse(acc));
+  }
+  V up = warp_scan<true>(inv, &all);
+  if (lane == 0) part[2 * kSeqWarps + warp] = all;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) lp.add(shfl_xor(lp, off));
+  if (lane == 0) h->lp[warp] = lp;
+  __syncthreads();
+  lp = h->lp[0];
+#pragma unroll
+  for (int w = 0; w < kSeqWarps; ++w) {
+    if (w > 0) lp.add(h->lp[w]);
+    if (w < warp) up = plus(up, part[2 * kSeqWarps + w]);
+  }
+  for (int t = c0; t < c1; ++t) {
+    up = plus(up, inverse(sums[t]));
+    sums[t] = up;
+  }
+  __syncthreads();
+  return lp;
+}
+
+template <typename V>
+__device__ __forceinline__ void sequence_grad(const SequenceShared& h, float* grad, int n, int k,
+                                              float g) {
+  const V* sums = reinterpret_cast<const V*>(h.sums);
+  if (threadIdx.x == 0) grad[0] = 0.f;                                      // CLS
+  for (int j = threadIdx.x; j < n; j += kSeqThreads) {
+    const int u = h.step[j];
+    grad[1 + j] = g * ((u > 0 ? 1.f : 0.f) - times_exp(h.s[j], sums[(u > 0 ? u : k) - 1]));
+  }
+}
+
+__global__ void __launch_bounds__(kSeqThreads, kSeqPerSm)
+    pl_policy_loss_kernel(Sequences q, Actions p) {
+  __shared__ SequenceShared h;
   pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Pair sum = {0.f, 0.f};
   for (int img = blockIdx.x; img < q.batch; img += gridDim.x) {
     const int lo = q.cu[img], hi = q.cu[img + 1];
     int n = hi - lo - 1, k = q.k[img];
-    const float w = p.weights != nullptr ? p.weights[img] : 1.f;
+    const RowIn in = row_in(p, img, q.batch);
     const bool inside = lo >= 0 && hi >= lo && hi <= q.t_cap;
     __syncthreads();                      // the image before is done with shared memory
-    if (threadIdx.x == 0) bad = 0;
+    if (threadIdx.x == 0) h.bad = 0;
     if (!inside || n > kMaxVisual) {
       if (threadIdx.x == 0) record_status(q.status, DORA_ERR_DEVICE_SEQLEN);
       n = 0;
@@ -998,20 +1072,41 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
       k = k < 0 ? 0 : (k > n ? n : k);
       k = k > q.k_cap ? q.k_cap : k;
     }
-    const bool takes = k > 0 && w != 0.f;
+    const bool takes = k > 0 && in.w != 0.f;
     const int32_t* seq = q.order + static_cast<size_t>(img) * q.k_cap;
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-      s[j] = takes ? q.scores[lo + 1 + j] : 0.f;
-      pos[j] = 0;
+    float top = -INFINITY, low = INFINITY;
+    if (takes)
+      for (int j = threadIdx.x; j < n; j += kSeqThreads) {
+        const float s = q.scores[lo + 1 + j];
+        h.s[j] = s;
+        h.step[j] = 0;
+        top = fmaxf(top, s);
+        low = fminf(low, s);
+      }
+    top = warp_max(top, 32);
+    low = -warp_max(-low, 32);
+    if (lane == 0) {
+      h.hi[warp] = top;
+      h.lo[warp] = low;
     }
     __syncthreads();
-    if (takes)
-      for (int t = threadIdx.x; t < k; t += kThreads) {
+#pragma unroll
+    for (int w = 0; w < kSeqWarps; ++w) {
+      top = fmaxf(top, h.hi[w]);
+      low = fminf(low, h.lo[w]);
+    }
+    if (takes) {
+      for (int j = threadIdx.x; j < n; j += kSeqThreads) h.s[j] -= top;
+      for (int t = threadIdx.x; t < k; t += kSeqThreads) {
         const int j = seq[t];
-        if (j < 0 || j >= n || atomicCAS(&pos[j], 0, t + 1) != 0) bad = 1;   // range, repeats
+        if (j < 0 || j >= n ||
+            atomicCAS(&h.step[j], static_cast<unsigned short>(0),
+                      static_cast<unsigned short>(t + 1)) != 0)
+          h.bad = 1;                      // out of range, or twice
       }
+    }
     __syncthreads();
-    if (!takes || bad) {
+    if (!takes || h.bad) {
       const float fill = takes ? NAN : 0.f;
       if (threadIdx.x == 0) {
         if (takes) record_status(q.status, DORA_ERR_DEVICE_BAD_COUNT);
@@ -1020,70 +1115,24 @@ __global__ void __launch_bounds__(kThreads) pl_policy_loss_kernel(Sequences q, A
       }
       sum.add(all_terms(fill).of(threadIdx.x));
       if (q.grad != nullptr && inside)
-        for (int r = lo + threadIdx.x; r < hi; r += kThreads) q.grad[r] = fill;
+        for (int r = lo + threadIdx.x; r < hi; r += kSeqThreads) q.grad[r] = fill;
       continue;
     }
-    // what is never removed
-    Lse rest = {-INFINITY, 0.f};
-    for (int j = threadIdx.x; j < n; j += kThreads)
-      if (pos[j] == 0) rest = lse_merge(rest, Lse{s[j], 1.f});
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
-      rest = lse_merge(rest, Lse{__shfl_xor_sync(0xffffffffu, rest.m, off),
-                                 __shfl_xor_sync(0xffffffffu, rest.s, off)});
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = rest;
-    __syncthreads();
-    rest = part[0];
-    for (int i = 1; i < kThreads / 32; ++i) rest = lse_merge(rest, part[i]);
-    // thread i holds steps [c0, c1); L_t from the back
-    const int chunk = (k + kThreads - 1) / kThreads;
-    const int c0 = min(static_cast<int>(threadIdx.x) * chunk, k), c1 = min(c0 + chunk, k);
-    float v[kPerThread];
-    Lse left[kPerThread];
-    Lse own = {-INFINITY, 0.f};
-#pragma unroll
-    for (int i = kPerThread - 1; i >= 0; --i)
-      if (c0 + i < c1) {
-        v[i] = s[seq[c0 + i]];
-        own = lse_merge(own, Lse{v[i], 1.f});
-      }
-    Lse acc = lse_merge(rest, block_scan<false>(own, part));
-    double lp = 0.;
-    Lse inv = {-INFINITY, 0.f};           // sum of exp(-L_t) over the thread's steps
-#pragma unroll
-    for (int i = kPerThread - 1; i >= 0; --i)
-      if (c0 + i < c1) {
-        acc = lse_merge(acc, Lse{v[i], 1.f});
-        left[i] = acc;
-        lp += (v[i] - acc.m) - logf(acc.s);
-        inv = lse_merge(inv, Lse{-acc.m, 1.f / acc.s});
-      }
-    if (q.grad != nullptr) {
-      Lse up = block_scan<true>(inv, part);
-#pragma unroll
-      for (int i = 0; i < kPerThread; ++i)
-        if (c0 + i < c1) {
-          up = lse_merge(up, Lse{-left[i].m, 1.f / left[i].s});
-          upto[c0 + i] = up;
-        }
-    }
-    lp = block_sum(lp, dpart);            // its barriers publish `upto`
-    const float x = p.ref_logp != nullptr ? static_cast<float>(p.ref_logp[img] - lp) : 0.f;
+    const bool narrow = top - low <= kRange;              // false for infinities
+    const Pair lp = narrow ? sequence_sums<float>(&h, seq, n, k)
+                           : sequence_sums<Scaled>(&h, seq, n, k);
+    // l - q from the pair: the ratio of a long sequence keeps its digits
+    const float x = p.ref_logp != nullptr ? (in.ref - lp.v) - lp.lost : 0.f;
     Terms terms;
-    const float g = row_terms(p, static_cast<float>(lp - p.old_logp[img]), x, p.advantages[img], w,
-                              0.f, &terms);
+    const float g = row_terms(p, (lp.v - in.old_logp) + lp.lost, x, in.adv, in.w, 0.f, &terms);
     sum.add(terms.of(threadIdx.x));
     if (threadIdx.x == 0) {
-      p.logp[img] = static_cast<float>(lp);
+      p.logp[img] = lp.v + lp.lost;
       if (p.row_loss != nullptr) p.row_loss[img] = terms.v[0];
     }
     if (q.grad == nullptr) continue;
-    if (threadIdx.x == 0) q.grad[lo] = 0.f;                                 // CLS
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-      const int u = pos[j];
-      const Lse a = upto[u > 0 ? u - 1 : k - 1];
-      q.grad[lo + 1 + j] = g * ((u > 0 ? 1.f : 0.f) - a.s * expf(s[j] + a.m));
-    }
+    if (narrow) sequence_grad<float>(h, q.grad + lo, n, k, g);
+    else sequence_grad<Scaled>(h, q.grad + lo, n, k, g);
   }
   finish_totals(p, sum);
 }
@@ -1300,8 +1349,9 @@ int dora_pl_policy_loss(const float* scores, const int32_t* cu, int32_t batch, i
                ? DORA_OK
                : launched(cudaMemsetAsync(totals, 0, policy::kTerms * sizeof(float), stream));
   const policy::Sequences q = {scores, grad, cu, batch, t_cap, k, order, k_cap, status};
-  return launched(launch_pdl(policy::pl_policy_loss_kernel, dim3(grid_for(batch, 6)),
-                             dim3(policy::kThreads), 0, stream, q, p));
+  return launched(launch_pdl(policy::pl_policy_loss_kernel,
+                             dim3(grid_for(batch, policy::kSeqPerSm)), dim3(policy::kSeqThreads),
+                             0, stream, q, p));
 }
 
 }  // extern "C"
