@@ -7,7 +7,8 @@
 // units, whatever the tensors' sizes.  A CTA walks its span, piece by piece.  To
 // begin a tensor costs a CTA about as long as kBegin units take (its entry, then its
 // first values: two round trips to memory), and counts as that many: a hundred
-// vectors in a row would otherwise be one CTA's, while the others wait for it.
+// vectors in a row would otherwise be one CTA's, while the others wait for it.  A list
+// with no more units than spans has a unit a span, and nothing to count.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -24,7 +25,7 @@ namespace optim {
 
 constexpr int kThreads = 256;
 constexpr int kUnit = 1024;               // elements
-constexpr int kBegin = 6;                 // units
+constexpr int kBegin = 12;                // units, in lists of more than kMaxSpans
 constexpr int kCtasPerSm = 4;             // resident, by their registers
 constexpr int kMaxSpans = 152 * kCtasPerSm;   // a span a CTA, all at once
 constexpr int kFill = 48;                 // entries written by one launch, passed by value
@@ -36,8 +37,9 @@ struct Entry {
   float *m, *v;
   uint16_t* copy;                         // nullable, bf16
   int64_t n;
-  int64_t first_unit;                     // of its elements; kBegin units before belong to it
-  int32_t grad_type, param_type;
+  int64_t first_unit;                     // of its elements; `begin` units before belong to it
+  int32_t begin;
+  int32_t grad_type, param_type, pad;
 };
 
 // Units [unit, unit_end) of the whole list, from tensor `tensor` to `last_tensor`,
@@ -48,10 +50,17 @@ struct Span {
   Entry first, last;
 };
 
+// A CTA's sum of squares: fp32, and what did not fit its range in 64 bits.
+struct Partial {
+  float sum;
+  int has_wide;                           // fp64 comparisons are as slow as the sums
+  double wide;
+};
+
 struct Header {
   unsigned ticket;                        // CTAs done; zero between calls
   unsigned pad[63];
-  double partial[kMaxSpans];
+  Partial partial[kMaxSpans];
 };
 
 struct List {
@@ -78,8 +87,7 @@ __device__ __forceinline__ int tensor_of(const List& list, int64_t unit) {
   int lo = 0, hi = list.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    const Entry& e = list.entries[mid];
-    if (e.first_unit - (e.n > 0 ? kBegin : 0) <= unit) lo = mid; else hi = mid - 1;
+    if (list.entries[mid].first_unit - list.entries[mid].begin <= unit) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
@@ -166,6 +174,7 @@ constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e25f;
 
 struct SumOfSquares {
   float sum, lost;
+  int has_wide;
   double wide;
   __device__ __forceinline__ bool add(float x) {         // false: out of range
     if (!(x > kSquaresLow && x < kSquaresHigh)) return false;
@@ -174,8 +183,12 @@ struct SumOfSquares {
     sum = t;
     return true;
   }
+  __device__ __forceinline__ void add_wide(double x) {
+    has_wide = 1;
+    wide += x;
+  }
   __device__ __forceinline__ void add_one(float v) {
-    if (!add(v * v)) wide += static_cast<double>(v) * v;
+    if (!add(v * v) && v != 0.f) add_wide(static_cast<double>(v) * v);
   }
 };
 
@@ -228,83 +241,101 @@ __device__ __forceinline__ void piece_squares(const void* p, int type, int n, Su
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u)
         if ((q[u].x | q[u].y | q[u].z | q[u].w) != 0)
-          acc->wide += type == DORA_F32    ? wide_squares<float>(q[u])
-                       : type == DORA_BF16 ? wide_squares<__nv_bfloat16>(q[u])
-                                           : wide_squares<__half>(q[u]);
+          acc->add_wide(type == DORA_F32    ? wide_squares<float>(q[u])
+                        : type == DORA_BF16 ? wide_squares<__nv_bfloat16>(q[u])
+                                            : wide_squares<__half>(q[u]));
     }
   }
 }
 
-// Sum over the block, for the threads of its first warp.
-__device__ __forceinline__ double block_sum(double v, double* scratch) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = threadIdx.x < kThreads / 32 ? scratch[threadIdx.x] : 0.;
-#pragma unroll
-  for (int off = kThreads / 64; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  return v;
-}
-
-// The same of what the threads summed: fp32 within a warp (a few roundings of values
-// that are in the middle of the range), 64 bits from there on.
-__device__ __forceinline__ double block_sum(const SumOfSquares& mine, double* scratch) {
+// The sum over the block of what its threads summed, in thread 0.  fp32 in a tree: a
+// few roundings of values in the middle of the range; 64 bits, slow here, only for
+// what left it.
+__device__ __forceinline__ Partial block_sum(const SumOfSquares& mine, Partial* scratch) {
   float f = mine.sum + mine.lost;
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) f += __shfl_xor_sync(0xffffffffu, f, off);
-  double v = f;
-  if (__any_sync(0xffffffffu, mine.wide != 0.)) {
-    v = mine.wide;
+  const int has_wide = __any_sync(0xffffffffu, mine.has_wide);
+  double wide = 0.;
+  if (has_wide) {
+    wide = mine.wide;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    v += f;
+    for (int off = 16; off > 0; off >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, off);
   }
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = Partial{f, has_wide, wide};
   __syncthreads();
-  v = threadIdx.x < kThreads / 32 ? scratch[threadIdx.x] : 0.;
+  Partial all = scratch[0];
+  if (threadIdx.x == 0)
 #pragma unroll
-  for (int off = kThreads / 64; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  return v;
+    for (int w = 1; w < kThreads / 32; ++w) {
+      all.sum += scratch[w].sum;
+      if (scratch[w].has_wide) {
+        all.has_wide = 1;
+        all.wide += scratch[w].wide;
+      }
+    }
+  return all;
 }
 
-// out[0] = the norm, out[1] = min(1, max_norm / norm), 1 for a norm that is not finite; the CTA that is last adds
-// the spans' sums in their order.
+// out[0] = the norm, out[1] = min(1, max_norm / norm), 1 for a norm that is not finite.
+__device__ __forceinline__ void write_norm(const Partial& all, float max_norm, float* out) {
+  float norm = sqrtf(all.sum);
+  if (all.has_wide) norm = static_cast<float>(sqrt(all.wide + all.sum));
+  out[0] = norm;
+  out[1] = isfinite(norm) && norm > max_norm ? max_norm / norm : 1.f;
+}
+
+// The CTA that is last adds the spans' sums in their order.
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     grad_norm_kernel(List list, float max_norm, float* __restrict__ out) {
-  __shared__ double scratch[kThreads / 32];
+  __shared__ Partial scratch[kThreads / 32];
   __shared__ bool last;
   pdl_wait();
-  SumOfSquares mine = {0.f, 0.f, 0.};
+  SumOfSquares mine = {0.f, 0.f, 0, 0.};
   for_pieces<true>(list, blockIdx.x, [&](const Entry& e, int64_t from, int n) {
     piece_squares(at_elem(e.grad, e.grad_type, from), e.grad_type, n, &mine);
   });
-  const double acc = block_sum(mine, scratch);
+  const Partial cta = block_sum(mine, scratch);
+  if (gridDim.x == 1) {
+    if (threadIdx.x == 0) write_norm(cta, max_norm, out);
+    return;
+  }
   if (threadIdx.x == 0) {
-    list.header->partial[blockIdx.x] = acc;
+    list.header->partial[blockIdx.x] = cta;
     __threadfence();
     last = atomicAdd(&list.header->ticket, 1u) == gridDim.x - 1;
   }
   __syncthreads();
   if (!last) return;
   __threadfence();
-  double t = 0.;
-  for (int b = threadIdx.x; b < static_cast<int>(gridDim.x); b += kThreads)
-    t += __ldcg(&list.header->partial[b]);
-  t = block_sum(t, scratch);
+  constexpr int kLoads = (kMaxSpans + kThreads - 1) / kThreads;
+  int4 x[kLoads];                         // all on their way before the first is added
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int b = threadIdx.x + u * kThreads;
+    x[u] = b < static_cast<int>(gridDim.x)
+               ? __ldcg(reinterpret_cast<const int4*>(&list.header->partial[b]))
+               : make_int4(0, 0, 0, 0);
+  }
+  mine = SumOfSquares{0.f, 0.f, 0, 0.};
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const float f = __int_as_float(x[u].x);
+    if (!mine.add(f) && f != 0.f) mine.add_wide(f);
+    if (x[u].y) mine.add_wide(__hiloint2double(x[u].w, x[u].z));
+  }
+  const Partial all = block_sum(mine, scratch);
   if (threadIdx.x == 0) {
-    // fp64 square roots are long; most sums have one in fp32
-    const float norm = t > kSquaresLow && t < kSquaresHigh ? sqrtf(static_cast<float>(t))
-                                                           : static_cast<float>(sqrt(t));
-    out[0] = norm;
-    out[1] = isfinite(norm) && norm > max_norm ? max_norm / norm : 1.f;
+    write_norm(all, max_norm, out);
     list.header->ticket = 0;
   }
 }
 
 // ---------------------------------------------------------------------------
 // Clipping.  A norm that is not finite leaves the gradients as they are.  Spans
-// are walked from their ends, which the norm has read last and L2 may still hold.
+// are walked from their ends, which the norm has read last and L2 may still hold
+// (67 MB of fp32 28.7 us, 32.3 from the beginnings; 344 MB 167 and 172, of which
+// three passes at the copy rate are 152).
 // ---------------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ uint4 scaled(uint4 q, float f) {
@@ -479,10 +510,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) adam_step_kernel(List li
     skip = !isfinite(a.clip[0]);
     s.f = a.clip[1];
   }
-  const double p1 = (st.step > 0 ? st.power1 : 1.) * a.beta1;
-  const double p2 = (st.step > 0 ? st.power2 : 1.) * a.beta2;
-  s.step_size = a.lr / static_cast<float>(1. - p1);
-  s.root_scale = 1.f / sqrtf(static_cast<float>(1. - p2));
+  // fp64 for one thread: for all of them it would take the CTA longer than a small tensor
+  __shared__ float scales[2];
+  double p1 = 0., p2 = 0.;
+  if (threadIdx.x == 0) {
+    p1 = (st.step > 0 ? st.power1 : 1.) * a.beta1;
+    p2 = (st.step > 0 ? st.power2 : 1.) * a.beta2;
+    scales[0] = a.lr / static_cast<float>(1. - p1);
+    scales[1] = 1.f / sqrtf(static_cast<float>(1. - p2));
+  }
+  __syncthreads();
+  s.step_size = scales[0];
+  s.root_scale = scales[1];
   if (!skip)
     for_pieces<false>(list, blockIdx.x, [&](const Entry& e, int64_t from, int n) {
       piece_adam(a, s, e, from, n);
@@ -528,38 +567,44 @@ bool aligned_to(const void* p, int32_t dtype) {
 
 bool known_type(int32_t t) { return t >= DORA_BF16 && t <= DORA_F32; }
 
-// A tensor's units, with those that count for its begin.
-int64_t units_of(int64_t n) {
-  return n > 0 ? optim::kBegin + (n + optim::kUnit - 1) / optim::kUnit : 0;
+int64_t units_of(int64_t n) { return (n + optim::kUnit - 1) / optim::kUnit; }
+
+// The units that a tensor's begin counts for in a list of so many, and all of them.
+struct Layout {
+  int begin, spans;
+  int64_t units;
+};
+Layout layout_of(int64_t units, int64_t tensors) {
+  if (units <= optim::kMaxSpans) return {0, units > 0 ? static_cast<int>(units) : 1, units};
+  return {optim::kBegin, optim::kMaxSpans, units + tensors * optim::kBegin};
 }
 
-// Checks the tensors and counts their units; -1 when one is not valid.
-int64_t count_units(const dora_param* params, int32_t count, int64_t* elements, bool* has_params) {
-  int64_t units = 0;
+// Checks the tensors and counts their units, elements and those that are not empty;
+// false when one is not valid.
+bool count_units(const dora_param* params, int32_t count, Layout* out, int64_t* elements,
+                 bool* has_params) {
+  int64_t units = 0, tensors = 0;
   *elements = 0;
   *has_params = true;
   for (int32_t i = 0; i < count; ++i) {
     const dora_param& t = params[i];
-    if (t.n < 0 || t.n > (int64_t{1} << 40) || !known_type(t.grad_dtype)) return -1;
+    if (t.n < 0 || t.n > (int64_t{1} << 40) || !known_type(t.grad_dtype)) return false;
     if (t.n > 0 && (t.grad == nullptr || !aligned_to(t.grad, t.grad_dtype) ||
                     !aligned_to(t.clipped, t.grad_dtype)))
-      return -1;
+      return false;
     const int given = (t.param != nullptr) + (t.exp_avg != nullptr) + (t.exp_avg_sq != nullptr);
-    if (t.n > 0 && given != 0 && given != 3) return -1;
+    if (t.n > 0 && given != 0 && given != 3) return false;
     if (t.n > 0 && given == 0) *has_params = false;
     if (given == 3 && (!known_type(t.param_dtype) || !aligned_to(t.param, t.param_dtype) ||
                        !aligned_to(t.exp_avg, DORA_F32) || !aligned_to(t.exp_avg_sq, DORA_F32) ||
                        !aligned_to(t.copy, DORA_BF16)))
-      return -1;
+      return false;
     units += units_of(t.n);
+    tensors += t.n > 0;
     *elements += t.n;
   }
-  return units;
-}
-
-int spans_for(int64_t units) {
-  if (units < 1) return 1;
-  return units < optim::kMaxSpans ? static_cast<int>(units) : optim::kMaxSpans;
+  *out = layout_of(units, tensors);
+  return true;
 }
 
 optim::List layout(void* data, int count, int spans) {
@@ -587,11 +632,11 @@ size_t dora_param_list_size(const dora_param* params, int32_t count) {
   if (params == nullptr || count < 1) return 0;
   int64_t elements;
   bool has_params;
-  const int64_t units = count_units(params, count, &elements, &has_params);
-  if (units < 0) return 0;
+  Layout plan;
+  if (!count_units(params, count, &plan, &elements, &has_params)) return 0;
   return round256(sizeof(optim::Header)) +
          round256(static_cast<size_t>(count) * sizeof(optim::Entry)) +
-         round256(static_cast<size_t>(spans_for(units)) * sizeof(optim::Span));
+         round256(static_cast<size_t>(plan.spans) * sizeof(optim::Span));
 }
 
 int dora_param_list_prepare(const dora_param* params, int32_t count, void* data, size_t bytes,
@@ -601,29 +646,31 @@ int dora_param_list_prepare(const dora_param* params, int32_t count, void* data,
     return DORA_ERR_INVALID_ARG;
   int64_t elements;
   bool has_params;
-  const int64_t units = count_units(params, count, &elements, &has_params);
-  if (units < 0 || bytes < dora_param_list_size(params, count)) return DORA_ERR_INVALID_ARG;
+  Layout plan;
+  if (!count_units(params, count, &plan, &elements, &has_params) ||
+      bytes < dora_param_list_size(params, count))
+    return DORA_ERR_INVALID_ARG;
   const int e = device_or_error();
   if (e != DORA_OK) return e;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-  const optim::List l = layout(data, count, spans_for(units));
+  const optim::List l = layout(data, count, plan.spans);
   int64_t unit = 0;
   for (int32_t first = 0; first < count; first += optim::kFill) {
     const int some = count - first < optim::kFill ? count - first : optim::kFill;
     optim::FillArgs args = {};
     for (int i = 0; i < some; ++i) {
       const dora_param& t = params[first + i];
+      const int begin = t.n > 0 ? plan.begin : 0;
       args.e[i] = optim::Entry{t.grad, t.clipped, t.param, t.exp_avg, t.exp_avg_sq, t.copy, t.n,
-                               unit + (t.n > 0 ? optim::kBegin : 0), t.grad_dtype,
-                               t.param_dtype};
-      unit += units_of(t.n);
+                               unit + begin, begin, t.grad_dtype, t.param_dtype, 0};
+      unit += begin + units_of(t.n);
     }
     const int rc = launched(launch_pdl(optim::fill_entries_kernel, dim3(1), dim3(optim::kFill), 0,
                                        stream, l.header, l.entries, first, some, args));
     if (rc != DORA_OK) return rc;
   }
   const int rc = launched(launch_pdl(optim::fill_spans_kernel, dim3((l.n_spans + 127) / 128),
-                                     dim3(128), 0, stream, l, units));
+                                     dim3(128), 0, stream, l, plan.units));
   if (rc != DORA_OK) return rc;
   *list = dora_param_list{data, elements, count, l.n_spans, has_params ? 1 : 0};
   return DORA_OK;

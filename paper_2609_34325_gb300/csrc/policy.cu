@@ -57,7 +57,7 @@ __device__ __forceinline__ Pair shfl_xor(Pair p, int off) {
 struct Workspace {
   unsigned ticket;                        // CTAs done; zero between calls
   unsigned pad[63];
-  Pair partial[kTerms][kMaxCtas];
+  Pair partial[kMaxCtas][kTerms];
 };
 
 // What both losses take per action, and the terms' coefficients.
@@ -108,10 +108,16 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   return g * w;
 }
 
+// Two terms of a CTA that is done.
+__device__ __forceinline__ float4 load_terms(const Workspace* ws, int cta, int i) {
+  return __ldcg(reinterpret_cast<const float4*>(ws->partial[cta]) + i);
+}
+
 // The totals.  Lanes i < kTerms of a CTA's first warp hold its sum of term i.  It goes
 // to the CTA's place in the workspace; the CTA that is last adds all of them in the
 // order of the CTAs, so that the totals do not depend on which one that is, and leaves
 // the ticket at zero for the next call.
+template <int kWarps>
 __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   if (p.totals == nullptr) return;
   if (gridDim.x == 1) {
@@ -122,7 +128,7 @@ __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   Workspace* ws = p.ws;
   if (threadIdx.x < 32) {
     if (threadIdx.x < kTerms) {
-      ws->partial[threadIdx.x][blockIdx.x] = sum;
+      ws->partial[blockIdx.x][threadIdx.x] = sum;
       __threadfence();
     }
     __syncwarp();
@@ -131,16 +137,42 @@ __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   __syncthreads();
   if (!last) return;
   __threadfence();
-  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  for (int i = threadIdx.x >> 5; i < kTerms; i += warps) {
-    Pair t = {0.f, 0.f};
-    for (int c = lane; c < static_cast<int>(gridDim.x); c += 32) {
-      const float2 x = __ldcg(reinterpret_cast<const float2*>(&ws->partial[i][c]));
-      t.add(Pair{x.x, x.y});
-    }
+  constexpr int kLoads = 3, kBatch = 3;   // a CTA's terms are three 16-byte loads
+  static_assert(kTerms == 2 * kLoads, "two pairs a load");
+  constexpr int threads = kWarps * 32;
+  const int lane = threadIdx.x & 31, ctas = gridDim.x;
+  Pair t[kTerms];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) t.add(shfl_xor(t, off));
-    if (lane == 0) p.totals[i] = t.v + t.lost;
+  for (int i = 0; i < kTerms; ++i) t[i] = Pair{0.f, 0.f};
+  for (int first = threadIdx.x; first < ctas; first += kBatch * threads) {
+    float4 x[kBatch][kLoads];             // all on their way before the first is added
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        x[u][i] = first + u * threads < ctas ? load_terms(ws, first + u * threads, i)
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        t[2 * i].add(Pair{x[u][i].x, x[u][i].y});
+        t[2 * i + 1].add(Pair{x[u][i].z, x[u][i].w});
+      }
+  }
+  __shared__ Pair warps[kWarps][kTerms];
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) t[i].add(shfl_xor(t[i], off));
+    if (lane == 0) warps[threadIdx.x >> 5][i] = t[i];
+  }
+  __syncthreads();
+  if (threadIdx.x < kTerms) {
+    Pair all = warps[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) all.add(warps[w][threadIdx.x]);
+    p.totals[threadIdx.x] = all.v + all.lost;
   }
   if (threadIdx.x == 0) ws->ticket = 0;
 }
@@ -537,7 +569,7 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
   if (threadIdx.x < kTerms)
 #pragma unroll
     for (int k = 1; k < kThreads / 32; ++k) sum.add(all[k][threadIdx.x]);
-  finish_totals(p, sum);
+  finish_totals<kThreads / 32>(p, sum);
 }
 
 // A part into the place `slot` of CTA `cta` of the cluster.
@@ -571,9 +603,9 @@ __device__ __forceinline__ Part join_parts(const Part* slots) {
 }
 
 // Longer rows: kCtas CTAs (a cluster when there are several) hold one, an equal part
-// each, in a ring of kStages stages of shared memory.  Three kinds of warps, so that
-// nothing waits for a row's one reduction: while it is on its way the next row is
-// being summed, and the one after it loaded.
+// each, in a ring of kStages stages of shared memory (more, where they fit, changed
+// nothing).  Three kinds of warps, so that nothing waits for a row's one reduction:
+// while it is on its way the next row is being summed, and the one after it loaded.
 //   warp 1          fills the stages: one bulk copy of a row's whole granules;
 //   warps 2..       sum their granules of row i (one read of the stage, kept in
 //                   registers for the maximum and the exponentials), send the parts
@@ -827,7 +859,7 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
   }
   __syncwarp();
   if (kCtas > 1) cluster_sync();          // nobody leaves while parts may be on their way to it
-  finish_totals(p, sum);
+  finish_totals<kSumWarps + 2>(p, sum);
 }
 
 // Rows longer than a cluster's registers: the same without the ring; a row is read a
@@ -901,7 +933,7 @@ __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, A
         for (int i = g0; i < end; i += kStride) fill_granule(z, dz, aligned, i, r.classes, fill);
     }
   }
-  finish_totals(p, sum);
+  finish_totals<kWarps>(p, sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -1134,7 +1166,7 @@ __global__ void __launch_bounds__(kSeqThreads, kSeqPerSm)
     if (narrow) sequence_grad<float>(h, q.grad + lo, n, k, g);
     else sequence_grad<Scaled>(h, q.grad + lo, n, k, g);
   }
-  finish_totals(p, sum);
+  finish_totals<kSeqWarps>(p, sum);
 }
 
 }  // namespace policy
@@ -1238,11 +1270,11 @@ int launch_ring(cudaStream_t stream, const policy::Rows<T>& r, const policy::Act
                                              static_cast<int>(smem));
   if (e != cudaSuccess) return launched(e);
   static std::atomic<int> cache[kMaxDevices];
+  constexpr int kThreads = kSumWarps * 32 + 64;
   const int most = kCtas == 1 ? num_sms() * kPerSm
-                              : resident_clusters<T>(kern, kSumWarps * 32 + 64, kCtas, smem, cache);
+                              : resident_clusters<T>(kern, kThreads, kCtas, smem, cache);
   if (most < 1) return DORA_ERR_CUDA;
-  return launch_rows<T>(kern, r.rows < most ? r.rows : most, kSumWarps * 32 + 64, kCtas, smem,
-                        stream, r, p);
+  return launch_rows<T>(kern, r.rows < most ? r.rows : most, kThreads, kCtas, smem, stream, r, p);
 }
 
 template <typename T>
@@ -1295,7 +1327,8 @@ int dora_policy_loss(const void* logits, int32_t dtype, int32_t rows, int32_t cl
                      float* logp, float* entropy, float* row_loss, void* grad, float* totals,
                      void* workspace, size_t workspace_bytes, int32_t* status,
                      dora_stream_t stream_) {
-  if (rows < 0 || rows > (1 << 30) || classes < 1 || ld < classes || dtype < DORA_BF16 || dtype > DORA_F32)
+  if (rows < 0 || rows > (1 << 30) || classes < 1 || ld < classes || dtype < DORA_BF16 ||
+      dtype > DORA_F32)
     return DORA_ERR_INVALID_ARG;
   if (rows > 0 && (logits == nullptr || actions == nullptr)) return DORA_ERR_INVALID_ARG;
   const uintptr_t size_mask = dtype == DORA_F32 ? 3u : 1u;
