@@ -604,26 +604,30 @@ __device__ __forceinline__ Part join_parts(const Part* slots) {
 
 // Longer rows: kCtas CTAs (a cluster when there are several) hold one, an equal part
 // each, in a ring of kStages stages of shared memory (more, where they fit, changed
-// nothing).  Three kinds of warps, so that nothing waits for a row's one reduction:
-// while it is on its way the next row is being summed, and the one after it loaded.
-//   warp 1          fills the stages: one bulk copy of a row's whole granules;
-//   warps 2..       sum their granules of row i (one read of the stage, kept in
-//                   registers for the maximum and the exponentials), send the parts
-//                   to every CTA of the cluster, then write the gradient of row i - 1;
-//   warp 0          joins the parts of row i, finishes its scalars and hands the
-//                   gradient's coefficients to its CTA.
-// Parts have four places: a warp sends those of row i + 4 after its CTA has joined
-// row i + 2, hence after every CTA's sums of row i + 2, which follow that CTA's
-// coefficients of row i and with them its last look at the parts of row i.
-template <typename T, int kSumWarps, int kCtas, int kStages, int kPerSm>
-__global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
+// nothing).  Four kinds of warps, so that a row's steps, which wait for one another,
+// run beside those of the rows before and after it:
+//   warp 1            fills the stages: one bulk copy of a row's whole granules;
+//   kSumWarps         sum their granules and leave the parts to warp 0;
+//   warp 0            joins the CTA's parts, sends the CTA's own to every CTA of the
+//                     cluster, joins those, finishes the row's scalars and hands the
+//                     gradient's coefficients to
+//   kGradWarps        which write the gradient and free the stage.
+// (One kind of warp that sums row i and then writes the gradient of row i - 1 took
+// 48 us for 2048 x 32000 bf16 and 179 for 4096 x 50000 fp16: a row costs a warp about a
+// microsecond besides its granules, of which nothing was hidden.)
+// Between CTAs only warp 0 speaks: an arrival that others may read behind waits for
+// all that its thread has stored, and other warps have gradients on their way.
+// Two places for the parts are enough: a warp leaves those of row i + 2 once warp 0 has
+// taken those of row i, and a CTA sends row i + 2 after it has had every CTA's part of
+// row i + 1, which they send when they are done with those of row i.
+template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas, int kPerSm>
+__global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
     policy_ring_kernel(Rows<T> r, Actions p) {
-  constexpr int kHeld = 8, kSum = kSumWarps * 32, kStage = kSum * kHeld;
-  constexpr int kParts = kSumWarps * kCtas;
+  constexpr int kStages = 3;
   extern __shared__ __align__(128) uint4 ring[];
-  __shared__ Part slots[4][kParts];
+  __shared__ Part slots[2][kSumWarps], ctas[2][kCtas];
   __shared__ RowGrad grads[2];
-  __shared__ uint64_t full[kStages], empty[kStages], joined[4], ready[2];
+  __shared__ uint64_t full[kStages], empty[kStages], summed[2], joined[2], ready[2], taken[2];
   __shared__ int abort;
   const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int step = gridDim.x / kCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -631,10 +635,14 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
     abort = 0;
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], kSumWarps);
+      mbar_init(&empty[s], kGradWarps);
     }
-    for (int s = 0; s < 4; ++s) mbar_init(&joined[s], kParts);
-    for (int s = 0; s < 2; ++s) mbar_init(&ready[s], 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&summed[s], kSumWarps);
+      mbar_init(&joined[s], kCtas);
+      mbar_init(&ready[s], 1);
+      mbar_init(&taken[s], kGradWarps);
+    }
     fence_barrier_init();
   }
   if (kCtas > 1) cluster_sync();          // the others' barriers are there to be written
@@ -659,9 +667,28 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
   auto wait = [&](uint64_t* bar, int phase) {
     if (!mbar_wait(bar, phase & 1, &abort)) record_status(r.status, DORA_ERR_TIMEOUT);
   };
+  // Whether the row's first granule (it starts inside it), or its last with legal logits
+  // (they end inside it), is this CTA's: thread 0 and thread 1 of a kind see to them.
+  auto is_part = [](const RowPtr<T>& z, int me, int lo, int hi) {
+    if (me == 0) return lo == 0 && z.whole_lo > 0;
+    return z.whole_hi < z.some_hi && z.whole_hi >= max(lo, z.whole_lo) && z.whole_hi < hi;
+  };
+  auto part_of = [&](const RowPtr<T>& z, int row, int lo, int hi, int i, int n,
+                     const uint4* held) {
+    int from, to;
+    copied(z, row, lo, hi, &from, &to);
+    return i >= from && i < to ? z.only_row(held[i], i, n) : z.load_part(i, n);
+  };
   Pair sum = {0.f, 0.f};
   int row = blockIdx.x / kCtas;
   int stage = 0, lap = 0, count = 0;      // of the rows that are computed
+  auto advance = [&]() {
+    ++count;
+    if (++stage == kStages) {
+      stage = 0;
+      ++lap;
+    }
+  };
   RowAhead next = row_ahead(r, p, row);
 
   if (warp == 1) {
@@ -669,25 +696,20 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       for (; row < r.rows; row += step) {
         const RowUse use = row_use(r, next);
         next = row_ahead(r, p, row + step);
-        if (computed(use)) {
-          const RowPtr<T> z(r.logits + row * r.ld, use.n);
-          int lo, hi;
-          bounds(z, &lo, &hi);
-          int from, to;
-          copied(z, row, lo, hi, &from, &to);
-          if (lap > 0) wait(&empty[stage], lap - 1);
-          if (to > from) {
-            mbar_arrive_expect_tx(&full[stage], (to - from) * 16);
-            bulk_load(ring + stage * kStage + (from - lo), z.at(from), (to - from) * 16,
-                      &full[stage]);
-          } else {
-            mbar_arrive(&full[stage]);
-          }
-          if (++stage == kStages) {
-            stage = 0;
-            ++lap;
-          }
+        if (!computed(use)) continue;
+        const RowPtr<T> z(r.logits + row * r.ld, use.n);
+        int lo, hi, from, to;
+        bounds(z, &lo, &hi);
+        copied(z, row, lo, hi, &from, &to);
+        if (lap > 0) wait(&empty[stage], lap - 1);
+        if (to > from) {
+          mbar_arrive_expect_tx(&full[stage], (to - from) * 16);
+          bulk_load(ring + stage * kStage + (from - lo), z.at(from), (to - from) * 16,
+                    &full[stage]);
+        } else {
+          mbar_arrive(&full[stage]);
         }
+        advance();
       }
       if (abort)                          // no copy may land after the CTA is gone
         for (int s = 0; s < kStages; ++s)
@@ -701,19 +723,28 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       next = row_ahead(r, p, row + step);
       const RowIn next_in = row_in(p, row + step, r.rows);
       if (computed(use)) {
-        const int slot = count & 3;
-        if (kCtas == 1) {
-          wait(&joined[slot], count >> 2);
-        } else if (!mbar_wait_cluster(&joined[slot], (count >> 2) & 1, &abort)) {
-          record_status(r.status, DORA_ERR_TIMEOUT);
-        }
+        const int slot = count & 1, phase = count >> 1;
+        wait(&summed[slot], phase);
         __syncwarp();
-        const Part x = join_parts<kParts>(slots[slot]);
+        Part x = join_parts<kSumWarps>(slots[slot]);
+        if (kCtas > 1) {
+          if (lane < kCtas) {
+            store_part_remote(x, &ctas[slot][rank], lane);
+            mbar_arrive_remote(&joined[slot], lane);
+          }
+          if (!mbar_wait_cluster(&joined[slot], phase & 1, &abort))
+            record_status(r.status, DORA_ERR_TIMEOUT);
+          __syncwarp();
+          x = join_parts<kCtas>(ctas[slot]);
+        }
         Terms terms;
         const RowGrad k = finish_row(r, p, in, row, x.za, x, leader, &terms);
+        // the coefficients before the last ones have been taken
+        if (count >= 2) wait(&taken[slot], phase - 1);
+        __syncwarp();
         if (lane == 0) {
-          grads[count & 1] = k;
-          mbar_arrive(&ready[count & 1]);
+          grads[slot] = k;
+          mbar_arrive(&ready[slot]);
         }
         if (rank == 0) sum.add(terms.of(lane));
         ++count;
@@ -724,69 +755,9 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       }
       in = next_in;
     }
-  } else {
+  } else if (warp < 2 + kSumWarps) {
+    constexpr int kSum = kSumWarps * 32;
     const int me = threadIdx.x - 64;
-    // Whether thread 0 has to see to the row's first granule (the row starts inside it),
-    // thread 1 to its last with legal logits (they end inside it).
-    auto is_part = [me](const RowPtr<T>& z, int lo, int hi) {
-      if (me == 0) return lo == 0 && z.whole_lo > 0;
-      return z.whole_hi < z.some_hi && z.whole_hi >= max(lo, z.whole_lo) && z.whole_hi < hi;
-    };
-    auto part_of = [&](const RowPtr<T>& z, int row, int lo, int hi, int i, int n,
-                       const uint4* held) {
-      int from, to;
-      copied(z, row, lo, hi, &from, &to);
-      return i >= from && i < to ? z.only_row(held[i], i, n) : z.load_part(i, n);
-    };
-    // the row whose gradient is due
-    int due = -1, due_stage = 0, due_count = 0;
-    RowUse due_use = {-1, 0, false};
-    auto gradient = [&]() {
-      const RowPtr<T> z(r.logits + due * r.ld, due_use.n);
-      T* dz = r.grad != nullptr ? r.grad + due * r.ld : nullptr;
-      const bool aligned = dz != nullptr && same_alignment(dz, z.z);
-      int lo, hi;
-      bounds(z, &lo, &hi);
-      if (computed(due_use)) {
-        const int n = due_use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
-        const uint4* held = ring + due_stage * kStage - lo;
-        wait(&ready[due_count & 1], due_count >> 1);
-        if (dz != nullptr) {
-          const RowGrad k = grads[due_count & 1];
-          int i = from + me;
-          if (aligned) {
-            uint4* out = z.as_granules(dz);
-            if (k.b == 0.f) {
-#pragma unroll 2
-              for (; i < to; i += kSum) out[i] = grad_granule<T, false>(held[i], k);
-            } else {
-#pragma unroll 2
-              for (; i < to; i += kSum) out[i] = grad_granule<T, true>(held[i], k);
-            }
-          } else {
-            for (; i < to; i += kSum)
-              z.store_part(dz, false, i, n, r.classes, grad_granule<T>(held[i], k));
-          }
-          // the granules that are not whole (threads 0 and 1), and those past the legal logits
-          i = me == 0 ? 0 : z.whole_hi;
-          if (me < 2 && is_part(z, lo, hi))
-            z.store_part(dz, aligned, i, n, r.classes,
-                         grad_granule<T>(part_of(z, due, lo, hi, i, n, held), k));
-          for (i = max(lo, z.some_hi) + me; i < hi; i += kSum)
-            fill_granule(z, dz, aligned, i, r.classes, 0.f);
-          // the thread that has stored the action's granule
-          const int ia = (due_use.action + z.mis) / z.kE;
-          const int owner = ia < z.whole_lo ? 0 : ia < z.whole_hi ? (ia - from) & (kSum - 1) : 1;
-          if (ia >= lo && ia < hi && owner == me) from_float(k.at_action, dz + due_use.action);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[due_stage]);
-      } else if (dz != nullptr) {
-        const float fill = due_use.takes ? NAN : 0.f;
-        for (int i = lo + me; i < hi; i += kSum)
-          fill_granule(z, dz, aligned, i, r.classes, fill);
-      }
-    };
     // The action's logit goes with the first warp's part: read before any CTA can write
     // the row's gradient, which may lie over its logits.  It and the row's scalars are
     // on their way a row and two rows ahead.
@@ -803,7 +774,6 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
       const RowUse next_use = row_use(r, next);
       next = row_ahead(r, p, row + 2 * step);
       const T next_za = action_logit(row + step, next_use);
-      int at_stage = 0, at_count = 0;
       if (computed(use)) {
         const RowPtr<T> z(r.logits + row * r.ld, use.n);
         int lo, hi;
@@ -822,44 +792,83 @@ __global__ void __launch_bounds__(kSumWarps * 32 + 64, kPerSm)
           const uint4 q[1] = {held[i]};
           x.add<T>(q);
         }
-        if (me < 2 && is_part(z, lo, hi)) {
+        if (me < 2 && is_part(z, me, lo, hi)) {
           i = me == 0 ? 0 : z.whole_hi;
           const uint4 q[1] = {part_of(z, row, lo, hi, i, n, held)};
           x.add<T>(q);
         }
         Part part = x.over(32);
         part.za = to_float(za);
-        const int slot = count & 3;
-        Part* at = &slots[slot][rank * kSumWarps + warp - 2];
-        if (kCtas == 1) {
-          if (lane == 0) {
-            *at = part;
-            mbar_arrive(&joined[slot]);
-          }
-        } else if (lane < kCtas) {
-          store_part_remote(part, at, lane);
-          mbar_arrive_remote(&joined[slot], lane);
+        const int slot = count & 1;
+        if (count >= 2) wait(&ready[slot], (count >> 1) - 1);   // warp 0 has taken them
+        if (lane == 0) {
+          slots[slot][warp - 2] = part;
+          mbar_arrive(&summed[slot]);
         }
-        at_stage = stage;
-        at_count = count++;
-        if (++stage == kStages) {
-          stage = 0;
-          ++lap;
-        }
+        advance();
       }
-      if (due >= 0) gradient();
-      due = row;
-      due_use = use;
-      due_stage = at_stage;
-      due_count = at_count;
       use = next_use;
       za = next_za;
     }
-    if (due >= 0) gradient();
+  } else {
+    constexpr int kGrad = kGradWarps * 32;
+    const int me = threadIdx.x - 64 - kSumWarps * 32;
+    for (; row < r.rows; row += step) {
+      const RowUse use = row_use(r, next);
+      next = row_ahead(r, p, row + step);
+      const RowPtr<T> z(r.logits + row * r.ld, use.n);
+      T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
+      const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+      int lo, hi;
+      bounds(z, &lo, &hi);
+      if (computed(use)) {
+        const int n = use.n, from = max(lo, z.whole_lo), to = min(hi, z.whole_hi);
+        const uint4* held = ring + stage * kStage - lo;
+        wait(&full[stage], lap);
+        wait(&ready[count & 1], count >> 1);
+        const RowGrad k = grads[count & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&taken[count & 1]);
+        if (dz != nullptr) {
+          int i = from + me;
+          if (aligned) {
+            uint4* out = z.as_granules(dz);
+            if (k.b == 0.f) {
+#pragma unroll 2
+              for (; i < to; i += kGrad) out[i] = grad_granule<T, false>(held[i], k);
+            } else {
+#pragma unroll 2
+              for (; i < to; i += kGrad) out[i] = grad_granule<T, true>(held[i], k);
+            }
+          } else {
+            for (; i < to; i += kGrad)
+              z.store_part(dz, false, i, n, r.classes, grad_granule<T>(held[i], k));
+          }
+          // the granules that are not whole, and those past the legal logits
+          i = me == 0 ? 0 : z.whole_hi;
+          if (me < 2 && is_part(z, me, lo, hi))
+            z.store_part(dz, aligned, i, n, r.classes,
+                         grad_granule<T>(part_of(z, row, lo, hi, i, n, held), k));
+          for (i = max(lo, z.some_hi) + me; i < hi; i += kGrad)
+            fill_granule(z, dz, aligned, i, r.classes, 0.f);
+          // the thread that has stored the action's granule
+          const int ia = (use.action + z.mis) / z.kE;
+          const int owner = ia < z.whole_lo ? 0 : ia < z.whole_hi ? (ia - from) % kGrad : 1;
+          if (ia >= lo && ia < hi && owner == me) from_float(k.at_action, dz + use.action);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[stage]);
+        advance();
+      } else if (dz != nullptr) {
+        const float fill = use.takes ? NAN : 0.f;
+        for (int i = lo + me; i < hi; i += kGrad)
+          fill_granule(z, dz, aligned, i, r.classes, fill);
+      }
+    }
   }
   __syncwarp();
   if (kCtas > 1) cluster_sync();          // nobody leaves while parts may be on their way to it
-  finish_totals<kSumWarps + 2>(p, sum);
+  finish_totals<2 + kSumWarps + kGradWarps>(p, sum);
 }
 
 // Rows longer than a cluster's registers: the same without the ring; a row is read a
@@ -1261,16 +1270,16 @@ int resident_clusters(RowsKernel<T> kern, int block, int ctas, size_t smem,
 }
 
 // kPerSm CTAs an SM; the grid is what is resident at once.
-template <typename T, int kSumWarps, int kCtas, int kPerSm>
+template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas, int kPerSm>
 int launch_ring(cudaStream_t stream, const policy::Rows<T>& r, const policy::Actions& p) {
-  constexpr int kStages = 3;
-  const RowsKernel<T> kern = policy::policy_ring_kernel<T, kSumWarps, kCtas, kStages, kPerSm>;
-  constexpr size_t smem = static_cast<size_t>(kStages) * kSumWarps * 32 * 8 * 16;
+  const RowsKernel<T> kern =
+      policy::policy_ring_kernel<T, kSumWarps, kGradWarps, kStage, kCtas, kPerSm>;
+  constexpr size_t smem = static_cast<size_t>(3) * kStage * 16;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(smem));
   if (e != cudaSuccess) return launched(e);
   static std::atomic<int> cache[kMaxDevices];
-  constexpr int kThreads = kSumWarps * 32 + 64;
+  constexpr int kThreads = (2 + kSumWarps + kGradWarps) * 32;
   const int most = kCtas == 1 ? num_sms() * kPerSm
                               : resident_clusters<T>(kern, kThreads, kCtas, smem, cache);
   if (most < 1) return DORA_ERR_CUDA;
@@ -1307,12 +1316,12 @@ int launch_policy(const void* logits, void* grad, int64_t ld, int rows, int clas
   int ctas = 1;
   while (need > 4096 * ctas) ctas *= 2;
   while (ctas < 8 && need > 1024 && rows * ctas * 2 <= num_sms()) ctas *= 2;   // few rows
-  if (ctas == 8) return launch_ring<T, 16, 8, 1>(stream, r, p);
-  if (ctas == 4) return launch_ring<T, 16, 4, 1>(stream, r, p);
-  if (ctas == 2) return launch_ring<T, 16, 2, 1>(stream, r, p);
-  if (need > 2048) return launch_ring<T, 16, 1, 1>(stream, r, p);
-  if (need > 1024) return launch_ring<T, 8, 1, 2>(stream, r, p);
-  return launch_ring<T, 4, 1, 4>(stream, r, p);
+  if (ctas == 8) return launch_ring<T, 12, 8, 4096, 8, 1>(stream, r, p);
+  if (ctas == 4) return launch_ring<T, 12, 8, 4096, 4, 1>(stream, r, p);
+  if (ctas == 2) return launch_ring<T, 12, 8, 4096, 2, 1>(stream, r, p);
+  if (need > 2048) return launch_ring<T, 12, 8, 4096, 1, 1>(stream, r, p);
+  if (need > 1024) return launch_ring<T, 6, 4, 2048, 1, 2>(stream, r, p);
+  return launch_ring<T, 3, 2, 1024, 1, 4>(stream, r, p);
 }
 }  // namespace
 
