@@ -526,7 +526,14 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
     next = row_ahead(r, p, row + step);
     RowSum x;
     x.clear();
-    x.add<T>(q);
+    constexpr int kStep = kHeld < 4 ? kHeld : 4;
+#pragma unroll
+    for (int u = 0; u < kHeld; u += kStep) {
+      uint4 some[kStep];
+#pragma unroll
+      for (int v = 0; v < kStep; ++v) some[v] = q[u + v];
+      x.add<T>(some);
+    }
     const Part part = x.over(kLanes);
     __syncwarp();                         // every lane has read its logits: grad may be logits
     if (exists) {
@@ -572,16 +579,6 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Action
   finish_totals<kThreads / 32>(p, sum);
 }
 
-// A part into the place `slot` of CTA `cta` of the cluster.
-__device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uint32_t cta) {
-  asm volatile(
-      "{\n\t.reg .b32 ra;\n\t"
-      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
-      "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(smem_u32(slot)),
-      "r"(cta), "f"(x.m), "f"(x.s), "f"(x.t), "f"(x.za)
-      : "memory");
-}
-
 // The row's sums from its kParts parts, in every lane of a warp.
 template <int kParts>
 __device__ __forceinline__ Part join_parts(const Part* slots) {
@@ -602,26 +599,106 @@ __device__ __forceinline__ Part join_parts(const Part* slots) {
   return Part{m, warp_sum(s, 32), warp_sum(t, 32), slots[0].za};
 }
 
+// Middling rows: a CTA holds one, kHeld granules a thread, and as many CTAs share an SM
+// as registers allow, so that one's loads cover another's barrier.
+template <typename T, int kBlock, int kHeld>
+__global__ void __launch_bounds__(kBlock, 1024 / kBlock)
+    policy_cta_kernel(Rows<T> r, Actions p) {
+  constexpr int kWarps = kBlock / 32, kStep = 4;
+  static_assert(kHeld % kStep == 0, "granules are added four at a time");
+  __shared__ Part slots[2][kWarps];
+  pdl_wait();
+  const int me = threadIdx.x, warp = me >> 5;
+  int parity = 0;
+  Pair sum = {0.f, 0.f};
+  int row = blockIdx.x;
+  RowAhead next = row_ahead(r, p, row);
+  for (; row < r.rows; row += gridDim.x) {
+    const RowUse use = row_use(r, next);
+    const RowPtr<T> z(r.logits + row * r.ld, use.n);
+    T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
+    const bool aligned = dz != nullptr && same_alignment(dz, z.z);
+    const int n = use.n, end = z.granules(r.classes);
+    if (computed(use)) {
+      uint4 q[kHeld];
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) {
+        const int i = me + u * kBlock;
+        if (z.whole(i)) q[u] = *z.at(i);
+        else q[u] = z.load_part(i, n);
+      }
+      const RowIn in = row_in(p, row, r.rows);
+      const float za = to_float(z.z[use.action]);
+      next = row_ahead(r, p, row + gridDim.x);
+      RowSum x;
+      x.clear();
+#pragma unroll
+      for (int u = 0; u < kHeld; u += kStep) {
+        const uint4 some[kStep] = {q[u], q[u + 1], q[u + 2], q[u + 3]};
+        if (me + u * kBlock < z.some_hi) x.add<T>(some);
+      }
+      Part part = x.over(32);
+      if ((me & 31) == 0) slots[parity][warp] = part;
+      // after this barrier every logit of the row has been read: grad may be logits;
+      // places alternate, so that a warp that is a row ahead writes where nobody reads
+      __syncthreads();
+      part = join_parts<kWarps>(slots[parity]);
+      parity ^= 1;
+      Terms terms;
+      const RowGrad k = finish_row(r, p, in, row, za, part, me == 0, &terms);
+      sum.add(terms.of(me));
+      if (dz == nullptr) continue;
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) {
+        const int i = me + u * kBlock;
+        if (i >= end) continue;
+        if (aligned && z.whole(i)) *(z.as_granules(dz) + i) = grad_granule<T>(q[u], k);
+        else z.store_part(dz, aligned, i, n, r.classes, grad_granule<T>(q[u], k));
+      }
+      // the thread that has stored the action's granule
+      if (((use.action + z.mis) / z.kE) % kBlock == me) from_float(k.at_action, dz + use.action);
+    } else {
+      next = row_ahead(r, p, row + gridDim.x);
+      const float fill = use.takes ? NAN : 0.f;
+      if (me == 0) fill_row(r, p, row, fill);
+      sum.add(all_terms(fill).of(me));
+      if (dz != nullptr)
+        for (int i = me; i < end; i += kBlock) fill_granule(z, dz, aligned, i, r.classes, fill);
+    }
+  }
+  finish_totals<kWarps>(p, sum);
+}
+
+// A part into the place `slot` of CTA `cta` of the cluster.
+__device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(smem_u32(slot)),
+      "r"(cta), "f"(x.m), "f"(x.s), "f"(x.t), "f"(x.za)
+      : "memory");
+}
+
 // Longer rows: kCtas CTAs (a cluster when there are several) hold one, an equal part
 // each, in a ring of kStages stages of shared memory (more, where they fit, changed
 // nothing).  Four kinds of warps, so that a row's steps, which wait for one another,
 // run beside those of the rows before and after it:
-//   warp 1            fills the stages: one bulk copy of a row's whole granules;
-//   kSumWarps         sum their granules and leave the parts to warp 0;
-//   warp 0            joins the CTA's parts, sends the CTA's own to every CTA of the
-//                     cluster, joins those, finishes the row's scalars and hands the
-//                     gradient's coefficients to
+//   warp 2            fills the stages: one bulk copy of a row's whole granules;
+//   kSumWarps         sum their granules and leave the parts to warp 0 or 1;
+//   warps 0 and 1     take every other row each: join the CTA's parts, send the CTA's
+//                     own to every CTA of the cluster, join those, finish the row's
+//                     scalars and hand the gradient's coefficients to
 //   kGradWarps        which write the gradient and free the stage.
 // (One kind of warp that sums row i and then writes the gradient of row i - 1 took
 // 48 us for 2048 x 32000 bf16 and 179 for 4096 x 50000 fp16: a row costs a warp about a
 // microsecond besides its granules, of which nothing was hidden.)
-// Between CTAs only warp 0 speaks: an arrival that others may read behind waits for
-// all that its thread has stored, and other warps have gradients on their way.
-// Two places for the parts are enough: a warp leaves those of row i + 2 once warp 0 has
-// taken those of row i, and a CTA sends row i + 2 after it has had every CTA's part of
+// Between CTAs only the joining warps speak: an arrival that others may read behind
+// waits for all that its thread has stored, and other warps have gradients on their way.
+// Two places for the parts are enough: a warp leaves those of row i + 2 once those of
+// row i are taken, and a CTA sends row i + 2 after it has had every CTA's part of
 // row i + 1, which they send when they are done with those of row i.
-template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas, int kPerSm>
-__global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
+template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas>
+__global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     policy_ring_kernel(Rows<T> r, Actions p) {
   constexpr int kStages = 3;
   extern __shared__ __align__(128) uint4 ring[];
@@ -691,7 +768,7 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
   };
   RowAhead next = row_ahead(r, p, row);
 
-  if (warp == 1) {
+  if (warp == 2) {
     if (lane == 0) {
       for (; row < r.rows; row += step) {
         const RowUse use = row_use(r, next);
@@ -715,7 +792,7 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
         for (int s = 0; s < kStages; ++s)
           mbar_wait_limited(&full[s], (s < stage ? lap : lap - 1) & 1, kWaitLimitNs / 8);
     }
-  } else if (warp == 0) {
+  } else if (warp < 2) {
     const bool leader = rank == 0 && lane == 0;
     RowIn in = row_in(p, row, r.rows);
     for (; row < r.rows; row += step) {
@@ -724,47 +801,49 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
       const RowIn next_in = row_in(p, row + step, r.rows);
       if (computed(use)) {
         const int slot = count & 1, phase = count >> 1;
-        wait(&summed[slot], phase);
-        __syncwarp();
-        Part x = join_parts<kSumWarps>(slots[slot]);
-        if (kCtas > 1) {
-          if (lane < kCtas) {
-            store_part_remote(x, &ctas[slot][rank], lane);
-            mbar_arrive_remote(&joined[slot], lane);
-          }
-          if (!mbar_wait_cluster(&joined[slot], phase & 1, &abort))
-            record_status(r.status, DORA_ERR_TIMEOUT);
+        if (slot == warp) {
+          wait(&summed[slot], phase);
           __syncwarp();
-          x = join_parts<kCtas>(ctas[slot]);
+          Part x = join_parts<kSumWarps>(slots[slot]);
+          if (kCtas > 1) {
+            if (lane < kCtas) {
+              store_part_remote(x, &ctas[slot][rank], lane);
+              mbar_arrive_remote(&joined[slot], lane);
+            }
+            if (!mbar_wait_cluster(&joined[slot], phase & 1, &abort))
+              record_status(r.status, DORA_ERR_TIMEOUT);
+            __syncwarp();
+            x = join_parts<kCtas>(ctas[slot]);
+          }
+          Terms terms;
+          const RowGrad k = finish_row(r, p, in, row, x.za, x, leader, &terms);
+          // the coefficients before the last ones have been taken
+          if (count >= 2) wait(&taken[slot], phase - 1);
+          __syncwarp();
+          if (lane == 0) {
+            grads[slot] = k;
+            mbar_arrive(&ready[slot]);
+          }
+          if (rank == 0) sum.add(terms.of(lane));
         }
-        Terms terms;
-        const RowGrad k = finish_row(r, p, in, row, x.za, x, leader, &terms);
-        // the coefficients before the last ones have been taken
-        if (count >= 2) wait(&taken[slot], phase - 1);
-        __syncwarp();
-        if (lane == 0) {
-          grads[slot] = k;
-          mbar_arrive(&ready[slot]);
-        }
-        if (rank == 0) sum.add(terms.of(lane));
         ++count;
-      } else {
+      } else if (warp == 0) {
         const float fill = use.takes ? NAN : 0.f;
         if (leader) fill_row(r, p, row, fill);
         if (rank == 0) sum.add(all_terms(fill).of(lane));
       }
       in = next_in;
     }
-  } else if (warp < 2 + kSumWarps) {
+  } else if (warp < 3 + kSumWarps) {
     constexpr int kSum = kSumWarps * 32;
-    const int me = threadIdx.x - 64;
+    const int me = threadIdx.x - 96;
     // The action's logit goes with the first warp's part: read before any CTA can write
     // the row's gradient, which may lie over its logits.  It and the row's scalars are
     // on their way a row and two rows ahead.
     auto action_logit = [&](int at, const RowUse& u) {
       T z;
       from_float(0.f, &z);
-      if (warp == 2 && computed(u)) z = r.logits[at * r.ld + u.action];
+      if (warp == 3 && computed(u)) z = r.logits[at * r.ld + u.action];
       return z;
     };
     RowUse use = row_use(r, next);
@@ -802,7 +881,7 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
         const int slot = count & 1;
         if (count >= 2) wait(&ready[slot], (count >> 1) - 1);   // warp 0 has taken them
         if (lane == 0) {
-          slots[slot][warp - 2] = part;
+          slots[slot][warp - 3] = part;
           mbar_arrive(&summed[slot]);
         }
         advance();
@@ -812,7 +891,7 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
     }
   } else {
     constexpr int kGrad = kGradWarps * 32;
-    const int me = threadIdx.x - 64 - kSumWarps * 32;
+    const int me = threadIdx.x - 96 - kSumWarps * 32;
     for (; row < r.rows; row += step) {
       const RowUse use = row_use(r, next);
       next = row_ahead(r, p, row + step);
@@ -868,7 +947,11 @@ __global__ void __launch_bounds__((2 + kSumWarps + kGradWarps) * 32, kPerSm)
   }
   __syncwarp();
   if (kCtas > 1) cluster_sync();          // nobody leaves while parts may be on their way to it
-  finish_totals<2 + kSumWarps + kGradWarps>(p, sum);
+  __shared__ Pair odd[kTerms];            // of warp 1's rows
+  if (warp == 1 && lane < kTerms) odd[lane] = sum;
+  __syncthreads();
+  if (threadIdx.x < kTerms) sum.add(odd[threadIdx.x]);
+  finish_totals<3 + kSumWarps + kGradWarps>(p, sum);
 }
 
 // Rows longer than a cluster's registers: the same without the ring; a row is read a
@@ -1269,18 +1352,18 @@ int resident_clusters(RowsKernel<T> kern, int block, int ctas, size_t smem,
   return n;
 }
 
-// kPerSm CTAs an SM; the grid is what is resident at once.
-template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas, int kPerSm>
+// One CTA an SM; the grid is what is resident at once.
+template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas>
 int launch_ring(cudaStream_t stream, const policy::Rows<T>& r, const policy::Actions& p) {
   const RowsKernel<T> kern =
-      policy::policy_ring_kernel<T, kSumWarps, kGradWarps, kStage, kCtas, kPerSm>;
+      policy::policy_ring_kernel<T, kSumWarps, kGradWarps, kStage, kCtas>;
   constexpr size_t smem = static_cast<size_t>(3) * kStage * 16;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(smem));
   if (e != cudaSuccess) return launched(e);
   static std::atomic<int> cache[kMaxDevices];
-  constexpr int kThreads = (2 + kSumWarps + kGradWarps) * 32;
-  const int most = kCtas == 1 ? num_sms() * kPerSm
+  constexpr int kThreads = (3 + kSumWarps + kGradWarps) * 32;
+  const int most = kCtas == 1 ? num_sms()
                               : resident_clusters<T>(kern, kThreads, kCtas, smem, cache);
   if (most < 1) return DORA_ERR_CUDA;
   return launch_rows<T>(kern, r.rows < most ? r.rows : most, kThreads, kCtas, smem, stream, r, p);
@@ -1296,15 +1379,29 @@ int launch_policy(const void* logits, void* grad, int64_t ld, int rows, int clas
   // granules that a row can touch: one more where rows may start inside one
   const bool aligned = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && ld % kE == 0;
   const int64_t need = (static_cast<int64_t>(classes) + (aligned ? 0 : kE - 1) + kE - 1) / kE;
-  if (need <= 8)
-    return launch_rows<T>(policy::policy_warp_kernel<T, 8, 1>, grid_for((rows + 31) / 32, 8), 256,
-                          1, 0, stream, r, p);
-  if (need <= 32)
-    return launch_rows<T>(policy::policy_warp_kernel<T, 8, 4>, grid_for((rows + 31) / 32, 8), 256,
-                          1, 0, stream, r, p);
+  // The fewest lanes that hold a row: what a row costs besides its granules is paid per
+  // warp (16384 x 2000 bf16: a warp a row 32 us, a CTA 79).
+  const int sms = num_sms();
+  if (need <= 32) {
+    const int ctas = grid_for((rows + 31) / 32, 8);
+    return need <= 8 ? launch_rows<T>(policy::policy_warp_kernel<T, 8, 1>, ctas, 256, 1, 0, stream,
+                                      r, p)
+                     : launch_rows<T>(policy::policy_warp_kernel<T, 8, 4>, ctas, 256, 1, 0, stream,
+                                      r, p);
+  }
+  const int eights = grid_for((rows + 7) / 8, 8);
   if (need <= 128)
-    return launch_rows<T>(policy::policy_warp_kernel<T, 32, 4>, grid_for((rows + 7) / 8, 8), 256,
-                          1, 0, stream, r, p);
+    return launch_rows<T>(policy::policy_warp_kernel<T, 32, 4>, eights, 256, 1, 0, stream, r, p);
+  // From here on few rows get more lanes each, as long as all have their place at once
+  // (256 x 4000 bf16: a CTA a row 6.2 us, a warp 8.5).
+  if (need <= 512 && rows > 8 * sms)
+    return need <= 256 ? launch_rows<T>(policy::policy_warp_kernel<T, 32, 8>, eights, 256, 1, 0,
+                                        stream, r, p)
+                       : launch_rows<T>(policy::policy_warp_kernel<T, 32, 16>, eights, 256, 1, 0,
+                                        stream, r, p);
+  if (need <= 1024)
+    return launch_rows<T>(policy::policy_cta_kernel<T, 128, 8>, grid_for(rows, 8), 128, 1, 0,
+                          stream, r, p);
   if (need > 4096 * 8) {
     static std::atomic<int> cache[kMaxDevices];
     const int most = resident_clusters<T>(policy::policy_long_kernel<T>, policy::kLongBlock,
@@ -1315,13 +1412,16 @@ int launch_policy(const void* logits, void* grad, int64_t ld, int rows, int clas
   }
   int ctas = 1;
   while (need > 4096 * ctas) ctas *= 2;
-  while (ctas < 8 && need > 1024 && rows * ctas * 2 <= num_sms()) ctas *= 2;   // few rows
-  if (ctas == 8) return launch_ring<T, 12, 8, 4096, 8, 1>(stream, r, p);
-  if (ctas == 4) return launch_ring<T, 12, 8, 4096, 4, 1>(stream, r, p);
-  if (ctas == 2) return launch_ring<T, 12, 8, 4096, 2, 1>(stream, r, p);
-  if (need > 2048) return launch_ring<T, 12, 8, 4096, 1, 1>(stream, r, p);
-  if (need > 1024) return launch_ring<T, 6, 4, 2048, 1, 2>(stream, r, p);
-  return launch_ring<T, 3, 2, 1024, 1, 4>(stream, r, p);
+  while (ctas < 8 && rows * ctas * 2 <= sms) ctas *= 2;
+  if (ctas == 1 && need <= 2048)
+    return launch_rows<T>(policy::policy_cta_kernel<T, 256, 8>, grid_for(rows, 4), 256, 1, 0,
+                          stream, r, p);
+  switch (ctas) {
+    case 1: return launch_ring<T, 8, 8, 4096, 1>(stream, r, p);
+    case 2: return launch_ring<T, 8, 8, 4096, 2>(stream, r, p);
+    case 4: return launch_ring<T, 8, 8, 4096, 4>(stream, r, p);
+    default: return launch_ring<T, 8, 8, 4096, 8>(stream, r, p);
+  }
 }
 }  // namespace
 
