@@ -995,33 +995,44 @@ class ParamList:
             raise ValueError("params, exp_avg and exp_avg_sq are given together")
         if copies is not None and params is None:
             raise ValueError("copies need params")
-        more = {"clipped": clipped, "params": params, "exp_avg": exp_avg,
-                "exp_avg_sq": exp_avg_sq, "copies": copies}
-        for name, ts in more.items():
-            ts = [None] * n if ts is None else list(ts)
-            if len(ts) != n:
+        for name, ts in (("clipped", clipped), ("params", params), ("exp_avg", exp_avg),
+                         ("exp_avg_sq", exp_avg_sq), ("copies", copies)):
+            if ts is not None and len(ts) != n:
                 raise ValueError(f"{name} must have as many tensors as grads")
+        g0 = self.grads[0]
+        device = g0.device if isinstance(g0, _Tensor) else None
+        columns, sizes = [], None
+        for name, ts, dtype in (("grads", self.grads, None), ("clipped", clipped, None),
+                                ("params", params, None), ("exp_avg", exp_avg, _F32),
+                                ("exp_avg_sq", exp_avg_sq, _F32), ("copies", copies, _BF16)):
+            if ts is None:
+                setattr(self, name, None)
+                columns.append([0] * n)
+                continue
+            ts = list(ts)
             setattr(self, name, ts)
-        c = (_ParamC * n)()
-        for i, g in enumerate(self.grads):
-            p = self.params[i]
-            for name, t, dtypes in (("grads", g, _DTYPES), ("clipped", self.clipped[i], (g.dtype,)),
-                                    ("params", p, _DTYPES), ("exp_avg", self.exp_avg[i], (_F32,)),
-                                    ("exp_avg_sq", self.exp_avg_sq[i], (_F32,)),
-                                    ("copies", self.copies[i], (_BF16,))):
-                if t is None and more.get(name, grads) is None:
-                    continue
-                if not isinstance(t, _Tensor) or not t.is_cuda or t.dtype not in dtypes or \
-                        not t.is_contiguous():
+            for i, t in enumerate(ts):
+                if not (isinstance(t, _Tensor) and t.is_cuda and t.is_contiguous() and
+                        (t.dtype is dtype or (dtype is None and t.dtype in _DTYPES))):
                     raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor of "
-                                    f"{', '.join(map(str, dtypes))}")
-                if t.numel() != g.numel() or t.device != self.grads[0].device:
-                    raise ValueError(f"{name}[{i}] must match grads[{i}] in size and device")
-            c[i] = _ParamC(_ptr(g), _ptr(self.clipped[i]), _ptr(p), _ptr(self.exp_avg[i]),
-                           _ptr(self.exp_avg_sq[i]), _ptr(self.copies[i]), g.numel(),
-                           _DTYPES[g.dtype], 2 if p is None else _DTYPES[p.dtype])
+                                    f"{dtype or 'bf16, fp16 or fp32'}")
+                if t.device != device:
+                    raise ValueError(f"{name}[{i}] must be on the device of grads[0]")
+            count = [t.numel() for t in ts]
+            sizes = sizes or count
+            if count != sizes:
+                raise ValueError(f"{name} must have the sizes of grads")
+            columns.append([t.data_ptr() for t in ts])
+        types = [_DTYPES[t.dtype] for t in self.grads]
+        if clipped is not None and [_DTYPES[t.dtype] for t in self.clipped] != types:
+            raise TypeError("clipped must have the types of grads")
+        weights = [2] * n if params is None else [_DTYPES[t.dtype] for t in self.params]
+        c = (_ParamC * n)()
+        for at, row in zip(c, zip(*columns, sizes, types, weights)):
+            (at.grad, at.clipped, at.param, at.exp_avg, at.exp_avg_sq, at.copy, at.n,
+             at.grad_dtype, at.param_dtype) = row
         size = int(load_library().dora_param_list_size(c, n))
-        self.data = torch.empty(size, dtype=torch.uint8, device=self.grads[0].device)
+        self.data = torch.empty(size, dtype=torch.uint8, device=device)
         self.c = _ParamListC()
         self.ref = ctypes.byref(self.c)
         _check(load_library().dora_param_list_prepare(c, n, _ptr(self.data), size, self.ref,
