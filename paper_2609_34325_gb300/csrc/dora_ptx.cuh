@@ -307,6 +307,14 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
   }
 }
 
+// One more CTA is done: its number, from 0.  What the thread wrote before is visible to
+// the one that gets the last number, and to what follows a barrier of its CTA.
+__device__ __forceinline__ unsigned take_ticket(unsigned* ticket) {
+  unsigned n;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(n) : "l"(ticket) : "memory");
+  return n;
+}
+
 // Arrive once on the mbarrier at the same shared-memory offset as `bar` in
 // CTA `rank` of this cluster (release at cluster scope).
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t* bar, uint32_t rank) {

@@ -302,12 +302,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   }
   if (threadIdx.x == 0) {
     list.header->partial[blockIdx.x] = cta;
-    __threadfence();
-    last = atomicAdd(&list.header->ticket, 1u) == gridDim.x - 1;
+    last = take_ticket(&list.header->ticket) == gridDim.x - 1;
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
   constexpr int kLoads = (kMaxSpans + kThreads - 1) / kThreads;
   int4 x[kLoads];                         // all on their way before the first is added
 #pragma unroll
@@ -458,21 +456,30 @@ __device__ __forceinline__ void piece_adam(const AdamArgs& a, const AdamStep& s,
   const void* g = at_elem(e.grad, gt, from);
   void* p = at_elem(e.param, pt, from);
   float *m = e.m + from, *v = e.v + from;
-  void* c = e.copy != nullptr ? e.copy + from : nullptr;
-  int done = 0;
-  if (has_quads(p, pt) && has_quads(g, gt) && has_quads(m, DORA_F32) && has_quads(v, DORA_F32) &&
-      has_quads(c, DORA_BF16)) {
-    const int quads = n / 4;
-    done = quads * 4;
+  uint16_t* c = e.copy != nullptr ? e.copy + from : nullptr;
+  // Whole quads where the buffers agree on where they lie: those of one flat buffer each,
+  // or of the framework's allocator, do, whatever the tensors' sizes.
+  const int misplaced = static_cast<int>(reinterpret_cast<uintptr_t>(p) / size_of(pt) & 3u);
+  const int head = min(n, (4 - misplaced) & 3);
+  int first = 0, done = 0;
+  if (has_quads(at_elem(g, gt, head), gt) && has_quads(m + head, DORA_F32) &&
+      has_quads(v + head, DORA_F32) && (c == nullptr || has_quads(c + head, DORA_BF16))) {
+    first = head;
+    const int quads = (n - head) / 4;
+    done = head + quads * 4;
+    const void* gq = at_elem(g, gt, head);
+    void* pq = at_elem(p, pt, head);
+    float *mq = m + head, *vq = v + head;
+    uint16_t* cq = c != nullptr ? c + head : nullptr;
     for (int i = quads - 1 - static_cast<int>(threadIdx.x); i >= 0; i -= kInFlight * kThreads) {
       uint4 qp[kInFlight], qg[kInFlight], qm[kInFlight], qv[kInFlight];
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u)
         if (i >= u * kThreads) {
-          qg[u] = load_quad(g, gt, i - u * kThreads);
-          qp[u] = load_quad(p, pt, i - u * kThreads);
-          qm[u] = load_quad(m, DORA_F32, i - u * kThreads);
-          qv[u] = load_quad(v, DORA_F32, i - u * kThreads);
+          qg[u] = load_quad(gq, gt, i - u * kThreads);
+          qp[u] = load_quad(pq, pt, i - u * kThreads);
+          qm[u] = load_quad(mq, DORA_F32, i - u * kThreads);
+          qv[u] = load_quad(vq, DORA_F32, i - u * kThreads);
         }
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u)
@@ -484,14 +491,17 @@ __device__ __forceinline__ void piece_adam(const AdamArgs& a, const AdamStep& s,
           unpack_quad(qv[u], DORA_F32, fv);
 #pragma unroll
           for (int k = 0; k < 4; ++k) adam_one(a, s, fg[k], fp + k, fm + k, fv + k);
-          store_quad(fp, p, pt, i - u * kThreads);
-          store_quad(fm, m, DORA_F32, i - u * kThreads);
-          store_quad(fv, v, DORA_F32, i - u * kThreads);
-          if (c != nullptr) store_quad(fp, c, DORA_BF16, i - u * kThreads);
+          store_quad(fp, pq, pt, i - u * kThreads);
+          store_quad(fm, mq, DORA_F32, i - u * kThreads);
+          store_quad(fv, vq, DORA_F32, i - u * kThreads);
+          if (cq != nullptr) store_quad(fp, cq, DORA_BF16, i - u * kThreads);
         }
     }
   }
-  for (int i = done + threadIdx.x; i < n; i += kThreads) {
+  // the rest by elements: the head, then what is past the quads (all of it where the
+  // buffers do not agree)
+  for (int k = threadIdx.x; k < first + n - done; k += kThreads) {
+    const int i = k < first ? k : k - first + done;
     float pi = load_one(p, pt, i), mi = m[i], vi = v[i];
     adam_one(a, s, load_one(g, gt, i), &pi, &mi, &vi);
     store_one(pi, p, pt, i);
@@ -528,8 +538,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) adam_step_kernel(List li
     });
   __syncthreads();                        // every thread of the CTA has read the state
   if (threadIdx.x == 0) {
-    __threadfence();
-    if (atomicAdd(&a.state->ticket, 1u) == gridDim.x - 1) {
+    if (take_ticket(&a.state->ticket) == gridDim.x - 1) {
       if (!skip) {
         a.state->step = st.step + 1;
         a.state->power1 = p1;

@@ -127,16 +127,12 @@ __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   __shared__ bool last;
   Workspace* ws = p.ws;
   if (threadIdx.x < 32) {
-    if (threadIdx.x < kTerms) {
-      ws->partial[blockIdx.x][threadIdx.x] = sum;
-      __threadfence();
-    }
+    if (threadIdx.x < kTerms) ws->partial[blockIdx.x][threadIdx.x] = sum;
     __syncwarp();
-    if (threadIdx.x == 0) last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+    if (threadIdx.x == 0) last = take_ticket(&ws->ticket) == gridDim.x - 1;
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
   constexpr int kLoads = 3, kBatch = 3;   // a CTA's terms are three 16-byte loads
   static_assert(kTerms == 2 * kLoads, "two pairs a load");
   constexpr int threads = kWarps * 32;

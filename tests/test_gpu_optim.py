@@ -203,6 +203,29 @@ def test_adam_steps(pt, gt, shift):
             assert pr.size == 0 or not np.array_equal(_np(p[i]), old[i])
 
 
+@pytest.mark.parametrize("shifts", [(1, 0, 0, 0), (0, 2, 1, 1), (3, 3, 3, 1), (0, 0, 1, 3)])
+def test_adam_on_buffers_that_lie_differently(shifts):
+    # gradients, weights and moments each so many elements into their storage
+    sizes = [1, 3, 5, 1027, 4099, 20001]
+    g = _tensors(sizes, (BF16,), 61, 1e-2, shifts[0])
+    p = _tensors(sizes, (F32,), 62, 0.05, shifts[1])
+    m = _tensors(sizes, (F32,), 63, 1e-3, shifts[2])
+    v = [t.square() for t in _tensors([n + shifts[3] for n in sizes], (F32,), 64, 1e-2)]
+    v = [t[shifts[3]:] for t in v]
+    ref = [O.adam_step(_np(p[i]), _np(m[i]), _np(v[i]), _np(g[i]), 1, 1e-2, 0.9, 0.999, 1e-8, 0.0)
+           for i in range(len(p))]
+    top = [1e-1 * (np.abs(_np(m[i])) + np.abs(_np(g[i]))) / (np.sqrt(ref[i][2] / 1e-3) + 1e-8)
+           for i in range(len(p))]
+    P.dora_adam_step(P.ParamList(g, params=p, exp_avg=m, exp_avg_sq=v), P.alloc_adam_state(dev()),
+                     1e-2)
+    torch.cuda.synchronize()
+    for i in range(len(p)):
+        pr, mr, vr = ref[i]
+        assert np.all(np.abs(_np(m[i]) - mr) <= 2.0 ** -21 * (np.abs(mr) + np.abs(_np(g[i]))) + 1e-9)
+        assert np.all(np.abs(_np(v[i]) - vr) <= 2.0 ** -20 * vr + 1e-12)
+        assert np.all(np.abs(_np(p[i]) - pr) <= 4e-6 * top[i] + 2.0 ** -21 * np.abs(pr) + 1e-9)
+
+
 def test_adam_skips_a_norm_that_is_not_finite():
     g, p, m, v = _adam_inputs([3000, 5], F32, F32, 31)
     state = P.alloc_adam_state(dev(), step=7)
