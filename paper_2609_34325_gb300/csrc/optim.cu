@@ -7,8 +7,15 @@
 // units, whatever the tensors' sizes.  A CTA walks its span, piece by piece.  To
 // begin a tensor costs a CTA about as long as kBegin units take (its entry, then its
 // first values: two round trips to memory), and counts as that many: a hundred
-// vectors in a row would otherwise be one CTA's, while the others wait for it.  A list
-// with no more units than spans has a unit a span, and nothing to count.
+// vectors in a row would otherwise be one CTA's, while the others wait for it (norm of
+// 86 M parameters, the vectors last: 75 us without, 39 with 6 units, 32 with 12).  A
+// list with no more units than spans has a unit a span, and nothing to count.
+//
+// All three are bound by memory: 86 M fp32 gradients are normed in 54 us (6.4 TB/s; a
+// copy 6.8) and clipped in 166 (three passes, 6.2 TB/s); an Adam step on 86 M fp32
+// weights, bf16 gradients and bf16 copies takes 384 after a norm of 32 (6.2 TB/s).  Lists
+// of a few hundred KB take the time of their chain (launch, span, values, sums, ticket):
+// 5 us for the norm, 8 with clipping, 10 for norm and step.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
