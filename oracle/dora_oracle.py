@@ -58,8 +58,12 @@ Readings where the paper is silent:
   formed in fp32, noise an input); the fidelity cost runs over the true
   classes only.
 
+* Policy update: the KL term is the one-action estimate exp x - 1 - x; a
+  clipping tie (the ratio inside its bounds) leaves the gradient; Adam's weight
+  decay is decoupled.
+
 Parity pins: every function here is checked in ``tests/test_oracle_pins.py``
-against brute force, closed forms, invariants the paper fixes, or an
+(the policy update in ``tests/test_policy_oracle.py``) against brute force, closed forms, invariants the paper fixes, or an
 independent library routine.
 """
 from __future__ import annotations

@@ -889,12 +889,26 @@ def alloc_policy_workspace(device=None) -> torch.Tensor:
     return torch.zeros(dora_policy_workspace_size(), dtype=torch.uint8, device=device or "cuda")
 
 
-def _entries(n, tensors, totals):
-    for t in tensors:
-        if t is not None and t.numel() != n:
-            raise ValueError("every per-action tensor must have one entry per row (per image)")
-    if totals is not None and totals.numel() < 6:
+def _vec(t, dtype, n, name):
+    """_arg of a tensor with n entries."""
+    if not (type(t) is _Tensor and t.dtype is dtype and t.numel() == n and t.is_cuda and
+            t.is_contiguous()):
+        _req(t, dtype, name)
+        if t.numel() != n:
+            raise ValueError(f"{name} must have {n} entries")
+    return t.data_ptr()
+
+
+def _vec_opt(t, dtype, n, name):
+    return None if t is None else _vec(t, dtype, n, name)
+
+
+def _totals(totals):
+    if totals is None:
+        return None
+    if totals.numel() < 6:
         raise ValueError("totals must hold 6 floats")
+    return _arg(totals, _F32, "totals")
 
 
 def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None, grad=None,
@@ -924,16 +938,14 @@ def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None
             grad.dim() == 2 and grad.size(0) == rows and grad.size(1) == cols and
             (grad.stride(0) == ld or rows <= 1) and (grad.stride(1) == 1 or cols == 1)):
         raise TypeError("grad must be like logits: device, type, shape and strides")
-    _entries(rows, (actions, old_logp, advantages, logp, legal, ref_logp, weights, entropy,
-                    row_loss), totals)
     code = load_library().dora_policy_loss(
-        logits.data_ptr(), dt, rows, classes, ld, _opt(legal, _I32, "legal"),
-        _arg(actions, _I32, "actions"), _arg(old_logp, _F32, "old_logp"),
-        _opt(ref_logp, _F32, "ref_logp"), _arg(advantages, _F32, "advantages"),
-        _opt(weights, _F32, "weights"), clip_low, clip_high, kl_coef, entropy_coef,
-        _arg(logp, _F32, "logp"), _opt(entropy, _F32, "entropy"),
-        _opt(row_loss, _F32, "row_loss"), None if grad is None else grad.data_ptr(),
-        _opt(totals, _F32, "totals"), _opt(workspace, _U8, "workspace"),
+        logits.data_ptr(), dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
+        _vec(actions, _I32, rows, "actions"), _vec(old_logp, _F32, rows, "old_logp"),
+        _vec_opt(ref_logp, _F32, rows, "ref_logp"), _vec(advantages, _F32, rows, "advantages"),
+        _vec_opt(weights, _F32, rows, "weights"), clip_low, clip_high, kl_coef, entropy_coef,
+        _vec(logp, _F32, rows, "logp"), _vec_opt(entropy, _F32, rows, "entropy"),
+        _vec_opt(row_loss, _F32, rows, "row_loss"), None if grad is None else grad.data_ptr(),
+        _totals(totals), _opt(workspace, _U8, "workspace"),
         0 if workspace is None else workspace.numel(), _opt(status, _I32, "status"),
         _stream(stream))
     if code:
@@ -947,20 +959,19 @@ def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, worksp
     """Clipped policy loss of the ordered removal sequences ``order`` (int32 [B,
     k_cap], the first k[i] entries of image i) and d loss / d scores (``grad``,
     row-aligned); the other arguments per image as in dora_policy_loss."""
-    s, c, kp = _arg(scores, _F32, "scores"), _arg(cu, _I32, "cu"), _arg(k, _I32, "k")
-    o, b = _arg(order, _I32, "order"), cu.numel() - 1
+    s, c, o = _arg(scores, _F32, "scores"), _arg(cu, _I32, "cu"), _arg(order, _I32, "order")
+    b, t_cap = cu.numel() - 1, scores.numel()
     if order.dim() != 2 or order.size(0) != b:
         raise ValueError("order must be [B, k_cap]")
-    _entries(b, (k, old_logp, advantages, logp, ref_logp, weights, row_loss), totals)
-    if grad is not None and grad.numel() != scores.numel():
-        raise ValueError("grad must match scores")
     code = load_library().dora_pl_policy_loss(
-        s, c, b, scores.numel(), kp, o, order.size(1), _arg(old_logp, _F32, "old_logp"),
-        _opt(ref_logp, _F32, "ref_logp"), _arg(advantages, _F32, "advantages"),
-        _opt(weights, _F32, "weights"), clip_low, clip_high, kl_coef, _arg(logp, _F32, "logp"),
-        _opt(row_loss, _F32, "row_loss"), _opt(grad, _F32, "grad"), _opt(totals, _F32, "totals"),
-        _opt(workspace, _U8, "workspace"), 0 if workspace is None else workspace.numel(),
-        _opt(status, _I32, "status"), _stream(stream))
+        s, c, b, t_cap, _vec(k, _I32, b, "k"), o, order.size(1),
+        _vec(old_logp, _F32, b, "old_logp"), _vec_opt(ref_logp, _F32, b, "ref_logp"),
+        _vec(advantages, _F32, b, "advantages"), _vec_opt(weights, _F32, b, "weights"), clip_low,
+        clip_high, kl_coef, _vec(logp, _F32, b, "logp"),
+        _vec_opt(row_loss, _F32, b, "row_loss"), _vec_opt(grad, _F32, t_cap, "grad"),
+        _totals(totals), _opt(workspace, _U8, "workspace"),
+        0 if workspace is None else workspace.numel(), _opt(status, _I32, "status"),
+        _stream(stream))
     if code:
         _check(code, "dora_pl_policy_loss")
     return logp

@@ -31,7 +31,7 @@ namespace dora {
 namespace optim {
 
 constexpr int kThreads = 256;
-constexpr int kUnit = 1024;               // elements
+constexpr int kUnit = 2048;               // elements
 constexpr int kBegin = 12;                // units, in lists of more than kMaxSpans
 constexpr int kCtasPerSm = 4;             // resident, by their registers
 constexpr int kMaxSpans = 152 * kCtasPerSm;   // a span a CTA, all at once
