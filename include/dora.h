@@ -757,8 +757,9 @@ int dora_policy_loss(const void* logits, int32_t dtype, int32_t rows, int32_t cl
  * entropy term (totals[3] is 0).  grad nullable fp32 [t_cap]: every row of
  * every image is written (CLS rows 0).  An image with k = 0 (its gate is
  * closed) or weight 0 takes no part.  Device errors as in dora_pl_logprob: a
- * repeated or out-of-range entry makes the image NaN.  l is summed in fp64, so
- * that the ratio of a long sequence keeps its digits.
+ * repeated or out-of-range entry makes the image NaN.  Scores of -inf are
+ * tokens of probability 0: absent where they stay.  l is summed in pairs of
+ * fp32 values, so that the ratio of a long sequence keeps its digits.
  */
 int dora_pl_policy_loss(const float* scores, const int32_t* cu, int32_t batch, int32_t t_cap,
                         const int32_t* k, const int32_t* order, int32_t k_cap,

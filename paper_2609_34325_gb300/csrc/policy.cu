@@ -56,6 +56,9 @@ struct Pair {
     add(o.v);
     lost += o.lost;
   }
+  // What an infinite sum lost is inf - inf.
+  __device__ __forceinline__ float rest() const { return isinf(v) ? 0.f : lost; }
+  __device__ __forceinline__ float value() const { return v + rest(); }
 };
 __device__ __forceinline__ Pair shfl_xor(Pair p, int off) {
   return {__shfl_xor_sync(0xffffffffu, p.v, off), __shfl_xor_sync(0xffffffffu, p.lost, off)};
@@ -128,7 +131,7 @@ template <int kWarps>
 __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
   if (p.totals == nullptr) return;
   if (gridDim.x == 1) {
-    if (threadIdx.x < kTerms) p.totals[threadIdx.x] = sum.v + sum.lost;
+    if (threadIdx.x < kTerms) p.totals[threadIdx.x] = sum.value();
     return;
   }
   __shared__ bool last;
@@ -175,7 +178,7 @@ __device__ __forceinline__ void finish_totals(const Actions& p, Pair sum) {
     Pair all = warps[0][threadIdx.x];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) all.add(warps[w][threadIdx.x]);
-    p.totals[threadIdx.x] = all.v + all.lost;
+    p.totals[threadIdx.x] = all.value();
   }
   if (threadIdx.x == 0) ws->ticket = 0;
 }
@@ -1068,7 +1071,9 @@ __device__ __forceinline__ Scaled from_lane(Scaled v, int lane) {
 }
 // For d = s - M: e^d, a sum's reciprocal, d less a sum's logarithm, e^d times a sum.
 __device__ __forceinline__ float term_of(float d, float) { return expf(d); }
-__device__ __forceinline__ Scaled term_of(float d, Scaled) { return {d, 1.f}; }
+__device__ __forceinline__ Scaled term_of(float d, Scaled) {
+  return {d, d == -INFINITY ? 0.f : 1.f};   // not 1 e^-inf: two of them would meet at inf - inf
+}
 __device__ __forceinline__ float inverse(float v) { return 1.f / v; }
 __device__ __forceinline__ Scaled inverse(Scaled v) { return {-v.m, 1.f / v.s}; }
 __device__ __forceinline__ float log_of(float d, float v) { return d - logf(v); }
@@ -1248,12 +1253,12 @@ __global__ void __launch_bounds__(kSeqThreads, kSeqPerSm)
     const Pair lp = narrow ? sequence_sums<float>(&h, seq, n, k)
                            : sequence_sums<Scaled>(&h, seq, n, k);
     // l - q from the pair: the ratio of a long sequence keeps its digits
-    const float x = p.ref_logp != nullptr ? (in.ref - lp.v) - lp.lost : 0.f;
+    const float x = p.ref_logp != nullptr ? (in.ref - lp.v) - lp.rest() : 0.f;
     Terms terms;
-    const float g = row_terms(p, (lp.v - in.old_logp) + lp.lost, x, in.adv, in.w, 0.f, &terms);
+    const float g = row_terms(p, (lp.v - in.old_logp) + lp.rest(), x, in.adv, in.w, 0.f, &terms);
     sum.add(terms.of(threadIdx.x));
     if (threadIdx.x == 0) {
-      p.logp[img] = lp.v + lp.lost;
+      p.logp[img] = lp.value();
       if (p.row_loss != nullptr) p.row_loss[img] = terms.v[0];
     }
     if (q.grad == nullptr) continue;

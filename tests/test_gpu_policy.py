@@ -428,6 +428,57 @@ def test_pl_policy_loss_agrees_with_the_logprob_entry():
     assert np.allclose(grad.cpu(), out["grad"][:len(s)].cpu(), rtol=1e-3, atol=1e-4)
 
 
+@pytest.mark.parametrize("value", [-np.inf, float(np.finfo(np.float32).min)])
+def test_pl_policy_loss_tokens_of_probability_zero(value):
+    """Tokens that are never removed because their score is -inf, or fp32's lowest
+    value, are as good as absent; more of them than threads."""
+    q = _sequences([7, 42, 173, 902], [2, 30, 130, 900], 1.5, 14)
+    s, cu, k, order = q[:4]
+    rng = np.random.default_rng(15)
+    scores, places, moved = [], [], np.full_like(order, -1)
+    for i in range(len(k)):
+        n = int(cu[i + 1] - cu[i]) - 1
+        at = np.sort(rng.permutation(n + 300)[:n])         # of the image's own tokens
+        img = np.full(n + 300, value, dtype=np.float32)
+        img[at] = s[cu[i] + 1:cu[i + 1]]
+        moved[i, :k[i]] = at[order[i, :k[i]]]
+        start = sum(len(x) for x in scores)
+        places.append(np.concatenate([[start], start + 1 + at]))
+        scores.append(np.concatenate([[0.0], img]).astype(np.float32))
+    cu2 = O.cu_from_counts([len(x) for x in scores])
+    out, st = _run_sequences((np.concatenate(scores), cu2, k, moved) + q[4:])
+    assert st == 0
+    places = torch.from_numpy(np.concatenate(places)).to(dev())
+    rest = torch.ones(int(cu2[-1]), dtype=torch.bool, device=dev())
+    rest[places] = False
+    assert not out["grad"][:int(cu2[-1])][rest].any()
+    out["grad"] = torch.cat([out["grad"][places], out["grad"][-5:]])
+    _check_sequences(q, out)
+
+
+def test_pl_policy_loss_removed_token_of_probability_zero():
+    s = np.array([0, .5, -np.inf, 1., 0, .5, -.5, 1.], dtype=np.float32)
+    cu, k = np.array([0, 4, 8]), np.array([2, 2])
+    order = np.array([[1, 0], [1, 0]])                     # log-probability -inf; finite
+    one, lp = np.ones(2, dtype=np.float32), O.pl_logprob(s[5:], [1, 0])
+    out, st = _run_sequences((s, cu, k, order, np.float32([-1, lp]), one, one, one), ref=False)
+    assert st == 0 and float(out["logp"][0]) == -np.inf
+    assert float(out["row_loss"][0]) == 0 and not out["grad"][:4].any()
+    assert abs(float(out["logp"][1]) - lp) < 1e-6 and abs(float(out["totals"][0]) + 1) < 1e-5
+
+
+def test_policy_loss_totals_of_an_infinite_loss():
+    """A ratio past fp32's range with A < 0 is a loss of +inf, and so is the total."""
+    rows = 3000
+    c = _Case(rows, 8, F32, 16)
+    c.old[7], c.adv[7], c.w[7] = -300.0, -1.0, 1.0
+    if c.actions[7] < 0:
+        c.actions[7] = 0
+    out = c.run()
+    assert float(out["row_loss"][7]) == np.inf and float(out["totals"][0]) == np.inf
+    assert float(out["totals"][1]) == np.inf and bool(torch.isfinite(out["totals"][2:]).all())
+
+
 def test_pl_policy_loss_device_errors():
     q = _sequences([6, 6, 6, 6], [2, 2, 2, 2], 1.0, 9)
     q[3][1] = [0, 0]                                       # repeated
