@@ -926,17 +926,18 @@ def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None
     dt = _DTYPES.get(logits.dtype) if isinstance(logits, _Tensor) and logits.is_cuda else None
     if dt is None or logits.dim() != 2:
         raise TypeError("logits must be a 2-D CUDA tensor of bf16, fp16 or fp32")
-    rows, cols = logits.size(0), logits.size(1)
-    ld = logits.stride(0) if rows > 1 else cols
-    if (cols > 1 and logits.stride(1) != 1) or ld < cols:
+    shape, strides = logits.shape, logits.stride()
+    rows, cols = shape
+    ld = strides[0] if rows > 1 else cols
+    if (cols > 1 and strides[1] != 1) or ld < cols:
         raise TypeError("the rows of logits must be contiguous and not overlap")
     classes = cols if classes is None else int(classes)
     if not 1 <= classes <= cols:
         raise ValueError("classes must be in [1, logits.shape[1]]")
     if grad is not None and grad is not logits and not (
             isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
-            grad.dim() == 2 and grad.size(0) == rows and grad.size(1) == cols and
-            (grad.stride(0) == ld or rows <= 1) and (grad.stride(1) == 1 or cols == 1)):
+            grad.shape == shape and (grad.stride() == strides or (
+                (grad.stride(0) == ld or rows <= 1) and (grad.stride(1) == 1 or cols == 1)))):
         raise TypeError("grad must be like logits: device, type, shape and strides")
     code = load_library().dora_policy_loss(
         logits.data_ptr(), dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
