@@ -12,7 +12,7 @@
 // list with no more units than spans has a unit a span, and nothing to count.
 //
 // All three are bound by memory: 86 M fp32 gradients are normed in 54 us (6.4 TB/s; a
-// copy 6.8) and clipped in 166 (three passes, 6.2 TB/s); an Adam step on 86 M fp32
+// copy 6.8) and clipped in 162 (three passes, 6.4 TB/s); an Adam step on 86 M fp32
 // weights, bf16 gradients and bf16 copies takes 384 after a norm of 32 (6.2 TB/s).  Lists
 // of a few hundred KB take the time of their chain (launch, span, values, sums, ticket):
 // 5 us for the norm, 8 with clipping, 10 for norm and step.
@@ -220,6 +220,31 @@ __device__ __forceinline__ double wide_squares(uint4 q) {
   return t;
 }
 
+// A second pass over the values begins at the spans' ends (below).  So that L2 still has
+// them, what lies more than kKeep bytes before a piece's end is read to be evicted first
+// (clip of 344 MB fp32 168 us, 162 with it; 600 MB bf16 292 and 284; shorter lists, and
+// a step after the norm, are as fast).
+constexpr int kKeep = 150 << 10;          // of 608 spans: 91 MB
+
+__device__ __forceinline__ uint64_t evict_first() {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ uint64_t evict_normal() {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ uint4 load_as(const uint4* p, uint64_t policy) {
+  uint4 q;
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+               : "l"(p), "l"(policy)
+               : "memory");
+  return q;
+}
+
 __device__ __forceinline__ void piece_squares(const void* p, int type, int n, SumOfSquares* acc) {
   constexpr int kInFlight = 8;
   const int elems = 16 / size_of(type);
@@ -228,11 +253,14 @@ __device__ __forceinline__ void piece_squares(const void* p, int type, int n, Su
   if (threadIdx.x < head) acc->add_one(load_one(p, type, threadIdx.x));
   if (tail + threadIdx.x < n) acc->add_one(load_one(p, type, tail + threadIdx.x));
   const uint4* g = reinterpret_cast<const uint4*>(at_elem(p, type, head));
+  const uint64_t once = evict_first(), again = evict_normal();
   for (int i = threadIdx.x; i < granules; i += kInFlight * kThreads) {
+    const uint64_t policy = granules - i > kKeep / 16 ? once : again;
     uint4 q[kInFlight];
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u)
-      q[u] = i + u * kThreads < granules ? g[i + u * kThreads] : make_uint4(0, 0, 0, 0);
+      q[u] = i + u * kThreads < granules ? load_as(g + i + u * kThreads, policy)
+                                           : make_uint4(0, 0, 0, 0);
     float a = 0.f, b = 0.f;
     if (type == DORA_F32) {
 #pragma unroll
@@ -339,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 // ---------------------------------------------------------------------------
 // Clipping.  A norm that is not finite leaves the gradients as they are.  Spans
 // are walked from their ends, which the norm has read last and L2 may still hold
-// (67 MB of fp32 28.7 us, 32.3 from the beginnings; 344 MB 167 and 172, of which
+// (67 MB of fp32 28.7 us, 32.3 from the beginnings; 344 MB 162, of which
 // three passes at the copy rate are 152).
 // ---------------------------------------------------------------------------
 template <typename T>
