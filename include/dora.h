@@ -709,7 +709,8 @@ enum dora_dtype { DORA_BF16 = 0, DORA_F16 = 1, DORA_F32 = 2 };
  *                  + kl_coef (exp x - 1 - x) - entropy_coef H ],
  *   grad_j   = g (1(j = a) - p_j) + w entropy_coef p_j (log p_j + H),
  *   g        = w [ -rho A (rho A <= clip(rho) A) + kl_coef (1 - exp x) ].
- * logits     [rows, ld] of `dtype` (dora_dtype), ld >= classes >= 1, aligned to
+ * logits     [rows, ld] of `dtype` (dora_dtype), rows and classes up to 2^30,
+ *            ld >= classes >= 1, aligned to
  *            its elements (rows may start at any alignment).
  * legal      nullable int32 [rows]: n_r, the legal actions come first (the
  *            budget grid's feasible counts do); logits past them are not read.

@@ -1443,8 +1443,9 @@ int dora_policy_loss(const void* logits, int32_t dtype, int32_t rows, int32_t cl
                      float* logp, float* entropy, float* row_loss, void* grad, float* totals,
                      void* workspace, size_t workspace_bytes, int32_t* status,
                      dora_stream_t stream_) {
-  if (rows < 0 || rows > (1 << 30) || classes < 1 || ld < classes || dtype < DORA_BF16 ||
-      dtype > DORA_F32)
+  // rows and granules are counted in 32 bits, with room for a step past the last
+  if (rows < 0 || rows > (1 << 30) || classes < 1 || classes > (1 << 30) || ld < classes ||
+      dtype < DORA_BF16 || dtype > DORA_F32)
     return DORA_ERR_INVALID_ARG;
   if (rows > 0 && (logits == nullptr || actions == nullptr)) return DORA_ERR_INVALID_ARG;
   const uintptr_t size_mask = dtype == DORA_F32 ? 3u : 1u;

@@ -113,6 +113,15 @@ def test_policy_loss_host_checks(lib):
     assert lib.dora_policy_loss(*good) == 1
 
 
+def test_policy_loss_refuses_rows_that_32_bit_indexes_do_not_hold(lib):
+    f = ctypes.c_float
+    args = [16, 0, 1, (1 << 30) + 1, 1 << 40, None, 16, 16, None, 16, None, f(.2), f(.2), f(0),
+            f(0), 16, None, None, None, None, None, 0, None, None]
+    for classes in ((1 << 30) + 1, (1 << 31) - 1):
+        args[3] = classes
+        assert lib.dora_policy_loss(*args) == 1
+
+
 def test_pl_policy_loss_host_checks(lib):
     f = ctypes.c_float
     good = [16, 16, 4, 100, 16, 16, 8, 16, None, 16, None, f(.2), f(.2), f(0), 16, None, None,
