@@ -703,17 +703,19 @@ __device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uin
 // microsecond besides its granules, of which nothing was hidden.)
 // Between CTAs only the joining warps speak: an arrival that others may read behind
 // waits for all that its thread has stored, and other warps have gradients on their way.
-// Two places for the parts are enough: a warp leaves those of row i + 2 once those of
-// row i are taken, and a CTA sends row i + 2 after it has had every CTA's part of
-// row i + 1, which they send when they are done with those of row i.
+// Within a CTA two places for the parts are enough: a warp leaves those of row i + 2
+// once those of row i are taken.  The cluster's need four, two a joining warp: a warp
+// that has row i + 2 does not know whether the other CTAs have read row i, only that
+// they have sent it; one that has row i + 4 has had row i + 2 from every CTA's own warp,
+// which sends it when it is done with row i.
 template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas>
 __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     policy_ring_kernel(Rows<T> r, Actions p) {
-  constexpr int kStages = 3;
+  constexpr int kStages = 3, kPlaces = 4;
   extern __shared__ __align__(128) uint4 ring[];
-  __shared__ Part slots[2][kSumWarps], ctas[2][kCtas];
+  __shared__ Part slots[2][kSumWarps], ctas[kPlaces][kCtas];
   __shared__ RowGrad grads[2];
-  __shared__ uint64_t full[kStages], empty[kStages], summed[2], joined[2], ready[2], taken[2];
+  __shared__ uint64_t full[kStages], empty[kStages], summed[2], joined[kPlaces], ready[2], taken[2];
   __shared__ int abort;
   const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int step = gridDim.x / kCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -725,10 +727,10 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&summed[s], kSumWarps);
-      mbar_init(&joined[s], kCtas);
       mbar_init(&ready[s], 1);
       mbar_init(&taken[s], kGradWarps);
     }
+    for (int s = 0; s < kPlaces; ++s) mbar_init(&joined[s], kCtas);
     fence_barrier_init();
   }
   if (kCtas > 1) cluster_sync();          // the others' barriers are there to be written
@@ -815,14 +817,15 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
           __syncwarp();
           Part x = join_parts<kSumWarps>(slots[slot]);
           if (kCtas > 1) {
+            const int place = count % kPlaces;
             if (lane < kCtas) {
-              store_part_remote(x, &ctas[slot][rank], lane);
-              mbar_arrive_remote(&joined[slot], lane);
+              store_part_remote(x, &ctas[place][rank], lane);
+              mbar_arrive_remote(&joined[place], lane);
             }
-            if (!mbar_wait_cluster(&joined[slot], phase & 1, &abort))
+            if (!mbar_wait_cluster(&joined[place], count / kPlaces & 1, &abort))
               record_status(r.status, DORA_ERR_TIMEOUT);
             __syncwarp();
-            x = join_parts<kCtas>(ctas[slot]);
+            x = join_parts<kCtas>(ctas[place]);
           }
           Terms terms;
           const RowGrad k = finish_row(r, p, in, row, x.za, x, leader, &terms);
@@ -888,7 +891,7 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
         Part part = x.over(32);
         part.za = to_float(za);
         const int slot = count & 1;
-        if (count >= 2) wait(&ready[slot], (count >> 1) - 1);   // warp 0 has taken them
+        if (count >= 2) wait(&ready[slot], (count >> 1) - 1);   // the last ones are taken
         if (lane == 0) {
           slots[slot][warp - 3] = part;
           mbar_arrive(&summed[slot]);
