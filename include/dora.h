@@ -718,7 +718,8 @@ enum dora_dtype { DORA_BF16 = 0, DORA_F16 = 1, DORA_F32 = 2 };
  * actions    int32 [rows]; a negative one means that the row has none.
  * old_logp   fp32 [rows], the log-probability when the action was taken;
  * ref_logp   nullable fp32 [rows], under the reference policy (required when
- *            kl_coef != 0; with it NULL the KL term is 0);
+ *            kl_coef != 0; with it NULL the KL term is 0, with kl_coef 0 it is
+ *            only reported in the totals);
  * advantages fp32 [rows]; weights nullable fp32 [rows] (NULL = 1): w, e.g. one
  *            over the number of actions, 0 for padding.
  * A row without an action or of weight 0 takes no part: its logits are not

@@ -648,7 +648,8 @@ def clipped_terms(logp: np.ndarray, old: np.ndarray, adv: np.ndarray, ref, low: 
     """(policy term, KL term, whether the clipping removed the gradient,
     d policy / d logp, d KL / d logp) of actions: the clipped surrogate
     -min(rho A, clip(rho, 1 - low, 1 + high) A), rho = exp(logp - old), and
-    exp x - 1 - x with x = ref - logp (0 without a reference)."""
+    exp x - 1 - x with x = ref - logp (0 without a reference).  A term that is
+    past the range of 64 bits is infinite."""
     rho = np.exp(logp - old)
     cut = np.clip(rho, 1 - low, 1 + high) * adv
     plain = rho * adv
@@ -656,7 +657,8 @@ def clipped_terms(logp: np.ndarray, old: np.ndarray, adv: np.ndarray, ref, low: 
     if ref is None:
         kl, dkl = np.zeros_like(logp), np.zeros_like(logp)
     else:
-        kl, dkl = np.expm1(ref - logp) - (ref - logp), -np.expm1(ref - logp)
+        with np.errstate(over="ignore"):
+            kl, dkl = np.expm1(ref - logp) - (ref - logp), -np.expm1(ref - logp)
     return -np.where(clipped, cut, plain), kl, clipped, -np.where(clipped, 0.0, plain), dkl
 
 
@@ -685,11 +687,12 @@ def policy_loss(logits: np.ndarray, actions, old, adv, ref=None, weights=None, l
         pol, kl, clipped, dpol, dkl = clipped_terms(
             lp, np.array([old[r]], dtype=np.float64), np.array([adv[r]], dtype=np.float64),
             None if ref is None else np.array([ref[r]], dtype=np.float64), low, high)
-        g = w * (dpol[0] + kl_coef * dkl[0])
+        g = w * (dpol[0] + (kl_coef * dkl[0] if kl_coef else 0.0))
         d = -g * p + w * entropy_coef * (plogp + p * h)
         d[actions[r]] += g
         out["logp"][r], out["entropy"][r] = lp[0], h
-        out["row_loss"][r] = w * (pol[0] + kl_coef * kl[0] - entropy_coef * h)
+        out["row_loss"][r] = w * (pol[0] + (kl_coef * kl[0] if kl_coef else 0.0) -
+                                  entropy_coef * h)
         out["grad"][r, :n] = d
         out["totals"] += [out["row_loss"][r], w * pol[0], w * kl[0], w * h, w * clipped[0], w]
     return out
@@ -712,9 +715,9 @@ def pl_policy_loss(scores: np.ndarray, cu, k, order, old, adv, ref=None, weights
         pol, kl, clipped, dpol, dkl = clipped_terms(
             lp, np.array([old[i]], dtype=np.float64), np.array([adv[i]], dtype=np.float64),
             None if ref is None else np.array([ref[i]], dtype=np.float64), low, high)
-        g = w * (dpol[0] + kl_coef * dkl[0])
+        g = w * (dpol[0] + (kl_coef * dkl[0] if kl_coef else 0.0))
         out["logp"][i] = lp[0]
-        out["row_loss"][i] = w * (pol[0] + kl_coef * kl[0])
+        out["row_loss"][i] = w * (pol[0] + (kl_coef * kl[0] if kl_coef else 0.0))
         out["grad"][cu[i] + 1:cu[i + 1]] = g * pl_logprob_grad(s, seq)
         out["totals"] += [out["row_loss"][i], w * pol[0], w * kl[0], 0.0, w * clipped[0], w]
     return out

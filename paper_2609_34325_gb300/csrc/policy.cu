@@ -97,7 +97,8 @@ struct Terms {
 __device__ __forceinline__ Terms all_terms(float x) { return {{x, x, x, x, x, x}}; }
 
 // One row's loss from l - q, x = q_ref - l and the entropy h; returns g.  A NaN
-// ratio is left to spread (comparisons, no fmin).
+// ratio is left to spread (comparisons, no fmin).  A term of coefficient 0 is not
+// multiplied by it: e^x passes fp32's range where x does 88.
 __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, float x, float adv,
                                            float w, float h, Terms* terms) {
   const float ratio = expf(log_ratio);
@@ -110,9 +111,10 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   if (p.ref_logp != nullptr) {
     const float em1 = expm1f(x);
     kl = em1 - x;
-    g = fmaf(-p.kl_coef, em1, g);
+    if (p.kl_coef != 0.f) g = fmaf(-p.kl_coef, em1, g);
   }
-  float row = fmaf(p.kl_coef, kl, surrogate);
+  float row = surrogate;
+  if (p.kl_coef != 0.f) row = fmaf(p.kl_coef, kl, row);
   if (p.entropy_coef != 0.f) row = fmaf(-p.entropy_coef, h, row);
   *terms = Terms{{w * row, w * surrogate, w * kl, w * h, inside ? 0.f : w, w}};
   return g * w;
