@@ -726,7 +726,9 @@ enum dora_dtype { DORA_BF16 = 0, DORA_F16 = 1, DORA_F32 = 2 };
  * read, its outputs and gradient are 0.  An action at or past n_r, or n_r
  * outside [0, classes], gives NaN outputs and gradients for the row (and NaN
  * totals) and DORA_ERR_DEVICE_BAD_COUNT.  Logits of -inf are actions of
- * probability 0; NaN, +inf, or a row of -inf alone make the row NaN.
+ * probability 0 (one that was taken has l = -inf and an infinite KL term; with
+ * kl_coef != 0 its loss is infinite and its gradient not finite); NaN, +inf, or a
+ * row of -inf alone make the row NaN.
  * clip_low in [0, 1], clip_high >= 0.
  * logp       out fp32 [rows]: l.  entropy nullable out fp32 [rows]: H.
  * row_loss   nullable out fp32 [rows].

@@ -649,7 +649,8 @@ def clipped_terms(logp: np.ndarray, old: np.ndarray, adv: np.ndarray, ref, low: 
     d policy / d logp, d KL / d logp) of actions: the clipped surrogate
     -min(rho A, clip(rho, 1 - low, 1 + high) A), rho = exp(logp - old), and
     exp x - 1 - x with x = ref - logp (0 without a reference).  A term that is
-    past the range of 64 bits is infinite."""
+    past the range of 64 bits is infinite, and so is the KL term of an action of
+    probability 0."""
     rho = np.exp(logp - old)
     cut = np.clip(rho, 1 - low, 1 + high) * adv
     plain = rho * adv
@@ -657,8 +658,9 @@ def clipped_terms(logp: np.ndarray, old: np.ndarray, adv: np.ndarray, ref, low: 
     if ref is None:
         kl, dkl = np.zeros_like(logp), np.zeros_like(logp)
     else:
+        x = ref - logp
         with np.errstate(over="ignore"):
-            kl, dkl = np.expm1(ref - logp) - (ref - logp), -np.expm1(ref - logp)
+            kl, dkl = np.expm1(x) - np.where(x == np.inf, 0.0, x), -np.expm1(x)
     return -np.where(clipped, cut, plain), kl, clipped, -np.where(clipped, 0.0, plain), dkl
 
 
@@ -688,7 +690,8 @@ def policy_loss(logits: np.ndarray, actions, old, adv, ref=None, weights=None, l
             lp, np.array([old[r]], dtype=np.float64), np.array([adv[r]], dtype=np.float64),
             None if ref is None else np.array([ref[r]], dtype=np.float64), low, high)
         g = w * (dpol[0] + (kl_coef * dkl[0] if kl_coef else 0.0))
-        d = -g * p + w * entropy_coef * (plogp + p * h)
+        with np.errstate(invalid="ignore"):                # an infinite g on p = 0
+            d = -g * p + w * entropy_coef * (plogp + p * h)
         d[actions[r]] += g
         out["logp"][r], out["entropy"][r] = lp[0], h
         out["row_loss"][r] = w * (pol[0] + (kl_coef * kl[0] if kl_coef else 0.0) -

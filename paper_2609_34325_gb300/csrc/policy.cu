@@ -110,7 +110,7 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   float g = inside ? -plain : 0.f, kl = 0.f;
   if (p.ref_logp != nullptr) {
     const float em1 = expm1f(x);
-    kl = em1 - x;
+    kl = em1 == INFINITY ? em1 : em1 - x;                 // x too is where l is -inf
     if (p.kl_coef != 0.f) g = fmaf(-p.kl_coef, em1, g);
   }
   float row = surrogate;

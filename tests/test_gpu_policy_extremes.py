@@ -95,3 +95,39 @@ def test_a_kl_term_of_coefficient_zero_is_only_reported_of_sequences(_built):
     for n in ("logp", "row_loss", "grad"):
         assert bool(torch.isfinite(a[n]).all()) and torch.equal(a[n], b[n]), n
     assert torch.equal(a["totals"][:2], b["totals"][:2]) and float(a["totals"][2]) == math.inf
+
+
+def test_oracle_kl_of_an_action_of_probability_zero():
+    o = O.policy_loss(np.array([[0., -np.inf, 1.]]), [1], [-1.0], [2.0], ref=[-0.5], kl_coef=0.1)
+    assert o["logp"][0] == -np.inf and o["row_loss"][0] == np.inf and o["totals"][2] == np.inf
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("classes", [50, 1500, 20000, 140000])
+def test_kl_of_an_action_of_probability_zero(classes, _built):
+    z, actions, lp = _rows(classes, -math.inf)
+    old, adv, ref = np.where(np.isinf(lp), -1.0, lp), np.linspace(-1, 1, 6), np.full(6, -0.5)
+    bad = np.isinf(lp)
+    out = _policy(z, actions, old, adv, ref_logp=f32(ref), kl_coef=0.1)
+    loss = out["row_loss"].cpu().numpy()
+    assert np.all(out["logp"].cpu().numpy()[bad] == -np.inf)
+    assert np.all(loss[bad] == np.inf) and np.isfinite(loss[~bad]).all()
+    assert float(out["totals"][0]) == math.inf and float(out["totals"][2]) == math.inf
+    assert not np.isfinite(out["grad"].cpu().numpy()[bad, actions[bad]]).any()
+    assert bool(torch.isfinite(out["grad"].cpu()[torch.from_numpy(~bad)]).all())
+    # where the term is only reported, the ratio 0 has its clipped loss and no gradient
+    out = _policy(z, actions, old, adv, ref_logp=f32(ref), kl_coef=0.0)
+    assert bool(torch.isfinite(out["grad"]).all()) and float(out["totals"][2]) == math.inf
+    want = np.where(adv < 0, -0.8 * adv, 0.0)
+    assert np.allclose(out["row_loss"].cpu().numpy()[bad], want[bad], rtol=1e-6, atol=0)
+    assert not out["grad"].cpu().numpy()[bad].any()
+
+
+@pytest.mark.gpu
+def test_kl_of_a_sequence_of_probability_zero(_built):
+    s, cu, k, order, lp = _images(-math.inf)
+    assert lp[1] == -np.inf
+    old, adv, ref = np.where(np.isinf(lp), -1.0, lp), np.ones(3), np.full(3, -0.5)
+    out = _sequences(s, cu, k, order, old, adv, ref_logp=f32(ref), kl_coef=0.1)
+    assert float(out["row_loss"][1]) == math.inf and bool(torch.isfinite(out["row_loss"][::2]).all())
+    assert float(out["totals"][0]) == math.inf and float(out["totals"][2]) == math.inf
