@@ -104,7 +104,8 @@ __device__ __forceinline__ float row_terms(const Actions& p, float log_ratio, fl
   const float ratio = expf(log_ratio);
   const float lo = 1.f - p.clip_low, hi = 1.f + p.clip_high;
   const float cut = (ratio < lo ? lo : (ratio > hi ? hi : ratio)) * adv;
-  const float plain = ratio * adv;
+  // an advantage of 0 has no policy term, also where the ratio passes fp32's range
+  const float plain = adv == 0.f && ratio == INFINITY ? 0.f : ratio * adv;
   const bool inside = !(plain > cut);
   const float surrogate = -(inside ? plain : cut);
   float g = inside ? -plain : 0.f, kl = 0.f;

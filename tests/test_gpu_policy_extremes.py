@@ -131,3 +131,25 @@ def test_kl_of_a_sequence_of_probability_zero(_built):
     out = _sequences(s, cu, k, order, old, adv, ref_logp=f32(ref), kl_coef=0.1)
     assert float(out["row_loss"][1]) == math.inf and bool(torch.isfinite(out["row_loss"][::2]).all())
     assert float(out["totals"][0]) == math.inf and float(out["totals"][2]) == math.inf
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("classes", [50, 1500, 20000, 140000])
+def test_an_advantage_of_zero_has_no_policy_term_at_any_ratio(classes, _built):
+    z, actions, lp = _rows(classes, 3.0)
+    old = lp - 0.1
+    old[1:3] = -300.0                                      # the ratio is past fp32
+    o = O.policy_loss(z, actions, old, np.zeros(6), entropy_coef=0.01)
+    out = _policy(z, actions, old, np.zeros(6), entropy_coef=0.01)
+    assert not o["totals"][1] and not out["totals"][1:2].any()
+    assert np.allclose(out["row_loss"].cpu().numpy(), o["row_loss"], rtol=1e-5, atol=0)
+    assert np.all(np.abs(out["grad"].cpu().numpy() - o["grad"]) <= 1e-6)
+    # a ratio that is no number is not hidden
+    assert math.isnan(float(_policy(z, actions, np.full(6, np.nan), np.zeros(6))["row_loss"][0]))
+
+
+@pytest.mark.gpu
+def test_an_advantage_of_zero_has_no_policy_term_of_sequences(_built):
+    s, cu, k, order, lp = _images(1.0)
+    out = _sequences(s, cu, k, order, np.full(3, -300.0), np.zeros(3))
+    assert not out["row_loss"].any() and not out["grad"].any() and not out["totals"][:3].any()
