@@ -17,16 +17,18 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libdora.so")
-# The timeout-path test library: the same objects, except that the attention
-# kernels' bounded waits give up after 5 ms and their first CTA withholds its
-# first K/V load, so a wait runs out (tests/test_gpu_timeout.py).
+# The timeout-path test library: the same objects, except that the bounded waits of
+# the attention and policy loss kernels give up after 5 ms and their first CTA
+# withholds its first K/V load, or its second row, so a wait runs out
+# (tests/test_gpu_timeout.py, tests/test_gpu_policy_timeout.py).
 TIMEOUT_TEST_LIB_PATH = os.path.join(HERE, "libdora_timeout_test.so")
-TIMEOUT_TEST_FLAGS = ["-DDORA_TEST_WITHHOLD_KV_LOAD", "-DDORA_TEST_WAIT_LIMIT_NS=5000000ull"]
+TIMEOUT_TEST_FLAGS = ["-DDORA_TEST_WITHHOLD_KV_LOAD", "-DDORA_TEST_WITHHOLD_ROW_LOAD",
+                      "-DDORA_TEST_WAIT_LIMIT_NS=5000000ull"]
 SOURCES = ["token_ops.cu", "gemm_tcgen05.cu", "attn_tcgen05.cu", "api.cu", "noalloc.cu",
            "actor.cu", "actor_front.cu", "actor_tail.cu", "embed_head.cu", "training.cu",
            "policy.cu", "optim.cu"]
-# the attention translation unit, rebuilt with the test flags for the timeout-path library
-ATTN_SOURCES = ("attn_tcgen05.cu",)
+# the translation units rebuilt with the test flags for the timeout-path library
+TIMEOUT_TEST_SOURCES = ("attn_tcgen05.cu", "policy.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -79,12 +81,12 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list | None =
         return obj
 
     jobs = [(src, "", []) for src in SOURCES] + [(src, "_timeout_test", TIMEOUT_TEST_FLAGS)
-                                                  for src in ATTN_SOURCES]
+                                                  for src in TIMEOUT_TEST_SOURCES]
     with ThreadPoolExecutor(len(jobs)) as ex:
         objs = list(ex.map(compile_one, jobs))
     main_objs = objs[:len(SOURCES)]
-    test_attn = dict(zip(ATTN_SOURCES, objs[len(SOURCES):]))
-    test_objs = [test_attn.get(s, o) for s, o in zip(SOURCES, main_objs)]
+    rebuilt = dict(zip(TIMEOUT_TEST_SOURCES, objs[len(SOURCES):]))
+    test_objs = [rebuilt.get(s, o) for s, o in zip(SOURCES, main_objs)]
 
     def link(objs_, path):
         tmp = path + ".tmp"

@@ -14,8 +14,8 @@ namespace dora {
 
 // A bounded wait gives up after this many nanoseconds of %globaltimer and
 // reports DORA_ERR_TIMEOUT instead of spinning forever.  The timeout-path test
-// library builds the attention kernel with a limit of a few milliseconds
-// (DORA_TEST_WAIT_LIMIT_NS); the product library never defines it.
+// library builds the attention and policy loss kernels with a limit of a few
+// milliseconds (DORA_TEST_WAIT_LIMIT_NS); the product library never defines it.
 #ifdef DORA_TEST_WAIT_LIMIT_NS
 constexpr uint64_t kWaitLimitNs = DORA_TEST_WAIT_LIMIT_NS;
 #else

@@ -487,13 +487,18 @@ __device__ __forceinline__ RowGrad finish_row(const Rows<T>& r, const Actions& p
   return RowGrad{x.m, a, b, fmaf(ex2(da * kLog2e), fmaf(b, fmaxf(da, kFloor), a), g)};
 }
 
+template <typename T>
+__device__ __forceinline__ void write_row(const Rows<T>& r, const Actions& p, int row,
+                                          float fill) {
+  p.logp[row] = fill;
+  if (r.entropy != nullptr) r.entropy[row] = fill;
+  if (p.row_loss != nullptr) p.row_loss[row] = fill;
+}
 // The outputs of a row that takes no part (0) or is not valid (NaN).
 template <typename T>
 __device__ __forceinline__ void fill_row(const Rows<T>& r, const Actions& p, int row, float fill) {
   if (fill != 0.f) record_status(r.status, DORA_ERR_DEVICE_BAD_COUNT);
-  p.logp[row] = fill;
-  if (r.entropy != nullptr) r.entropy[row] = fill;
-  if (p.row_loss != nullptr) p.row_loss[row] = fill;
+  write_row(r, p, row, fill);
 }
 
 template <typename T>
@@ -691,6 +696,16 @@ __device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uin
       : "memory");
 }
 
+// A word into CTA `cta` of the cluster.
+__device__ __forceinline__ void store_remote(int v, int* to, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.shared::cluster.u32 [ra], %2;\n\t}" ::"r"(smem_u32(to)),
+      "r"(cta), "r"(v)
+      : "memory");
+}
+
 // Longer rows: kCtas CTAs (a cluster when there are several) hold one, an equal part
 // each, in a ring of kStages stages of shared memory (more, where they fit, changed
 // nothing).  Four kinds of warps, so that a row's steps, which wait for one another,
@@ -711,6 +726,11 @@ __device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uin
 // that has row i + 2 does not know whether the other CTAs have read row i, only that
 // they have sent it; one that has row i + 4 has had row i + 2 from every CTA's own warp,
 // which sends it when it is done with row i.
+//
+// A wait is bounded.  Where one runs out, its warp is out of step with the others and
+// with the other CTAs, which may take one row's parts for another's.  The rows carry on
+// as they are, at a wait's first look each, and at the end all of the cluster's become
+// NaN, so that no call without a status word takes them for results.
 template <typename T, int kSumWarps, int kGradWarps, int kStage, int kCtas>
 __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     policy_ring_kernel(Rows<T> r, Actions p) {
@@ -754,9 +774,10 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     *lo = min(rank * per, all);
     *hi = min(*lo + per, all);
   };
-  // a wait that ran out is reported, and what follows computed from what is there
   auto wait = [&](uint64_t* bar, int phase) {
-    if (!mbar_wait(bar, phase & 1, &abort)) record_status(r.status, DORA_ERR_TIMEOUT);
+    const bool done = mbar_wait(bar, phase & 1, &abort);
+    if (!done) record_status(r.status, DORA_ERR_TIMEOUT);
+    return done;
   };
   // Whether the row's first granule (it starts inside it), or its last with legal logits
   // (they end inside it), is this CTA's: thread 0 and thread 1 of a kind see to them.
@@ -792,7 +813,15 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
         int lo, hi, from, to;
         bounds(z, &lo, &hi);
         copied(z, row, lo, hi, &from, &to);
-        if (lap > 0) wait(&empty[stage], lap - 1);
+        if (lap > 0 && !wait(&empty[stage], lap - 1)) break;
+#ifdef DORA_TEST_WITHHOLD_ROW_LOAD
+        // timeout-path test library only: the first CTA's second row is never copied nor
+        // its bytes expected, so that the waits for it run out with no copy in flight
+        if (blockIdx.x == 0 && count == 1) {
+          advance();
+          continue;
+        }
+#endif
         if (to > from) {
           mbar_arrive_expect_tx(&full[stage], (to - from) * 16);
           bulk_load(ring + stage * kStage + (from - lo), z.at(from), (to - from) * 16,
@@ -802,9 +831,8 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
         }
         advance();
       }
-      if (abort)                          // no copy may land after the CTA is gone
-        for (int s = 0; s < kStages; ++s)
-          mbar_wait_limited(&full[s], (s < stage ? lap : lap - 1) & 1, kWaitLimitNs / 8);
+      for (int s = 0; s < kStages; ++s)   // no copy may land after the CTA is gone
+        mbar_wait_limited(&full[s], (s < stage ? lap : lap - 1) & 1, kWaitLimitNs / 8);
     }
   } else if (warp < 2) {
     const bool leader = rank == 0 && lane == 0;
@@ -960,12 +988,30 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
       }
     }
   }
-  __syncwarp();
-  if (kCtas > 1) cluster_sync();          // nobody leaves while parts may be on their way to it
   __shared__ Pair odd[kTerms];            // of warp 1's rows
   if (warp == 1 && lane < kTerms) odd[lane] = sum;
   __syncthreads();
+  if (kCtas > 1) {
+    if (abort != 0 && threadIdx.x < kCtas) store_remote(1, &abort, threadIdx.x);
+    __syncwarp();
+    cluster_sync();                       // nobody leaves while parts may be on their way to it
+  }
   if (threadIdx.x < kTerms) sum.add(odd[threadIdx.x]);
+  if (abort != 0) {
+    for (row = blockIdx.x / kCtas; row < r.rows; row += step) {
+      const RowUse use = row_use(r, row_ahead(r, p, row));
+      if (!computed(use)) continue;
+      const RowPtr<T> z(r.logits + row * r.ld, use.n);
+      T* dz = r.grad != nullptr ? r.grad + row * r.ld : nullptr;
+      int lo, hi;
+      bounds(z, &lo, &hi);
+      if (rank == 0 && threadIdx.x == 0) write_row(r, p, row, NAN);
+      if (dz != nullptr)
+        for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += blockDim.x)
+          fill_granule(z, dz, same_alignment(dz, z.z), i, r.classes, NAN);
+    }
+    if (rank == 0) sum.add(all_terms(NAN).of(threadIdx.x));
+  }
   finish_totals<3 + kSumWarps + kGradWarps>(p, sum);
 }
 
