@@ -988,6 +988,14 @@ class _ParamListC(ctypes.Structure):
                 ("has_params", _i32)]
 
 
+def _bytes_on(n, device, stream):
+    """Device memory that is written on ``stream`` at once.  Taken from the current
+    stream's, it could be what a freed tensor left there, whose kernels still run;
+    freed, it could be given out while ``stream`` uses it."""
+    with torch.cuda.stream(stream):       # None: the current one
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 class ParamList:
     """Tensors that are updated together, laid out on the device once
     (dora_param_list_prepare): gradients (bf16, fp16 or fp32, contiguous) and,
@@ -995,7 +1003,8 @@ class ParamList:
     writes; None: in place), ``params`` with ``exp_avg`` and ``exp_avg_sq``
     (fp32), and bf16 ``copies`` of the updated weights.  The tensors are kept
     alive here; make a new list when any of them moves.  Calls on one list are
-    ordered on one stream."""
+    ordered on one stream, ``stream`` (the current one by default): the list's
+    own memory belongs to it."""
 
     def __init__(self, grads, params=None, exp_avg=None, exp_avg_sq=None, copies=None,
                  clipped=None, stream=None):
@@ -1044,7 +1053,7 @@ class ParamList:
             (at.grad, at.clipped, at.param, at.exp_avg, at.exp_avg_sq, at.copy, at.n,
              at.grad_dtype, at.param_dtype) = row
         size = int(load_library().dora_param_list_size(c, n))
-        self.data = torch.empty(size, dtype=torch.uint8, device=device)
+        self.data = _bytes_on(size, device, stream)
         self.c = _ParamListC()
         self.ref = ctypes.byref(self.c)
         _check(load_library().dora_param_list_prepare(c, n, _ptr(self.data), size, self.ref,
@@ -1092,11 +1101,10 @@ def dora_adam_init(state, step=0, beta1=0.9, beta2=0.999, stream=None):
 
 
 def alloc_adam_state(device=None, step=0, beta1=0.9, beta2=0.999, stream=None) -> torch.Tensor:
-    """Device state of dora_adam_step; ``state[:8].view(torch.int64)`` is the
-    number of steps taken."""
+    """Device state of dora_adam_step, of the stream that the steps run on;
+    ``state[:8].view(torch.int64)`` is the number of steps taken."""
     n = int(load_library().dora_adam_state_size())
-    return dora_adam_init(torch.empty(n, dtype=torch.uint8, device=device or "cuda"), step, beta1,
-                          beta2, stream)
+    return dora_adam_init(_bytes_on(n, device or "cuda", stream), step, beta1, beta2, stream)
 
 
 def dora_adam_step(plist, state, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0,
