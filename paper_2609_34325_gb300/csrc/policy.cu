@@ -1096,11 +1096,12 @@ __global__ void __launch_bounds__(kLongBlock, 2) policy_long_kernel(Rows<T> r, A
 // s e^m, each with a maximum of its own, at two exponentials an addition.
 //
 // One CTA an image, a thread an equal run of steps.  An image takes the time of its
-// chain (boundaries, scores, order, two scans, five barriers), so the CTAs are small
-// and all of a batch are resident at once: 256 images of 197 tokens, up to 60 removed,
-// 6 us, 1024 of 577, up to 120 removed, 10, of which the totals are 2 and 4.
+// chain (boundaries, scores, order, two scans, five barriers), so the CTAs are small,
+// and the grid is what is resident at once, seven CTAs an SM by their shared memory: 256
+// images of 197 tokens, up to 60 removed, 6 us, 1024 of 577, up to 120 removed, 10, of
+// which the totals are 2 and 4; 1200 of 577 12.2 (13.1 with a grid of eight an SM).
 // ---------------------------------------------------------------------------
-constexpr int kSeqThreads = 128, kSeqWarps = kSeqThreads / 32, kSeqPerSm = 8;
+constexpr int kSeqThreads = 128, kSeqWarps = kSeqThreads / 32, kSeqPerSm = 7;
 constexpr float kRange = 80.f;            // e^-kRange and its reciprocal are far from fp32's ends
 
 struct Scaled {                           // s e^m
@@ -1168,6 +1169,8 @@ struct SequenceShared {
   float hi[kSeqWarps], lo[kSeqWarps];
   int bad;
 };
+// Of an SM's 228 KB; a CTA takes another 1 KB, and less than that for its totals.
+static_assert(kSeqPerSm * (sizeof(SequenceShared) + 2048) <= 228 * 1024, "resident at once");
 
 // An image's log-probability (in every thread); Q_t in h->sums.
 template <typename V>
