@@ -903,6 +903,15 @@ def _vec_opt(t, dtype, n, name):
     return None if t is None else _vec(t, dtype, n, name)
 
 
+_I32_MAX = 2 ** 31 - 1
+
+
+def _in_32_bits(*sizes):
+    """ctypes cuts an integer down to its 32 bits."""
+    if max(sizes) > _I32_MAX:
+        raise ValueError(f"sizes must be below 2^31, got {max(sizes)}")
+
+
 def _totals(totals):
     if totals is None:
         return None
@@ -934,6 +943,7 @@ def dora_policy_loss(logits, actions, old_logp, advantages, logp, workspace=None
     classes = cols if classes is None else int(classes)
     if not 1 <= classes <= cols:
         raise ValueError("classes must be in [1, logits.shape[1]]")
+    _in_32_bits(rows, classes)
     if grad is not None and grad is not logits and not (
             isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
             grad.shape == shape and (grad.stride() == strides or (
@@ -964,6 +974,7 @@ def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, worksp
     b, t_cap = cu.numel() - 1, scores.numel()
     if order.dim() != 2 or order.size(0) != b:
         raise ValueError("order must be [B, k_cap]")
+    _in_32_bits(b, t_cap, order.size(1))
     code = load_library().dora_pl_policy_loss(
         s, c, b, t_cap, _vec(k, _I32, b, "k"), o, order.size(1),
         _vec(old_logp, _F32, b, "old_logp"), _vec_opt(ref_logp, _F32, b, "ref_logp"),
