@@ -14,8 +14,8 @@ namespace dora {
 
 // A bounded wait gives up after this many nanoseconds of %globaltimer and
 // reports DORA_ERR_TIMEOUT instead of spinning forever.  The timeout-path test
-// library builds the attention and policy loss kernels with a limit of a few
-// milliseconds (DORA_TEST_WAIT_LIMIT_NS); the product library never defines it.
+// library builds the attention kernel with a limit of a few milliseconds
+// (DORA_TEST_WAIT_LIMIT_NS); the product library never defines it.
 #ifdef DORA_TEST_WAIT_LIMIT_NS
 constexpr uint64_t kWaitLimitNs = DORA_TEST_WAIT_LIMIT_NS;
 #else
@@ -275,44 +275,6 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
                "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// mbar_wait on a barrier that other CTAs of the cluster arrive on: what they wrote
-// here before (release at cluster scope) is visible after it.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity,
-                                                  volatile int* abort) {
-  if (mbar_try_wait_cluster(bar, parity)) return true;
-  const uint64_t t0 = globaltimer_ns();
-  uint32_t spins = 0;
-  while (true) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    if ((++spins & 63u) == 0u) {
-      if (*abort) return false;
-      if (globaltimer_ns() - t0 > kWaitLimitNs) {
-        *abort = 1;
-        return false;
-      }
-    }
-  }
-}
-
-// One more CTA is done: its number, from 0.  What the thread wrote before is visible to
-// the one that gets the last number, and to what follows a barrier of its CTA.
-__device__ __forceinline__ unsigned take_ticket(unsigned* ticket) {
-  unsigned n;
-  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(n) : "l"(ticket) : "memory");
-  return n;
 }
 
 // Arrive once on the mbarrier at the same shared-memory offset as `bar` in
@@ -588,11 +550,6 @@ __device__ __forceinline__ void f2_unpack(uint64_t v, float& lo, float& hi) {
 __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t d;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {

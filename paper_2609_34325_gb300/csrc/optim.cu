@@ -26,6 +26,7 @@
 #include "dora_ptx.cuh"
 #include "granule.cuh"
 #include "token_ops.cuh"
+#include "update_ptx.cuh"
 
 namespace dora {
 namespace optim {

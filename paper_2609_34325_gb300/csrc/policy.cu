@@ -32,6 +32,7 @@
 #include "dora_ptx.cuh"
 #include "granule.cuh"
 #include "token_ops.cuh"
+#include "update_ptx.cuh"
 
 namespace dora {
 namespace policy {
@@ -693,16 +694,6 @@ __device__ __forceinline__ void store_part_remote(const Part& x, Part* slot, uin
       "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
       "st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(smem_u32(slot)),
       "r"(cta), "f"(x.m), "f"(x.s), "f"(x.t), "f"(x.za)
-      : "memory");
-}
-
-// A word into CTA `cta` of the cluster.
-__device__ __forceinline__ void store_remote(int v, int* to, uint32_t cta) {
-  asm volatile(
-      "{\n\t.reg .b32 ra;\n\t"
-      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
-      "st.shared::cluster.u32 [ra], %2;\n\t}" ::"r"(smem_u32(to)),
-      "r"(cta), "r"(v)
       : "memory");
 }
 
