@@ -729,7 +729,9 @@ enum dora_dtype { DORA_BF16 = 0, DORA_F16 = 1, DORA_F32 = 2 };
  * probability 0 (one that was taken has l = -inf and an infinite KL term; with
  * kl_coef != 0 its loss is infinite and its gradient not finite); NaN, +inf, or a
  * row of -inf alone make the row NaN.
- * clip_low in [0, 1], clip_high >= 0.
+ * clip_low in [0, 1], clip_high >= 0.  An advantage of 0 has no policy term,
+ * whatever the ratio.  Should a bounded wait run out (long rows), the rows of the
+ * CTAs concerned and the totals are NaN, with DORA_ERR_TIMEOUT.
  * logp       out fp32 [rows]: l.  entropy nullable out fp32 [rows]: H.
  * row_loss   nullable out fp32 [rows].
  * grad       nullable out [rows, ld] of `dtype`: columns [0, classes) are

@@ -1013,8 +1013,11 @@ class ParamList:
     each a list of as many tensors or None, ``clipped`` (where dora_clip_grads
     writes; None: in place), ``params`` with ``exp_avg`` and ``exp_avg_sq``
     (fp32), and bf16 ``copies`` of the updated weights.  The tensors are kept
-    alive here; make a new list when any of them moves.  Calls on one list are
-    ordered on one stream, ``stream`` (the current one by default): the list's
+    alive here; make a new list when any of them moves.  That takes the host 1 to
+    3 us a tensor (32 gradients 60 us, 152 tensors with weights and moments
+    390), so gradients are best kept in buffers of their own, zeroed in place
+    rather than allocated anew at every step.  Calls on one list are ordered on
+    one stream, ``stream`` (the current one by default): the list's
     own memory belongs to it."""
 
     def __init__(self, grads, params=None, exp_avg=None, exp_avg_sq=None, copies=None,

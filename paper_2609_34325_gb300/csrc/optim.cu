@@ -173,10 +173,12 @@ __device__ __forceinline__ int head_of(const void* p, int type, int n) {
 
 // ---------------------------------------------------------------------------
 // Norm.  Squares are summed in 32 bits over the elements that a thread has at
-// hand at once; the sums are carried on in pairs of fp32 values, the second what
-// the first lost (Knuth's two-sum: six additions where an fp64 one takes the warp
-// 16 cycles or more), and joined in 64 bits.  A sum out of the middle of the
-// range (gradients above about 1e11 or below 1e-16) is taken again in 64 bits.
+// hand at once; a thread carries the sums on in a pair of fp32 values, the second
+// what the first lost (Knuth's two-sum: six additions where an fp64 one takes the
+// warp 16 cycles or more).  A CTA's threads are joined by a tree of fp32 additions
+// (of positive values: a few 2^-24 of the sum, half of that on the norm), the CTAs
+// in pairs again.  A sum out of the middle of the range (gradients above about 1e11
+// or below 1e-16) is taken again, and joined, in 64 bits.
 // ---------------------------------------------------------------------------
 constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e25f;
 

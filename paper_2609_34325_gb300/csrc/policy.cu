@@ -16,8 +16,8 @@
 //
 // What bounds them: the categorical loss reads the logits and writes the gradient once
 // each.  2048 rows of 32000 bf16 logits, a seventh of them idle, 46 us, 5.2 TB/s (a copy
-// 6.8); 4095 x 50001 fp16 161, 4.9; 1024 x 131072 fp32 194, 5.5; 16384 x 2000 bf16 32,
-// 4.1; a rollout's 256 x 96 fp32 5, of which the totals are 2.  About a dozen
+// 6.8); 4095 x 50001 fp16 162, 4.9; 1024 x 131072 fp32 194, 5.5; 16384 x 2000 bf16 33,
+// 4.0; a rollout's 256 x 96 fp32 5, of which the totals are 2.  About a dozen
 // instructions an element, two of them exponentials, on warps that wait for one another
 // at every row: issue slots are 58% busy where memory is at 75%.
 #include <cuda_bf16.h>
@@ -516,7 +516,7 @@ __device__ __forceinline__ bool same_alignment(const void* a, const void* b) {
 }
 
 // Short rows: kLanes lanes of a warp hold one, kHeld granules each (65536 x 96 fp32 14 us,
-// 3.6 TB/s; 16384 x 1000 bf16 16, 4.0; 16384 x 2000 32, 4.1; 8192 x 4096 37, 3.6): no
+// 3.6 TB/s; 16384 x 1000 bf16 16, 4.0; 16384 x 2000 33, 4.0; 8192 x 4096 38, 3.5): no
 // barrier, and what a row costs besides its elements is paid by one warp.
 template <typename T, int kLanes, int kHeld>
 __global__ void __launch_bounds__(kThreads) policy_warp_kernel(Rows<T> r, Actions p) {
@@ -1006,8 +1006,10 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
   finish_totals<3 + kSumWarps + kGradWarps>(p, sum);
 }
 
-// Rows longer than a cluster's registers: the same without the ring; a row is read a
-// second time (from L2, where the clusters' rows fit) for its gradient.
+// Rows longer than eight CTAs' rings: eight CTAs a row without one, which read it a
+// second time (from L2, where the clusters' rows fit) for its gradient: 128 x 400000
+// bf16, a seventh of them idle, 58 us, 3.0 TB/s of the two passes that it needs (26 at
+// a copy's rate).
 constexpr int kLongBlock = 512, kLongCtas = 8, kLongStep = 4;
 
 template <typename T>
