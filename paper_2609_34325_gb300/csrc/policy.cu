@@ -766,9 +766,7 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
     *hi = min(*lo + per, all);
   };
   auto wait = [&](uint64_t* bar, int phase) {
-    const bool done = mbar_wait(bar, phase & 1, &abort);
-    if (!done) record_status(r.status, DORA_ERR_TIMEOUT);
-    return done;
+    if (!mbar_wait(bar, phase & 1, &abort)) record_status(r.status, DORA_ERR_TIMEOUT);
   };
   // Whether the row's first granule (it starts inside it), or its last with legal logits
   // (they end inside it), is this CTA's: thread 0 and thread 1 of a kind see to them.
@@ -804,7 +802,10 @@ __global__ void __launch_bounds__((3 + kSumWarps + kGradWarps) * 32, 1)
         int lo, hi, from, to;
         bounds(z, &lo, &hi);
         copied(z, row, lo, hi, &from, &to);
-        if (lap > 0 && !wait(&empty[stage], lap - 1)) break;
+        if (lap > 0) wait(&empty[stage], lap - 1);
+        // warps that have given up waiting for a stage leave it too: no copy then, whose
+        // bytes would count for a phase that is not theirs
+        if (abort) break;
 #ifdef DORA_TEST_WITHHOLD_ROW_LOAD
         // timeout-path test library only: the first CTA's second row is never copied nor
         // its bytes expected, so that the waits for it run out with no copy in flight

@@ -132,3 +132,12 @@ def test_the_model_tells_one_place_a_joining_warp_from_two():
     one = _Order(2, 3, 2).faults()
     assert {what for what, *_ in one} == {"cluster's parts", "joined"}
     assert _Order(2, 3, 4).faults() == []
+
+
+def test_no_copy_follows_a_wait_that_ran_out():
+    # warps that give up arrive like those that are done, so the copying warp's own wait
+    # may succeed: it has to look at the CTA's flag before each copy into a used stage
+    src = _kernel()
+    producer = src[src.index("if (warp == 2) {"):src.index("bulk_load(")]
+    assert producer.count("wait(") == 1
+    assert "if (abort) break;" in producer[producer.index("wait(&empty[stage], lap - 1)"):]
