@@ -16,7 +16,7 @@
 //
 // What bounds them: the categorical loss reads the logits and writes the gradient once
 // each.  2048 rows of 32000 bf16 logits, a seventh of them idle, 46 us, 5.2 TB/s (a copy
-// 6.8); 4095 x 50001 fp16 162, 4.9; 1024 x 131072 fp32 194, 5.5; 16384 x 2000 bf16 33,
+// 6.8); 4095 x 50001 fp16 163, 4.9; 1024 x 131072 fp32 196, 5.5; 16384 x 2000 bf16 33,
 // 4.0; a rollout's 256 x 96 fp32 5, of which the totals are 2.  About a dozen
 // instructions an element, two of them exponentials, on warps that wait for one another
 // at every row: issue slots are 58% busy where memory is at 75%.
