@@ -775,6 +775,54 @@ int dora_pl_policy_loss(const float* scores, const int32_t* cu, int32_t batch, i
                         size_t workspace_bytes, int32_t* status, dora_stream_t stream);
 
 /*
+ * dora_token_logprob -- what a rollout takes down of its actions: the
+ * log-probability of a given token a_r in every row, the entropy, and the `top`
+ * most probable tokens.  With z the legal logits of row r (its first n_r),
+ * y = z / temperature, m the largest z:
+ *   logp = y_a - log sum_j exp y_j,   entropy = -sum_j p_j log p_j,
+ *   norm = (m, log sum_j exp((z_j - m) / temperature)).
+ * logits, dtype, rows, classes, ld, legal as in dora_policy_loss.
+ * tokens     nullable int32 [rows]; a row whose token is negative takes no part:
+ *            its logits are not read, its outputs are 0, its alternatives (-inf,
+ *            -1).  NULL: there are no tokens (logp is NULL too), all rows take
+ *            part but those with n_r = 0.  A token at or past n_r, or n_r outside
+ *            [0, classes], gives NaN outputs (alternatives NaN, -1) and
+ *            DORA_ERR_DEVICE_BAD_COUNT.
+ * temperature  finite and above 0, as is one over it.
+ * top        alternatives for every row, 0 to 32: top_logp fp32 and top_tokens
+ *            int32 [rows, top], most probable first, equal logits by the lower
+ *            index (-0 equals 0).  Logits of -inf are no alternatives; where a row
+ *            has fewer than `top`, the rest is (-inf, -1).
+ * logp fp32 [rows]; entropy nullable fp32 [rows]; norm nullable fp32 [rows, 2].
+ * A token of logit -inf has logp -inf.  NaN, +inf, or a row of -inf alone make a
+ * row's outputs NaN (alternatives NaN, -1).  fp32 statistics; same inputs, same
+ * bits.
+ */
+int dora_token_logprob(const void* logits, int32_t dtype, int32_t rows, int32_t classes,
+                       int64_t ld, const int32_t* legal, const int32_t* tokens,
+                       float temperature, int32_t top, float* logp, float* entropy, float* norm,
+                       float* top_logp, int32_t* top_tokens, int32_t* status,
+                       dora_stream_t stream);
+
+/*
+ * dora_token_logprob_grad -- d loss / d logits of a loss of the caller's own, from
+ * dlogp = d loss / d logp and dentropy = d loss / d entropy (fp32 [rows], one of
+ * them may be NULL), in one pass over the logits:
+ *   grad_j = [dlogp (1(j = a) - p_j) - dentropy p_j (log p_j + entropy)] / temperature.
+ * logits ... temperature as in the forward, whose norm and (with dentropy) entropy it
+ * takes; tokens may be NULL without dlogp.  norm is 8-byte aligned.
+ * grad       out [rows, ld] of `dtype`: columns [0, classes) are written, 0 past
+ *            n_r and in rows that take no part, NaN in those that are not valid;
+ *            grad == logits is allowed.
+ * fp32, rounded once.
+ */
+int dora_token_logprob_grad(const void* logits, int32_t dtype, int32_t rows, int32_t classes,
+                            int64_t ld, const int32_t* legal, const int32_t* tokens,
+                            float temperature, const float* norm, const float* entropy,
+                            const float* dlogp, const float* dentropy, void* grad,
+                            int32_t* status, dora_stream_t stream);
+
+/*
  * A list of tensors that are updated together.  dora_param (host): one
  * contiguous tensor of n elements, its gradient (grad_dtype), and, nullable,
  *   clipped     where dora_clip_grads writes (grad_dtype; NULL = in place);

@@ -745,3 +745,55 @@ def adam_step(p: np.ndarray, m: np.ndarray, v: np.ndarray, grad: np.ndarray, ste
     v = beta2 * v + (1 - beta2) * d * d
     mh, vh = m / (1 - beta1 ** step), v / (1 - beta2 ** step)
     return p * (1 - lr * decay) - lr * mh / (np.sqrt(vh) + eps), m, v
+
+
+def token_logprob(logits: np.ndarray, tokens=None, legal=None, temperature: float = 1.0,
+                  top: int = 0) -> dict:
+    """Log-probabilities of tokens [R] under softmax(logits / temperature) over the
+    first legal[r] logits, entropies, norm = (largest logit, log of the sum over
+    it) and the `top` most probable tokens, equal logits by the lower index,
+    logits of -inf left out (-inf, -1).  Rows of a negative token, or without
+    legal logits, take no part."""
+    rows, classes = logits.shape
+    out = {"logp": np.zeros(rows), "entropy": np.zeros(rows), "norm": np.zeros((rows, 2)),
+           "top_logp": np.full((rows, top), -np.inf),
+           "top_tokens": np.full((rows, top), -1, dtype=np.int64)}
+    for r in range(rows):
+        n = classes if legal is None else int(legal[r])
+        if n == 0 or (tokens is not None and tokens[r] < 0):
+            continue
+        z = np.asarray(logits[r, :n], dtype=np.float64)
+        y = (z - z.max()) / temperature         # a sum next to 0, also of huge logits
+        with np.errstate(divide="ignore"):
+            lq = y - _logsumexp(y)
+        p = np.exp(lq)
+        out["entropy"][r] = -np.where(p > 0, p * np.where(p > 0, lq, 0.0), 0.0).sum()
+        out["norm"][r] = z.max(), _logsumexp(y)
+        if tokens is not None:
+            out["logp"][r] = lq[tokens[r]]
+        best = [j for j in np.lexsort((np.arange(n), -z))[:top] if z[j] > -np.inf]
+        out["top_logp"][r, :len(best)], out["top_tokens"][r, :len(best)] = lq[best], best
+    return out
+
+
+def token_logprob_grad(logits: np.ndarray, tokens=None, dlogp=None, dentropy=None, legal=None,
+                       temperature: float = 1.0) -> np.ndarray:
+    """d loss / d logits from d loss / d logp and d loss / d entropy [R]."""
+    f = token_logprob(logits, tokens, legal, temperature)
+    grad = np.zeros(logits.shape)
+    for r in range(logits.shape[0]):
+        n = logits.shape[1] if legal is None else int(legal[r])
+        if n == 0 or (tokens is not None and tokens[r] < 0):
+            continue
+        z = np.asarray(logits[r, :n], dtype=np.float64)
+        y = (z - z.max()) / temperature
+        with np.errstate(divide="ignore"):
+            lq = y - _logsumexp(y)
+        p = np.exp(lq)
+        if dlogp is not None:
+            grad[r, :n] -= dlogp[r] * p
+            grad[r, tokens[r]] += dlogp[r]
+        if dentropy is not None:
+            grad[r, :n] -= dentropy[r] * np.where(p > 0, p * (np.where(p > 0, lq, 0.0) +
+                                                              f["entropy"][r]), 0.0)
+    return grad / temperature

@@ -27,7 +27,7 @@ __all__ = [
     "dora_classifier_head", "dora_classifier_head_lc1", "dora_fold_layerscale",
     "dora_pl_sample", "dora_pl_logprob", "dora_branch", "dora_kd_cost", "dora_step_rewards",
     "dora_policy_loss", "dora_pl_policy_loss", "dora_policy_workspace_size",
-    "alloc_policy_workspace", "ParamList", "dora_grad_norm", "dora_clip_grads",
+    "alloc_policy_workspace", "dora_token_logprob", "dora_token_logprob_grad", "ParamList", "dora_grad_norm", "dora_clip_grads",
     "dora_adam_step", "dora_adam_init", "alloc_adam_state",
 ]
 
@@ -110,6 +110,10 @@ _SIGS = {
     "dora_pl_policy_loss": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp,
                                            _vp, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _sz,
                                            _vp, _vp]),
+    "dora_token_logprob": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _f32, _i32, _vp,
+                                          _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dora_token_logprob_grad": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _f32, _vp,
+                                               _vp, _vp, _vp, _vp, _vp, _vp]),
     "dora_param_list_size": (_sz, [_vp, _i32]),
     "dora_param_list_prepare": (ctypes.c_int, [_vp, _i32, _vp, _sz, _vp, _vp]),
     "dora_grad_norm": (ctypes.c_int, [_vp, _f32, _vp, _vp]),
@@ -987,6 +991,82 @@ def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, worksp
     if code:
         _check(code, "dora_pl_policy_loss")
     return logp
+
+
+def _logit_rows(logits, classes):
+    """(data pointer, type, rows, classes, row stride) of a 2-D tensor of logits whose rows are
+    contiguous."""
+    dt = _DTYPES.get(logits.dtype) if isinstance(logits, _Tensor) and logits.is_cuda else None
+    if dt is None or logits.dim() != 2:
+        raise TypeError("logits must be a 2-D CUDA tensor of bf16, fp16 or fp32")
+    rows, cols = logits.shape
+    ld = logits.stride(0) if rows > 1 else cols
+    if (cols > 1 and logits.stride(1) != 1) or ld < cols:
+        raise TypeError("the rows of logits must be contiguous and not overlap")
+    classes = cols if classes is None else int(classes)
+    if not 1 <= classes <= cols:
+        raise ValueError("classes must be in [1, logits.shape[1]]")
+    _in_32_bits(rows, classes)
+    return logits.data_ptr(), dt, rows, classes, ld
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors must be on one device")
+
+
+def dora_token_logprob(logits, tokens, logp, classes=None, legal=None, temperature=1.0,
+                       entropy=None, norm=None, top_logp=None, top_tokens=None, status=None,
+                       stream=None):
+    """Log-probabilities logp (fp32 [R]) of ``tokens`` (int32 [R], negative: the row takes no
+    part; both None: no tokens) under softmax(logits / temperature), and, where given, the
+    entropies and ``norm`` (fp32 [R], [R, 2]: the largest logit and the log of the sum over it)
+    and the most probable tokens top_logp fp32 and top_tokens int32 [R, k], k up to 32.
+    ``logits``, ``classes`` and ``legal`` as in dora_policy_loss."""
+    at, dt, rows, classes, ld = _logit_rows(logits, classes)
+    top = 0
+    if (top_logp is None) != (top_tokens is None) or (tokens is None) != (logp is None):
+        raise ValueError("top_logp and top_tokens, and tokens and logp, are given together")
+    if top_logp is not None:
+        if top_logp.dim() != 2 or top_logp.size(0) != rows or top_tokens.shape != top_logp.shape:
+            raise ValueError("top_logp and top_tokens must be [R, k]")
+        top = top_logp.size(1)
+    _same_device(logits, tokens, logp, legal, entropy, norm, top_logp, top_tokens, status)
+    code = load_library().dora_token_logprob(
+        at, dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
+        _vec_opt(tokens, _I32, rows, "tokens"), temperature, top,
+        _vec_opt(logp, _F32, rows, "logp"), _vec_opt(entropy, _F32, rows, "entropy"),
+        _vec_opt(norm, _F32, 2 * rows, "norm"), _opt(top_logp, _F32, "top_logp"),
+        _opt(top_tokens, _I32, "top_tokens"), _opt(status, _I32, "status"), _stream(stream))
+    if code:
+        _check(code, "dora_token_logprob")
+    return logp
+
+
+def dora_token_logprob_grad(logits, tokens, norm, grad, dlogp=None, dentropy=None, entropy=None,
+                            classes=None, legal=None, temperature=1.0, status=None, stream=None):
+    """d loss / d logits into ``grad`` (like logits, or logits itself) from dlogp and dentropy
+    (fp32 [R], one of them may be None), with the forward's norm and, for dentropy, entropy."""
+    at, dt, rows, classes, ld = _logit_rows(logits, classes)
+    if grad is not logits and not (
+            isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
+            grad.shape == logits.shape and (grad.stride(0) == ld or rows <= 1) and
+            (grad.stride(1) == 1 or grad.size(1) == 1)):
+        raise TypeError("grad must be like logits: device, type, shape and strides")
+    if (dlogp is None and dentropy is None) or (dlogp is not None and tokens is None) or (
+            dentropy is not None and entropy is None):
+        raise ValueError("dlogp, which needs tokens, or dentropy, which needs entropy, is required")
+    _same_device(logits, tokens, norm, grad, dlogp, dentropy, entropy, legal, status)
+    code = load_library().dora_token_logprob_grad(
+        at, dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
+        _vec_opt(tokens, _I32, rows, "tokens"), temperature, _vec(norm, _F32, 2 * rows, "norm"),
+        _vec_opt(entropy, _F32, rows, "entropy"), _vec_opt(dlogp, _F32, rows, "dlogp"),
+        _vec_opt(dentropy, _F32, rows, "dentropy"), grad.data_ptr(), _opt(status, _I32, "status"),
+        _stream(stream))
+    if code:
+        _check(code, "dora_token_logprob_grad")
+    return grad
 
 
 class _ParamC(ctypes.Structure):
