@@ -897,6 +897,77 @@ int dora_adam_init(void* state, int64_t step, double beta1, double beta2, dora_s
 int dora_adam_step(const dora_param_list* list, void* state, double lr, double beta1, double beta2,
                    double eps, double weight_decay, const float* clip, dora_stream_t stream);
 
+/*
+ * A list of matrices that are orthogonalised together.  dora_matrix (host): the
+ * gradient of a contiguous row-major matrix [rows, cols] (grad_dtype), and, nullable,
+ *   param, momentum  weights (param_dtype) and fp32 momentum of dora_muon_step, both
+ *                    or none;
+ *   copy             bf16: the updated weights, rounded;
+ *   out              bf16: what dora_orthogonalize writes;
+ *   scale            of the matrix's update in dora_muon_step (e.g.
+ *                    sqrt(max(1, rows / cols)), or 0.2 sqrt(max(rows, cols)) for
+ *                    updates as large as Adam's).
+ * The shorter side is at most 16384, the longer 2^24.  Pointers are aligned to their
+ * elements; 16-byte alignment is faster.  No two buffers overlap.
+ * dora_matrix_list_prepare writes the list into `data` (device,
+ * dora_matrix_list_size bytes, 256-byte aligned) and fills the host handle *list, which
+ * the calls below take; done once for a set of buffers.  The list's memory also holds the
+ * iterations' matrices (about 6 bytes an element, 4 for the square of the shorter side):
+ * calls on one list, captured ones that are replayed among them, are ordered on one
+ * stream.  dora_matrix_list_size is 0 for arguments that prepare refuses.
+ */
+typedef struct dora_matrix {
+  const void* grad;
+  void* param;
+  float* momentum;
+  dora_bf16* copy;
+  dora_bf16* out;
+  int32_t rows, cols;
+  int32_t grad_dtype, param_dtype;
+  float scale;
+} dora_matrix;
+typedef struct dora_matrix_list {
+  void* data;
+  int64_t chunks, x_tiles, symmetric, outputs, tiles, diagonals;
+  int32_t count;
+  int32_t has_params;   /* 1: every matrix has param and momentum */
+  int32_t has_outs;     /* 1: every matrix has out */
+  int32_t pad;
+  uint64_t map[16];
+} dora_matrix_list;
+size_t dora_matrix_list_size(const dora_matrix* matrices, int32_t count);
+int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* data, size_t bytes,
+                             dora_matrix_list* list, dora_stream_t stream);
+
+/*
+ * dora_orthogonalize -- out = NS(grad) of every matrix of the list: with X = grad over
+ * its Frobenius norm (its transpose where rows > cols), `steps` (1 to 32) times
+ *   A = X X^T,   X <- 3.4445 X + (-4.7750 A + 2.0315 A^2) X,
+ * which brings all singular values near 1 (five steps: those above a hundredth of
+ * the norm to 0.7 .. 1.2).  A matrix of zeros stays one; one that holds a value that is
+ * not finite becomes NaN.  fp16 products added in fp32, X carried in 22 bits: 1.2e-3 off
+ * at most (2-norm), less than the rounding of `out`.  Same inputs, same bits.
+ * status     nullable device int32: DORA_ERR_TIMEOUT should a bounded wait run out,
+ *            which leaves `out` unfinished.
+ */
+int dora_orthogonalize(const dora_matrix_list* list, int32_t steps, int32_t* status,
+                       dora_stream_t stream);
+
+/*
+ * dora_muon_step -- one Muon step on every matrix of the list: with d = f grad, mu the
+ * momentum,
+ *   momentum  m <- mu m + (1 - mu) d
+ *   update    u = (1 - mu) d + mu m (nesterov != 0), or m
+ *   param     p <- p (1 - lr weight_decay) - lr scale NS(u)
+ * NS as in dora_orthogonalize, mu in [0, 1).  clip nullable: the norm fp32 [2] of
+ * dora_grad_norm; f = clip[1], and a norm that is not finite skips the step (nothing
+ * changes).  NULL: f = 1.  A wait that runs out (status) leaves the weights of the
+ * matrices concerned as they were, or partly updated.
+ */
+int dora_muon_step(const dora_matrix_list* list, double lr, double momentum, int32_t nesterov,
+                   double weight_decay, int32_t steps, const float* clip, int32_t* status,
+                   dora_stream_t stream);
+
 /* Synchronises the current device and copies the status word at `status_dev`
  * (a device int32, e.g. dora_workspace_status(ws)) to *code.  Test/debug
  * only: it blocks the host. */

@@ -797,3 +797,34 @@ def token_logprob_grad(logits: np.ndarray, tokens=None, dlogp=None, dentropy=Non
             grad[r, :n] -= dentropy[r] * np.where(p > 0, p * (np.where(p > 0, lq, 0.0) +
                                                               f["entropy"][r]), 0.0)
     return grad / temperature
+
+
+NS_COEF = (3.4445, -4.7750, 2.0315)
+
+
+def newton_schulz(u: np.ndarray, steps: int = 5) -> np.ndarray:
+    """X = u / |u|_F, then `steps` times X <- a X + (b A + c A^2) X with A = X X^T (on the
+    transpose of a tall matrix); a matrix of zeros stays one."""
+    x = np.asarray(u, dtype=np.float64)
+    if x.shape[0] > x.shape[1]:
+        return newton_schulz(x.T, steps).T
+    peak = np.abs(x).max()
+    if peak == 0:
+        return x
+    x = x / peak
+    x = x / np.sqrt((x * x).sum())
+    a, b, c = NS_COEF
+    for _ in range(steps):
+        gram = x @ x.T
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x
+
+
+def muon_step(p: np.ndarray, m: np.ndarray, grad: np.ndarray, lr: float, mu: float,
+              nesterov: bool, decay: float, scale: float, steps: int = 5,
+              factor: float = 1.0) -> tuple:
+    """(p, m) after one Muon step on factor * grad, with decoupled weight decay."""
+    d = factor * grad
+    m = mu * m + (1 - mu) * d
+    u = (1 - mu) * d + mu * m if nesterov else m
+    return p * (1 - lr * decay) - lr * scale * newton_schulz(u, steps), m

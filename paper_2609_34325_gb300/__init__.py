@@ -28,7 +28,8 @@ __all__ = [
     "dora_pl_sample", "dora_pl_logprob", "dora_branch", "dora_kd_cost", "dora_step_rewards",
     "dora_policy_loss", "dora_pl_policy_loss", "dora_policy_workspace_size",
     "alloc_policy_workspace", "dora_token_logprob", "dora_token_logprob_grad", "ParamList", "dora_grad_norm", "dora_clip_grads",
-    "dora_adam_step", "dora_adam_init", "alloc_adam_state",
+    "dora_adam_step", "dora_adam_init", "alloc_adam_state", "MatrixList", "dora_orthogonalize",
+    "dora_muon_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -121,6 +122,10 @@ _SIGS = {
     "dora_adam_state_size": (_sz, []),
     "dora_adam_init": (ctypes.c_int, [_vp, _i64, _f64, _f64, _vp]),
     "dora_adam_step": (ctypes.c_int, [_vp, _vp, _f64, _f64, _f64, _f64, _f64, _vp, _vp]),
+    "dora_matrix_list_size": (_sz, [_vp, _i32]),
+    "dora_matrix_list_prepare": (ctypes.c_int, [_vp, _i32, _vp, _sz, _vp, _vp]),
+    "dora_orthogonalize": (ctypes.c_int, [_vp, _i32, _vp, _vp]),
+    "dora_muon_step": (ctypes.c_int, [_vp, _f64, _f64, _i32, _f64, _i32, _vp, _vp, _vp]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -1213,3 +1218,116 @@ def dora_adam_step(plist, state, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_de
                                          _opt(clip, _F32, "clip"), _stream(stream))
     if code:
         _check(code, "dora_adam_step")
+
+
+class _MatrixC(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("grad", "param", "momentum", "copy", "out")] + [
+        (n, _i32) for n in ("rows", "cols", "grad_dtype", "param_dtype")] + [("scale", _f32)]
+
+
+class _MatrixListC(ctypes.Structure):
+    _fields_ = [("data", _vp)] + [(n, _i64) for n in ("chunks", "x_tiles", "symmetric", "outputs",
+                                                      "tiles", "diagonals")] + [
+        (n, _i32) for n in ("count", "has_params", "has_outs", "pad")] + [
+        ("map", ctypes.c_uint64 * 16)]
+
+
+class MatrixList:
+    """Matrices that are orthogonalised together, laid out on the device once
+    (dora_matrix_list_prepare): gradients (2-D, contiguous, bf16, fp16 or fp32) and, each a list
+    of as many tensors or None, ``params`` (bf16, fp16 or fp32) with ``momentum`` (fp32), bf16
+    ``copies`` of the updated weights, and bf16 ``outs`` (of dora_orthogonalize).  ``scales``:
+    a factor for every matrix's update in dora_muon_step (sqrt(max(1, rows / cols)) by
+    default).  Matrices that lie in one tensor, such as queries, keys and values, are given as
+    views of their own.  The tensors are kept alive here; make a new list when any of them
+    moves.  The list holds the iterations' matrices too, about 6 bytes an element, and calls on
+    it are ordered on one stream, ``stream`` (the current one by default)."""
+
+    def __init__(self, grads, params=None, momentum=None, copies=None, outs=None, scales=None,
+                 stream=None):
+        self.grads = list(grads)
+        n = len(self.grads)
+        if n == 0:
+            raise ValueError("a list needs at least one matrix")
+        if (params is None) != (momentum is None):
+            raise ValueError("params and momentum are given together")
+        if copies is not None and params is None:
+            raise ValueError("copies need params")
+        for name, ts in (("params", params), ("momentum", momentum), ("copies", copies),
+                         ("outs", outs), ("scales", scales)):
+            if ts is not None and len(ts) != n:
+                raise ValueError(f"{name} must have as many entries as grads")
+        g0 = self.grads[0]
+        device = g0.device if isinstance(g0, _Tensor) else None
+        columns = []
+        for name, ts, dtype in (("grads", self.grads, None), ("params", params, None),
+                                ("momentum", momentum, _F32), ("copies", copies, _BF16),
+                                ("outs", outs, _BF16)):
+            if ts is None:
+                setattr(self, name, None)
+                columns.append([0] * n)
+                continue
+            ts = list(ts)
+            setattr(self, name, ts)
+            for i, t in enumerate(ts):
+                if not (isinstance(t, _Tensor) and t.is_cuda and t.is_contiguous() and
+                        t.dim() == 2 and
+                        (t.dtype is dtype or (dtype is None and t.dtype in _DTYPES))):
+                    raise TypeError(f"{name}[{i}] must be a contiguous 2-D CUDA tensor of "
+                                    f"{dtype or 'bf16, fp16 or fp32'}")
+                if t.device != device:
+                    raise ValueError(f"{name}[{i}] must be on the device of grads[0]")
+                if t.shape != self.grads[i].shape:
+                    raise ValueError(f"{name}[{i}] must have the shape of grads[{i}]")
+            columns.append([t.data_ptr() for t in ts])
+        if scales is None:
+            scales = [max(1.0, t.size(0) / max(1, t.size(1))) ** 0.5 for t in self.grads]
+        self.scales = [float(x) for x in scales]
+        c = (_MatrixC * n)()
+        for at, t, scale, row in zip(c, self.grads, self.scales, zip(*columns)):
+            _in_32_bits(*t.shape)
+            (at.grad, at.param, at.momentum, at.copy, at.out) = row
+            at.rows, at.cols, at.scale = t.size(0), t.size(1), scale
+            at.grad_dtype = _DTYPES[t.dtype]
+        for at, t in zip(c, self.params or ()):
+            at.param_dtype = _DTYPES[t.dtype]
+        size = int(load_library().dora_matrix_list_size(c, n))
+        if size == 0:
+            raise ValueError("a matrix is empty, larger than 16384 x 2^24, or its scale is not "
+                             "finite")
+        self.data = _bytes_on(size, device, stream)
+        self.c = _MatrixListC()
+        self.ref = ctypes.byref(self.c)
+        _check(load_library().dora_matrix_list_prepare(c, n, _ptr(self.data), size, self.ref,
+                                                       _stream(stream)),
+               "dora_matrix_list_prepare")
+
+
+def _matrices(mlist):
+    if not isinstance(mlist, MatrixList):
+        raise TypeError("a MatrixList is required")
+    return mlist.ref
+
+
+def dora_orthogonalize(mlist, steps=5, status=None, stream=None):
+    """The list's ``outs`` from its gradients: Newton-Schulz iterations that bring every
+    matrix's singular values near 1."""
+    code = load_library().dora_orthogonalize(_matrices(mlist), int(steps),
+                                             _opt(status, _I32, "status"), _stream(stream))
+    if code:
+        _check(code, "dora_orthogonalize")
+    return mlist.outs
+
+
+def dora_muon_step(mlist, lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, clip=None,
+                   status=None, stream=None):
+    """One Muon step (decoupled weight decay) on every matrix of the list; with ``clip``, the
+    norm of dora_grad_norm, on the clipped gradients, and no step at all when that norm is not
+    finite."""
+    if clip is not None and clip.numel() < 2:
+        raise ValueError("clip must hold 2 floats")
+    code = load_library().dora_muon_step(_matrices(mlist), lr, momentum, int(bool(nesterov)),
+                                         weight_decay, int(steps), _opt(clip, _F32, "clip"),
+                                         _opt(status, _I32, "status"), _stream(stream))
+    if code:
+        _check(code, "dora_muon_step")

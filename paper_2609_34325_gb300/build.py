@@ -26,7 +26,7 @@ TIMEOUT_TEST_FLAGS = ["-DDORA_TEST_WITHHOLD_KV_LOAD", "-DDORA_TEST_WITHHOLD_ROW_
                       "-DDORA_TEST_WAIT_LIMIT_NS=5000000ull"]
 SOURCES = ["token_ops.cu", "gemm_tcgen05.cu", "attn_tcgen05.cu", "api.cu", "noalloc.cu",
            "actor.cu", "actor_front.cu", "actor_tail.cu", "embed_head.cu", "training.cu",
-           "policy.cu", "logprob.cu", "optim.cu"]
+           "policy.cu", "logprob.cu", "optim.cu", "ortho.cu"]
 # the translation units rebuilt with the test flags for the timeout-path library
 TIMEOUT_TEST_SOURCES = ("attn_tcgen05.cu", "policy.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
