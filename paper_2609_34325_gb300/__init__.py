@@ -1229,7 +1229,7 @@ class _MatrixListC(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(n, _i64) for n in ("chunks", "x_tiles", "symmetric", "outputs",
                                                       "tiles", "diagonals")] + [
         (n, _i32) for n in ("count", "has_params", "has_outs", "pad")] + [
-        ("map", ctypes.c_uint64 * 16)]
+        ("map", ctypes.c_uint64 * 48)]
 
 
 class MatrixList:

@@ -47,9 +47,11 @@ constexpr float kLoScale = 2048.f;        // of lo, on top of it
 constexpr int kMaxSteps = 32;
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
-constexpr int kChunk = 8192;              // elements of a matrix that a CTA takes at once
-constexpr int kRowThreads = 256;
+constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
+constexpr int kRowThreads = 256, kRowCtas = 4;
 constexpr int kMaxShort = 16384, kMaxLong = 1 << 24;
+
+struct Squares;
 
 struct Entry {
   const void* grad;
@@ -59,11 +61,12 @@ struct Entry {
   int32_t rows, cols, grad_type, param_type;
   float scale;
   int32_t m, n, tall;                     // X is m x n; tall: X = U^T
-  int32_t mb, nb;                         // blocks of 128 rows, of 128 columns
+  int32_t mb, nb;                         // blocks of 128 rows, of 128 columns; X, F and G
+                                          // have an even number of the first
   int64_t x[2], lo, f, g;                 // first tiles of X hi (two, in turn), X lo, F, G
-  float *d, *e;                           // the diagonals of A and B [128 mb]
-  float2* partial;                        // of its chunks: sum of squares and exponent
-  float2* norm;                           // one over the norm of u 2^-k, and 2^-k's exponent
+  float *d, *e;                           // the diagonals of A and B
+  Squares* partial;                       // of its chunks
+  float2* norm;                           // one over the norm of u 2^-k, and 2^-k
   unsigned* ticket;                       // chunks done; zero between calls
   int32_t chunks, pad;
   // first of its chunks, of its tiles of X and of its output tiles among the list's
@@ -75,9 +78,9 @@ struct Header {
   int pad[63];
 };
 
-// One piece of work: block row and block column of a matrix.
+// One piece of work: block row and block column of a matrix, and its columns.
 struct Tile {
-  int32_t matrix, i, j, pad;
+  int32_t matrix, i, j, width;
 };
 
 struct List {
@@ -126,17 +129,19 @@ __global__ void fill_tiles_kernel(List list) {
   }
   if (t < list.n_all) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_all; });
-    const int at = static_cast<int>(t - list.entries[q].first_all), w = list.entries[q].nb;
-    list.all[t] = Tile{q, at / w, at % w, 0};
+    const int at = static_cast<int>(t - list.entries[q].first_all), nb = list.entries[q].nb;
+    const int w = (nb + 1) / 2, j = at % w;
+    list.all[t] = Tile{q, at / w, j, 2 * j + 1 < nb ? 256 : 128};
   }
   if (t < list.n_sym) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_sym; });
-    int at = static_cast<int>(t - list.entries[q].first_sym), i = 0, left = list.entries[q].mb;
+    const int mb = list.entries[q].mb;
+    int at = static_cast<int>(t - list.entries[q].first_sym), i = 0, left = (mb + 1) / 2;
     while (at >= left) {
       at -= left--;
       ++i;
     }
-    list.sym[t] = Tile{q, i, i + at, 0};
+    list.sym[t] = Tile{q, i, i + at, 2 * (i + at) + 1 < mb ? 256 : 128};
   }
 }
 
@@ -150,6 +155,41 @@ __device__ __forceinline__ void store_one(float v, void* p, int type, int64_t i)
   if (type == DORA_F32) static_cast<float*>(p)[i] = v;
   else if (type == DORA_BF16) from_float(v, static_cast<__nv_bfloat16*>(p) + i);
   else from_float(v, static_cast<__half*>(p) + i);
+}
+
+// Four elements from the k-th, zeros past the last: 16 bytes of fp32, 8 (in x and y) of the
+// others, at once where `quads` says that they are aligned to that.
+__device__ __forceinline__ bool in_quads(const void* p, int type) {
+  return (reinterpret_cast<uintptr_t>(p) & (4 * size_of(type) - 1)) == 0;
+}
+__device__ __forceinline__ uint4 whole_quad(const void* p, int type, int64_t k) {
+  if (type == DORA_F32) return *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + k);
+  const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + k);
+  return make_uint4(q.x, q.y, 0u, 0u);
+}
+__device__ __forceinline__ uint4 load_quad(const void* p, int type, int64_t k, int64_t total,
+                                           bool quads) {
+  if (quads && k + 4 <= total) return whole_quad(p, type, k);
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  if (type == DORA_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (k + j < total) w[j] = static_cast<const uint32_t*>(p)[k + j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (k + j < total)
+        w[j >> 1] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[k + j]) << (16 * (j & 1));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void unpack_quad(uint4 q, int type, float* v) {
+  float w[8];
+  if (type == DORA_F32) Granule<float>::unpack(q, w);
+  else if (type == DORA_BF16) Granule<__nv_bfloat16>::unpack(q, w);
+  else Granule<__half>::unpack(q, w);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = w[j];
 }
 
 // What all kernels of a call take.
@@ -176,87 +216,138 @@ __device__ __forceinline__ float update_of(const Args& a, float d, float m) {
 }
 
 // ---------------------------------------------------------------------------
-// Momentum, and the update's norm.  Squares are summed of u 2^-k with k the exponent of the
-// chunk's largest |u|, so that no finite update overflows or vanishes; the chunks are joined
-// in their order by the CTA that is last of the matrix.
+// Momentum, and the update's norm.  A CTA takes a run of chunks, a matrix's one after the
+// other.  A thread sums its squares in fp32; where that leaves the middle of the range, it sums
+// those of u 2^-k, with k the exponent of its largest |u|, so that no finite update
+// overflows or vanishes.  The chunks are joined in their order by the CTA that is last
+// of the matrix.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float block_reduce(float v, bool largest, float* scratch) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const float o = __shfl_xor_sync(0xffffffffu, v, off);
-    v = largest ? fmaxf(v, o) : v + o;
+// A sum of squares of values times 2^-k.
+struct Squares {
+  float sum;
+  int k;
+  __device__ __forceinline__ void add(Squares o) {
+    if (o.k == k) {
+      sum += o.sum;
+    } else if (o.sum != 0.f) {
+      const int most = k > o.k ? k : o.k;
+      sum = ldexpf(sum, 2 * (k - most)) + ldexpf(o.sum, 2 * (o.k - most));
+      k = most;
+    }
   }
-  __syncthreads();                        // the places are free
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = scratch[0];
+};
+__device__ __forceinline__ Squares warp_squares(Squares s) {
 #pragma unroll
-  for (int w = 1; w < kRowThreads / 32; ++w) v = largest ? fmaxf(v, scratch[w]) : v + scratch[w];
-  return v;
+  for (int off = 16; off > 0; off >>= 1)
+    s.add(Squares{__shfl_xor_sync(0xffffffffu, s.sum, off),
+                  __shfl_xor_sync(0xffffffffu, s.k, off)});
+  return s;
+}
+// Over the block, in thread 0.
+__device__ __forceinline__ Squares block_squares(Squares s, Squares* scratch) {
+  s = warp_squares(s);
+  __syncthreads();                        // the places are free
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int w = 1; w < kRowThreads / 32; ++w) s.add(scratch[w]);
+  return s;
 }
 
-// The exponent by which values up to `top` are brought near 1.
-__device__ __forceinline__ int exponent_of(float top) {
-  const int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;   // top >= 0
-  return e < -126 ? -126 : (e > 127 ? 127 : e);
+template <int kN>
+__device__ __forceinline__ Squares squares_of(const float (&u)[kN]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) sum = fmaf(u[i], u[i], sum);
+  if (sum > 1e-25f && sum < 1e30f) return {sum, 0};
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) top = fmaxf(top, fabsf(u[i]));
+  int k = static_cast<int>(__float_as_uint(top) >> 23) - 127;
+  k = k < -126 ? -126 : (k > 126 ? 126 : k);
+  const float scale = __uint_as_float(static_cast<uint32_t>(127 - k) << 23);   // 2^-k
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) sum = fmaf(u[i] * scale, u[i] * scale, sum);
+  return {sum, k};
 }
 
-__global__ void __launch_bounds__(kRowThreads) momentum_kernel(List list, Args a) {
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) momentum_kernel(List list, Args a) {
   constexpr int kPer = kChunk / kRowThreads;
-  __shared__ float scratch[kRowThreads / 32];
+  __shared__ Squares scratch[kRowThreads / 32];
   __shared__ bool last;
   pdl_wait();
   if (skipped(a)) return;
   const float f = factor(a);
   if (blockIdx.x == 0 && threadIdx.x == 0) list.header->abort = 0;
-  for (int c = blockIdx.x; c < list.n_chunks; c += gridDim.x) {
-    const Entry& e = list.entries[list.chunk_of[c]];
-    const int at = static_cast<int>(c - e.first_chunk);
-    const int64_t total = static_cast<int64_t>(e.rows) * e.cols;
-    const int64_t from = static_cast<int64_t>(at) * kChunk;
-    float u[kPer], top = 0.f;
+  int c = static_cast<int>(static_cast<int64_t>(list.n_chunks) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<int64_t>(list.n_chunks) * (blockIdx.x + 1) /
+                                   gridDim.x);
+  const Entry* at = list.entries + (c < end ? list.chunk_of[c] : 0);
+  for (; c < end; ++c) {
+    if (c - at->first_chunk >= at->chunks) ++at;
+    const Entry& e = *at;
+    const int64_t total = static_cast<int64_t>(e.m) * e.n;
+    const int64_t from = static_cast<int64_t>(c - e.first_chunk) * kChunk;
+    // quads of elements, all on their way before the first is looked at
+    const bool quads = in_quads(e.grad, e.grad_type) && (!a.muon || in_quads(e.momentum, DORA_F32));
+    uint4 qg[kPer / 4], qm[kPer / 4];
+    if (quads && from + kChunk <= total) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int64_t k = from + threadIdx.x + i * kRowThreads;
-      u[i] = 0.f;
-      if (k < total) {
-        const float d = load_one(e.grad, e.grad_type, k) * f;
-        float m = 0.f;
-        if (a.muon) {
-          m = fmaf(a.mu, e.momentum[k], a.omu * d);
-          e.momentum[k] = m;
-        }
-        u[i] = update_of(a, d, m);
-        top = fmaxf(top, fabsf(u[i]));
+      for (int i = 0; i < kPer / 4; ++i) {
+        const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
+        qg[i] = whole_quad(e.grad, e.grad_type, k);
+        qm[i] = a.muon ? whole_quad(e.momentum, DORA_F32, k) : make_uint4(0, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer / 4; ++i) {
+        const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
+        qg[i] = load_quad(e.grad, e.grad_type, k, total, quads);
+        qm[i] = a.muon ? load_quad(e.momentum, DORA_F32, k, total, quads) : make_uint4(0, 0, 0, 0);
       }
     }
-    const int k = exponent_of(block_reduce(top, true, scratch));
-    float sum = 0.f;
+    float u[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const float v = ldexpf(u[i], -k);
-      sum = fmaf(v, v, sum);
+    for (int i = 0; i < kPer / 4; ++i) {
+      const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
+      float d[4], m[4];
+      unpack_quad(qg[i], e.grad_type, d);
+      Granule<float>::unpack(qm[i], m);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        d[j] *= f;
+        if (a.muon) m[j] = fmaf(a.mu, m[j], a.omu * d[j]);
+        u[4 * i + j] = update_of(a, d[j], m[j]);
+      }
+      if (!a.muon) continue;
+      if (quads && k + 4 <= total) {
+        *reinterpret_cast<uint4*>(e.momentum + k) = Granule<float>::pack(m);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (k + j < total) e.momentum[k + j] = m[j];
+      }
     }
-    sum = block_reduce(sum, false, scratch);
+    const Squares sum = block_squares(squares_of(u), scratch);
     if (threadIdx.x == 0) {
-      e.partial[at] = make_float2(sum, static_cast<float>(k));
+      e.partial[c - e.first_chunk] = sum;
       last = take_ticket(e.ticket) == static_cast<unsigned>(e.chunks) - 1;
     }
     __syncthreads();
     if (!last) continue;
-    float most = -126.f;
-    for (int i = threadIdx.x; i < e.chunks; i += kRowThreads)
-      most = fmaxf(most, __ldcg(&e.partial[i]).y);
-    most = block_reduce(most, true, scratch);
-    float all = 0.f;
+    Squares all = {0.f, -126};
     for (int i = threadIdx.x; i < e.chunks; i += kRowThreads) {
-      const float2 p = __ldcg(&e.partial[i]);
-      all += ldexpf(p.x, 2 * static_cast<int>(p.y - most));
+      const int2 p = __ldcg(reinterpret_cast<const int2*>(&e.partial[i]));
+      all.add(Squares{__int_as_float(p.x), p.y});
     }
-    all = block_reduce(all, false, scratch);
+    all = block_squares(all, scratch);
     if (threadIdx.x == 0) {
       // a matrix of zeros stays one; one that is not finite becomes NaN
-      *e.norm = make_float2(all == 0.f ? 0.f : (isfinite(all) ? rsqrtf(all) : NAN), -most);
+      *e.norm = make_float2(
+          all.sum == 0.f ? 0.f : (isfinite(all.sum) ? 1.f / sqrtf(all.sum) : NAN),
+          __uint_as_float(static_cast<uint32_t>(127 - all.k) << 23));
       *e.ticket = 0;
     }
   }
@@ -275,6 +366,13 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b) {
   return Granule<__half>::pair(a, b);
 }
 
+// Eight values `step` apart, zeros from the some-th on.
+template <typename T>
+__device__ __forceinline__ void load_eight(const T* p, int64_t step, int some, float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = i < some ? to_float(p[i * step]) : 0.f;
+}
+
 // hi and lo of eight values that are scaled already.
 __device__ __forceinline__ void split(const float* v, uint4* hi, uint4* lo) {
   float rest[8], back[8];
@@ -285,62 +383,113 @@ __device__ __forceinline__ void split(const float* v, uint4* hi, uint4* lo) {
   *lo = Granule<__half>::pack(rest);
 }
 
-// The normalised update into its tiles, a tile a CTA.
-__global__ void __launch_bounds__(kRowThreads) normalise_kernel(List list, Args a) {
+// The normalised update into its tiles; a CTA takes a run of them.
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List list, Args a) {
   pdl_wait();
   if (skipped(a)) return;
   const float f = factor(a);
-  for (int t = blockIdx.x; t < list.n_x; t += gridDim.x) {
-    const Tile tile = list.x[t];
-    const Entry& e = list.entries[tile.matrix];
+  int t = static_cast<int>(static_cast<int64_t>(list.n_x) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<int64_t>(list.n_x) * (blockIdx.x + 1) / gridDim.x);
+  if (t >= end) return;
+  const Tile first = list.x[t];
+  int matrix = first.matrix, ti = first.i, tj = first.j;
+  for (; t < end; ++t) {
+    const Entry& e = list.entries[matrix];
     const float2 norm = *e.norm;
-    const int64_t at = static_cast<int64_t>(tile.i) * (2 * e.nb) + tile.j;
+    const int64_t at = static_cast<int64_t>(ti) * (2 * e.nb) + tj;
     char* hi = tile_at(list, e.x[0] + at);
     char* lo = tile_at(list, e.lo + at);
-    for (int w = threadIdx.x; w < kTileRows * 8; w += kRowThreads) {
-      // the lanes along what is contiguous in the matrix
-      const int r = e.tall ? w % kTileRows : w / 8, piece = e.tall ? w / kTileRows : w % 8;
-      const int row = tile.i * kTileRows + r, col = tile.j * kTileCols + piece * 8;
-      float v[8];
+    const bool quads = !e.tall && (e.n & 7) == 0 && in_quads(e.grad, e.grad_type) &&
+                       (!a.muon || in_quads(e.momentum, DORA_F32));
+    constexpr int kItems = kTileRows * 8 / kRowThreads, kSome = 2;
+    // pieces of eight columns, the lanes along what is contiguous in the matrix
+    for (int w0 = 0; w0 < kItems; w0 += kSome) {
+      float d[kSome][8], m[kSome][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = 0.f;
-        if (row < e.m && col + i < e.n) {
-          const int64_t k = e.tall ? static_cast<int64_t>(col + i) * e.m + row
-                                   : static_cast<int64_t>(row) * e.n + col + i;
-          const float d = load_one(e.grad, e.grad_type, k) * f;
-          const float u = update_of(a, d, a.muon ? e.momentum[k] : 0.f);
-          v[i] = ldexpf(u, static_cast<int>(norm.y)) * norm.x * kScale;
+      for (int y = 0; y < kSome; ++y) {
+        const int w = threadIdx.x + (w0 + y) * kRowThreads;
+        const int r = e.tall ? w % kTileRows : w / 8, piece = e.tall ? w / kTileRows : w % 8;
+        const int row = ti * kTileRows + r, col = tj * kTileCols + piece * 8;
+        const int some = row < e.m ? e.n - col : 0;     // columns that there are
+        const int64_t step = e.tall ? e.m : 1;
+        const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
+                                 : static_cast<int64_t>(row) * e.n + col;
+        if (quads && some >= 8) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 4) {
+            unpack_quad(whole_quad(e.grad, e.grad_type, k + i), e.grad_type, d[y] + i);
+            if (a.muon) Granule<float>::unpack(whole_quad(e.momentum, DORA_F32, k + i), m[y] + i);
+          }
+        } else if (e.grad_type == DORA_F32) {
+          load_eight(static_cast<const float*>(e.grad) + k, step, some, d[y]);
+        } else if (e.grad_type == DORA_BF16) {
+          load_eight(static_cast<const __nv_bfloat16*>(e.grad) + k, step, some, d[y]);
+        } else {
+          load_eight(static_cast<const __half*>(e.grad) + k, step, some, d[y]);
         }
+        if (a.muon && !(quads && some >= 8)) load_eight(e.momentum + k, step, some, m[y]);
       }
-      uint4 h, l;
-      split(v, &h, &l);
-      const uint32_t to = tile_offset(r, piece * 8);
-      *reinterpret_cast<uint4*>(hi + to) = h;
-      *reinterpret_cast<uint4*>(lo + to) = l;
+#pragma unroll
+      for (int y = 0; y < kSome; ++y) {
+        const int w = threadIdx.x + (w0 + y) * kRowThreads;
+        const int r = e.tall ? w % kTileRows : w / 8, piece = e.tall ? w / kTileRows : w % 8;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          v[i] = update_of(a, d[y][i] * f, a.muon ? m[y][i] : 0.f) * norm.y * norm.x * kScale;
+        uint4 h, l;
+        split(v, &h, &l);
+        const uint32_t to = tile_offset(r, piece * 8);
+        *reinterpret_cast<uint4*>(hi + to) = h;
+        *reinterpret_cast<uint4*>(lo + to) = l;
+      }
+    }
+    if (++tj == 2 * e.nb) {
+      tj = 0;
+      if (++ti == 2 * ((e.mb + 1) / 2)) {
+        ti = 0;
+        ++matrix;
+      }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// The products.  One persistent CTA an SM takes output tiles of 128 x 128: one warp copies
-// operands into a ring of stages, one issues the MMAs into one of two accumulators, four
-// read the other one and write what comes of it.
+// The products.  Persistent CTAs in pairs take output tiles of 256 rows and 256 or 128
+// columns: one MMA spans the pair, each CTA holding its 128 rows of the left operand and half
+// of the right one, so that a stage is 32 KB for each.  In a CTA one warp copies operands into
+// a ring of stages, one issues the MMAs (in the first CTA) into one of two accumulators, and
+// eight finish the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo)
+// comes by copies of its own into three places a warp, two of them ahead, and is written
+// over there and copied out.
 // ---------------------------------------------------------------------------
 enum Phase { kGram, kSquare, kApply, kLast };
 
-constexpr int kStages = 6;
-constexpr int kBlock = 128;               // of an output tile
+constexpr int kStages = 4;
+constexpr int kBlock = 128;               // rows of a CTA's part of an output tile
+constexpr int kWide = 256;                // columns of one
 constexpr int kK = 64;                    // of a stage
-constexpr int kThreads = 192;
-constexpr int kHalfTile = kTileBytes / 2; // 64 rows: what one copy brings
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kHalfTile = kTileBytes / 2; // 64 rows
+constexpr int kPlaces = 3;
+constexpr int kPiece = 32 * 32;           // values that a warp finishes at once
+constexpr uint16_t kPairMask = 0x3;
 
 struct Smem {
   uint8_t a[kStages][kTileBytes];
   uint8_t b[kStages][kTileBytes];
+  uint16_t piece[kEpiWarps][kPlaces][2][kPiece];
   uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+  uint64_t piece_full[kEpiWarps][kPlaces];
   uint32_t tmem;
   int abort, issued, consumed;
+};
+static_assert(sizeof(Smem) <= 227 * 1024, "shared memory");
+
+// The maps of all tiles: whole ones, their halves of 64 rows, and 32 x 32 values.
+struct Maps {
+  CUtensorMap tile, half, piece;
 };
 
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
@@ -348,105 +497,54 @@ __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) 
          (static_cast<uint32_t>(m >> 4) << 24);
 }
 
-// A row of 32 fp32 values of the accumulator at hand, with its place in the matrix.
-template <Phase kPhase>
-__device__ __forceinline__ void finish_row(const List& list, const Entry& e, const Args& a,
-                                           const Tile& t, int from, int r, int c,
-                                           const uint32_t (&acc)[32]) {
-  const int row = t.i * kBlock + r, col = t.j * kBlock + c;   // c: the first of 32 columns
-  if (kPhase == kGram || kPhase == kSquare) {
-    const int64_t first = kPhase == kGram ? e.f : e.g;
-    char* to = tile_at(list, first + static_cast<int64_t>(t.i) * 2 * e.mb + 2 * t.j + (c >> 6));
-    char* mirror = tile_at(list, first + static_cast<int64_t>(t.j) * 2 * e.mb + 2 * t.i + (r >> 6));
-    const char* f = kPhase == kSquare
-                        ? tile_at(list, e.f + static_cast<int64_t>(t.i) * 2 * e.mb + 2 * t.j +
-                                            (c >> 6))
-                        : nullptr;
-    const float di = kPhase == kSquare ? e.d[row] : 0.f;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      float v[8];
-      if constexpr (kPhase == kGram) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float x = __uint_as_float(acc[8 * p + i]);
-          if (row == col + 8 * p + i) e.d[row] = x * (1.f / (kScale * kScale));
-          v[i] = row == col + 8 * p + i ? 0.f : x * (1.f / kScale);
-        }
-      } else {
-        float off[8];
-        Granule<__half>::unpack(
-            *reinterpret_cast<const uint4*>(f + tile_offset(r, (c & 63) + 8 * p)), off);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float ff = __uint_as_float(acc[8 * p + i]) * (1.f / kScale);   // scaled once
-          const float dj = e.d[col + 8 * p + i];
-          v[i] = fmaf(kC, fmaf(di + dj, off[i], ff), kB * off[i]);
-          if (row == col + 8 * p + i) {
-            e.e[row] = fmaf(kC, fmaf(di, di, ff * (1.f / kScale)), kB * di);
-            v[i] = 0.f;
-          }
-        }
-      }
-      const uint4 q = Granule<__half>::pack(v);
-      *reinterpret_cast<uint4*>(to + tile_offset(r, (c & 63) + 8 * p)) = q;
-      if (t.i != t.j) {
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *reinterpret_cast<uint16_t*>(mirror + tile_offset(c + 8 * p + i, r & 63)) =
-              static_cast<uint16_t>(w[i >> 1] >> (16 * (i & 1)));
-      }
-    }
-    return;
-  }
-  const int64_t at = static_cast<int64_t>(t.i) * (2 * e.nb) + 2 * t.j + (c >> 6);
-  const char* hi = tile_at(list, e.x[from] + at);
-  char* lo = tile_at(list, e.lo + at);
-  char* to = tile_at(list, e.x[from ^ 1] + at);
-  const float ae = kA + e.e[row];
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const uint32_t o = tile_offset(r, (c & 63) + 8 * p);
-    float h[8], l[8], v[8];
-    Granule<__half>::unpack(*reinterpret_cast<const uint4*>(hi + o), h);
-    Granule<__half>::unpack(*reinterpret_cast<const uint4*>(lo + o), l);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      v[i] = fmaf(ae, fmaf(l[i], 1.f / kLoScale, h[i]),
-                  __uint_as_float(acc[8 * p + i]) * (1.f / kScale));
-    if constexpr (kPhase == kApply) {
-      uint4 vh, vl;
-      split(v, &vh, &vl);
-      *reinterpret_cast<uint4*>(to + o) = vh;
-      *reinterpret_cast<uint4*>(lo + o) = vl;
-    } else if (row < e.m) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int cc = col + 8 * p + i;
-        if (cc >= e.n) continue;
-        const int64_t k = e.tall ? static_cast<int64_t>(cc) * e.m + row
-                                 : static_cast<int64_t>(row) * e.n + cc;
-        const float x = v[i] * (1.f / kScale);
-        if (!a.muon) {
-          store_one(x, e.out, DORA_BF16, k);
-        } else {
-          const float w = fmaf(load_one(e.param, e.param_type, k), a.keep, -(a.lr * e.scale) * x);
-          store_one(w, e.param, e.param_type, k);
-          if (e.copy != nullptr) store_one(w, e.copy, DORA_BF16, k);
-        }
-      }
-    }
-  }
+// 16-byte part `p` of lane's row of a piece (rows of 64 bytes, as a copy swizzles them).
+__device__ __forceinline__ uint4* piece_at(uint16_t* piece, int row, int p) {
+  return reinterpret_cast<uint4*>(reinterpret_cast<char*>(piece) + row * 64 +
+                                  ((p ^ ((row >> 1) & 3)) << 4));
 }
+__device__ __forceinline__ uint16_t* value_in(uint16_t* piece, int row, int c) {
+  return reinterpret_cast<uint16_t*>(piece_at(piece, row, c >> 3)) + (c & 7);
+}
+
+// 32 values `pitch` apart: the first `some` of x, times f, are written there, or the weights
+// there are updated by them, which leaves the new weights in x.
+template <typename T>
+__device__ __forceinline__ void store_rows(const float (&x)[32], T* p, int64_t pitch, int some,
+                                           float f) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < some) from_float(x[i] * f, p + i * pitch);
+}
+template <typename T>
+__device__ __forceinline__ void update_rows(float (&x)[32], T* p, int64_t pitch, int some,
+                                            float keep, float step) {
+  T old[32];                              // all on their way before the first is used
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < some) old[i] = p[i * pitch];
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < some) {
+      x[i] = fmaf(to_float(old[i]), keep, step * x[i]);
+      from_float(x[i], p + i * pitch);
+    }
+}
+
+// A warp's part of an output tile.
+struct Part {
+  int row, col;                           // first row, first column in the matrix
+  int pieces;
+};
 
 template <Phase kPhase>
 __global__ void __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ CUtensorMap map, List list, Args a, int from) {
+    product_kernel(const __grid_constant__ Maps maps, List list, Args a, int from) {
   extern __shared__ __align__(1024) uint8_t raw[];
   pdl_trigger();
   Smem& s = *reinterpret_cast<Smem*>(raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_ctarank()), cid = blockIdx.x >> 1;
+  const int n_clusters = gridDim.x >> 1;
   constexpr bool kSym = kPhase == kGram || kPhase == kSquare;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -455,16 +553,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.acc_full[i], 1);
-      mbar_init(&s.acc_empty[i], 4);
+      mbar_init(&s.acc_empty[i], 2 * kEpiWarps);
     }
+    for (int w = 0; w < kEpiWarps; ++w)
+      for (int i = 0; i < kPlaces; ++i) mbar_init(&s.piece_full[w][i], 1);
     mbar_init(&s.drain, 1);
     s.abort = s.issued = s.consumed = 0;
     fence_barrier_init();
-    tma_prefetch_desc(&map);
+    tma_prefetch_desc(&maps.tile);
+    tma_prefetch_desc(&maps.half);
+    tma_prefetch_desc(&maps.piece);
   }
-  if (warp == 1) tmem_alloc(&s.tmem, 2 * kBlock);
+  if (warp == 1) tmem_alloc_pair(&s.tmem, 2 * kWide);
   tc_fence_before();
-  __syncthreads();
+  cluster_sync();
   tc_fence_after();
   pdl_wait();
   const Tile* tiles = kSym ? list.sym : list.all;
@@ -472,55 +574,65 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = s.tmem;
   volatile int* abort = &s.abort;
   // stages of a tile: the K of its product over 64
-  auto steps = [&](const Entry& e) { return kPhase == kGram ? 2 * e.nb : 2 * e.mb; };
+  auto steps = [&](const Entry& e) { return ((kPhase == kGram ? e.n : e.m) + kK - 1) / kK; };
 
   if (warp == 0) {
     if (elect_one()) {
       int it = 0;
       bool ok = true;
-      for (int w = blockIdx.x; ok && w < n_tiles; w += gridDim.x) {
+      for (int w = cid; ok && w < n_tiles; w += n_clusters) {
         const Tile t = tiles[w];
         const Entry& e = list.entries[t.matrix];
-        const int n = steps(e), wide = kPhase == kGram ? 2 * e.nb : 2 * e.mb;
-        const int64_t first_a = kPhase == kGram ? e.x[from] : (kPhase == kSquare ? e.f : e.g);
-        const int64_t row_a = first_a + static_cast<int64_t>(t.i) * wide;
+        const int n = steps(e), row_tiles = kPhase == kGram ? 2 * e.nb : 2 * e.mb;
+        const int64_t left = kPhase == kGram ? e.x[from] : (kPhase == kSquare ? e.f : e.g);
+        const bool wide = t.width == kWide;
+        const int32_t ya =
+            static_cast<int32_t>((left + static_cast<int64_t>(2 * t.i + rank) * row_tiles) * kTileRows);
+        // symmetric: rows of the left operand, 128 or 64 for each CTA; else 64 rows of X, two
+        // column tiles or one for each CTA
+        int32_t yb;
+        if (kSym)
+          yb = static_cast<int32_t>(
+                   (left + static_cast<int64_t>(2 * t.j + (wide ? rank : 0)) * row_tiles) *
+                   kTileRows) +
+               (wide ? 0 : rank * 64);
+        else
+          yb = static_cast<int32_t>((e.x[from] + 4 * t.j + (wide ? 2 * rank : rank)) * kTileRows);
         for (int k = 0; k < n; ++k, ++it) {
           const int st = it % kStages;
           if (!mbar_wait(&s.empty[st], ((it / kStages) & 1) ^ 1, abort)) {
             ok = false;
             break;
           }
-          mbar_arrive_expect_tx(&s.full[st], 2 * kTileBytes);
-          const int32_t ya = static_cast<int32_t>((row_a + k) * kTileRows);
-          tma_load_2d(s.a[st], &map, &s.full[st], 0, ya);
-          tma_load_2d(s.a[st] + kHalfTile, &map, &s.full[st], 0, ya + 64);
-          int32_t yb, yb2;
+          // the bytes of both CTAs are counted on the first one's barrier
+          if (rank == 0)
+            mbar_arrive_expect_tx(&s.full[st], 2 * (kTileBytes + (wide ? kTileBytes : kHalfTile)));
+          tma_load_2d_pair(s.a[st], &maps.tile, &s.full[st], 0, 0, ya + k * kTileRows);
           if (kSym) {
-            yb = static_cast<int32_t>((first_a + static_cast<int64_t>(t.j) * wide + k) * kTileRows);
-            yb2 = yb + 64;
-          } else {                        // 64 rows of X, of two tiles side by side
-            yb = static_cast<int32_t>(
-                (e.x[from] + static_cast<int64_t>(k >> 1) * 2 * e.nb + 2 * t.j) * kTileRows +
-                (k & 1) * 64);
-            yb2 = yb + kTileRows;
+            tma_load_2d_pair(s.b[st], wide ? &maps.tile : &maps.half, &s.full[st], 0, 0,
+                             yb + k * kTileRows);
+          } else {
+            const int32_t y = yb + (k >> 1) * 2 * e.nb * kTileRows + (k & 1) * 64;
+            tma_load_2d_pair(s.b[st], &maps.half, &s.full[st], 0, 0, y);
+            if (wide)
+              tma_load_2d_pair(s.b[st] + kHalfTile, &maps.half, &s.full[st], 0, 0, y + kTileRows);
           }
-          tma_load_2d(s.b[st], &map, &s.full[st], 0, yb);
-          tma_load_2d(s.b[st] + kHalfTile, &map, &s.full[st], 0, yb2);
         }
       }
       s.issued = it;
     }
   } else if (warp == 1) {
-    if (elect_one()) {
-      constexpr uint32_t idesc = idesc_f16(kBlock, kBlock, !kSym);
+    if (elect_one() && rank == 0) {
       int it = 0, ti = 0;
       bool ok = true;
-      for (int w = blockIdx.x; ok && w < n_tiles; w += gridDim.x, ++ti) {
-        const int n = steps(list.entries[tiles[w].matrix]);
+      for (int w = cid; ok && w < n_tiles; w += n_clusters, ++ti) {
+        const Tile t = tiles[w];
+        const int n = steps(list.entries[t.matrix]);
+        const uint32_t idesc = idesc_f16(2 * kBlock, t.width, !kSym);
         const int acc = ti & 1;
         if (!mbar_wait(&s.acc_empty[acc], ((ti >> 1) & 1) ^ 1, abort)) break;
         tc_fence_after();
-        const uint32_t d = tmem + static_cast<uint32_t>(acc * kBlock);
+        const uint32_t d = tmem + static_cast<uint32_t>(acc * kWide);
         for (int k = 0; k < n; ++k, ++it) {
           const int st = it % kStages;
           if (!mbar_wait(&s.full[st], (it / kStages) & 1, abort)) {
@@ -533,32 +645,226 @@ __global__ void __launch_bounds__(kThreads, 1)
                                    : sdesc_sw128(smem_u32(s.b[st]), kHalfTile, 1024);
 #pragma unroll
           for (int q = 0; q < kK / 16; ++q)   // 16 of K: 32 bytes of a row, or 16 rows
-            mma_bf16_ss(d, ad + 2 * q, bd + (kSym ? 2 : 128) * q, idesc, (k | q) != 0 ? 1u : 0u);
-          mma_commit(&s.empty[st]);
+            mma_bf16_ss_pair(d, ad + 2 * q, bd + (kSym ? 2 : 128) * q, idesc,
+                             (k | q) != 0 ? 1u : 0u);
+          mma_commit_pair(&s.empty[st], kPairMask);
         }
-        if (ok) mma_commit(&s.acc_full[acc]);
+        if (ok) mma_commit_pair(&s.acc_full[acc], kPairMask);
       }
       s.consumed = it;
-      mma_commit(&s.drain);
+      mma_commit_pair(&s.drain, 0x1);
       mbar_wait_limited(&s.drain, 0, kWaitLimitNs);
     }
   } else {
-    const int q = warp & 3, r = q * 32 + lane;
-    int ti = 0;
-    for (int w = blockIdx.x; w < n_tiles; w += gridDim.x, ++ti) {
+    const int ew = warp - 2, q = warp & 3, half = ew >> 2;
+    constexpr bool kReads = kPhase != kGram;
+    auto part_of = [&](const Tile& t) {
+      return Part{(2 * t.i + rank) * kBlock + q * 32, t.j * kWide + half * (t.width >> 1),
+                  t.width >> 6};
+    };
+    // map row of the piece at (row, col) of a matrix whose tiles begin at `first`, row_tiles a
+    // block row; its map column is col & 32
+    auto piece_row = [&](int64_t first, int row_tiles, int row, int col) {
+      return static_cast<int32_t>((first + static_cast<int64_t>(row >> 7) * row_tiles + (col >> 6)) *
+                                      kTileRows + (row & 127));
+    };
+    // The copies run two pieces ahead, over the ends of tiles.
+    int ahead_w = cid, ahead_c = 0, loads = 0;
+    auto load_next = [&]() {
+      if (!kReads || ahead_w >= n_tiles) return;
+      const Tile t = tiles[ahead_w];
+      const Entry& e = list.entries[t.matrix];
+      const Part p = part_of(t);
+      const int place = loads % kPlaces, col = p.col + 32 * ahead_c;
+      if (lane == 0) {
+        uint64_t* bar = &s.piece_full[ew][place];
+        if (kPhase == kSquare) {
+          mbar_arrive_expect_tx(bar, kPiece * 2);
+          tma_load_2d(s.piece[ew][place][0], &maps.piece, bar, col & 32,
+                      piece_row(e.f, 2 * e.mb, p.row, col));
+        } else {
+          mbar_arrive_expect_tx(bar, 2 * kPiece * 2);
+          tma_load_2d(s.piece[ew][place][0], &maps.piece, bar, col & 32,
+                      piece_row(e.x[from], 2 * e.nb, p.row, col));
+          tma_load_2d(s.piece[ew][place][1], &maps.piece, bar, col & 32,
+                      piece_row(e.lo, 2 * e.nb, p.row, col));
+        }
+      }
+      ++loads;
+      if (++ahead_c == p.pieces) {
+        ahead_c = 0;
+        ahead_w += n_clusters;
+      }
+    };
+    load_next();
+    load_next();
+    int ti = 0, done = 0;
+    bool ok = true;
+    for (int w = cid; ok && w < n_tiles; w += n_clusters, ++ti) {
       const Tile t = tiles[w];
       const Entry& e = list.entries[t.matrix];
-      const int acc = ti & 1;
+      const Part p = part_of(t);
+      const int row = p.row + lane, acc = ti & 1;
+      const bool mirrored = kSym && t.i != t.j && p.row < e.mb * kBlock;
+      float di = 0.f, ae = 0.f;
+      if (kPhase == kSquare) di = e.d[row];
+      if (!kSym) ae = kA + e.e[row];
       if (!mbar_wait_warp(&s.acc_full[acc], (ti >> 1) & 1, abort)) break;
       tc_fence_after();
-      for (int c = 0; c < kBlock; c += 32) {
+      for (int c = 0; c < p.pieces; ++c, ++done) {
+        const int col = p.col + 32 * c, place = done % kPlaces;
+        uint16_t *one = s.piece[ew][place][0], *two = s.piece[ew][place][1];
+        float dj = 0.f;
+        if (kPhase == kSquare) dj = e.d[col + lane];
         uint32_t v[32];
-        tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kBlock + c, v);
+        tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide + (col - t.j * kWide),
+                  v);
+        if (kReads) {
+          if (!mbar_wait_warp(&s.piece_full[ew][place], (done / kPlaces) & 1, abort)) {
+            tmem_ld_wait();
+            ok = false;
+            break;
+          }
+        } else {                          // the copy out of this place has read it
+          if (lane == 0) bulk_wait_group_read1();
+          __syncwarp();
+        }
         tmem_ld_wait();
-        finish_row<kPhase>(list, e, a, t, from, r, c, v);
+        if (c == p.pieces - 1) {          // this warp is done with the accumulator
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
+        }
+        if constexpr (kSym) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float x[8];
+            if constexpr (kPhase == kGram) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * k + i]) * (1.f / kScale);
+              if (row >= col && row < col + 32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  if (row == col + 8 * k + i) {
+                    e.d[row] = x[i] * (1.f / kScale);
+                    x[i] = 0.f;
+                  }
+              }
+            } else {
+              float off[8];
+              Granule<__half>::unpack(*piece_at(one, lane, k), off);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float ff = __uint_as_float(v[8 * k + i]) * (1.f / kScale);   // scaled once
+                const float d2 = di + __shfl_sync(0xffffffffu, dj, 8 * k + i);
+                x[i] = fmaf(kC, fmaf(d2, off[i], ff), kB * off[i]);
+                if (row == col + 8 * k + i) {
+                  e.e[row] = fmaf(kC, fmaf(di, di, ff * (1.f / kScale)), kB * di);
+                  x[i] = 0.f;
+                }
+              }
+            }
+            const uint4 h = Granule<__half>::pack(x);
+            *piece_at(one, lane, k) = h;
+            if (mirrored) {
+              const uint32_t words[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *value_in(two, 8 * k + i, lane) =
+                    static_cast<uint16_t>(words[i >> 1] >> (16 * (i & 1)));
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int64_t to = kPhase == kGram ? e.f : e.g;
+            tma_store_2d(&maps.piece, one, col & 32, piece_row(to, 2 * e.mb, p.row, col));
+            if (mirrored)
+              tma_store_2d(&maps.piece, two, p.row & 32, piece_row(to, 2 * e.mb, col, p.row));
+            bulk_commit_group();
+          }
+        } else {
+          float x[32];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float h[8], l[8];
+            Granule<__half>::unpack(*piece_at(one, lane, k), h);
+            Granule<__half>::unpack(*piece_at(two, lane, k), l);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              x[8 * k + i] = fmaf(ae, fmaf(l[i], 1.f / kLoScale, h[i]),
+                                  __uint_as_float(v[8 * k + i]) * (1.f / kScale));
+          }
+          if constexpr (kPhase == kApply) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint4 h, l;
+              split(x + 8 * k, &h, &l);
+              *piece_at(one, lane, k) = h;
+              *piece_at(two, lane, k) = l;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_2d(&maps.piece, one, col & 32,
+                           piece_row(e.x[from ^ 1], 2 * e.nb, p.row, col));
+              tma_store_2d(&maps.piece, two, col & 32, piece_row(e.lo, 2 * e.nb, p.row, col));
+              bulk_commit_group();
+            }
+          } else {
+            // 32 x 32 values to the weights: lanes along what is contiguous there, which for
+            // a wide matrix are columns (the values change places in shared memory)
+            if (!e.tall) {
+              float* swap = reinterpret_cast<float*>(one);
+              __syncwarp();               // every lane has read its part of the piece
+#pragma unroll
+              for (int i = 0; i < 32; ++i) swap[lane * 32 + ((i + lane) & 31)] = x[i];
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = swap[i * 32 + ((lane + i) & 31)];
+              __syncwarp();
+              fence_proxy_async_smem();
+            }
+            const int outer = e.tall ? col : p.row, inner = (e.tall ? p.row : col) + lane;
+            const int outers = e.tall ? e.n : e.m, inners = e.tall ? e.m : e.n;
+            if (inner < inners) {
+              const int64_t at = static_cast<int64_t>(outer) * inners + inner;
+              const int some = outers - outer < 32 ? outers - outer : 32;
+              if (!a.muon) {
+                store_rows(x, reinterpret_cast<__nv_bfloat16*>(e.out) + at, inners, some,
+                           1.f / kScale);
+              } else {
+                const float step = -(a.lr * e.scale) * (1.f / kScale);
+                if (e.param_type == DORA_F32)
+                  update_rows(x, static_cast<float*>(e.param) + at, inners, some, a.keep, step);
+                else if (e.param_type == DORA_BF16)
+                  update_rows(x, static_cast<__nv_bfloat16*>(e.param) + at, inners, some, a.keep,
+                              step);
+                else
+                  update_rows(x, static_cast<__half*>(e.param) + at, inners, some, a.keep, step);
+                if (e.copy != nullptr)
+                  store_rows(x, reinterpret_cast<__nv_bfloat16*>(e.copy) + at, inners, some, 1.f);
+              }
+            }
+            __syncwarp();
+          }
+        }
+        if (kReads) {
+          // the place two pieces on was copied out one piece ago
+          if (kPhase != kLast && lane == 0) bulk_wait_group_read1();
+          __syncwarp();
+          load_next();
+        }
       }
-      warp_arrive(&s.acc_empty[acc]);
     }
+    if (lane == 0) {
+      bulk_wait_group0();                 // copies are done before the CTA ends
+      // after an abort: those that nobody waited for
+      for (; kReads && done < loads; ++done)
+        mbar_wait_limited(&s.piece_full[ew][done % kPlaces], (done / kPlaces) & 1,
+                          100ull * 1000 * 1000);
+    }
+    __syncwarp();
   }
 
   __syncwarp();
@@ -568,16 +874,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) {
       list.header->abort = 1;
       record_status(a.status, DORA_ERR_TIMEOUT);
-      // loads that were issued but never consumed land first
-      for (int it = s.consumed; it < s.issued; ++it)
-        mbar_wait_limited(&s.full[it % kStages], (it / kStages) & 1, 100ull * 1000 * 1000);
+      if (rank == 0)                      // loads that were issued but never consumed land first
+        for (int it = s.consumed; it < s.issued; ++it)
+          mbar_wait_limited(&s.full[it % kStages], (it / kStages) & 1, 100ull * 1000 * 1000);
     }
     __syncthreads();
   }
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, 2 * kBlock);
+    tmem_dealloc_pair(tmem, 2 * kWide);
   }
+  cluster_sync();                         // no CTA leaves while its peer may still signal it
 }
 
 }  // namespace ortho
@@ -604,7 +911,7 @@ bool known_type(int32_t t) { return t >= DORA_BF16 && t <= DORA_F32; }
 // Sizes of a matrix, and of all of them.
 struct Shape {
   int32_t m, n, mb, nb;
-  int64_t chunks, x_tiles, f_tiles, sym, all;
+  int64_t chunks, x_tiles, f_tiles, sym, all, diag;   // diag: blocks of 128 of a diagonal
 };
 Shape shape_of(const dora_matrix& t) {
   Shape s;
@@ -613,10 +920,12 @@ Shape shape_of(const dora_matrix& t) {
   s.mb = (s.m + 127) / 128;
   s.nb = (s.n + 127) / 128;
   s.chunks = (static_cast<int64_t>(s.m) * s.n + ortho::kChunk - 1) / ortho::kChunk;
-  s.x_tiles = static_cast<int64_t>(s.mb) * 2 * s.nb;
-  s.f_tiles = static_cast<int64_t>(s.mb) * 2 * s.mb;
-  s.sym = static_cast<int64_t>(s.mb) * (s.mb + 1) / 2;
-  s.all = static_cast<int64_t>(s.mb) * s.nb;
+  const int64_t pairs = (s.mb + 1) / 2;
+  s.x_tiles = pairs * 2 * 2 * s.nb;
+  s.f_tiles = pairs * 2 * 2 * s.mb;
+  s.sym = pairs * (pairs + 1) / 2;
+  s.all = pairs * ((s.nb + 1) / 2);
+  s.diag = pairs * 2;
   return s;
 }
 struct Sizes {
@@ -646,7 +955,7 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
     z.sym += s.sym;
     z.all += s.all;
     z.tiles += 3 * s.x_tiles + 2 * s.f_tiles;
-    z.diag += s.mb;
+    z.diag += s.diag;
     if (t.param == nullptr) z.has_params = false;
     if (t.out == nullptr) z.has_outs = false;
     // counted in 32 bits, the tiles' rows among them
@@ -700,36 +1009,49 @@ bool valid_list(const dora_matrix_list* l) {
 }
 
 template <ortho::Phase kPhase>
-int launch_product(const CUtensorMap& map, const ortho::List& l, const ortho::Args& a, int from,
+int launch_product(const ortho::Maps& maps, const ortho::List& l, const ortho::Args& a, int from,
                    cudaStream_t stream) {
   constexpr int smem = sizeof(ortho::Smem);
-  const cudaError_t e = cudaFuncSetAttribute(ortho::product_kernel<kPhase>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  auto kern = ortho::product_kernel<kPhase>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return launched(e);
   const int tiles = kPhase == ortho::kGram || kPhase == ortho::kSquare ? l.n_sym : l.n_all;
-  return launched(launch_pdl(ortho::product_kernel<kPhase>,
-                             dim3(tiles < num_sms() ? tiles : num_sms()), dim3(ortho::kThreads),
-                             smem, stream, map, l, a, from));
+  const int pairs = num_sms() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(2 * (tiles < pairs ? tiles : pairs));
+  cfg.blockDim = dim3(ortho::kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return launched(cudaLaunchKernelEx(&cfg, kern, maps, l, a, from));
 }
 
 int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaStream_t stream) {
   const int dev = device_or_error();
   if (dev != DORA_OK) return dev;
   const ortho::List l = list_of(*list);
-  CUtensorMap map;
-  memcpy(&map, list->map, sizeof(map));
-  const int most = num_sms() * 4;
+  ortho::Maps maps;
+  static_assert(sizeof(maps) == sizeof(list->map), "the maps' size is part of the interface");
+  memcpy(&maps, list->map, sizeof(maps));
+  const int most = num_sms() * ortho::kRowCtas;
   int e = launched(launch_pdl(ortho::momentum_kernel, dim3(l.n_chunks < most ? l.n_chunks : most),
                               dim3(ortho::kRowThreads), 0, stream, l, a));
   if (e == DORA_OK)
     e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
                             dim3(ortho::kRowThreads), 0, stream, l, a));
   for (int s = 0; s < steps && e == DORA_OK; ++s) {
-    e = launch_product<ortho::kGram>(map, l, a, s & 1, stream);
-    if (e == DORA_OK) e = launch_product<ortho::kSquare>(map, l, a, s & 1, stream);
+    e = launch_product<ortho::kGram>(maps, l, a, s & 1, stream);
+    if (e == DORA_OK) e = launch_product<ortho::kSquare>(maps, l, a, s & 1, stream);
     if (e == DORA_OK)
-      e = s + 1 < steps ? launch_product<ortho::kApply>(map, l, a, s & 1, stream)
-                        : launch_product<ortho::kLast>(map, l, a, s & 1, stream);
+      e = s + 1 < steps ? launch_product<ortho::kApply>(maps, l, a, s & 1, stream)
+                        : launch_product<ortho::kLast>(maps, l, a, s & 1, stream);
   }
   return e;
 }
@@ -766,13 +1088,14 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   l.count = count;
   l.has_params = z.has_params;
   l.has_outs = z.has_outs;
-  CUtensorMap map;
   // all tiles as one tall matrix of 64 columns
-  if (encode_tmap_2d_bf16(&map, at + p.tiles, ortho::kTileCols,
-                          static_cast<uint64_t>(z.tiles) * ortho::kTileRows, 128,
-                          ortho::kTileCols, 64) != 0)
+  ortho::Maps maps;
+  const uint64_t rows = static_cast<uint64_t>(z.tiles) * ortho::kTileRows;
+  if (encode_tmap_2d_bf16(&maps.tile, at + p.tiles, 64, rows, 128, 64, 128) != 0 ||
+      encode_tmap_2d_bf16(&maps.half, at + p.tiles, 64, rows, 128, 64, 64) != 0 ||
+      encode_tmap_2d_bf16(&maps.piece, at + p.tiles, 64, rows, 128, 32, 32, 64) != 0)
     return DORA_ERR_CUDA;
-  memcpy(l.map, &map, sizeof(map));
+  memcpy(l.map, &maps, sizeof(maps));
   const ortho::List o = list_of(l);
   int64_t tile = 0, chunk = 0, x = 0, sym = 0, all = 0, diag = 0;
   for (int32_t first = 0; first < count; first += ortho::kFill) {
@@ -804,9 +1127,9 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.g = e.f + s.f_tiles;
       tile = e.g + s.f_tiles;
       e.d = reinterpret_cast<float*>(at + p.diag) + diag * 256;
-      e.e = e.d + s.mb * 128;
-      diag += s.mb;
-      e.partial = reinterpret_cast<float2*>(at + p.partial) + chunk;
+      e.e = e.d + s.diag * 128;
+      diag += s.diag;
+      e.partial = reinterpret_cast<ortho::Squares*>(at + p.partial) + chunk;
       e.norm = reinterpret_cast<float2*>(at + p.norm) + first + i;
       e.ticket = reinterpret_cast<unsigned*>(at + p.ticket) + first + i;
       e.chunks = static_cast<int32_t>(s.chunks);

@@ -78,9 +78,10 @@ def test_list_host_checks(lib):
     def size(**more):
         return lib.dora_matrix_list_size(ctypes.byref(_matrix(**more)), 1)
 
-    # three copies of X in whole tiles of 128 columns, two of the square of the shorter side
+    # three copies of X in tiles of 128 x 64, an even number down and across, two of the square
+    # of the shorter side
     one = size()
-    assert 5 * 2 * 16384 <= one < 5 * 2 * 16384 + 16384
+    assert 5 * 4 * 16384 <= one < 5 * 4 * 16384 + 16384
     assert size(rows=300, cols=200) >= (3 * 2 * 6 + 2 * 2 * 4) * 16384
     assert size(param=0, momentum=0, copy=0) == one and size(out=0) == one and size(copy=0) == one
     for bad in (dict(rows=0), dict(cols=0), dict(rows=-1), dict(grad=0), dict(grad=257),
