@@ -907,8 +907,8 @@ int dora_adam_step(const dora_param_list* list, void* state, double lr, double b
  *   scale            of the matrix's update in dora_muon_step (e.g.
  *                    sqrt(max(1, rows / cols)), or 0.2 sqrt(max(rows, cols)) for
  *                    updates as large as Adam's).
- * The shorter side is at most 16384, the longer 2^24.  Pointers are aligned to their
- * elements; 16-byte alignment is faster.  No two buffers overlap.
+ * The shorter side is at most 16384, and there are at most 2^32 elements.  Pointers are
+ * aligned to their elements; 16-byte alignment is faster.  No two buffers overlap.
  * dora_matrix_list_prepare writes the list into `data` (device,
  * dora_matrix_list_size bytes, 256-byte aligned) and fills the host handle *list, which
  * the calls below take; done once for a set of buffers.  The list's memory also holds the
@@ -933,7 +933,7 @@ typedef struct dora_matrix_list {
   int32_t has_params;   /* 1: every matrix has param and momentum */
   int32_t has_outs;     /* 1: every matrix has out */
   int32_t pad;
-  uint64_t map[48];
+  uint64_t map[64];
 } dora_matrix_list;
 size_t dora_matrix_list_size(const dora_matrix* matrices, int32_t count);
 int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* data, size_t bytes,

@@ -1229,7 +1229,7 @@ class _MatrixListC(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(n, _i64) for n in ("chunks", "x_tiles", "symmetric", "outputs",
                                                       "tiles", "diagonals")] + [
         (n, _i32) for n in ("count", "has_params", "has_outs", "pad")] + [
-        ("map", ctypes.c_uint64 * 48)]
+        ("map", ctypes.c_uint64 * 64)]
 
 
 class MatrixList:
@@ -1293,8 +1293,8 @@ class MatrixList:
             at.param_dtype = _DTYPES[t.dtype]
         size = int(load_library().dora_matrix_list_size(c, n))
         if size == 0:
-            raise ValueError("a matrix is empty, larger than 16384 x 2^24, or its scale is not "
-                             "finite")
+            raise ValueError("a matrix is empty, has a shorter side above 16384 or more than "
+                             "2^32 elements, or its scale is not finite")
         self.data = _bytes_on(size, device, stream)
         self.c = _MatrixListC()
         self.ref = ctypes.byref(self.c)

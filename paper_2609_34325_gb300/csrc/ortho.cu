@@ -45,11 +45,13 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kScale = 256.f;           // of X, F and G in fp16: their values are below 4
 constexpr float kLoScale = 2048.f;        // of lo, on top of it
 constexpr int kMaxSteps = 32;
+constexpr int64_t kGroup = 24 << 20;      // elements of a group of matrices, about
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
 constexpr int kRowThreads = 256, kRowCtas = 4;
-constexpr int kMaxShort = 16384, kMaxLong = 1 << 24;
+constexpr int kMaxShort = 16384;
+constexpr int64_t kMaxElements = int64_t{1} << 32;   // a phase of one takes 50 ms, far from a wait's limit
 
 struct Squares;
 
@@ -61,6 +63,7 @@ struct Entry {
   int32_t rows, cols, grad_type, param_type;
   float scale;
   int32_t m, n, tall;                     // X is m x n; tall: X = U^T
+  int32_t quads;                          // what is written is aligned to four values, row by row
   int32_t mb, nb;                         // blocks of 128 rows, of 128 columns; X, F and G
                                           // have an even number of the first
   int64_t x[2], lo, f, g;                 // first tiles of X hi (two, in turn), X lo, F, G
@@ -68,17 +71,28 @@ struct Entry {
   Squares* partial;                       // of its chunks
   float2* norm;                           // one over the norm of u 2^-k, and 2^-k
   unsigned* ticket;                       // chunks done; zero between calls
-  int32_t chunks, pad;
+  unsigned* done;                         // CTAs' parts of its tiles that are done, in this call
+  int32_t chunks;
+  int32_t n_sym, n_all;                   // its tiles of A and B, and of X
+  int32_t sym_width, all_width;           // their columns
   // first of its chunks, of its tiles of X and of its output tiles among the list's
   int64_t first_chunk, first_x, first_sym, first_all;
 };
 
 struct Header {
   int abort;                              // a bounded wait of this call has run out
-  int pad[63];
+  unsigned ticket;                        // tiles taken in this call
+  int n_groups;
+  int pad[61];
 };
 
-// One piece of work: block row and block column of a matrix, and its columns.
+// The tiles of a group of matrices.
+struct Group {
+  int sym0, sym1, all0, all1;
+};
+
+// One piece of work: a pair of block rows (or one) of a matrix, its first block column and
+// its columns.
 struct Tile {
   int32_t matrix, i, j, width;
 };
@@ -88,6 +102,7 @@ struct List {
   Entry* entries;
   int32_t* chunk_of;                      // matrix of every chunk
   Tile *x, *sym, *all;
+  Group* groups;
   char* tiles;
   int count;
   int n_chunks, n_x, n_sym, n_all;
@@ -129,19 +144,41 @@ __global__ void fill_tiles_kernel(List list) {
   }
   if (t < list.n_all) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_all; });
-    const int at = static_cast<int>(t - list.entries[q].first_all), nb = list.entries[q].nb;
-    const int w = (nb + 1) / 2, j = at % w;
-    list.all[t] = Tile{q, at / w, j, 2 * j + 1 < nb ? 256 : 128};
+    const Entry& e = list.entries[q];
+    const int at = static_cast<int>(t - e.first_all), each = e.all_width / 128;
+    const int w = (e.nb + each - 1) / each, j = at % w * each;
+    list.all[t] = Tile{q, at / w, j, j + each <= e.nb ? e.all_width : 128};
   }
   if (t < list.n_sym) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_sym; });
-    const int mb = list.entries[q].mb;
-    int at = static_cast<int>(t - list.entries[q].first_sym), i = 0, left = (mb + 1) / 2;
+    const Entry& e = list.entries[q];
+    const int each = e.sym_width / 128;
+    int at = static_cast<int>(t - e.first_sym), i = 0, left = (e.mb + each - 1) / each;
     while (at >= left) {
-      at -= left--;
+      at -= left;
       ++i;
+      left = (e.mb - 2 * i + each - 1) / each;
     }
-    list.sym[t] = Tile{q, i, i + at, 2 * (i + at) + 1 < mb ? 256 : 128};
+    const int j = 2 * i + at * each;
+    list.sym[t] = Tile{q, i, j, j + each <= e.mb ? e.sym_width : 128};
+  }
+  if (t == 0) {                           // whole matrices until a group is large enough
+    int n = 0;
+    int64_t size = 0;
+    Group g = {0, 0, 0, 0};
+    for (int q = 0; q < list.count; ++q) {
+      const Entry& e = list.entries[q];
+      g.sym1 += e.n_sym;
+      g.all1 += e.n_all;
+      size += static_cast<int64_t>(e.m) * e.n;
+      if (size >= kGroup || q == list.count - 1) {
+        list.groups[n++] = g;
+        g.sym0 = g.sym1;
+        g.all0 = g.all1;
+        size = 0;
+      }
+    }
+    list.header->n_groups = n;
   }
 }
 
@@ -190,6 +227,17 @@ __device__ __forceinline__ void unpack_quad(uint4 q, int type, float* v) {
   else Granule<__half>::unpack(q, w);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = w[j];
+}
+
+__device__ __forceinline__ void store_quad(const float* v, void* p, int type, int64_t k) {
+  if (type == DORA_F32)
+    *reinterpret_cast<uint4*>(static_cast<float*>(p) + k) = Granule<float>::pack(v);
+  else
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + k) =
+        type == DORA_BF16 ? make_uint2(Granule<__nv_bfloat16>::pair(v[0], v[1]),
+                                       Granule<__nv_bfloat16>::pair(v[2], v[3]))
+                          : make_uint2(Granule<__half>::pair(v[0], v[1]),
+                                       Granule<__half>::pair(v[2], v[3]));
 }
 
 // What all kernels of a call take.
@@ -280,7 +328,13 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) momentum_kernel(List li
   pdl_wait();
   if (skipped(a)) return;
   const float f = factor(a);
-  if (blockIdx.x == 0 && threadIdx.x == 0) list.header->abort = 0;
+  if (blockIdx.x == 0) {                  // what the products count
+    if (threadIdx.x == 0) {
+      list.header->abort = 0;
+      list.header->ticket = 0;
+    }
+    for (int i = threadIdx.x; i < list.count; i += kRowThreads) *list.entries[i].done = 0;
+  }
   int c = static_cast<int>(static_cast<int64_t>(list.n_chunks) * blockIdx.x / gridDim.x);
   const int end = static_cast<int>(static_cast<int64_t>(list.n_chunks) * (blockIdx.x + 1) /
                                    gridDim.x);
@@ -455,13 +509,20 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
 }
 
 // ---------------------------------------------------------------------------
-// The products.  Persistent CTAs in pairs take output tiles of 256 rows and 256 or 128
-// columns: one MMA spans the pair, each CTA holding its 128 rows of the left operand and half
-// of the right one, so that a stage is 32 KB for each.  In a CTA one warp copies operands into
-// a ring of stages, one issues the MMAs (in the first CTA) into one of two accumulators, and
-// eight finish the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo)
-// comes by copies of its own into three places a warp, two of them ahead, and is written
-// over there and copied out.
+// The products, all iterations of all matrices in one launch.  The work is a list of
+// output tiles (256 rows, 256 or 128 columns) in an order in which each depends on
+// earlier ones only: the matrices in groups that fit L2, of a group one phase of all its
+// matrices after the other.  CTA pairs take the tiles as they get done with others
+// (a counter), and a tile waits until its matrix has finished the phase before (a counter
+// a matrix).  Whoever holds a tile runs, and the earliest unfinished one waits for
+// nobody, so that there is always progress, however many CTAs are resident.
+//
+// One MMA spans a pair, each CTA holding its 128 rows of the left operand and half of the right
+// one, so that a stage is 32 KB for each.  In a CTA one warp copies operands into a ring of
+// stages, one issues the MMAs (in the first CTA) into one of two accumulators, and eight finish
+// the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo) an eleventh
+// warp copies ahead of them, into three places for each, where it is written over and
+// copied out.  A last warp of the first CTA fetches the tiles.
 // ---------------------------------------------------------------------------
 enum Phase { kGram, kSquare, kApply, kLast };
 
@@ -470,26 +531,40 @@ constexpr int kBlock = 128;               // rows of a CTA's part of an output t
 constexpr int kWide = 256;                // columns of one
 constexpr int kK = 64;                    // of a stage
 constexpr int kEpiWarps = 8;
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kThreads = 128 + 32 * kEpiWarps;
 constexpr int kHalfTile = kTileBytes / 2; // 64 rows
 constexpr int kPlaces = 3;
 constexpr int kPiece = 32 * 32;           // values that a warp finishes at once
+constexpr int kRing = 4;                  // tiles fetched ahead
+constexpr int kTileArrivals = 2;           // at a matrix' counter: one a CTA
 constexpr uint16_t kPairMask = 0x3;
+
+// A tile as the roles of a pair receive it, with its matrix' entry: waiting for other CTAs
+// empties the L1 cache, and every look at the list would go to L2.
+struct Task {
+  int matrix, i, j, width, phase, from, need, pad;
+  Entry e;
+};
+constexpr int kTaskWords = sizeof(Task) / 4;
 
 struct Smem {
   uint8_t a[kStages][kTileBytes];
   uint8_t b[kStages][kTileBytes];
-  uint16_t piece[kEpiWarps][kPlaces][2][kPiece];
+  uint16_t piece[kPlaces][2][2][4][kPiece];   // of each half of the columns, four warps' rows
+  float dj[kPlaces][2][32];               // of the diagonal of A
   uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
-  uint64_t piece_full[kEpiWarps][kPlaces];
+  uint64_t piece_full[2][kPlaces], piece_empty[2][kPlaces];
+  uint64_t task_full[kRing], task_empty[kRing];
+  Task task[kRing];
   uint32_t tmem;
   int abort, issued, consumed;
+  int finished[4];                        // warps that have finished a tile, of four in turn
 };
 static_assert(sizeof(Smem) <= 227 * 1024, "shared memory");
 
-// The maps of all tiles: whole ones, their halves of 64 rows, and 32 x 32 values.
+// The maps of all tiles: whole ones, their halves of 64 rows, 32 columns of 128 and of 32 rows.
 struct Maps {
-  CUtensorMap tile, half, piece;
+  CUtensorMap tile, half, column, piece;
 };
 
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
@@ -506,46 +581,285 @@ __device__ __forceinline__ uint16_t* value_in(uint16_t* piece, int row, int c) {
   return reinterpret_cast<uint16_t*>(piece_at(piece, row, c >> 3)) + (c & 7);
 }
 
-// 32 values `pitch` apart: the first `some` of x, times f, are written there, or the weights
-// there are updated by them, which leaves the new weights in x.
-template <typename T>
-__device__ __forceinline__ void store_rows(const float (&x)[32], T* p, int64_t pitch, int some,
-                                           float f) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i < some) from_float(x[i] * f, p + i * pitch);
+// Between CTAs: what a warp wrote, by copies or by itself, is there for whoever has seen
+// the counter that it adds to afterwards.
+__device__ __forceinline__ void fence_proxy_async_all() {
+  asm volatile("fence.proxy.async;" ::: "memory");
 }
-template <typename T>
-__device__ __forceinline__ void update_rows(float (&x)[32], T* p, int64_t pitch, int some,
-                                            float keep, float step) {
-  T old[32];                              // all on their way before the first is used
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i < some) old[i] = p[i * pitch];
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i < some) {
-      x[i] = fmaf(to_float(old[i]), keep, step * x[i]);
-      from_float(x[i], p + i * pitch);
+__device__ __forceinline__ void signal(unsigned* done) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(done) : "memory");
+}
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned load_relaxed(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ int atom_add_cta(int* p) {
+  int v;
+  asm volatile("atom.acq_rel.cta.shared::cta.add.s32 %0, [%1], 1;"
+               : "=r"(v)
+               : "r"(smem_u32(p))
+               : "memory");
+  return v;
+}
+// Wait until at most one bulk group of this thread has not completed.
+__device__ __forceinline__ void bulk_wait_group1() {
+  asm volatile("cp.async.bulk.wait_group 1;" ::: "memory");
+}
+// Waits until `need` arrivals were counted; the limit runs anew with each that comes.
+__device__ __forceinline__ bool wait_done(const unsigned* done, unsigned need, volatile int* abort,
+                                          const Header* header) {
+  unsigned v = load_relaxed(done);
+  if (v < need) {
+    uint64_t t0 = globaltimer_ns();
+    while (true) {
+      const unsigned now = load_relaxed(done);
+      if (now >= need) break;
+      if (*abort) return false;
+      if (now != v) {
+        v = now;
+        t0 = globaltimer_ns();
+      } else if (globaltimer_ns() - t0 > kWaitLimitNs || __ldcg(&header->abort) != 0) {
+        *abort = 1;
+        return false;
+      }
+      __nanosleep(32);
     }
+  }
+  (void)load_acquire(done);
+  fence_proxy_async_all();
+  return true;
 }
 
-// A warp's part of an output tile.
-struct Part {
+// The weights of a CTA's part of an output tile to L2, a line a lane.
+__device__ __forceinline__ void prefetch_weights(const Entry& e, int block, int col, int width,
+                                                 int lane) {
+  const int inners = e.tall ? e.m : e.n, outers = e.tall ? e.n : e.m;
+  const int inner = e.tall ? block * kBlock : col, outer = e.tall ? col : block * kBlock;
+  const int inner_end = min(inner + (e.tall ? kBlock : width), inners);
+  const int outer_end = min(outer + (e.tall ? width : kBlock), outers);
+  const int step = 128 / size_of(e.param_type);
+  for (int o = outer + lane; o < outer_end; o += 32)
+    for (int i = inner; i < inner_end; i += step)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(e.param) +
+                                                    (static_cast<int64_t>(o) * inners + i) *
+                                                        size_of(e.param_type)));
+}
+
+// The part of an output tile that warp w of a CTA finishes: 32 rows (those of the lanes of
+// tensor memory that the warp may read), half of the columns.
+struct Place {
   int row, col;                           // first row, first column in the matrix
   int pieces;
 };
+__device__ __forceinline__ Place place_of(const Task& t, int rank, int w) {
+  return Place{(2 * t.i + rank) * kBlock + ((w + 2) & 3) * 32,
+               t.j * kBlock + (w >> 2) * (t.width >> 1), t.width >> 6};
+}
 
+// Map row of the piece at (row, col) of a matrix whose tiles begin at `first`, row_tiles to
+// a block row; its map column is col & 32.
+__device__ __forceinline__ int32_t piece_row(int64_t first, int row_tiles, int row, int col) {
+  return static_cast<int32_t>((first + static_cast<int64_t>(row >> 7) * row_tiles + (col >> 6)) *
+                                  kTileRows + (row & 127));
+}
+
+// Two values of a 16-byte part, as a pair of fp32.
+__device__ __forceinline__ uint64_t halves(uint32_t w) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return f2_pack(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t to_halves(uint64_t v) {
+  float lo, hi;
+  f2_unpack(v, lo, hi);
+  return Granule<__half>::pair(lo, hi);
+}
+__device__ __forceinline__ uint64_t twice(float v) { return f2_pack(v, v); }
+
+// The mirror image of a row's 16-byte part: eight values of a column.
+__device__ __forceinline__ void mirror(uint16_t* piece, int first, int lane, uint4 q) {
+  const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *value_in(piece, first + i, lane) = static_cast<uint16_t>(words[i >> 1] >> (16 * (i & 1)));
+}
+
+// 32 x 32 new values of X (scaled; a row a lane) to where the caller wants them, lanes along
+// what is contiguous there: four values each, where sizes and alignment allow, after they have
+// changed places in shared memory, 16 rows in `low`, 16 in `high`.
+__device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int row0, int col0,
+                                            int lane, float (&x)[32], uint16_t* low,
+                                            uint16_t* high) {
+  const int outer = e.tall ? col0 : row0, inner = e.tall ? row0 : col0;
+  const int outers = e.tall ? e.n : e.m, inners = e.tall ? e.m : e.n;
+  const bool quads = e.quads && inner + 32 <= inners && outer + 32 <= outers;
+  // where row i of what is written begins; 16-byte parts change places with the row
+  auto part = [&](int i, int k) {
+    return reinterpret_cast<float4*>(i < 16 ? low : high) + (i & 15) * 8 + (k ^ (i & 7));
+  };
+  __syncwarp();                           // every lane has read its part of the piece
+  if (e.tall) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) reinterpret_cast<float*>(part(i, lane >> 2))[lane & 3] = x[i];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      *part(lane, k) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+  }
+  __syncwarp();
+  const float step = a.muon ? -(a.lr * e.scale) * (1.f / kScale) : 1.f / kScale;
+  if (quads) {
+    const int k = lane & 7, i0 = lane >> 3;
+    const int64_t at = static_cast<int64_t>(outer + i0) * inners + inner + 4 * k;
+    const int64_t next = 4 * static_cast<int64_t>(inners);
+    uint4 old[8];                         // all on their way before the first is used
+    if (a.muon)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) old[u] = whole_quad(e.param, e.param_type, at + u * next);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float4 y = *part(i0 + 4 * u, k);
+      float w[4] = {y.x * step, y.y * step, y.z * step, y.w * step};
+      if (a.muon) {
+        float v[4];
+        unpack_quad(old[u], e.param_type, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = fmaf(v[j], a.keep, w[j]);
+        store_quad(w, e.param, e.param_type, at + u * next);
+        if (e.copy != nullptr) store_quad(w, e.copy, DORA_BF16, at + u * next);
+      } else {
+        store_quad(w, e.out, DORA_BF16, at + u * next);
+      }
+    }
+  } else if (inner + lane < inners) {
+    const int64_t at = static_cast<int64_t>(outer) * inners + inner + lane;
+    const int some = outers - outer < 32 ? outers - outer : 32;
+    for (int i = 0; i < some; ++i) {
+      const float y = reinterpret_cast<const float*>(part(i, lane >> 2))[lane & 3] * step;
+      const int64_t k = at + static_cast<int64_t>(i) * inners;
+      if (a.muon) {
+        const float w = fmaf(load_one(e.param, e.param_type, k), a.keep, y);
+        store_one(w, e.param, e.param_type, k);
+        if (e.copy != nullptr) store_one(w, e.copy, DORA_BF16, k);
+      } else {
+        store_one(y, e.out, DORA_BF16, k);
+      }
+    }
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
+// What finishes 32 x 32 values of an accumulator, v, whose other inputs lie in `one`, `two`
+// and, the diagonal over its columns, `dj`.
 template <Phase kPhase>
+__device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, const Args& a,
+                                             const Task& t, const Place& p, int col, int lane,
+                                             float own, const float* dj, const uint32_t (&v)[32],
+                                             uint16_t* one, uint16_t* two) {
+  const int row = p.row + lane;
+  if constexpr (kPhase == kGram || kPhase == kSquare) {
+    const bool mirrored = t.j >= 2 * t.i + 2 && p.row < e.mb * kBlock;
+    const bool diagonal = col == p.row;   // pieces hold it or nothing of it
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t words[4];
+      const uint4 f = kPhase == kSquare ? *piece_at(one, lane, k) : make_uint4(0, 0, 0, 0);
+      const uint32_t old[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 8 * k + 2 * i;
+        // scaled once
+        uint64_t x = f2_mul(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])),
+                            twice(1.f / kScale));
+        float d0, d1;
+        if (kPhase == kGram) {
+          if (diagonal) {
+            f2_unpack(x, d0, d1);
+            if (lane == c || lane == c + 1) e.d[row] = (lane == c ? d0 : d1) * (1.f / kScale);
+          }
+        } else {
+          if (diagonal) {
+            f2_unpack(x, d0, d1);
+            if (lane == c || lane == c + 1)
+              e.e[row] = fmaf(kC, fmaf(own, own, (lane == c ? d0 : d1) * (1.f / kScale)), kB * own);
+          }
+          // b f + c (F F + (d_i + d_j) f)
+          const float2 d = *reinterpret_cast<const float2*>(dj + c);
+          const uint64_t off = halves(old[i]);
+          const uint64_t d2 = f2_add(f2_pack(d.x, d.y), twice(own));
+          x = f2_fma(twice(kC), f2_fma(d2, off, x), f2_mul(twice(kB), off));
+        }
+        if (diagonal) {
+          f2_unpack(x, d0, d1);
+          x = f2_pack(lane == c ? 0.f : d0, lane == c + 1 ? 0.f : d1);
+        }
+        words[i] = to_halves(x);
+      }
+      const uint4 h = make_uint4(words[0], words[1], words[2], words[3]);
+      *piece_at(one, lane, k) = h;
+      if (mirrored) mirror(two, 8 * k, lane, h);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      const int64_t to = kPhase == kGram ? e.f : e.g;
+      tma_store_2d(&maps.piece, one, col & 32, piece_row(to, 2 * e.mb, p.row, col));
+      if (mirrored)
+        tma_store_2d(&maps.piece, two, p.row & 32, piece_row(to, 2 * e.mb, col, p.row));
+    }
+  } else {
+    float x[32];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint4 h = *piece_at(one, lane, k), l = *piece_at(two, lane, k);
+      const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
+      uint32_t nh[4], nl[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 8 * k + 2 * i;
+        // (a + E) X + G X_hi, scaled once
+        const uint64_t old = f2_fma(halves(ls[i]), twice(1.f / kLoScale), halves(hs[i]));
+        const uint64_t y =
+            f2_fma(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), twice(1.f / kScale),
+                   f2_mul(twice(own), old));
+        if (kPhase == kApply) {
+          nh[i] = to_halves(y);
+          nl[i] = to_halves(f2_fma(halves(nh[i]), twice(-kLoScale), f2_mul(y, twice(kLoScale))));
+        } else {
+          f2_unpack(y, x[c], x[c + 1]);
+        }
+      }
+      if (kPhase == kApply) {
+        *piece_at(one, lane, k) = make_uint4(nh[0], nh[1], nh[2], nh[3]);
+        *piece_at(two, lane, k) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
+      }
+    }
+    if constexpr (kPhase == kApply) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(&maps.piece, one, col & 32, piece_row(e.x[t.from ^ 1], 2 * e.nb, p.row, col));
+        tma_store_2d(&maps.piece, two, col & 32, piece_row(e.lo, 2 * e.nb, p.row, col));
+      }
+    } else {
+      finish_last(e, a, p.row, col, lane, x, one, two);
+    }
+  }
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ Maps maps, List list, Args a, int from) {
+    product_kernel(const __grid_constant__ Maps maps, List list, Args a, int steps) {
   extern __shared__ __align__(1024) uint8_t raw[];
   pdl_trigger();
   Smem& s = *reinterpret_cast<Smem*>(raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(cluster_ctarank()), cid = blockIdx.x >> 1;
-  const int n_clusters = gridDim.x >> 1;
-  constexpr bool kSym = kPhase == kGram || kPhase == kSquare;
+  const int rank = static_cast<int>(cluster_ctarank());
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&s.full[i], 1);
@@ -555,10 +869,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&s.acc_full[i], 1);
       mbar_init(&s.acc_empty[i], 2 * kEpiWarps);
     }
-    for (int w = 0; w < kEpiWarps; ++w)
-      for (int i = 0; i < kPlaces; ++i) mbar_init(&s.piece_full[w][i], 1);
+    for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < kPlaces; ++i) {
+        mbar_init(&s.piece_full[h][i], 1);
+        mbar_init(&s.piece_empty[h][i], kEpiWarps / 2);
+      }
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&s.task_full[i], 1);
+      mbar_init(&s.task_empty[i], 2 * (2 + kEpiWarps) + 1);
+    }
     mbar_init(&s.drain, 1);
     s.abort = s.issued = s.consumed = 0;
+    for (int i = 0; i < 4; ++i) s.finished[i] = 0;
     fence_barrier_init();
     tma_prefetch_desc(&maps.tile);
     tma_prefetch_desc(&maps.half);
@@ -569,37 +891,60 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();
   tc_fence_after();
   pdl_wait();
-  const Tile* tiles = kSym ? list.sym : list.all;
-  const int n_tiles = skipped(a) || list.header->abort ? 0 : (kSym ? list.n_sym : list.n_all);
+  const bool none = skipped(a);
   const uint32_t tmem = s.tmem;
   volatile int* abort = &s.abort;
   // stages of a tile: the K of its product over 64
-  auto steps = [&](const Entry& e) { return ((kPhase == kGram ? e.n : e.m) + kK - 1) / kK; };
+  auto stages_of = [&](const Entry& e, const Task& t) {
+    return ((t.phase == kGram ? e.n : e.m) + kK - 1) / kK;
+  };
+  // The n-th task, null when there are no more; its place is used again once all roles are
+  // done with it.
+  auto task = [&](int n) -> const Task* {
+    const int i = n % kRing;
+    if (none || !mbar_wait_cluster(&s.task_full[i], (n / kRing) & 1, abort)) return nullptr;
+    return s.task[i].matrix >= 0 ? &s.task[i] : nullptr;
+  };
+  auto task_done = [&](int n) { mbar_arrive_remote(&s.task_empty[n % kRing], 0); };
 
   if (warp == 0) {
     if (elect_one()) {
       int it = 0;
       bool ok = true;
-      for (int w = cid; ok && w < n_tiles; w += n_clusters) {
-        const Tile t = tiles[w];
-        const Entry& e = list.entries[t.matrix];
-        const int n = steps(e), row_tiles = kPhase == kGram ? 2 * e.nb : 2 * e.mb;
-        const int64_t left = kPhase == kGram ? e.x[from] : (kPhase == kSquare ? e.f : e.g);
+      bool known = false;                 // that what the task needs is there
+      const Task* at;
+      for (int n = 0; ok && (at = task(n)) != nullptr; ++n) {
+        const Task& t = *at;
+        const Entry& e = t.e;
+        if (!known && !wait_done(e.done, t.need, abort, list.header)) break;
+        known = false;
+        const bool gram = t.phase == kGram, sym = gram || t.phase == kSquare;
+        const int count = stages_of(e, t), row_tiles = gram ? 2 * e.nb : 2 * e.mb;
+        const int64_t left = gram ? e.x[t.from] : (sym ? e.f : e.g);
         const bool wide = t.width == kWide;
+        const int nb = e.nb;
         const int32_t ya =
             static_cast<int32_t>((left + static_cast<int64_t>(2 * t.i + rank) * row_tiles) * kTileRows);
         // symmetric: rows of the left operand, 128 or 64 for each CTA; else 64 rows of X, two
         // column tiles or one for each CTA
         int32_t yb;
-        if (kSym)
-          yb = static_cast<int32_t>(
-                   (left + static_cast<int64_t>(2 * t.j + (wide ? rank : 0)) * row_tiles) *
-                   kTileRows) +
-               (wide ? 0 : rank * 64);
+        if (sym)
+          yb = static_cast<int32_t>((left + static_cast<int64_t>(t.j + (wide ? rank : 0)) * row_tiles) *
+                                    kTileRows) + (wide ? 0 : rank * 64);
         else
-          yb = static_cast<int32_t>((e.x[from] + 4 * t.j + (wide ? 2 * rank : rank)) * kTileRows);
-        for (int k = 0; k < n; ++k, ++it) {
+          yb = static_cast<int32_t>((e.x[t.from] + 2 * t.j + (wide ? 2 * rank : rank)) * kTileRows);
+        for (int k = 0; k < count; ++k, ++it) {
           const int st = it % kStages;
+          // a look at the next task while the stages are full anyway
+          if (k == count - 1 && k >= kStages &&
+              mbar_test(&s.task_full[(n + 1) % kRing], ((n + 1) / kRing) & 1)) {
+            const Task* next = task(n + 1);
+            if (next != nullptr &&
+                load_acquire(next->e.done) >= static_cast<unsigned>(next->need)) {
+              fence_proxy_async_all();
+              known = true;
+            }
+          }
           if (!mbar_wait(&s.empty[st], ((it / kStages) & 1) ^ 1, abort)) {
             ok = false;
             break;
@@ -608,32 +953,37 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (rank == 0)
             mbar_arrive_expect_tx(&s.full[st], 2 * (kTileBytes + (wide ? kTileBytes : kHalfTile)));
           tma_load_2d_pair(s.a[st], &maps.tile, &s.full[st], 0, 0, ya + k * kTileRows);
-          if (kSym) {
+          if (sym) {
             tma_load_2d_pair(s.b[st], wide ? &maps.tile : &maps.half, &s.full[st], 0, 0,
                              yb + k * kTileRows);
           } else {
-            const int32_t y = yb + (k >> 1) * 2 * e.nb * kTileRows + (k & 1) * 64;
+            const int32_t y = yb + (k >> 1) * 2 * nb * kTileRows + (k & 1) * 64;
             tma_load_2d_pair(s.b[st], &maps.half, &s.full[st], 0, 0, y);
             if (wide)
               tma_load_2d_pair(s.b[st] + kHalfTile, &maps.half, &s.full[st], 0, 0, y + kTileRows);
           }
         }
+        task_done(n);
       }
       s.issued = it;
     }
   } else if (warp == 1) {
     if (elect_one() && rank == 0) {
-      int it = 0, ti = 0;
+      int it = 0;
       bool ok = true;
-      for (int w = cid; ok && w < n_tiles; w += n_clusters, ++ti) {
-        const Tile t = tiles[w];
-        const int n = steps(list.entries[t.matrix]);
-        const uint32_t idesc = idesc_f16(2 * kBlock, t.width, !kSym);
-        const int acc = ti & 1;
-        if (!mbar_wait(&s.acc_empty[acc], ((ti >> 1) & 1) ^ 1, abort)) break;
+      const Task* at;
+      for (int n = 0; ok && (at = task(n)) != nullptr; ++n) {
+        const int count = stages_of(at->e, *at);
+        const bool sym = at->phase == kGram || at->phase == kSquare;
+        const uint32_t idesc = idesc_f16(2 * kBlock, at->width, !sym);
+        task_done(n);
+        // 16 of K further on: 32 bytes of a row, or 16 rows
+        const uint64_t step = sym ? 2 : 128;
+        const int acc = n & 1;
+        if (!mbar_wait(&s.acc_empty[acc], ((n >> 1) & 1) ^ 1, abort)) break;
         tc_fence_after();
         const uint32_t d = tmem + static_cast<uint32_t>(acc * kWide);
-        for (int k = 0; k < n; ++k, ++it) {
+        for (int k = 0; k < count; ++k, ++it) {
           const int st = it % kStages;
           if (!mbar_wait(&s.full[st], (it / kStages) & 1, abort)) {
             ok = false;
@@ -641,12 +991,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tc_fence_after();
           const uint64_t ad = sdesc_sw128(smem_u32(s.a[st]), 16, 1024);
-          const uint64_t bd = kSym ? sdesc_sw128(smem_u32(s.b[st]), 16, 1024)
-                                   : sdesc_sw128(smem_u32(s.b[st]), kHalfTile, 1024);
+          const uint64_t bd = sdesc_sw128(smem_u32(s.b[st]), sym ? 16 : kHalfTile, 1024);
 #pragma unroll
-          for (int q = 0; q < kK / 16; ++q)   // 16 of K: 32 bytes of a row, or 16 rows
-            mma_bf16_ss_pair(d, ad + 2 * q, bd + (kSym ? 2 : 128) * q, idesc,
-                             (k | q) != 0 ? 1u : 0u);
+          for (int q = 0; q < kK / 16; ++q)
+            mma_bf16_ss_pair(d, ad + 2 * q, bd + step * q, idesc, (k | q) != 0 ? 1u : 0u);
           mma_commit_pair(&s.empty[st], kPairMask);
         }
         if (ok) mma_commit_pair(&s.acc_full[acc], kPairMask);
@@ -655,79 +1003,156 @@ __global__ void __launch_bounds__(kThreads, 1)
       mma_commit_pair(&s.drain, 0x1);
       mbar_wait_limited(&s.drain, 0, kWaitLimitNs);
     }
+  } else if (warp == 3 + kEpiWarps) {
+    // tiles for the pair, a few ahead
+    if (rank == 0 && !none) {
+      const int n_groups = list.header->n_groups;
+      int g = 0;
+      unsigned base = 0;
+      for (int n = 0;; ++n) {
+        const int i = n % kRing;
+        if (!__all_sync(0xffffffffu,
+                        mbar_wait_cluster(&s.task_empty[i], ((n / kRing) & 1) ^ 1, abort)))
+          break;
+        unsigned w = 0;
+        if (lane == 0) w = atomicAdd(&list.header->ticket, 1u);
+        w = __shfl_sync(0xffffffffu, w, 0);
+        Tile x = {-1, 0, 0, 0};
+        int phase = 0, step = 0;
+        unsigned before = 0;
+        for (; g < n_groups; ++g) {
+          const Group q = list.groups[g];
+          const unsigned sym = q.sym1 - q.sym0, all = q.all1 - q.all0, each = 2 * sym + all;
+          if (w - base >= each * steps) {
+            base += each * steps;
+            continue;
+          }
+          step = static_cast<int>((w - base) / each);
+          const unsigned r = (w - base) % each;
+          x = r < 2 * sym ? list.sym[q.sym0 + (r < sym ? r : r - sym)]
+                          : list.all[q.all0 + (r - 2 * sym)];
+          phase = r < sym ? kGram : (r < 2 * sym ? kSquare : (step + 1 < steps ? kApply : kLast));
+          break;
+        }
+        if (__ldcg(&list.header->abort) != 0) x.matrix = -1;
+        x.matrix = __shfl_sync(0xffffffffu, x.matrix, 0);
+        // the entry by words, a few a lane
+        const Entry* e = list.entries + (x.matrix < 0 ? 0 : x.matrix);
+        before = phase == kGram ? 0u : (phase == kSquare ? e->n_sym : 2u * e->n_sym);
+        const int need =
+            static_cast<int>(kTileArrivals * (step * (2u * e->n_sym + e->n_all) + before));
+        const int head[8] = {x.matrix, x.i, x.j, x.width, phase, step & 1, need, 0};
+        int* to = reinterpret_cast<int*>(&s.task[i]);
+        for (int cta = 0; cta < 2; ++cta) {
+          if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) store_remote(head[k], to + k, cta);
+          for (int k = lane; k < kTaskWords - 8; k += 32)
+            store_remote(reinterpret_cast<const int*>(e)[k], to + 8 + k, cta);
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(&s.task_full[i], cta);
+        }
+        if (x.matrix < 0) break;
+      }
+    }
+  } else if (warp == 2 + kEpiWarps) {
+    // The inputs of the pieces, in the order in which they are finished: 32 columns of the
+    // CTA's 128 rows at a time, for each half of the tile's columns.  What the last phase
+    // reads besides, the weights, is brought to L2.
+    int loads = 0;                        // pieces of every warp
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      const Task* at = task(n);
+      if (!__all_sync(0xffffffffu, at != nullptr)) break;
+      const Entry& e = at->e;
+      const int phase = at->phase, half = at->width >> 1, pieces = at->width >> 6;
+      const int first_col = at->j * kBlock, block = 2 * at->i + rank;
+      const int64_t one = (phase == kSquare ? e.f : e.x[at->from]) +
+                          static_cast<int64_t>(block) * 2 * (phase == kSquare ? e.mb : e.nb);
+      const int64_t two = e.lo + static_cast<int64_t>(block) * 2 * e.nb;
+      bool there = true;
+      if (lane == 0) there = wait_done(e.done, at->need, abort, list.header);
+      if (!__all_sync(0xffffffffu, there)) break;
+      if (phase == kLast && e.param != nullptr) prefetch_weights(e, block, first_col, at->width, lane);
+      for (int c = 0; ok && c < pieces; ++c, ++loads) {
+        const int i = loads % kPlaces;
+        for (int h = 0; ok && h < 2; ++h) {
+          ok = mbar_wait_warp(&s.piece_empty[h][i], ((loads / kPlaces) & 1) ^ 1, abort);
+          if (!ok || !elect_one()) continue;
+          const int col = first_col + h * half + 32 * c;
+          uint64_t* bar = &s.piece_full[h][i];
+          if (phase == kGram) {           // nothing to read: the place is free
+            mbar_arrive(bar);
+            continue;
+          }
+          mbar_arrive_expect_tx(bar, phase == kSquare ? 4 * kPiece * 2 + 128 : 8 * kPiece * 2);
+          if (phase == kSquare) bulk_load(s.dj[i][h], e.d + col, 128, bar);
+          tma_load_2d(s.piece[i][0][h], &maps.column, bar, col & 32,
+                      static_cast<int32_t>((one + (col >> 6)) * kTileRows));
+          if (phase != kSquare)
+            tma_load_2d(s.piece[i][1][h], &maps.column, bar, col & 32,
+                        static_cast<int32_t>((two + (col >> 6)) * kTileRows));
+        }
+        __syncwarp();
+      }
+      __syncwarp();
+      if (lane == 0) task_done(n);
+    }
+    // after an abort too: what was issued lands before the CTA ends
+    if (lane == 0)
+      for (int k = loads - kPlaces; *abort && k <= loads; ++k)
+        for (int h = 0; k >= 0 && h < 2; ++h)
+          mbar_wait_limited(&s.piece_full[h][k % kPlaces], (k / kPlaces) & 1, 10ull * 1000 * 1000);
   } else {
     const int ew = warp - 2, q = warp & 3, half = ew >> 2;
-    constexpr bool kReads = kPhase != kGram;
-    auto part_of = [&](const Tile& t) {
-      return Part{(2 * t.i + rank) * kBlock + q * 32, t.j * kWide + half * (t.width >> 1),
-                  t.width >> 6};
-    };
-    // map row of the piece at (row, col) of a matrix whose tiles begin at `first`, row_tiles a
-    // block row; its map column is col & 32
-    auto piece_row = [&](int64_t first, int row_tiles, int row, int col) {
-      return static_cast<int32_t>((first + static_cast<int64_t>(row >> 7) * row_tiles + (col >> 6)) *
-                                      kTileRows + (row & 127));
-    };
-    // The copies run two pieces ahead, over the ends of tiles.
-    int ahead_w = cid, ahead_c = 0, loads = 0;
-    auto load_next = [&]() {
-      if (!kReads || ahead_w >= n_tiles) return;
-      const Tile t = tiles[ahead_w];
-      const Entry& e = list.entries[t.matrix];
-      const Part p = part_of(t);
-      const int place = loads % kPlaces, col = p.col + 32 * ahead_c;
+    unsigned* unsaid = nullptr;           // counter of a tile that this warp has not reported
+    int done = 0;
+    // Reports it once all but `newer` groups of copies are complete: the last of the warps
+    // tells the other CTAs.
+    auto report = [&](int tile, bool newer) {
       if (lane == 0) {
-        uint64_t* bar = &s.piece_full[ew][place];
-        if (kPhase == kSquare) {
-          mbar_arrive_expect_tx(bar, kPiece * 2);
-          tma_load_2d(s.piece[ew][place][0], &maps.piece, bar, col & 32,
-                      piece_row(e.f, 2 * e.mb, p.row, col));
-        } else {
-          mbar_arrive_expect_tx(bar, 2 * kPiece * 2);
-          tma_load_2d(s.piece[ew][place][0], &maps.piece, bar, col & 32,
-                      piece_row(e.x[from], 2 * e.nb, p.row, col));
-          tma_load_2d(s.piece[ew][place][1], &maps.piece, bar, col & 32,
-                      piece_row(e.lo, 2 * e.nb, p.row, col));
+        if (newer) bulk_wait_group1(); else bulk_wait_group0();
+        fence_proxy_async_all();
+        if (atom_add_cta(&s.finished[tile & 3]) == kEpiWarps - 1) {
+          s.finished[tile & 3] = 0;
+          signal(unsaid);
         }
       }
-      ++loads;
-      if (++ahead_c == p.pieces) {
-        ahead_c = 0;
-        ahead_w += n_clusters;
-      }
+      unsaid = nullptr;
     };
-    load_next();
-    load_next();
-    int ti = 0, done = 0;
     bool ok = true;
-    for (int w = cid; ok && w < n_tiles; w += n_clusters, ++ti) {
-      const Tile t = tiles[w];
-      const Entry& e = list.entries[t.matrix];
-      const Part p = part_of(t);
-      const int row = p.row + lane, acc = ti & 1;
-      const bool mirrored = kSym && t.i != t.j && p.row < e.mb * kBlock;
-      float di = 0.f, ae = 0.f;
-      if (kPhase == kSquare) di = e.d[row];
-      if (!kSym) ae = kA + e.e[row];
-      if (!mbar_wait_warp(&s.acc_full[acc], (ti >> 1) & 1, abort)) break;
+    int n = 0;
+    for (; ok; ++n) {
+      const int slot = n % kRing, acc = n & 1;
+      if (none) break;
+      // no waiting with a report to make: others may wait for it
+      if (unsaid != nullptr &&
+          !__all_sync(0xffffffffu, mbar_test(&s.task_full[slot], (n / kRing) & 1)))
+        report(n - 1, false);
+      if (!__all_sync(0xffffffffu, mbar_wait_cluster(&s.task_full[slot], (n / kRing) & 1, abort)))
+        break;
+      const Task& t = s.task[slot];
+      if (t.matrix < 0) break;
+      const Entry& e = t.e;
+      const Place p = place_of(t, rank, ew);
+      if (unsaid != nullptr &&
+          !__all_sync(0xffffffffu, mbar_test(&s.acc_full[acc], (n >> 1) & 1)))
+        report(n - 1, false);
+      if (!mbar_wait_warp(&s.acc_full[acc], (n >> 1) & 1, abort)) break;
       tc_fence_after();
-      for (int c = 0; c < p.pieces; ++c, ++done) {
+      float own = 0.f;                    // of the lane's row: d, or a + e
+      if (t.phase == kSquare) own = __ldcg(&e.d[p.row + lane]);
+      if (t.phase >= kApply) own = kA + __ldcg(&e.e[p.row + lane]);
+      for (int c = 0; c < p.pieces; ++c) {
         const int col = p.col + 32 * c, place = done % kPlaces;
-        uint16_t *one = s.piece[ew][place][0], *two = s.piece[ew][place][1];
-        float dj = 0.f;
-        if (kPhase == kSquare) dj = e.d[col + lane];
+        uint16_t *one = s.piece[place][0][half][q], *two = s.piece[place][1][half][q];
         uint32_t v[32];
-        tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide + (col - t.j * kWide),
-                  v);
-        if (kReads) {
-          if (!mbar_wait_warp(&s.piece_full[ew][place], (done / kPlaces) & 1, abort)) {
-            tmem_ld_wait();
-            ok = false;
-            break;
-          }
-        } else {                          // the copy out of this place has read it
-          if (lane == 0) bulk_wait_group_read1();
-          __syncwarp();
+        tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
+                      (col - t.j * kBlock), v);
+        if (!mbar_wait_warp(&s.piece_full[half][place], (done / kPlaces) & 1, abort)) {
+          tmem_ld_wait();
+          ok = false;
+          break;
         }
         tmem_ld_wait();
         if (c == p.pieces - 1) {          // this warp is done with the accumulator
@@ -735,135 +1160,32 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
         }
-        if constexpr (kSym) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float x[8];
-            if constexpr (kPhase == kGram) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * k + i]) * (1.f / kScale);
-              if (row >= col && row < col + 32) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  if (row == col + 8 * k + i) {
-                    e.d[row] = x[i] * (1.f / kScale);
-                    x[i] = 0.f;
-                  }
-              }
-            } else {
-              float off[8];
-              Granule<__half>::unpack(*piece_at(one, lane, k), off);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float ff = __uint_as_float(v[8 * k + i]) * (1.f / kScale);   // scaled once
-                const float d2 = di + __shfl_sync(0xffffffffu, dj, 8 * k + i);
-                x[i] = fmaf(kC, fmaf(d2, off[i], ff), kB * off[i]);
-                if (row == col + 8 * k + i) {
-                  e.e[row] = fmaf(kC, fmaf(di, di, ff * (1.f / kScale)), kB * di);
-                  x[i] = 0.f;
-                }
-              }
-            }
-            const uint4 h = Granule<__half>::pack(x);
-            *piece_at(one, lane, k) = h;
-            if (mirrored) {
-              const uint32_t words[4] = {h.x, h.y, h.z, h.w};
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                *value_in(two, 8 * k + i, lane) =
-                    static_cast<uint16_t>(words[i >> 1] >> (16 * (i & 1)));
-            }
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            const int64_t to = kPhase == kGram ? e.f : e.g;
-            tma_store_2d(&maps.piece, one, col & 32, piece_row(to, 2 * e.mb, p.row, col));
-            if (mirrored)
-              tma_store_2d(&maps.piece, two, p.row & 32, piece_row(to, 2 * e.mb, col, p.row));
-            bulk_commit_group();
-          }
-        } else {
-          float x[32];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float h[8], l[8];
-            Granule<__half>::unpack(*piece_at(one, lane, k), h);
-            Granule<__half>::unpack(*piece_at(two, lane, k), l);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              x[8 * k + i] = fmaf(ae, fmaf(l[i], 1.f / kLoScale, h[i]),
-                                  __uint_as_float(v[8 * k + i]) * (1.f / kScale));
-          }
-          if constexpr (kPhase == kApply) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint4 h, l;
-              split(x + 8 * k, &h, &l);
-              *piece_at(one, lane, k) = h;
-              *piece_at(two, lane, k) = l;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store_2d(&maps.piece, one, col & 32,
-                           piece_row(e.x[from ^ 1], 2 * e.nb, p.row, col));
-              tma_store_2d(&maps.piece, two, col & 32, piece_row(e.lo, 2 * e.nb, p.row, col));
-              bulk_commit_group();
-            }
-          } else {
-            // 32 x 32 values to the weights: lanes along what is contiguous there, which for
-            // a wide matrix are columns (the values change places in shared memory)
-            if (!e.tall) {
-              float* swap = reinterpret_cast<float*>(one);
-              __syncwarp();               // every lane has read its part of the piece
-#pragma unroll
-              for (int i = 0; i < 32; ++i) swap[lane * 32 + ((i + lane) & 31)] = x[i];
-              __syncwarp();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = swap[i * 32 + ((lane + i) & 31)];
-              __syncwarp();
-              fence_proxy_async_smem();
-            }
-            const int outer = e.tall ? col : p.row, inner = (e.tall ? p.row : col) + lane;
-            const int outers = e.tall ? e.n : e.m, inners = e.tall ? e.m : e.n;
-            if (inner < inners) {
-              const int64_t at = static_cast<int64_t>(outer) * inners + inner;
-              const int some = outers - outer < 32 ? outers - outer : 32;
-              if (!a.muon) {
-                store_rows(x, reinterpret_cast<__nv_bfloat16*>(e.out) + at, inners, some,
-                           1.f / kScale);
-              } else {
-                const float step = -(a.lr * e.scale) * (1.f / kScale);
-                if (e.param_type == DORA_F32)
-                  update_rows(x, static_cast<float*>(e.param) + at, inners, some, a.keep, step);
-                else if (e.param_type == DORA_BF16)
-                  update_rows(x, static_cast<__nv_bfloat16*>(e.param) + at, inners, some, a.keep,
-                              step);
-                else
-                  update_rows(x, static_cast<__half*>(e.param) + at, inners, some, a.keep, step);
-                if (e.copy != nullptr)
-                  store_rows(x, reinterpret_cast<__nv_bfloat16*>(e.copy) + at, inners, some, 1.f);
-              }
-            }
-            __syncwarp();
-          }
+        const float* dj = s.dj[place][half];
+        if (t.phase == kGram)
+          finish_piece<kGram>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
+        else if (t.phase == kSquare)
+          finish_piece<kSquare>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
+        else if (t.phase == kApply)
+          finish_piece<kApply>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
+        else
+          finish_piece<kLast>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
+        // a group of copies for every piece, also where it has none; the one before has read its
+        // place
+        if (lane == 0) {
+          bulk_commit_group();
+          bulk_wait_group_read1();
+          if (done > 0) mbar_arrive(&s.piece_empty[half][(done - 1) % kPlaces]);
         }
-        if (kReads) {
-          // the place two pieces on was copied out one piece ago
-          if (kPhase != kLast && lane == 0) bulk_wait_group_read1();
-          __syncwarp();
-          load_next();
-        }
+        __syncwarp();
+        ++done;
+        if (unsaid != nullptr) report(n - 1, true);
       }
+      unsaid = e.done;
+      __syncwarp();
+      if (lane == 0) task_done(n);
     }
-    if (lane == 0) {
-      bulk_wait_group0();                 // copies are done before the CTA ends
-      // after an abort: those that nobody waited for
-      for (; kReads && done < loads; ++done)
-        mbar_wait_limited(&s.piece_full[ew][done % kPlaces], (done / kPlaces) & 1,
-                          100ull * 1000 * 1000);
-    }
+    if (unsaid != nullptr && ok && !*abort) report(n - 1, false);
+    if (lane == 0) bulk_wait_group0();    // copies are done before the CTA ends
     __syncwarp();
   }
 
@@ -906,12 +1228,16 @@ int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 bool aligned_to(const void* p, int32_t dtype) {
   return (reinterpret_cast<uintptr_t>(p) & (dtype == DORA_F32 ? 3u : 1u)) == 0;
 }
+bool in_quads(const void* p, int32_t dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & (dtype == DORA_F32 ? 15u : 7u)) == 0;
+}
 bool known_type(int32_t t) { return t >= DORA_BF16 && t <= DORA_F32; }
 
 // Sizes of a matrix, and of all of them.
 struct Shape {
   int32_t m, n, mb, nb;
-  int64_t chunks, x_tiles, f_tiles, sym, all, diag;   // diag: blocks of 128 of a diagonal
+  int64_t chunks, x_tiles, f_tiles, diag;   // diag: blocks of 128 of a diagonal
+  int64_t sym[2], all[2];
 };
 Shape shape_of(const dora_matrix& t) {
   Shape s;
@@ -923,18 +1249,24 @@ Shape shape_of(const dora_matrix& t) {
   const int64_t pairs = (s.mb + 1) / 2;
   s.x_tiles = pairs * 2 * 2 * s.nb;
   s.f_tiles = pairs * 2 * 2 * s.mb;
-  s.sym = pairs * (pairs + 1) / 2;
-  s.all = pairs * ((s.nb + 1) / 2);
   s.diag = pairs * 2;
+  // of 256 columns, and of 128
+  s.sym[0] = pairs * (pairs + 1) / 2;
+  s.all[0] = pairs * ((s.nb + 1) / 2);
+  s.sym[1] = pairs * s.mb - pairs * (pairs - 1);
+  s.all[1] = pairs * s.nb;
   return s;
 }
+constexpr int64_t kFewTiles = 76;
 struct Sizes {
   int64_t chunks = 0, x_tiles = 0, sym = 0, all = 0, tiles = 0, diag = 0;
+  int narrow_sym = 0, narrow_all = 0;     // 1: tiles of 128 columns
   bool has_params = true, has_outs = true;
 };
 
 bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
   Sizes z;
+  int64_t sym[2] = {0, 0}, all[2] = {0, 0};
   for (int32_t i = 0; i < count; ++i) {
     const dora_matrix& t = ms[i];
     if (t.rows < 1 || t.cols < 1 || t.grad == nullptr || !known_type(t.grad_dtype) ||
@@ -949,11 +1281,14 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
         !aligned_to(t.out, DORA_BF16))
       return false;
     const Shape s = shape_of(t);
-    if (s.m > ortho::kMaxShort || s.n > ortho::kMaxLong) return false;
+    if (s.m > ortho::kMaxShort || static_cast<int64_t>(s.m) * s.n > ortho::kMaxElements)
+      return false;
     z.chunks += s.chunks;
     z.x_tiles += s.x_tiles;
-    z.sym += s.sym;
-    z.all += s.all;
+    for (int k = 0; k < 2; ++k) {
+      sym[k] += s.sym[k];
+      all[k] += s.all[k];
+    }
     z.tiles += 3 * s.x_tiles + 2 * s.f_tiles;
     z.diag += s.diag;
     if (t.param == nullptr) z.has_params = false;
@@ -961,12 +1296,17 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
     // counted in 32 bits, the tiles' rows among them
     if (z.tiles > (1 << 23) || z.chunks > (1 << 30)) return false;
   }
+  // Narrow tiles where wide ones would leave pairs of SMs without any.
+  z.narrow_sym = sym[0] < kFewTiles;
+  z.narrow_all = all[0] < kFewTiles;
+  z.sym = sym[z.narrow_sym];
+  z.all = all[z.narrow_all];
   *out = z;
   return true;
 }
 
 struct Places {
-  int64_t entries, chunk_of, x, sym, all, partial, norm, ticket, diag, tiles, end;
+  int64_t entries, chunk_of, x, sym, all, groups, partial, norm, ticket, done, diag, tiles, end;
 };
 Places places_of(const Sizes& z, int64_t count) {
   Places p;
@@ -975,17 +1315,25 @@ Places places_of(const Sizes& z, int64_t count) {
   p.x = p.chunk_of + round256(z.chunks * 4);
   p.sym = p.x + round256(z.x_tiles * sizeof(ortho::Tile));
   p.all = p.sym + round256(z.sym * sizeof(ortho::Tile));
-  p.partial = p.all + round256(z.all * sizeof(ortho::Tile));
+  p.groups = p.all + round256(z.all * sizeof(ortho::Tile));
+  p.partial = p.groups + round256(count * sizeof(ortho::Group));
   p.norm = p.partial + round256(z.chunks * 8);
   p.ticket = p.norm + round256(count * 8);
-  p.diag = p.ticket + round256(count * 4);
+  p.done = p.ticket + round256(count * 4);
+  p.diag = p.done + round256(count * 4);
   p.tiles = p.diag + z.diag * 2 * 512;
   p.end = p.tiles + z.tiles * ortho::kTileBytes;
   return p;
 }
 
 ortho::List list_of(const dora_matrix_list& l) {
-  const Sizes z = {l.chunks, l.x_tiles, l.symmetric, l.outputs, l.tiles, l.diagonals};
+  Sizes z;
+  z.chunks = l.chunks;
+  z.x_tiles = l.x_tiles;
+  z.sym = l.symmetric;
+  z.all = l.outputs;
+  z.tiles = l.tiles;
+  z.diag = l.diagonals;
   const Places p = places_of(z, l.count);
   char* at = static_cast<char*>(l.data);
   ortho::List o;
@@ -995,6 +1343,7 @@ ortho::List list_of(const dora_matrix_list& l) {
   o.x = reinterpret_cast<ortho::Tile*>(at + p.x);
   o.sym = reinterpret_cast<ortho::Tile*>(at + p.sym);
   o.all = reinterpret_cast<ortho::Tile*>(at + p.all);
+  o.groups = reinterpret_cast<ortho::Group*>(at + p.groups);
   o.tiles = at + p.tiles;
   o.count = l.count;
   o.n_chunks = static_cast<int>(z.chunks);
@@ -1008,15 +1357,13 @@ bool valid_list(const dora_matrix_list* l) {
   return l != nullptr && l->data != nullptr && l->count >= 1 && l->chunks >= 1 && l->tiles >= 1;
 }
 
-template <ortho::Phase kPhase>
-int launch_product(const ortho::Maps& maps, const ortho::List& l, const ortho::Args& a, int from,
-                   cudaStream_t stream) {
+int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::Args& a, int steps,
+                    cudaStream_t stream) {
   constexpr int smem = sizeof(ortho::Smem);
-  auto kern = ortho::product_kernel<kPhase>;
+  auto kern = ortho::product_kernel;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return launched(e);
-  const int tiles = kPhase == ortho::kGram || kPhase == ortho::kSquare ? l.n_sym : l.n_all;
-  const int pairs = num_sms() / 2;
+  const int tiles = l.n_sym > l.n_all ? l.n_sym : l.n_all, pairs = num_sms() / 2;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1030,7 +1377,7 @@ int launch_product(const ortho::Maps& maps, const ortho::List& l, const ortho::A
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  return launched(cudaLaunchKernelEx(&cfg, kern, maps, l, a, from));
+  return launched(cudaLaunchKernelEx(&cfg, kern, maps, l, a, steps));
 }
 
 int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaStream_t stream) {
@@ -1046,13 +1393,7 @@ int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaS
   if (e == DORA_OK)
     e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
                             dim3(ortho::kRowThreads), 0, stream, l, a));
-  for (int s = 0; s < steps && e == DORA_OK; ++s) {
-    e = launch_product<ortho::kGram>(maps, l, a, s & 1, stream);
-    if (e == DORA_OK) e = launch_product<ortho::kSquare>(maps, l, a, s & 1, stream);
-    if (e == DORA_OK)
-      e = s + 1 < steps ? launch_product<ortho::kApply>(maps, l, a, s & 1, stream)
-                        : launch_product<ortho::kLast>(maps, l, a, s & 1, stream);
-  }
+  if (e == DORA_OK) e = launch_products(maps, l, a, steps, stream);
   return e;
 }
 }  // namespace
@@ -1093,6 +1434,7 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   const uint64_t rows = static_cast<uint64_t>(z.tiles) * ortho::kTileRows;
   if (encode_tmap_2d_bf16(&maps.tile, at + p.tiles, 64, rows, 128, 64, 128) != 0 ||
       encode_tmap_2d_bf16(&maps.half, at + p.tiles, 64, rows, 128, 64, 64) != 0 ||
+      encode_tmap_2d_bf16(&maps.column, at + p.tiles, 64, rows, 128, 32, 128, 64) != 0 ||
       encode_tmap_2d_bf16(&maps.piece, at + p.tiles, 64, rows, 128, 32, 32, 64) != 0)
     return DORA_ERR_CUDA;
   memcpy(l.map, &maps, sizeof(maps));
@@ -1118,6 +1460,8 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.m = s.m;
       e.n = s.n;
       e.tall = t.rows > t.cols;
+      e.quads = (t.cols & 3) == 0 && in_quads(t.param, t.param_dtype) && in_quads(t.copy, DORA_BF16) &&
+                in_quads(t.out, DORA_BF16);
       e.mb = s.mb;
       e.nb = s.nb;
       e.x[0] = tile;
@@ -1132,15 +1476,20 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.partial = reinterpret_cast<ortho::Squares*>(at + p.partial) + chunk;
       e.norm = reinterpret_cast<float2*>(at + p.norm) + first + i;
       e.ticket = reinterpret_cast<unsigned*>(at + p.ticket) + first + i;
+      e.done = reinterpret_cast<unsigned*>(at + p.done) + first + i;
       e.chunks = static_cast<int32_t>(s.chunks);
+      e.n_sym = static_cast<int32_t>(s.sym[z.narrow_sym]);
+      e.n_all = static_cast<int32_t>(s.all[z.narrow_all]);
+      e.sym_width = z.narrow_sym ? 128 : 256;
+      e.all_width = z.narrow_all ? 128 : 256;
       e.first_chunk = chunk;
       e.first_x = x;
       e.first_sym = sym;
       e.first_all = all;
       chunk += s.chunks;
       x += s.x_tiles;
-      sym += s.sym;
-      all += s.all;
+      sym += e.n_sym;
+      all += e.n_all;
     }
     const int rc = launched(launch_pdl(ortho::fill_entries_kernel, dim3(1), dim3(32), 0, stream, o,
                                        first, some, args));
@@ -1148,6 +1497,7 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   }
   int64_t most = z.chunks > z.x_tiles ? z.chunks : z.x_tiles;
   if (z.sym > most) most = z.sym;
+  if (z.all > most) most = z.all;
   const int rc = launched(launch_pdl(ortho::fill_tiles_kernel,
                                      dim3(static_cast<unsigned>((most + 127) / 128)), dim3(128), 0,
                                      stream, o));
