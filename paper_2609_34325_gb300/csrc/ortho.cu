@@ -17,7 +17,8 @@
 //   E = b D + c (D^2 + diag(F F)),  G = b F + c (D F + F D + F F) off the diagonal,
 //   X <- (a + E) X + G X_hi,
 // so that what is rounded is multiplied by the small G rather than by B, whose product with
-// X nearly cancels against a X.  The result is 2e-4 to 1.2e-3 off the iteration in 64 bits
+// X nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
+// step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the iteration in 64 bits
 // (relative 2-norm), half the rounding of a bf16 output.
 //
 // Layout.  X hi, X lo, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
@@ -42,10 +43,10 @@ namespace dora {
 namespace ortho {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr float kScale = 256.f;           // of X, F and G in fp16: their values are below 4
-constexpr float kLoScale = 2048.f;        // of lo, on top of it
+// Factors of X and F in fp16, whose values stay below 1.21 and 1.5; G has none.
+constexpr float kXScale = 32768.f, kFScale = 256.f;
 constexpr int kMaxSteps = 32;
-constexpr int64_t kGroup = 24 << 20;      // elements of a group of matrices, about
+constexpr int64_t kGroup = 64 << 20;      // elements of a group of matrices, about
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
@@ -433,7 +434,7 @@ __device__ __forceinline__ void split(const float* v, uint4* hi, uint4* lo) {
   *hi = Granule<__half>::pack(v);
   Granule<__half>::unpack(*hi, back);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rest[i] = (v[i] - back[i]) * kLoScale;
+  for (int i = 0; i < 8; ++i) rest[i] = v[i] - back[i];
   *lo = Granule<__half>::pack(rest);
 }
 
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          v[i] = update_of(a, d[y][i] * f, a.muon ? m[y][i] : 0.f) * norm.y * norm.x * kScale;
+          v[i] = update_of(a, d[y][i] * f, a.muon ? m[y][i] : 0.f) * norm.y * norm.x * kXScale;
         uint4 h, l;
         split(v, &h, &l);
         const uint32_t to = tile_offset(r, piece * 8);
@@ -520,9 +521,10 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
 // One MMA spans a pair, each CTA holding its 128 rows of the left operand and half of the right
 // one, so that a stage is 32 KB for each.  In a CTA one warp copies operands into a ring of
 // stages, one issues the MMAs (in the first CTA) into one of two accumulators, and eight finish
-// the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo) an eleventh
-// warp copies ahead of them, into three places for each, where it is written over and
-// copied out.  A last warp of the first CTA fetches the tiles.
+// the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo) a warp
+// copies ahead of them, into three places for each, where it is written over, and from where
+// another one copies it out and reports the tile.  The second CTA's idle MMA warp fetches
+// the tiles.
 // ---------------------------------------------------------------------------
 enum Phase { kGram, kSquare, kApply, kLast };
 
@@ -553,12 +555,11 @@ struct Smem {
   uint16_t piece[kPlaces][2][2][4][kPiece];   // of each half of the columns, four warps' rows
   float dj[kPlaces][2][32];               // of the diagonal of A
   uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
-  uint64_t piece_full[2][kPlaces], piece_empty[2][kPlaces];
+  uint64_t piece_full[2][kPlaces], piece_done[2][kPlaces], piece_empty[2][kPlaces];
   uint64_t task_full[kRing], task_empty[kRing];
   Task task[kRing];
   uint32_t tmem;
   int abort, issued, consumed;
-  int finished[4];                        // warps that have finished a tile, of four in turn
 };
 static_assert(sizeof(Smem) <= 227 * 1024, "shared memory");
 
@@ -597,14 +598,6 @@ __device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
 __device__ __forceinline__ unsigned load_relaxed(const unsigned* p) {
   unsigned v;
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-  return v;
-}
-__device__ __forceinline__ int atom_add_cta(int* p) {
-  int v;
-  asm volatile("atom.acq_rel.cta.shared::cta.add.s32 %0, [%1], 1;"
-               : "=r"(v)
-               : "r"(smem_u32(p))
-               : "memory");
   return v;
 }
 // Wait until at most one bulk group of this thread has not completed.
@@ -651,24 +644,6 @@ __device__ __forceinline__ void prefetch_weights(const Entry& e, int block, int 
                                                         size_of(e.param_type)));
 }
 
-// The part of an output tile that warp w of a CTA finishes: 32 rows (those of the lanes of
-// tensor memory that the warp may read), half of the columns.
-struct Place {
-  int row, col;                           // first row, first column in the matrix
-  int pieces;
-};
-__device__ __forceinline__ Place place_of(const Task& t, int rank, int w) {
-  return Place{(2 * t.i + rank) * kBlock + ((w + 2) & 3) * 32,
-               t.j * kBlock + (w >> 2) * (t.width >> 1), t.width >> 6};
-}
-
-// Map row of the piece at (row, col) of a matrix whose tiles begin at `first`, row_tiles to
-// a block row; its map column is col & 32.
-__device__ __forceinline__ int32_t piece_row(int64_t first, int row_tiles, int row, int col) {
-  return static_cast<int32_t>((first + static_cast<int64_t>(row >> 7) * row_tiles + (col >> 6)) *
-                                  kTileRows + (row & 127));
-}
-
 // Two values of a 16-byte part, as a pair of fp32.
 __device__ __forceinline__ uint64_t halves(uint32_t w) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -712,7 +687,7 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
       *part(lane, k) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
   }
   __syncwarp();
-  const float step = a.muon ? -(a.lr * e.scale) * (1.f / kScale) : 1.f / kScale;
+  const float step = a.muon ? -(a.lr * e.scale) * (1.f / kXScale) : 1.f / kXScale;
   if (quads) {
     const int k = lane & 7, i0 = lane >> 3;
     const int64_t at = static_cast<int64_t>(outer + i0) * inners + inner + 4 * k;
@@ -751,21 +726,19 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
       }
     }
   }
-  fence_proxy_async_smem();
-  __syncwarp();
 }
 
 // What finishes 32 x 32 values of an accumulator, v, whose other inputs lie in `one`, `two`
 // and, the diagonal over its columns, `dj`.
 template <Phase kPhase>
-__device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, const Args& a,
-                                             const Task& t, const Place& p, int col, int lane,
-                                             float own, const float* dj, const uint32_t (&v)[32],
-                                             uint16_t* one, uint16_t* two) {
-  const int row = p.row + lane;
+__device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int row0, int col,
+                                             bool mirrored, int lane, float own, const float* dj,
+                                             const uint32_t (&v)[32], uint16_t* one,
+                                             uint16_t* two) {
+  const int row = row0 + lane;
   if constexpr (kPhase == kGram || kPhase == kSquare) {
-    const bool mirrored = t.j >= 2 * t.i + 2 && p.row < e.mb * kBlock;
-    const bool diagonal = col == p.row;   // pieces hold it or nothing of it
+    const bool diagonal = col == row0;    // pieces hold it or nothing of it
+    const uint64_t base = twice(fmaf(kC, own, kB) * (1.f / kFScale));
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t words[4];
@@ -774,26 +747,25 @@ __device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, c
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = 8 * k + 2 * i;
-        // scaled once
-        uint64_t x = f2_mul(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])),
-                            twice(1.f / kScale));
+        const uint64_t acc = f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+        uint64_t x;
         float d0, d1;
         if (kPhase == kGram) {
+          x = f2_mul(acc, twice(kFScale / (kXScale * kXScale)));
           if (diagonal) {
             f2_unpack(x, d0, d1);
-            if (lane == c || lane == c + 1) e.d[row] = (lane == c ? d0 : d1) * (1.f / kScale);
+            if (lane == c || lane == c + 1) e.d[row] = (lane == c ? d0 : d1) * (1.f / kFScale);
           }
         } else {
+          // c F F + (b + c (d_i + d_j)) f
+          x = f2_mul(acc, twice(kC / (kFScale * kFScale)));
           if (diagonal) {
             f2_unpack(x, d0, d1);
             if (lane == c || lane == c + 1)
-              e.e[row] = fmaf(kC, fmaf(own, own, (lane == c ? d0 : d1) * (1.f / kScale)), kB * own);
+              e.e[row] = fmaf(fmaf(kC, own, kB), own, lane == c ? d0 : d1);
           }
-          // b f + c (F F + (d_i + d_j) f)
           const float2 d = *reinterpret_cast<const float2*>(dj + c);
-          const uint64_t off = halves(old[i]);
-          const uint64_t d2 = f2_add(f2_pack(d.x, d.y), twice(own));
-          x = f2_fma(twice(kC), f2_fma(d2, off, x), f2_mul(twice(kB), off));
+          x = f2_fma(halves(old[i]), f2_fma(f2_pack(d.x, d.y), twice(kC / kFScale), base), x);
         }
         if (diagonal) {
           f2_unpack(x, d0, d1);
@@ -805,14 +777,6 @@ __device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, c
       *piece_at(one, lane, k) = h;
       if (mirrored) mirror(two, 8 * k, lane, h);
     }
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      const int64_t to = kPhase == kGram ? e.f : e.g;
-      tma_store_2d(&maps.piece, one, col & 32, piece_row(to, 2 * e.mb, p.row, col));
-      if (mirrored)
-        tma_store_2d(&maps.piece, two, p.row & 32, piece_row(to, 2 * e.mb, col, p.row));
-    }
   } else {
     float x[32];
 #pragma unroll
@@ -823,14 +787,12 @@ __device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, c
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = 8 * k + 2 * i;
-        // (a + E) X + G X_hi, scaled once
-        const uint64_t old = f2_fma(halves(ls[i]), twice(1.f / kLoScale), halves(hs[i]));
-        const uint64_t y =
-            f2_fma(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), twice(1.f / kScale),
-                   f2_mul(twice(own), old));
+        // (a + E) X + G X_hi
+        const uint64_t y = f2_fma(twice(own), f2_add(halves(hs[i]), halves(ls[i])),
+                                  f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])));
         if (kPhase == kApply) {
           nh[i] = to_halves(y);
-          nl[i] = to_halves(f2_fma(halves(nh[i]), twice(-kLoScale), f2_mul(y, twice(kLoScale))));
+          nl[i] = to_halves(f2_fma(halves(nh[i]), twice(-1.f), y));
         } else {
           f2_unpack(y, x[c], x[c + 1]);
         }
@@ -840,16 +802,7 @@ __device__ __forceinline__ void finish_piece(const Maps& maps, const Entry& e, c
         *piece_at(two, lane, k) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
       }
     }
-    if constexpr (kPhase == kApply) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        tma_store_2d(&maps.piece, one, col & 32, piece_row(e.x[t.from ^ 1], 2 * e.nb, p.row, col));
-        tma_store_2d(&maps.piece, two, col & 32, piece_row(e.lo, 2 * e.nb, p.row, col));
-      }
-    } else {
-      finish_last(e, a, p.row, col, lane, x, one, two);
-    }
+    if constexpr (kPhase == kLast) finish_last(e, a, row0, col, lane, x, one, two);
   }
 }
 
@@ -872,15 +825,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int h = 0; h < 2; ++h)
       for (int i = 0; i < kPlaces; ++i) {
         mbar_init(&s.piece_full[h][i], 1);
-        mbar_init(&s.piece_empty[h][i], kEpiWarps / 2);
+        mbar_init(&s.piece_done[h][i], kEpiWarps / 2);
+        mbar_init(&s.piece_empty[h][i], 1);
       }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(&s.task_full[i], 1);
-      mbar_init(&s.task_empty[i], 2 * (2 + kEpiWarps) + 1);
+      mbar_init(&s.task_empty[i], 2 * (3 + kEpiWarps) + 1);
     }
     mbar_init(&s.drain, 1);
     s.abort = s.issued = s.consumed = 0;
-    for (int i = 0; i < 4; ++i) s.finished[i] = 0;
     fence_barrier_init();
     tma_prefetch_desc(&maps.tile);
     tma_prefetch_desc(&maps.half);
@@ -905,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (none || !mbar_wait_cluster(&s.task_full[i], (n / kRing) & 1, abort)) return nullptr;
     return s.task[i].matrix >= 0 ? &s.task[i] : nullptr;
   };
-  auto task_done = [&](int n) { mbar_arrive_remote(&s.task_empty[n % kRing], 0); };
+  auto task_done = [&](int n) { mbar_arrive_remote(&s.task_empty[n % kRing], 1); };
 
   if (warp == 0) {
     if (elect_one()) {
@@ -967,8 +920,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       s.issued = it;
     }
-  } else if (warp == 1) {
-    if (elect_one() && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
+    if (elect_one()) {
       int it = 0;
       bool ok = true;
       const Task* at;
@@ -1003,9 +956,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       mma_commit_pair(&s.drain, 0x1);
       mbar_wait_limited(&s.drain, 0, kWaitLimitNs);
     }
-  } else if (warp == 3 + kEpiWarps) {
+  } else if (warp == 1) {
     // tiles for the pair, a few ahead
-    if (rank == 0 && !none) {
+    if (!none) {
       const int n_groups = list.header->n_groups;
       int g = 0;
       unsigned base = 0;
@@ -1103,89 +1056,126 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int k = loads - kPlaces; *abort && k <= loads; ++k)
         for (int h = 0; k >= 0 && h < 2; ++h)
           mbar_wait_limited(&s.piece_full[h][k % kPlaces], (k / kPlaces) & 1, 10ull * 1000 * 1000);
-  } else {
-    const int ew = warp - 2, q = warp & 3, half = ew >> 2;
-    unsigned* unsaid = nullptr;           // counter of a tile that this warp has not reported
-    int done = 0;
-    // Reports it once all but `newer` groups of copies are complete: the last of the warps
-    // tells the other CTAs.
-    auto report = [&](int tile, bool newer) {
-      if (lane == 0) {
-        if (newer) bulk_wait_group1(); else bulk_wait_group0();
+  } else if (warp == 3 + kEpiWarps) {
+    // What the pieces became, out of their places: half a tile's columns, the CTA's rows.
+    if (elect_one()) {
+      unsigned* unsaid = nullptr;         // counter of a tile that is not reported
+      uint64_t* place = nullptr;          // of the copies before the newest
+      int done = 0;
+      bool ok = true;
+      // a tile is reported once its copies are complete: all but the newest, or all
+      auto report = [&](bool newest_too) {
+        if (newest_too) bulk_wait_group0(); else bulk_wait_group1();
         fence_proxy_async_all();
-        if (atom_add_cta(&s.finished[tile & 3]) == kEpiWarps - 1) {
-          s.finished[tile & 3] = 0;
-          signal(unsaid);
+        signal(unsaid);
+        unsaid = nullptr;
+      };
+      for (int n = 0; ok; ++n) {
+        // no waiting with a report to make: others may wait for it
+        if (unsaid != nullptr && !mbar_test(&s.task_full[n % kRing], (n / kRing) & 1)) report(true);
+        const Task* at = task(n);
+        if (at == nullptr) break;
+        const Entry& e = at->e;
+        const int phase = at->phase, half = at->width >> 1, pieces = at->width >> 6;
+        const int first_col = at->j * kBlock, block = 2 * at->i + rank, mb = e.mb;
+        const int row_tiles = phase == kApply ? 2 * e.nb : 2 * mb;
+        const int64_t to = phase == kGram ? e.f : (phase == kSquare ? e.g : e.x[at->from ^ 1]);
+        const int64_t one = to + static_cast<int64_t>(block) * row_tiles;
+        const int64_t two = e.lo + static_cast<int64_t>(block) * row_tiles;
+        const bool mirrored = phase < kApply && at->j >= 2 * at->i + 2 && block < mb;
+        for (int c = 0; ok && c < pieces; ++c, ++done) {
+          const int i = done % kPlaces;
+          for (int h = 0; h < 2; ++h) {
+            if (unsaid != nullptr && !mbar_test(&s.piece_done[h][i], (done / kPlaces) & 1))
+              report(true);
+            ok = mbar_wait(&s.piece_done[h][i], (done / kPlaces) & 1, abort);
+            if (!ok) break;
+            const int col = first_col + h * half + 32 * c;
+            if (phase != kLast)
+              tma_store_2d(&maps.column, s.piece[i][0][h], col & 32,
+                           static_cast<int32_t>((one + (col >> 6)) * kTileRows));
+            if (phase == kApply)
+              tma_store_2d(&maps.column, s.piece[i][1][h], col & 32,
+                           static_cast<int32_t>((two + (col >> 6)) * kTileRows));
+            if (mirrored)
+              for (int w = 0; w < 4; ++w)   // 32 columns of the mirror image each
+                tma_store_2d(&maps.piece, s.piece[i][1][h][w], (w & 1) * 32,
+                             static_cast<int32_t>(
+                                 (to + static_cast<int64_t>(col >> 7) * row_tiles + 2 * block +
+                                  (w >> 1)) * kTileRows + (col & 127)));
+            bulk_commit_group();          // also without any: one for every place
+            bulk_wait_group_read1();
+            if (place != nullptr) mbar_arrive(place);
+            place = &s.piece_empty[h][i];
+            if (unsaid != nullptr) report(false);
+          }
         }
+        unsaid = e.done;
+        task_done(n);
       }
-      unsaid = nullptr;
-    };
+      if (unsaid != nullptr && ok && !*abort) report(true);
+      bulk_wait_group0();                 // copies are done before the CTA ends
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    int done = 0;
     bool ok = true;
-    int n = 0;
-    for (; ok; ++n) {
+    for (int n = 0; ok; ++n) {
       const int slot = n % kRing, acc = n & 1;
-      if (none) break;
-      // no waiting with a report to make: others may wait for it
-      if (unsaid != nullptr &&
-          !__all_sync(0xffffffffu, mbar_test(&s.task_full[slot], (n / kRing) & 1)))
-        report(n - 1, false);
-      if (!__all_sync(0xffffffffu, mbar_wait_cluster(&s.task_full[slot], (n / kRing) & 1, abort)))
+      if (none || !__all_sync(0xffffffffu,
+                              mbar_wait_cluster(&s.task_full[slot], (n / kRing) & 1, abort)))
         break;
       const Task& t = s.task[slot];
       if (t.matrix < 0) break;
       const Entry& e = t.e;
-      const Place p = place_of(t, rank, ew);
-      if (unsaid != nullptr &&
-          !__all_sync(0xffffffffu, mbar_test(&s.acc_full[acc], (n >> 1) & 1)))
-        report(n - 1, false);
+      const int phase = t.phase, pieces = t.width >> 6;
+      const int row0 = (2 * t.i + rank) * kBlock + q * 32;
+      const int col0 = t.j * kBlock + half * (t.width >> 1);
+      const bool mirrored = t.j >= 2 * t.i + 2;
       if (!mbar_wait_warp(&s.acc_full[acc], (n >> 1) & 1, abort)) break;
       tc_fence_after();
+      const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
+                            half * (t.width >> 1);
+      uint32_t next[32];
+      tmem_ld32(from, next);
       float own = 0.f;                    // of the lane's row: d, or a + e
-      if (t.phase == kSquare) own = __ldcg(&e.d[p.row + lane]);
-      if (t.phase >= kApply) own = kA + __ldcg(&e.e[p.row + lane]);
-      for (int c = 0; c < p.pieces; ++c) {
-        const int col = p.col + 32 * c, place = done % kPlaces;
+      if (phase == kSquare) own = __ldcg(&e.d[row0 + lane]);
+      if (phase >= kApply) own = kA + __ldcg(&e.e[row0 + lane]);
+      for (int c = 0; c < pieces; ++c, ++done) {
+        const int col = col0 + 32 * c, place = done % kPlaces;
         uint16_t *one = s.piece[place][0][half][q], *two = s.piece[place][1][half][q];
+        tmem_ld_wait();
         uint32_t v[32];
-        tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
-                      (col - t.j * kBlock), v);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = next[i];
+        if (c + 1 < pieces) {
+          tmem_ld32(from + 32 * (c + 1), next);
+        } else {                          // this warp is done with the accumulator
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
+        }
         if (!mbar_wait_warp(&s.piece_full[half][place], (done / kPlaces) & 1, abort)) {
           tmem_ld_wait();
           ok = false;
           break;
         }
-        tmem_ld_wait();
-        if (c == p.pieces - 1) {          // this warp is done with the accumulator
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
-        }
         const float* dj = s.dj[place][half];
-        if (t.phase == kGram)
-          finish_piece<kGram>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
-        else if (t.phase == kSquare)
-          finish_piece<kSquare>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
-        else if (t.phase == kApply)
-          finish_piece<kApply>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
+        if (phase == kGram)
+          finish_piece<kGram>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+        else if (phase == kSquare)
+          finish_piece<kSquare>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+        else if (phase == kApply)
+          finish_piece<kApply>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
         else
-          finish_piece<kLast>(maps, e, a, t, p, col, lane, own, dj, v, one, two);
-        // a group of copies for every piece, also where it has none; the one before has read its
-        // place
-        if (lane == 0) {
-          bulk_commit_group();
-          bulk_wait_group_read1();
-          if (done > 0) mbar_arrive(&s.piece_empty[half][(done - 1) % kPlaces]);
-        }
+          finish_piece<kLast>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+        fence_proxy_async_smem();
         __syncwarp();
-        ++done;
-        if (unsaid != nullptr) report(n - 1, true);
+        if (lane == 0) mbar_arrive(&s.piece_done[half][place]);
       }
-      unsaid = e.done;
       __syncwarp();
       if (lane == 0) task_done(n);
     }
-    if (unsaid != nullptr && ok && !*abort) report(n - 1, false);
-    if (lane == 0) bulk_wait_group0();    // copies are done before the CTA ends
     __syncwarp();
   }
 
