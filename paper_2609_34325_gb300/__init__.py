@@ -1016,8 +1016,9 @@ def _logit_rows(logits, classes):
 
 
 def _same_device(first, *others):
+    at = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != at:
             raise ValueError("all tensors must be on one device")
 
 

@@ -34,7 +34,16 @@ using policy::RowSum;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxTop = 32;
-constexpr int kCandidates = 256;
+
+// A key into CTA `cta` of the cluster.
+__device__ __forceinline__ void store_key_remote(uint64_t v, uint64_t* to, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.shared::cluster.u64 [ra], %2;\n\t}" ::"r"(smem_u32(to)),
+      "r"(cta), "l"(v)
+      : "memory");
+}
 
 // A batch of rows; T is their type.
 template <typename T>
@@ -165,124 +174,287 @@ __device__ __forceinline__ float threshold(const float (&m)[kPer], int top) {
   return unordered(lo);
 }
 
-// A CTA a row, its granules dealt out to the threads in turn.
+// Puts the found keys in order, `mine` of them for each of `lanes` lanes, and writes the row's
+// alternatives; equal keys there are none.
+__device__ __forceinline__ void write_top(const Outputs& o, int64_t at, const uint64_t* keys,
+                                          int found, int lane, int lanes, float m, float inv_t,
+                                          float ls) {
+  for (int i = lane; i < found; i += lanes) {
+    const uint64_t key = keys[i];
+    int before = 0;
+    for (int c = 0; c < found; ++c) before += keys[c] > key;
+    if (before < o.top) {
+      o.top_logp[at + before] = fmaf(value_of(key) - m, inv_t, -ls);
+      o.top_tokens[at + before] = index_of(key);
+    }
+  }
+  for (int i = found + lane; i < o.top; i += lanes) {
+    o.top_logp[at + i] = -INFINITY;
+    o.top_tokens[at + i] = -1;
+  }
+}
+// A row that is not finite has no order.
+__device__ __forceinline__ void write_no_top(const Outputs& o, int64_t at, int lane, int lanes) {
+  for (int i = lane; i < o.top; i += lanes) {
+    o.top_logp[at + i] = NAN;
+    o.top_tokens[at + i] = -1;
+  }
+}
+__device__ __forceinline__ uint64_t warp_largest(uint64_t key) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const uint64_t other = __shfl_xor_sync(0xffffffffu, key, off);
+    key = other > key ? other : key;
+  }
+  return key;
+}
+// The keys of granule i that are at or above tau, to `keep`.
+template <typename T, typename F>
+__device__ __forceinline__ void for_candidates(uint4 q, int first, float tau, F keep) {
+  constexpr int kE = Granule<T>::kElems;
+  float v[kE];
+  Granule<T>::unpack(q, v);
+#pragma unroll
+  for (int e = 0; e < kE; ++e)
+    if (v[e] >= tau && v[e] > -INFINITY) keep(key_of(v[e], first + e));
+}
+// The largest key of granule i below `last`, or `best`.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) logprob_cta_kernel(Batch<T> b, Outputs o) {
-  constexpr int kE = Granule<T>::kElems, kU = 4;
-  __shared__ Part slots[kWarps];
-  __shared__ float maxima[kThreads], tau_at;
-  __shared__ int owners[kThreads], n_owners, n_candidates;
-  __shared__ uint64_t candidates[kCandidates], best[kWarps];
+__device__ __forceinline__ uint64_t largest_below(uint4 q, int first, uint64_t last,
+                                                  uint64_t best) {
+  for_candidates<T>(q, first, -INFINITY, [&](uint64_t key) {
+    if (key < last && key > best) best = key;
+  });
+  return best;
+}
+
+// Short rows: a warp holds one, kHeld granules a lane.
+template <typename T, int kHeld>
+__global__ void __launch_bounds__(kThreads) logprob_warp_kernel(Batch<T> b, Outputs o) {
+  constexpr int kE = Granule<T>::kElems, kKeys = 128;
+  __shared__ uint64_t all_keys[kWarps][kKeys];
+  __shared__ int n_keys[kWarps];
   pdl_wait();
-  const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint64_t* keys = all_keys[warp];
   const float scale = b.inv_t * policy::kLog2e;
-  for (int row = blockIdx.x; row < b.rows; row += gridDim.x) {
+  const int step = gridDim.x * kWarps;
+  for (int row = blockIdx.x * kWarps + warp; row < b.rows; row += step) {
     const RowUse use = row_use(b, row);
     if (use.kind != kComputed) {
-      fill_row(o, row, use.kind == kNone ? 0.f : NAN, me, kThreads, b.status);
+      fill_row(o, row, use.kind == kNone ? 0.f : NAN, lane, 32, b.status);
       continue;
     }
     const int n = use.n;
     const RowPtr<T> z(b.logits + row * b.ld, n);
+    uint4 q[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) q[u] = z.load(lane + 32 * u, n);
     float za = 0.f;
-    if (me == 0 && use.token >= 0) za = to_float(z.z[use.token]);
+    if (use.token >= 0) za = to_float(z.z[use.token]);
     RowSum x;
     x.clear();
-    for (int i = me; i < z.some_hi; i += kU * kThreads) {
-      uint4 q[kU];
+    constexpr int kStep = kHeld < 4 ? kHeld : 4;
 #pragma unroll
-      for (int u = 0; u < kU; ++u) q[u] = z.load(i + u * kThreads, n);
-      x.add<T>(q, scale);
+    for (int u = 0; u < kHeld; u += kStep) {
+      uint4 some[kStep];
+#pragma unroll
+      for (int v = 0; v < kStep; ++v) some[v] = q[u + v];
+      if (kHeld <= 4 || 32 * u < z.some_hi) x.add<T>(some, scale);
     }
+    const Part part = x.over(32, scale);
+    const float ls = write_row(o, row, part, za, use.token >= 0, b.inv_t, lane == 0);
+    if (o.top == 0) continue;
+    const int64_t at = static_cast<int64_t>(row) * o.top;
+    if (!isfinite(ls)) {
+      write_no_top(o, at, lane, 32);
+      continue;
+    }
+    const float mine[1] = {x.m};
+    const float tau = threshold<1>(mine, o.top);
+    if (lane == 0) n_keys[warp] = 0;
+    __syncwarp();
+    // few lanes have any: read again, so that the others' registers are not held
+    if (x.m >= tau && x.m > -INFINITY)
+#pragma unroll 1
+      for (int i = lane; i < z.some_hi; i += 32)
+        for_candidates<T>(z.load(i, n), i * kE - z.mis, tau, [&](uint64_t key) {
+          const int c = atomicAdd(&n_keys[warp], 1);
+          if (c < kKeys) keys[c] = key;
+        });
+    __syncwarp();
+    int found = n_keys[warp];
+    if (found > kKeys) {                  // many equal logits: one by one
+      uint64_t last = ~0ull;
+      __syncwarp();
+      for (found = 0; found < o.top; ++found) {
+        uint64_t best = 0;
+#pragma unroll 1
+        for (int i = lane; i < z.some_hi; i += 32)
+          best = largest_below<T>(z.load(i, n), i * kE - z.mis, last, best);
+        last = warp_largest(best);
+        if (last == 0) break;
+        if (lane == 0) keys[found] = last;
+      }
+      __syncwarp();
+    }
+    write_top(o, at, keys, found, lane, 32, part.m, b.inv_t, ls);
+    __syncwarp();
+  }
+}
+
+// Longer rows: a CTA a row, or a cluster of kCtas, an equal part of its granules each, dealt
+// out to the threads in turn.  The next granules are on their way while some are added, and a
+// row's first while the one before is put in order.
+template <typename T, int kBlock, int kCtas>
+__global__ void __launch_bounds__(kBlock, 1024 / kBlock)
+    logprob_cta_kernel(Batch<T> b, Outputs o) {
+  constexpr int kE = Granule<T>::kElems, kW = kBlock / 32, kU = 4;
+  constexpr int kKeys = kCtas > 1 ? 64 : 256;   // of a CTA
+  __shared__ Part slots[kW], parts[kCtas];
+  __shared__ float maxima[kBlock], tau_at;
+  __shared__ int owners[kBlock], n_owners, n_keys, found_in[kCtas];
+  __shared__ uint64_t keys[kCtas * kKeys], best[kW];
+  const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
+  const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const float scale = b.inv_t * policy::kLog2e;
+  const int step = gridDim.x / kCtas;
+  if (me == 0) n_owners = n_keys = 0;
+  if (kCtas > 1) cluster_sync();          // the others are there to be written to
+  pdl_wait();
+
+  RowUse use = {kNone, -1, 0};
+  uint4 q[kU];
+  // a row and its first granules
+  auto begin = [&](int row) {
+    use = row < b.rows ? row_use(b, row) : RowUse{kNone, -1, 0};
+    if (use.kind != kComputed) return;
+    const RowPtr<T> z(b.logits + row * b.ld, use.n);
+    const int each = (z.some_hi + kCtas - 1) / kCtas, hi = min((rank + 1) * each, z.some_hi);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = rank * each + me + u * kBlock;
+      q[u] = z.load(i < hi ? i : z.some_hi, use.n);
+    }
+  };
+  int row = blockIdx.x / kCtas;
+  begin(row);
+  for (; row < b.rows; row += step) {
+    const RowUse now = use;
+    if (now.kind != kComputed) {
+      if (rank == 0)
+        fill_row(o, row, now.kind == kNone ? 0.f : NAN, me, kBlock, b.status);
+      begin(row + step);
+      continue;
+    }
+    const int n = now.n;
+    const RowPtr<T> z(b.logits + row * b.ld, n);
+    const int each = (z.some_hi + kCtas - 1) / kCtas;
+    const int lo = rank * each, hi = min(lo + each, z.some_hi);
+    float za = 0.f;
+    if (me == 0 && now.token >= 0) za = to_float(z.z[now.token]);
+    RowSum x;
+    x.clear();
+    for (int i = lo + me; i < hi; i += kU * kBlock) {
+      uint4 next[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int k = i + (kU + u) * kBlock;
+        next[u] = z.load(k < hi ? k : z.some_hi, n);
+      }
+      x.add<T>(q, scale);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) q[u] = next[u];
+    }
+    begin(row + step);
     Part part = x.over(32, scale);
     if (lane == 0) slots[warp] = part;
     maxima[me] = x.m;
-    if (me == 0) n_owners = n_candidates = 0;
     __syncthreads();
-    part = policy::join_parts<kWarps>(slots, scale);
-    const float ls = write_row(o, row, part, za, use.token >= 0, b.inv_t, me == 0);
+    part = policy::join_parts<kW>(slots, scale);
+    if (kCtas > 1) {
+      if (me < kCtas) policy::store_part_remote(part, &parts[rank], me);
+    }
+    const int64_t at = static_cast<int64_t>(row) * o.top;
     if (o.top > 0) {
-      const int64_t at = static_cast<int64_t>(row) * o.top;
-      if (!isfinite(ls)) {                // a row that is not finite has no order
-        for (int i = me; i < o.top; i += kThreads) {
-          o.top_logp[at + i] = NAN;
-          o.top_tokens[at + i] = -1;
-        }
-      } else {
-        if (warp == 0) {
-          float m[kWarps];
+      if (warp == 0) {
+        float m[kW];
 #pragma unroll
-          for (int i = 0; i < kWarps; ++i) m[i] = maxima[lane + 32 * i];
-          const float t = threshold<kWarps>(m, o.top);
-          if (lane == 0) tau_at = t;
+        for (int i = 0; i < kW; ++i) m[i] = maxima[lane + 32 * i];
+        const float t = threshold<kW>(m, o.top);
+        if (lane == 0) tau_at = t;
+      }
+      __syncthreads();
+      const float tau = tau_at;
+      if (x.m >= tau && x.m > -INFINITY) owners[atomicAdd(&n_owners, 1)] = me;
+      __syncthreads();
+      const int own = n_owners;
+      for (int w = warp; w < own; w += kW)
+        for (int i = lo + owners[w] + lane * kBlock; i < hi; i += 32 * kBlock)
+          for_candidates<T>(z.load(i, n), i * kE - z.mis, tau, [&](uint64_t key) {
+            const int c = atomicAdd(&n_keys, 1);
+            if (c < kKeys) keys[rank * kKeys + c] = key;
+          });
+      __syncthreads();
+      int found = n_keys;
+      if (found > kKeys) {                // many equal logits: one by one
+        uint64_t last = ~0ull;
+        __syncthreads();
+        for (found = 0; found < o.top; ++found) {
+          uint64_t mine = 0;
+          for (int i = lo + me; i < hi; i += kBlock)
+            mine = largest_below<T>(z.load(i, n), i * kE - z.mis, last, mine);
+          mine = warp_largest(mine);
+          if (lane == 0) best[warp] = mine;
+          __syncthreads();
+          last = best[0];
+#pragma unroll
+          for (int w = 1; w < kW; ++w) last = best[w] > last ? best[w] : last;
+          __syncthreads();
+          if (last == 0) break;
+          if (me == 0) keys[rank * kKeys + found] = last;
         }
         __syncthreads();
-        const float tau = tau_at;
-        if (x.m >= tau && x.m > -INFINITY) owners[atomicAdd(&n_owners, 1)] = me;
-        __syncthreads();
-        const int own = n_owners;
-        for (int w = warp; w < own; w += kWarps)
-          for (int i = owners[w] + lane * kThreads; i < z.some_hi; i += 32 * kThreads) {
-            float v[kE];
-            Granule<T>::unpack(z.load(i, n), v);
-#pragma unroll
-            for (int e = 0; e < kE; ++e)
-              if (v[e] >= tau && v[e] > -INFINITY) {
-                const int c = atomicAdd(&n_candidates, 1);
-                if (c < kCandidates) candidates[c] = key_of(v[e], i * kE - z.mis + e);
-              }
-          }
-        __syncthreads();
-        const int found = n_candidates;
-        if (found <= kCandidates) {
-          if (me < found) {
-            const uint64_t key = candidates[me];
-            int before = 0;
-            for (int c = 0; c < found; ++c) before += candidates[c] > key;
-            if (before < o.top) {
-              o.top_logp[at + before] = fmaf(value_of(key) - part.m, b.inv_t, -ls);
-              o.top_tokens[at + before] = index_of(key);
-            }
-          }
-          if (me >= found && me < o.top) {
-            o.top_logp[at + me] = -INFINITY;
-            o.top_tokens[at + me] = -1;
-          }
+      }
+      if (kCtas > 1) {                    // to the first CTA
+        if (rank != 0)
+          for (int i = me; i < found; i += kBlock)
+            store_key_remote(keys[rank * kKeys + i], &keys[rank * kKeys + i], 0);
+        if (me == 0) store_remote(found, &found_in[rank], 0);
+      } else if (me == 0) {
+        found_in[0] = found;
+      }
+    }
+    if (kCtas > 1) cluster_sync();        // the parts and the keys have arrived
+    else if (o.top > 0) __syncthreads();
+    if (me == 0) n_owners = n_keys = 0;
+    if (rank == 0) {
+      if (kCtas > 1) part = policy::join_parts<kCtas>(parts, scale);
+      const float ls = write_row(o, row, part, za, now.token >= 0, b.inv_t, me == 0);
+      if (o.top > 0) {
+        if (!isfinite(ls)) {
+          write_no_top(o, at, me, kBlock);
         } else {
-          uint64_t last = ~0ull;
-          for (int rank = 0; rank < o.top; ++rank) {
-            uint64_t mine = 0;
-            for (int i = me; i < z.some_hi; i += kThreads) {
-              float v[kE];
-              Granule<T>::unpack(z.load(i, n), v);
-#pragma unroll
-              for (int e = 0; e < kE; ++e) {
-                const uint64_t key = v[e] > -INFINITY ? key_of(v[e], i * kE - z.mis + e) : 0;
-                if (key < last && key > mine) mine = key;
-              }
+          int found = found_in[0];
+          if (kCtas > 1) {                // close the gaps between the CTAs' keys
+            found = 0;
+            for (int c = 0; c < kCtas; ++c) {
+              const int some = found_in[c];
+              uint64_t key = 0;
+              if (me < some) key = keys[c * kKeys + me];
+              __syncthreads();
+              if (me < some) keys[found + me] = key;
+              found += some;
             }
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) {
-              const uint64_t other = __shfl_xor_sync(0xffffffffu, mine, off);
-              mine = other > mine ? other : mine;
-            }
-            if (lane == 0) best[warp] = mine;
             __syncthreads();
-            mine = best[0];
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) mine = best[w] > mine ? best[w] : mine;
-            __syncthreads();
-            if (me == 0) {
-              o.top_logp[at + rank] =
-                  mine != 0 ? fmaf(value_of(mine) - part.m, b.inv_t, -ls) : -INFINITY;
-              o.top_tokens[at + rank] = mine != 0 ? index_of(mine) : -1;
-            }
-            last = mine;
           }
+          write_top(o, at, keys, found, me, kBlock, part.m, b.inv_t, ls);
         }
       }
     }
-    __syncthreads();                      // the shared places are free for the next row
+    // the shared places are free for the next row
+    if (kCtas > 1) cluster_sync();
+    else __syncthreads();
   }
 }
 
@@ -329,36 +501,57 @@ __device__ __forceinline__ uint4 grad_granule(uint4 q, const RowGrad& k, float s
   return Granule<T>::pack(d);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(Batch<T> b, GradIn<T> g) {
-  constexpr int kE = Granule<T>::kElems;
+// A row, or kUnit granules of one: kU granules for each of kLanes lanes, all loaded before the
+// first is computed.  Rows of up to 128 granules are a warp's; longer ones are cut, and the units
+// dealt out in turn.
+constexpr int kUnit = 4 * kThreads;
+
+template <typename T, int kLanes, int kU>
+__global__ void __launch_bounds__(kThreads, 4)
+    logprob_grad_kernel(Batch<T> b, GradIn<T> g, int64_t units, int a_row) {
+  constexpr int kE = Granule<T>::kElems, kTeams = kThreads / kLanes;
   pdl_wait();
-  const int me = threadIdx.x;
+  const int me = threadIdx.x % kLanes;
   const float scale = b.inv_t * policy::kLog2e;
-  for (int row = blockIdx.x; row < b.rows; row += gridDim.x) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kTeams;
+  for (int64_t unit = static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / kLanes;
+       unit < units; unit += step) {
+    const int row = a_row == 1 ? static_cast<int>(unit) : static_cast<int>(unit / a_row);
+    const int first = a_row == 1 ? 0 : static_cast<int>(unit - static_cast<int64_t>(row) * a_row) *
+                                           (kU * kLanes);
     const RowUse use = row_use(b, row);
-    const int n = use.kind == kComputed ? use.n : 0;
+    const bool live = use.kind == kComputed;
+    const int n = live ? use.n : 0;
     const RowPtr<T> z(b.logits + row * b.ld, n);
+    uint4 q[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) q[u] = z.load(first + me + u * kLanes, n);
     T* dz = g.grad + row * b.ld;
     const bool aligned = policy::same_alignment(dz, z.z);
     const int end = z.granules(b.classes);
-    if (use.kind != kComputed) {
-      if (use.kind == kInvalid && me == 0) record_status(b.status, DORA_ERR_DEVICE_BAD_COUNT);
+    if (live) {
+      const RowGrad k = row_grad(b, g, row);
+      const int at = use.token + z.mis;   // of the token among the granules' elements
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = first + me + u * kLanes;
+        if (i >= end) continue;
+        const uint4 v = grad_granule<T>(q[u], k, scale, use.token >= 0 ? at - i * kE : -1);
+        if (aligned && z.whole(i)) *(z.as_granules(dz) + i) = v;
+        else z.store_part(dz, aligned, i, n, b.classes, v);
+      }
+    } else {
+      if (use.kind == kInvalid && me == 0 && first == 0)
+        record_status(b.status, DORA_ERR_DEVICE_BAD_COUNT);
       float v[kE];
 #pragma unroll
       for (int e = 0; e < kE; ++e) v[e] = use.kind == kInvalid ? NAN : 0.f;
-      const uint4 q = Granule<T>::pack(v);
-      for (int i = me; i < end; i += kThreads)
-        z.store_part(dz, aligned, i, b.classes, b.classes, q);
-      continue;
-    }
-    const RowGrad k = row_grad(b, g, row);
-    const int at = use.token + z.mis;     // of the token among the granules' elements
-    for (int i = me; i < end; i += kThreads) {
-      const int token = use.token >= 0 ? at - i * kE : -1;
-      const uint4 v = grad_granule<T>(z.load(i, n), k, scale, token);
-      if (aligned && z.whole(i)) *(z.as_granules(dz) + i) = v;
-      else z.store_part(dz, aligned, i, n, b.classes, v);
+      const uint4 fill = Granule<T>::pack(v);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = first + me + u * kLanes;
+        if (i < end) z.store_part(dz, aligned, i, b.classes, b.classes, fill);
+      }
     }
   }
 }
@@ -402,16 +595,64 @@ logprob::Batch<T> batch_of(const void* logits, int32_t rows, int32_t classes, in
           status};
 }
 
+template <typename T, int kBlock, int kCtas>
+int launch_rows(const logprob::Batch<T>& b, const logprob::Outputs& o, int teams,
+                cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (kCtas > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = kCtas;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl_enabled()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.gridDim = dim3(teams * kCtas);
+  cfg.blockDim = dim3(kBlock);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return launched(cudaLaunchKernelEx(&cfg, logprob::logprob_cta_kernel<T, kBlock, kCtas>, b, o));
+}
+
 template <typename T>
 int launch_logprob(const logprob::Batch<T>& b, const logprob::Outputs& o, cudaStream_t stream) {
-  return launched(launch_pdl(logprob::logprob_cta_kernel<T>, dim3(grid_for(b.rows, 4)),
-                             dim3(logprob::kThreads), 0, stream, b, o));
+  // granules that a row may touch
+  const int64_t need = (b.classes + 2 * Granule<T>::kElems - 2) / Granule<T>::kElems;
+  const int sms = num_sms(), eights = grid_for((b.rows + 7) / 8, 8);
+  const auto warps = [&](auto kern) {
+    return launched(launch_pdl(kern, dim3(eights), dim3(logprob::kThreads), 0, stream, b, o));
+  };
+  if (need <= 32) return warps(logprob::logprob_warp_kernel<T, 1>);
+  if (need <= 128) return warps(logprob::logprob_warp_kernel<T, 4>);
+  if (need <= 256 && b.rows > 8 * sms) return warps(logprob::logprob_warp_kernel<T, 8>);
+  int ctas = 1;
+  while (ctas < 8 && b.rows * ctas * 2 <= sms && need > 512 * ctas) ctas *= 2;
+  switch (ctas) {
+    case 1: return launch_rows<T, 128, 1>(b, o, grid_for(b.rows, 8), stream);
+    case 2: return launch_rows<T, 256, 2>(b, o, b.rows, stream);
+    case 4: return launch_rows<T, 256, 4>(b, o, b.rows, stream);
+    default: return launch_rows<T, 256, 8>(b, o, b.rows, stream);
+  }
 }
 
 template <typename T>
 int launch_grad(const logprob::Batch<T>& b, const logprob::GradIn<T>& g, cudaStream_t stream) {
-  return launched(launch_pdl(logprob::logprob_grad_kernel<T>, dim3(grid_for(b.rows, 8)),
-                             dim3(logprob::kThreads), 0, stream, b, g));
+  const int64_t need = (b.classes + 2 * Granule<T>::kElems - 2) / Granule<T>::kElems;
+  const int64_t most = num_sms() * 8;
+  const auto run = [&](auto kern, int64_t units, int a_row, int teams) {
+    const int64_t ctas = (units + teams - 1) / teams;
+    return launched(launch_pdl(kern, dim3(static_cast<unsigned>(ctas < most ? ctas : most)),
+                               dim3(logprob::kThreads), 0, stream, b, g, units, a_row));
+  };
+  if (need <= 32) return run(logprob::logprob_grad_kernel<T, 32, 1>, b.rows, 1, 8);
+  if (need <= 128) return run(logprob::logprob_grad_kernel<T, 32, 4>, b.rows, 1, 8);
+  const int64_t a_row = (need + logprob::kUnit - 1) / logprob::kUnit;
+  return run(logprob::logprob_grad_kernel<T, 256, 4>, b.rows * a_row, static_cast<int>(a_row), 1);
 }
 }  // namespace
 
