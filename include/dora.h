@@ -912,7 +912,8 @@ int dora_adam_step(const dora_param_list* list, void* state, double lr, double b
  * dora_matrix_list_prepare writes the list into `data` (device,
  * dora_matrix_list_size bytes, 256-byte aligned) and fills the host handle *list, which
  * the calls below take; done once for a set of buffers.  The list's memory also holds the
- * iterations' matrices (about 6 bytes an element, 4 for the square of the shorter side):
+ * iterations' matrices (about 6 bytes an element, 4 for the square of the shorter side; none for
+ * matrices of at most 128 x 2048):
  * calls on one list, captured ones that are replayed among them, are ordered on one
  * stream.  dora_matrix_list_size is 0 for arguments that prepare refuses.
  */
@@ -932,7 +933,7 @@ typedef struct dora_matrix_list {
   int32_t count;
   int32_t has_params;   /* 1: every matrix has param and momentum */
   int32_t has_outs;     /* 1: every matrix has out */
-  int32_t pad;
+  int32_t large, parts, pad;
   uint64_t map[64];
 } dora_matrix_list;
 size_t dora_matrix_list_size(const dora_matrix* matrices, int32_t count);

@@ -999,27 +999,35 @@ def dora_pl_policy_loss(scores, cu, k, order, old_logp, advantages, logp, worksp
 
 
 def _logit_rows(logits, classes):
-    """(data pointer, type, rows, classes, row stride) of a 2-D tensor of logits whose rows are
-    contiguous."""
+    """(data pointer, type, rows, classes, row stride, device) of a 2-D tensor of logits whose
+    rows are contiguous."""
     dt = _DTYPES.get(logits.dtype) if isinstance(logits, _Tensor) and logits.is_cuda else None
     if dt is None or logits.dim() != 2:
         raise TypeError("logits must be a 2-D CUDA tensor of bf16, fp16 or fp32")
     rows, cols = logits.shape
-    ld = logits.stride(0) if rows > 1 else cols
-    if (cols > 1 and logits.stride(1) != 1) or ld < cols:
+    ld, one = logits.stride()
+    if rows <= 1:
+        ld = cols
+    if (one != 1 and cols > 1) or ld < cols:
         raise TypeError("the rows of logits must be contiguous and not overlap")
     classes = cols if classes is None else int(classes)
     if not 1 <= classes <= cols:
         raise ValueError("classes must be in [1, logits.shape[1]]")
-    _in_32_bits(rows, classes)
-    return logits.data_ptr(), dt, rows, classes, ld
+    if rows > _I32_MAX or classes > _I32_MAX:
+        _in_32_bits(rows, classes)
+    return logits.data_ptr(), dt, rows, classes, ld, logits.get_device()
 
 
-def _same_device(first, *others):
-    at = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != at:
+def _rows(t, dtype, n, device, name):
+    """_vec_opt of a tensor on that device."""
+    if t is None:
+        return None
+    if not (type(t) is _Tensor and t.dtype is dtype and t.numel() == n and
+            t.get_device() == device and t.is_contiguous()):
+        _vec(t, dtype, n, name)
+        if t.get_device() != device:
             raise ValueError("all tensors must be on one device")
+    return t.data_ptr()
 
 
 def dora_token_logprob(logits, tokens, logp, classes=None, legal=None, temperature=1.0,
@@ -1030,7 +1038,7 @@ def dora_token_logprob(logits, tokens, logp, classes=None, legal=None, temperatu
     entropies and ``norm`` (fp32 [R], [R, 2]: the largest logit and the log of the sum over it)
     and the most probable tokens top_logp fp32 and top_tokens int32 [R, k], k up to 32.
     ``logits``, ``classes`` and ``legal`` as in dora_policy_loss."""
-    at, dt, rows, classes, ld = _logit_rows(logits, classes)
+    at, dt, rows, classes, ld, dev = _logit_rows(logits, classes)
     top = 0
     if (top_logp is None) != (top_tokens is None) or (tokens is None) != (logp is None):
         raise ValueError("top_logp and top_tokens, and tokens and logp, are given together")
@@ -1038,13 +1046,14 @@ def dora_token_logprob(logits, tokens, logp, classes=None, legal=None, temperatu
         if top_logp.dim() != 2 or top_logp.size(0) != rows or top_tokens.shape != top_logp.shape:
             raise ValueError("top_logp and top_tokens must be [R, k]")
         top = top_logp.size(1)
-    _same_device(logits, tokens, logp, legal, entropy, norm, top_logp, top_tokens, status)
     code = load_library().dora_token_logprob(
-        at, dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
-        _vec_opt(tokens, _I32, rows, "tokens"), temperature, top,
-        _vec_opt(logp, _F32, rows, "logp"), _vec_opt(entropy, _F32, rows, "entropy"),
-        _vec_opt(norm, _F32, 2 * rows, "norm"), _opt(top_logp, _F32, "top_logp"),
-        _opt(top_tokens, _I32, "top_tokens"), _opt(status, _I32, "status"), _stream(stream))
+        at, dt, rows, classes, ld, _rows(legal, _I32, rows, dev, "legal"),
+        _rows(tokens, _I32, rows, dev, "tokens"), temperature, top,
+        _rows(logp, _F32, rows, dev, "logp"), _rows(entropy, _F32, rows, dev, "entropy"),
+        _rows(norm, _F32, 2 * rows, dev, "norm"),
+        _rows(top_logp, _F32, top * rows, dev, "top_logp"),
+        _rows(top_tokens, _I32, top * rows, dev, "top_tokens"), _opt(status, _I32, "status"),
+        _stream(stream))
     if code:
         _check(code, "dora_token_logprob")
     return logp
@@ -1054,22 +1063,25 @@ def dora_token_logprob_grad(logits, tokens, norm, grad, dlogp=None, dentropy=Non
                             classes=None, legal=None, temperature=1.0, status=None, stream=None):
     """d loss / d logits into ``grad`` (like logits, or logits itself) from dlogp and dentropy
     (fp32 [R], one of them may be None), with the forward's norm and, for dentropy, entropy."""
-    at, dt, rows, classes, ld = _logit_rows(logits, classes)
+    at, dt, rows, classes, ld, dev = _logit_rows(logits, classes)
     if grad is not logits and not (
-            isinstance(grad, _Tensor) and grad.is_cuda and grad.dtype is logits.dtype and
-            grad.shape == logits.shape and (grad.stride(0) == ld or rows <= 1) and
-            (grad.stride(1) == 1 or grad.size(1) == 1)):
+            isinstance(grad, _Tensor) and grad.dtype is logits.dtype and
+            grad.get_device() == dev and grad.shape == logits.shape and
+            (grad.stride() == logits.stride() or (
+                (grad.stride(0) == ld or rows <= 1) and
+                (grad.stride(1) == 1 or grad.size(1) == 1)))):
         raise TypeError("grad must be like logits: device, type, shape and strides")
     if (dlogp is None and dentropy is None) or (dlogp is not None and tokens is None) or (
             dentropy is not None and entropy is None):
         raise ValueError("dlogp, which needs tokens, or dentropy, which needs entropy, is required")
-    _same_device(logits, tokens, norm, grad, dlogp, dentropy, entropy, legal, status)
+    if norm is None:
+        raise TypeError("norm is required")
     code = load_library().dora_token_logprob_grad(
-        at, dt, rows, classes, ld, _vec_opt(legal, _I32, rows, "legal"),
-        _vec_opt(tokens, _I32, rows, "tokens"), temperature, _vec(norm, _F32, 2 * rows, "norm"),
-        _vec_opt(entropy, _F32, rows, "entropy"), _vec_opt(dlogp, _F32, rows, "dlogp"),
-        _vec_opt(dentropy, _F32, rows, "dentropy"), grad.data_ptr(), _opt(status, _I32, "status"),
-        _stream(stream))
+        at, dt, rows, classes, ld, _rows(legal, _I32, rows, dev, "legal"),
+        _rows(tokens, _I32, rows, dev, "tokens"), temperature,
+        _rows(norm, _F32, 2 * rows, dev, "norm"), _rows(entropy, _F32, rows, dev, "entropy"),
+        _rows(dlogp, _F32, rows, dev, "dlogp"), _rows(dentropy, _F32, rows, dev, "dentropy"),
+        grad.data_ptr(), _opt(status, _I32, "status"), _stream(stream))
     if code:
         _check(code, "dora_token_logprob_grad")
     return grad
@@ -1229,7 +1241,7 @@ class _MatrixC(ctypes.Structure):
 class _MatrixListC(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(n, _i64) for n in ("chunks", "x_tiles", "symmetric", "outputs",
                                                       "tiles", "diagonals")] + [
-        (n, _i32) for n in ("count", "has_params", "has_outs", "pad")] + [
+        (n, _i32) for n in ("count", "has_params", "has_outs", "large", "parts", "pad")] + [
         ("map", ctypes.c_uint64 * 64)]
 
 

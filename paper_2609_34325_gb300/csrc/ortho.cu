@@ -76,6 +76,7 @@ struct Entry {
   int32_t chunks;
   int32_t n_sym, n_all;                   // its tiles of A and B, and of X
   int32_t sym_width, all_width;           // their columns
+  int32_t parts;                          // of a small matrix: CTAs
   // first of its chunks, of its tiles of X and of its output tiles among the list's
   int64_t first_chunk, first_x, first_sym, first_all;
 };
@@ -100,7 +101,7 @@ struct Tile {
 
 struct List {
   Header* header;
-  Entry* entries;
+  Entry* entries;                         // `count` of them, then the small matrices'
   int32_t* chunk_of;                      // matrix of every chunk
   Tile *x, *sym, *all;
   Group* groups;
@@ -119,7 +120,7 @@ __global__ void fill_entries_kernel(List list, int first, int count, FillArgs ar
   if (first == 0 && threadIdx.x == 0) list.header->abort = 0;
   if (threadIdx.x < count) {
     list.entries[first + threadIdx.x] = args.e[threadIdx.x];
-    *args.e[threadIdx.x].ticket = 0;
+    if (args.e[threadIdx.x].ticket != nullptr) *args.e[threadIdx.x].ticket = 0;
   }
 }
 
@@ -163,7 +164,7 @@ __global__ void fill_tiles_kernel(List list) {
     const int j = 2 * i + at * each;
     list.sym[t] = Tile{q, i, j, j + each <= e.mb ? e.sym_width : 128};
   }
-  if (t == 0) {                           // whole matrices until a group is large enough
+  if (t == 0 && list.count > 0) {         // whole matrices until a group is large enough
     int n = 0;
     int64_t size = 0;
     Group g = {0, 0, 0, 0};
@@ -1199,6 +1200,371 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();                         // no CTA leaves while its peer may still signal it
 }
 
+// ---------------------------------------------------------------------------
+// Small matrices (m <= 128, n <= 2048): a whole step in one launch.  A CTA, or a cluster of 2, 4
+// or 8, holds one, 256 columns of X each, in shared memory; A, B and what they are made of are
+// 128 x 128.  Where there are several CTAs each adds up its rows of X X^T over all of them and
+// sends every one its rows of F.  What bounds it is the chain of three products an iteration,
+// each with its reading of tensor memory: the twelve matrices of the actor took 126 us of
+// hand-offs between CTAs in the kernel above.
+// ---------------------------------------------------------------------------
+constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
+constexpr int kSmallThreads = 256;
+
+struct SmallSmem {
+  uint8_t hi[kSmallTiles][kTileBytes], lo[kSmallTiles][kTileBytes];
+  uint8_t f[2][kTileBytes], g[2][kTileBytes], extra[2][kTileBytes];
+  float d[kSmallRows], e[kSmallRows];
+  Squares sums[kMaxParts], scratch[kSmallThreads / 32];
+  uint64_t done;                          // the MMAs of a product
+  uint32_t tmem;
+  int abort, bad[kMaxParts];
+};
+static_assert(sizeof(SmallSmem) <= 227 * 1024, "shared memory");
+
+// 16-byte part k of row r of a tile, where the tensor cores look for it.
+__device__ __forceinline__ uint4* tile_part(uint8_t* tile, int r, int k) {
+  return reinterpret_cast<uint4*>(tile + r * 128 + ((k ^ (r & 7)) << 4));
+}
+// Part k of row r of a 128 x 128 matrix of fp32 values.
+__device__ __forceinline__ uint4* wide_part(uint8_t* matrix, int r, int k) {
+  return reinterpret_cast<uint4*>(matrix + r * 512 + ((k ^ (r & 31)) << 4));
+}
+__device__ __forceinline__ uint4 load_remote(const uint4* from, uint32_t cta) {
+  uint4 q;
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %4, %5;\n\t"
+      "ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [ra];\n\t}"
+      : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+      : "r"(smem_u32(from)), "r"(cta)
+      : "memory");
+  return q;
+}
+__device__ __forceinline__ void store_remote_part(uint4 q, uint4* to, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.shared::cluster.v4.u32 [ra], {%2, %3, %4, %5};\n\t}" ::"r"(smem_u32(to)),
+      "r"(cta), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w)
+      : "memory");
+}
+
+// The gradient and momentum of eight columns from `col` of a row; what is not there is 0.
+__device__ __forceinline__ void load_update(const Entry& e, const Args& a, int row, int col,
+                                            bool quads, float* d, float* m) {
+  const int some = row < e.m ? e.n - col : 0;
+  const int64_t step = e.tall ? e.m : 1;
+  const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
+                           : static_cast<int64_t>(row) * e.n + col;
+  if (quads && some >= 8) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      unpack_quad(whole_quad(e.grad, e.grad_type, k + i), e.grad_type, d + i);
+      if (a.muon) Granule<float>::unpack(whole_quad(e.momentum, DORA_F32, k + i), m + i);
+    }
+    return;
+  }
+  if (e.grad_type == DORA_F32)
+    load_eight(static_cast<const float*>(e.grad) + k, step, some, d);
+  else if (e.grad_type == DORA_BF16)
+    load_eight(static_cast<const __nv_bfloat16*>(e.grad) + k, step, some, d);
+  else
+    load_eight(static_cast<const __half*>(e.grad) + k, step, some, d);
+  if (a.muon) load_eight(e.momentum + k, step, some, m);
+}
+__device__ __forceinline__ void store_momentum(const Entry& e, int row, int col, bool quads,
+                                               const float* m) {
+  const int some = row < e.m ? e.n - col : 0;
+  const int64_t step = e.tall ? e.m : 1;
+  const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
+                           : static_cast<int64_t>(row) * e.n + col;
+  if (quads && some >= 8) {
+    store_quad(m, e.momentum, DORA_F32, k);
+    store_quad(m + 4, e.momentum, DORA_F32, k + 4);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < some) e.momentum[k + i * step] = m[i];
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1)
+    small_kernel(List list, Args a, int steps, int cluster) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  SmallSmem& s = *reinterpret_cast<SmallSmem*>(raw);
+  const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
+  const int rank = cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  pdl_wait();
+  const Entry& e = list.entries[list.count + blockIdx.x / cluster];
+  const int parts = e.parts;
+  if (skipped(a) || rank >= parts) return;  // those that have left are not waited for
+  if (me == 0) {
+    mbar_init(&s.done, 1);
+    s.abort = 0;
+    fence_barrier_init();
+  }
+  if (warp == 0) tmem_alloc(&s.tmem, 512);
+  tc_fence_before();
+  // all CTAs of the matrix: also that the others are there
+  auto sync = [&]() {
+    if (parts > 1) cluster_sync();
+    else __syncthreads();
+  };
+  sync();
+  tc_fence_after();
+  const uint32_t tmem = s.tmem;
+  volatile int* abort = &s.abort;
+  const int all = (e.n + 63) / 64, each = (all + parts - 1) / parts;
+  const int tile0 = rank * each, tiles = max(0, min(each, all - tile0)), col0 = 64 * tile0;
+  const int halves = (e.m + 63) / 64;     // of the products over m
+  const float f = factor(a);
+  const bool quads = !e.tall && (e.n & 7) == 0 && in_quads(e.grad, e.grad_type) &&
+                     (!a.muon || in_quads(e.momentum, DORA_F32));
+
+  // momentum and the update's norm, then the normalised update
+  auto place = [&](int w, int* r, int* k) {   // lanes along what is contiguous
+    *r = e.tall ? w % kSmallRows : w / (8 * tiles);
+    *k = e.tall ? w / kSmallRows : w % (8 * tiles);
+  };
+  Squares sum = {0.f, -126};
+  for (int w = me; w < kSmallRows * 8 * tiles; w += kSmallThreads) {
+    int r, k;
+    place(w, &r, &k);
+    float d[8], m[8], u[8];
+    load_update(e, a, r, col0 + 8 * k, quads, d, m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      d[i] *= f;
+      if (a.muon) m[i] = fmaf(a.mu, m[i], a.omu * d[i]);
+      u[i] = update_of(a, d[i], m[i]);
+    }
+    if (a.muon) store_momentum(e, r, col0 + 8 * k, quads, m);
+    sum.add(squares_of(u));
+  }
+  sum = block_squares(sum, s.scratch);
+  if (me == 0)
+    for (int c = 0; c < parts; ++c) {
+      if (parts > 1) {
+        store_remote(__float_as_int(sum.sum), reinterpret_cast<int*>(&s.sums[rank].sum), c);
+        store_remote(sum.k, &s.sums[rank].k, c);
+      } else {
+        s.sums[0] = sum;
+      }
+    }
+  sync();
+  sum = s.sums[0];
+  for (int c = 1; c < parts; ++c) sum.add(s.sums[c]);
+  const float inv = (sum.sum == 0.f ? 0.f : (isfinite(sum.sum) ? 1.f / sqrtf(sum.sum) : NAN)),
+              near1 = __uint_as_float(static_cast<uint32_t>(127 - sum.k) << 23);
+  for (int w = me; w < kSmallRows * 8 * tiles; w += kSmallThreads) {
+    int r, k;
+    place(w, &r, &k);
+    float d[8], m[8], v[8];
+    load_update(e, a, r, col0 + 8 * k, quads, d, m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      v[i] = update_of(a, d[i] * f, a.muon ? m[i] : 0.f) * near1 * inv *
+             kXScale;
+    uint4 h, l;
+    split(v, &h, &l);
+    *tile_part(s.hi[k >> 3], r, k & 7) = h;
+    *tile_part(s.lo[k >> 3], r, k & 7) = l;
+  }
+
+  const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  const uint32_t lanes = static_cast<uint32_t>(q * 32) << 16;
+  int products = 0;
+  // What the threads wrote to shared memory is there for the tensor cores; one thread issues the
+  // MMAs of a product, all wait for it.
+  auto product = [&](auto issue) {
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0 && elect_one()) {
+      issue();
+      mma_commit(&s.done);
+    }
+    __syncwarp();
+    mbar_wait_warp(&s.done, products++ & 1, abort);
+    tc_fence_after();
+  };
+  for (int step = 0; step < steps; ++step) {
+    product([&] {
+      for (int t = 0; t < tiles; ++t) {
+        const uint64_t x = sdesc_sw128(smem_u32(s.hi[t]), 16, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_bf16_ss(tmem, x + 2 * k, x + 2 * k, idesc_f16(128, 128, false), (t | k) != 0);
+      }
+    });
+    // F and d, from A
+    auto keep = [&](int r, int k, float (&x)[8], auto store) {   // part k of row r, scaled
+      if ((r >> 3) == k) {
+        float own = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i == (r & 7)) {
+            own = x[i] * (1.f / kFScale);
+            x[i] = 0.f;
+          }
+        store(own, true, Granule<__half>::pack(x));
+      } else {
+        store(0.f, false, Granule<__half>::pack(x));
+      }
+    };
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {         // 32 columns at a time
+      uint32_t v[32];
+      tmem_ld32(tmem + lanes + 64 * half + 32 * c, v);
+      tmem_ld_wait();
+      if (tiles == 0)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = 0u;
+      if (parts > 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          *wide_part(s.g[0], row, 16 * half + 8 * c + k) =
+              make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            x[i] = __uint_as_float(v[8 * k + i]) * (kFScale / (kXScale * kXScale));
+          keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, uint4 h) {
+            if (diagonal) s.d[row] = own;
+            *tile_part(s.f[half], row, 4 * c + k) = h;
+          });
+        }
+      }
+    }
+    if (parts > 1) {
+      cluster_sync();                     // all parts of A are there
+      const int rows = kSmallRows / parts, per_row = kSmallThreads / rows, some = 128 / per_row;
+      const int r = rank * rows + me / per_row, first = me % per_row * some;
+      for (int c = first; c < first + some; c += 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        uint4 part[kMaxParts][2];         // all on their way before the first is added
+#pragma unroll
+        for (int p = 0; p < kMaxParts; ++p)
+          if (p < parts) {
+            part[p][0] = load_remote(wide_part(s.g[0], r, c >> 2), p);
+            part[p][1] = load_remote(wide_part(s.g[0], r, (c >> 2) + 1), p);
+          }
+#pragma unroll
+        for (int p = 0; p < kMaxParts; ++p)
+          if (p < parts) {
+            float y[8];
+            Granule<float>::unpack(part[p][0], y);
+            Granule<float>::unpack(part[p][1], y + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] += y[i];
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= kFScale / (kXScale * kXScale);
+        keep(r, c >> 3, x, [&](float own, bool diagonal, uint4 h) {
+          for (int p = 0; p < parts; ++p) {
+            if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), p);
+            store_remote_part(h, tile_part(s.f[c >> 6], r, (c >> 3) & 7), p);
+          }
+        });
+      }
+      cluster_sync();                     // all of F
+    }
+    product([&] {
+      for (int t = 0; t < halves; ++t) {
+        const uint64_t x = sdesc_sw128(smem_u32(s.f[t]), 16, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_bf16_ss(tmem + 128, x + 2 * k, x + 2 * k, idesc_f16(128, 128, false), (t | k) != 0);
+      }
+    });
+    const float di = s.d[row], base = fmaf(kC, di, kB) * (1.f / kFScale);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t v[32];
+      tmem_ld32(tmem + 128 + lanes + 64 * half + 32 * c, v);
+      tmem_ld_wait();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int col = 64 * half + 32 * c + 8 * k;
+        float x[8], off[8];
+        Granule<__half>::unpack(*tile_part(s.f[half], row, 4 * c + k), off);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float ff = __uint_as_float(v[8 * k + i]) * (kC / (kFScale * kFScale));
+          x[i] = fmaf(off[i], fmaf(s.d[col + i], kC / kFScale, base), ff);
+          if (row == col + i) {
+            s.e[row] = fmaf(fmaf(kC, di, kB), di, ff);
+            x[i] = 0.f;
+          }
+        }
+        *tile_part(s.g[half], row, 4 * c + k) = Granule<__half>::pack(x);
+      }
+    }
+    product([&] {
+      if (tiles == 0) return;
+      const uint32_t idesc = idesc_f16(128, 64 * tiles, true);
+      for (int t = 0; t < halves; ++t) {
+        const uint64_t x = sdesc_sw128(smem_u32(s.g[t]), 16, 1024);
+        const uint64_t y = sdesc_sw128(smem_u32(s.hi[0]) + t * kHalfTile, kTileBytes, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_bf16_ss(tmem + 256, x + 2 * k, y + 128 * k, idesc, (t | k) != 0);
+      }
+    });
+    const bool last = step + 1 == steps;
+    if (last) {
+      // where a wait has run out in any of the CTAs the matrix stays as it is
+      if (me < parts) {
+        if (parts > 1) store_remote(*abort, &s.bad[rank], me);
+        else s.bad[0] = *abort;
+      }
+      sync();
+      int bad = 0;
+      for (int c = 0; c < parts; ++c) bad |= s.bad[c];
+      if (bad) {
+        if (me == 0) record_status(a.status, DORA_ERR_TIMEOUT);
+        break;
+      }
+    }
+    const float own = kA + s.e[row];
+    for (int p = half; p < 2 * tiles; p += 2) {
+      uint32_t v[32];
+      tmem_ld32(tmem + 256 + lanes + 32 * p, v);
+      tmem_ld_wait();
+      float x[32];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint4 *hi = tile_part(s.hi[p >> 1], row, 4 * (p & 1) + k),
+              *lo = tile_part(s.lo[p >> 1], row, 4 * (p & 1) + k);
+        float h[8], l[8];
+        Granule<__half>::unpack(*hi, h);
+        Granule<__half>::unpack(*lo, l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          x[8 * k + i] = fmaf(own, h[i] + l[i], __uint_as_float(v[8 * k + i]));
+        if (!last) split(x + 8 * k, hi, lo);
+      }
+      if (last) {
+        uint16_t* scratch = reinterpret_cast<uint16_t*>(s.extra[0]) + warp * 2 * kPiece;
+        finish_last(e, a, q * 32, col0 + 32 * p, lane, x, scratch, scratch + kPiece);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
 }  // namespace ortho
 }  // namespace dora
 
@@ -1228,6 +1594,7 @@ struct Shape {
   int32_t m, n, mb, nb;
   int64_t chunks, x_tiles, f_tiles, diag;   // diag: blocks of 128 of a diagonal
   int64_t sym[2], all[2];
+  int32_t parts;                          // of a small matrix: CTAs; 0: it is not small
 };
 Shape shape_of(const dora_matrix& t) {
   Shape s;
@@ -1235,6 +1602,14 @@ Shape shape_of(const dora_matrix& t) {
   s.n = t.rows < t.cols ? t.cols : t.rows;
   s.mb = (s.m + 127) / 128;
   s.nb = (s.n + 127) / 128;
+  s.parts = 0;
+  if (s.m <= ortho::kSmallRows && s.n <= 64 * ortho::kSmallTiles * ortho::kMaxParts) {
+    s.chunks = s.x_tiles = s.f_tiles = s.diag = 0;
+    s.sym[0] = s.sym[1] = s.all[0] = s.all[1] = 0;
+    s.parts = 1;
+    while ((s.n + 63) / 64 > s.parts * ortho::kSmallTiles) s.parts *= 2;
+    return s;
+  }
   s.chunks = (static_cast<int64_t>(s.m) * s.n + ortho::kChunk - 1) / ortho::kChunk;
   const int64_t pairs = (s.mb + 1) / 2;
   s.x_tiles = pairs * 2 * 2 * s.nb;
@@ -1251,6 +1626,7 @@ constexpr int64_t kFewTiles = 76;
 struct Sizes {
   int64_t chunks = 0, x_tiles = 0, sym = 0, all = 0, tiles = 0, diag = 0;
   int narrow_sym = 0, narrow_all = 0;     // 1: tiles of 128 columns
+  int32_t large = 0, parts = 1;           // matrices that are not small; most CTAs of a small one
   bool has_params = true, has_outs = true;
 };
 
@@ -1281,6 +1657,8 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
     }
     z.tiles += 3 * s.x_tiles + 2 * s.f_tiles;
     z.diag += s.diag;
+    z.large += s.parts == 0;
+    if (s.parts > z.parts) z.parts = s.parts;
     if (t.param == nullptr) z.has_params = false;
     if (t.out == nullptr) z.has_outs = false;
     // counted in 32 bits, the tiles' rows among them
@@ -1312,7 +1690,7 @@ Places places_of(const Sizes& z, int64_t count) {
   p.done = p.ticket + round256(count * 4);
   p.diag = p.done + round256(count * 4);
   p.tiles = p.diag + z.diag * 2 * 512;
-  p.end = p.tiles + z.tiles * ortho::kTileBytes;
+  p.end = p.tiles + (z.tiles > 0 ? z.tiles : 1) * ortho::kTileBytes;
   return p;
 }
 
@@ -1335,7 +1713,7 @@ ortho::List list_of(const dora_matrix_list& l) {
   o.all = reinterpret_cast<ortho::Tile*>(at + p.all);
   o.groups = reinterpret_cast<ortho::Group*>(at + p.groups);
   o.tiles = at + p.tiles;
-  o.count = l.count;
+  o.count = l.large;
   o.n_chunks = static_cast<int>(z.chunks);
   o.n_x = static_cast<int>(z.x_tiles);
   o.n_sym = static_cast<int>(z.sym);
@@ -1344,7 +1722,8 @@ ortho::List list_of(const dora_matrix_list& l) {
 }
 
 bool valid_list(const dora_matrix_list* l) {
-  return l != nullptr && l->data != nullptr && l->count >= 1 && l->chunks >= 1 && l->tiles >= 1;
+  return l != nullptr && l->data != nullptr && l->count >= 1 && l->large >= 0 &&
+         l->large <= l->count && l->parts >= 1 && l->parts <= ortho::kMaxParts;
 }
 
 int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::Args& a, int steps,
@@ -1370,6 +1749,34 @@ int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::
   return launched(cudaLaunchKernelEx(&cfg, kern, maps, l, a, steps));
 }
 
+int launch_small(const ortho::List& l, const ortho::Args& a, int steps, int matrices, int parts,
+                 cudaStream_t stream) {
+  constexpr int smem = sizeof(ortho::SmallSmem);
+  const cudaError_t e = cudaFuncSetAttribute(
+      ortho::small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return launched(e);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (parts > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = parts;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl_enabled()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.gridDim = dim3(matrices * parts);
+  cfg.blockDim = dim3(ortho::kSmallThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return launched(cudaLaunchKernelEx(&cfg, ortho::small_kernel, l, a, steps, parts));
+}
+
 int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaStream_t stream) {
   const int dev = device_or_error();
   if (dev != DORA_OK) return dev;
@@ -1378,12 +1785,17 @@ int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaS
   static_assert(sizeof(maps) == sizeof(list->map), "the maps' size is part of the interface");
   memcpy(&maps, list->map, sizeof(maps));
   const int most = num_sms() * ortho::kRowCtas;
-  int e = launched(launch_pdl(ortho::momentum_kernel, dim3(l.n_chunks < most ? l.n_chunks : most),
-                              dim3(ortho::kRowThreads), 0, stream, l, a));
-  if (e == DORA_OK)
-    e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
+  int e = DORA_OK;
+  if (l.count > 0) {
+    e = launched(launch_pdl(ortho::momentum_kernel, dim3(l.n_chunks < most ? l.n_chunks : most),
                             dim3(ortho::kRowThreads), 0, stream, l, a));
-  if (e == DORA_OK) e = launch_products(maps, l, a, steps, stream);
+    if (e == DORA_OK)
+      e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
+                              dim3(ortho::kRowThreads), 0, stream, l, a));
+    if (e == DORA_OK) e = launch_products(maps, l, a, steps, stream);
+  }
+  if (e == DORA_OK && list->count > list->large)
+    e = launch_small(l, a, steps, list->count - list->large, list->parts, stream);
   return e;
 }
 }  // namespace
@@ -1417,11 +1829,13 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   l.tiles = z.tiles;
   l.diagonals = z.diag;
   l.count = count;
+  l.large = z.large;
+  l.parts = z.parts;
   l.has_params = z.has_params;
   l.has_outs = z.has_outs;
   // all tiles as one tall matrix of 64 columns
   ortho::Maps maps;
-  const uint64_t rows = static_cast<uint64_t>(z.tiles) * ortho::kTileRows;
+  const uint64_t rows = static_cast<uint64_t>(z.tiles > 0 ? z.tiles : 1) * ortho::kTileRows;
   if (encode_tmap_2d_bf16(&maps.tile, at + p.tiles, 64, rows, 128, 64, 128) != 0 ||
       encode_tmap_2d_bf16(&maps.half, at + p.tiles, 64, rows, 128, 64, 64) != 0 ||
       encode_tmap_2d_bf16(&maps.column, at + p.tiles, 64, rows, 128, 32, 128, 64) != 0 ||
@@ -1430,11 +1844,18 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   memcpy(l.map, &maps, sizeof(maps));
   const ortho::List o = list_of(l);
   int64_t tile = 0, chunk = 0, x = 0, sym = 0, all = 0, diag = 0;
+  // the small ones after the others
+  int32_t at_small[2] = {0, 0};           // next of either kind among the caller's
+  const auto next = [&](bool small) -> const dora_matrix& {
+    int32_t& i = at_small[small];
+    while ((shape_of(matrices[i]).parts > 0) != small) ++i;
+    return matrices[i++];
+  };
   for (int32_t first = 0; first < count; first += ortho::kFill) {
     const int some = count - first < ortho::kFill ? count - first : ortho::kFill;
     ortho::FillArgs args = {};
     for (int i = 0; i < some; ++i) {
-      const dora_matrix& t = matrices[first + i];
+      const dora_matrix& t = next(first + i >= z.large);
       const Shape s = shape_of(t);
       ortho::Entry& e = args.e[i];
       e.grad = t.grad;
@@ -1465,7 +1886,8 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       diag += s.diag;
       e.partial = reinterpret_cast<ortho::Squares*>(at + p.partial) + chunk;
       e.norm = reinterpret_cast<float2*>(at + p.norm) + first + i;
-      e.ticket = reinterpret_cast<unsigned*>(at + p.ticket) + first + i;
+      e.ticket = s.parts > 0 ? nullptr : reinterpret_cast<unsigned*>(at + p.ticket) + first + i;
+      e.parts = s.parts;
       e.done = reinterpret_cast<unsigned*>(at + p.done) + first + i;
       e.chunks = static_cast<int32_t>(s.chunks);
       e.n_sym = static_cast<int32_t>(s.sym[z.narrow_sym]);
@@ -1488,6 +1910,7 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   int64_t most = z.chunks > z.x_tiles ? z.chunks : z.x_tiles;
   if (z.sym > most) most = z.sym;
   if (z.all > most) most = z.all;
+  if (most == 0) most = 1;
   const int rc = launched(launch_pdl(ortho::fill_tiles_kernel,
                                      dim3(static_cast<unsigned>((most + 127) / 128)), dim3(128), 0,
                                      stream, o));

@@ -78,11 +78,12 @@ def test_list_host_checks(lib):
     def size(**more):
         return lib.dora_matrix_list_size(ctypes.byref(_matrix(**more)), 1)
 
-    # three copies of X in tiles of 128 x 64, an even number down and across, two of the square
-    # of the shorter side
+    # small matrices need no memory of their own; others three copies of X in tiles of 128 x 64, an
+    # even number down and across, two of the square of the shorter side
     one = size()
-    assert 5 * 4 * 16384 <= one < 5 * 4 * 16384 + 16384
-    assert size(rows=300, cols=200) >= (3 * 2 * 6 + 2 * 2 * 4) * 16384
+    assert 0 < one < 3 * 16384 and size(rows=128, cols=2048) == one
+    for r, c, tiles in ((300, 200, 3 * 2 * 6 + 2 * 2 * 4), (100, 2049, 3 * 2 * 34 + 2 * 2 * 2)):
+        assert tiles * 16384 <= size(rows=r, cols=c) < (tiles + 2) * 16384
     assert size(param=0, momentum=0, copy=0) == one and size(out=0) == one and size(copy=0) == one
     for bad in (dict(rows=0), dict(cols=0), dict(rows=-1), dict(grad=0), dict(grad=257),
                 dict(grad_dtype=3), dict(grad_dtype=2, grad=258), dict(momentum=0),
@@ -104,7 +105,7 @@ def test_list_host_checks(lib):
 
 def test_call_host_checks(lib):
     l = P._MatrixListC(data=256, chunks=1, x_tiles=2, symmetric=1, outputs=1, tiles=10,
-                       diagonals=1, count=1, has_params=1, has_outs=1)
+                       diagonals=1, count=1, has_params=1, has_outs=1, large=1, parts=1)
     r = ctypes.byref(l)
     assert lib.dora_orthogonalize(None, 5, None, None) == 1
     assert lib.dora_orthogonalize(r, 0, None, None) == 1
