@@ -933,7 +933,7 @@ typedef struct dora_matrix_list {
   int32_t count;
   int32_t has_params;   /* 1: every matrix has param and momentum */
   int32_t has_outs;     /* 1: every matrix has out */
-  int32_t large, parts, pad;
+  int32_t large, parts, ragged;
   uint64_t map[64];
 } dora_matrix_list;
 size_t dora_matrix_list_size(const dora_matrix* matrices, int32_t count);

@@ -1241,7 +1241,7 @@ class _MatrixC(ctypes.Structure):
 class _MatrixListC(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(n, _i64) for n in ("chunks", "x_tiles", "symmetric", "outputs",
                                                       "tiles", "diagonals")] + [
-        (n, _i32) for n in ("count", "has_params", "has_outs", "large", "parts", "pad")] + [
+        (n, _i32) for n in ("count", "has_params", "has_outs", "large", "parts", "ragged")] + [
         ("map", ctypes.c_uint64 * 64)]
 
 

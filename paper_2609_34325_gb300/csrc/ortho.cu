@@ -422,11 +422,74 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b) {
   return Granule<__half>::pair(a, b);
 }
 
-// Eight values `step` apart, zeros from the some-th on.
-template <typename T>
-__device__ __forceinline__ void load_eight(const T* p, int64_t step, int some, float* v) {
+// The gradient and the momentum of eight columns from `col` of a row of X, as they are loaded:
+// nothing is made of them before all loads of a thread are on their way.  What is not there is 0.
+struct Eight {
+  uint32_t g[8], m[8];
+};
+__device__ __forceinline__ bool aligned16(const void* p) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+}
+// Whether eight columns are 16-byte loads.
+__device__ __forceinline__ bool in_eights(const Entry& e, const Args& a) {
+  return !e.tall && (e.n & 7) == 0 && aligned16(e.grad) && (!a.muon || aligned16(e.momentum));
+}
+__device__ __forceinline__ void put(uint32_t* w, uint4 q) {
+  w[0] = q.x;
+  w[1] = q.y;
+  w[2] = q.z;
+  w[3] = q.w;
+}
+__device__ __forceinline__ Eight load_eight(const Entry& e, const Args& a, bool eights, int row,
+                                            int col) {
+  Eight x;
+  const int some = row < e.m ? e.n - col : 0;
+  const int64_t step = e.tall ? e.m : 1;
+  const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
+                           : static_cast<int64_t>(row) * e.n + col;
+  if (eights && some > 0) {               // a multiple of eight columns: all of them
+    const uint4* g = reinterpret_cast<const uint4*>(static_cast<const char*>(e.grad) +
+                                                    k * size_of(e.grad_type));
+    put(x.g, g[0]);
+    if (e.grad_type == DORA_F32) put(x.g + 4, g[1]);
+    if (a.muon) {
+      put(x.m, reinterpret_cast<const uint4*>(e.momentum + k)[0]);
+      put(x.m + 4, reinterpret_cast<const uint4*>(e.momentum + k)[1]);
+    }
+    return x;
+  }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < some ? to_float(p[i * step]) : 0.f;
+  for (int i = 0; i < 8; ++i) x.g[i] = x.m[i] = 0u;
+  if (e.grad_type == DORA_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < some) x.g[i] = static_cast<const uint32_t*>(e.grad)[k + i * step];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < some) x.g[i] = static_cast<const uint16_t*>(e.grad)[k + i * step];
+  }
+  if (a.muon)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < some) x.m[i] = reinterpret_cast<const uint32_t*>(e.momentum)[k + i * step];
+  return x;
+}
+// Their values; `packed`: 16-bit ones lie two in a word.
+__device__ __forceinline__ void values_of(const Entry& e, const Eight& x, bool packed, float* d,
+                                          float* m) {
+  if (e.grad_type == DORA_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = __uint_as_float(x.g[i]);
+  } else {
+    const uint4 q = packed ? make_uint4(x.g[0], x.g[1], x.g[2], x.g[3])
+                           : make_uint4(x.g[0] | x.g[1] << 16, x.g[2] | x.g[3] << 16,
+                                        x.g[4] | x.g[5] << 16, x.g[6] | x.g[7] << 16);
+    if (e.grad_type == DORA_BF16) Granule<__nv_bfloat16>::unpack(q, d);
+    else Granule<__half>::unpack(q, d);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m[i] = __uint_as_float(x.m[i]);
 }
 
 // hi and lo of eight values that are scaled already.
@@ -455,44 +518,35 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
     const int64_t at = static_cast<int64_t>(ti) * (2 * e.nb) + tj;
     char* hi = tile_at(list, e.x[0] + at);
     char* lo = tile_at(list, e.lo + at);
-    const bool quads = !e.tall && (e.n & 7) == 0 && in_quads(e.grad, e.grad_type) &&
-                       (!a.muon || in_quads(e.momentum, DORA_F32));
-    constexpr int kItems = kTileRows * 8 / kRowThreads, kSome = 2;
+    const bool eights = in_eights(e, a);
+    constexpr int kItems = kTileRows * 8 / kRowThreads;
     // pieces of eight columns, the lanes along what is contiguous in the matrix
-    for (int w0 = 0; w0 < kItems; w0 += kSome) {
-      float d[kSome][8], m[kSome][8];
+    auto place = [&](int y, int* r, int* piece) {
+      const int w = threadIdx.x + y * kRowThreads;
+      *r = e.tall ? w % kTileRows : w / 8;
+      *piece = e.tall ? w / kTileRows : w % 8;
+    };
+    constexpr int kSome = 2;
+#pragma unroll 1
+    for (int y0 = 0; y0 < kItems; y0 += kSome) {
+      Eight x[kSome];
 #pragma unroll
       for (int y = 0; y < kSome; ++y) {
-        const int w = threadIdx.x + (w0 + y) * kRowThreads;
-        const int r = e.tall ? w % kTileRows : w / 8, piece = e.tall ? w / kTileRows : w % 8;
-        const int row = ti * kTileRows + r, col = tj * kTileCols + piece * 8;
-        const int some = row < e.m ? e.n - col : 0;     // columns that there are
-        const int64_t step = e.tall ? e.m : 1;
-        const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
-                                 : static_cast<int64_t>(row) * e.n + col;
-        if (quads && some >= 8) {
-#pragma unroll
-          for (int i = 0; i < 8; i += 4) {
-            unpack_quad(whole_quad(e.grad, e.grad_type, k + i), e.grad_type, d[y] + i);
-            if (a.muon) Granule<float>::unpack(whole_quad(e.momentum, DORA_F32, k + i), m[y] + i);
-          }
-        } else if (e.grad_type == DORA_F32) {
-          load_eight(static_cast<const float*>(e.grad) + k, step, some, d[y]);
-        } else if (e.grad_type == DORA_BF16) {
-          load_eight(static_cast<const __nv_bfloat16*>(e.grad) + k, step, some, d[y]);
-        } else {
-          load_eight(static_cast<const __half*>(e.grad) + k, step, some, d[y]);
-        }
-        if (a.muon && !(quads && some >= 8)) load_eight(e.momentum + k, step, some, m[y]);
+        int r, piece;
+        place(y0 + y, &r, &piece);
+        x[y] = load_eight(e, a, eights, ti * kTileRows + r, tj * kTileCols + piece * 8);
       }
 #pragma unroll
       for (int y = 0; y < kSome; ++y) {
-        const int w = threadIdx.x + (w0 + y) * kRowThreads;
-        const int r = e.tall ? w % kTileRows : w / 8, piece = e.tall ? w / kTileRows : w % 8;
-        float v[8];
+        int r, piece;
+        place(y0 + y, &r, &piece);
+        // a row or columns past the end were loaded one by one
+        const bool packed = eights && ti * kTileRows + r < e.m && tj * kTileCols + piece * 8 < e.n;
+        float d[8], m[8], v[8];
+        values_of(e, x[y], packed, d, m);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          v[i] = update_of(a, d[y][i] * f, a.muon ? m[y][i] : 0.f) * norm.y * norm.x * kXScale;
+          v[i] = update_of(a, d[i] * f, a.muon ? m[i] : 0.f) * norm.y * norm.x * kXScale;
         uint4 h, l;
         split(v, &h, &l);
         const uint32_t to = tile_offset(r, piece * 8);
@@ -665,19 +719,65 @@ __device__ __forceinline__ void mirror(uint16_t* piece, int first, int lane, uin
     *value_in(piece, first + i, lane) = static_cast<uint16_t>(words[i >> 1] >> (16 * (i & 1)));
 }
 
+// One value a lane in each of `some` rows: keep times the weight at p (none: 0) plus value(row),
+// to p and, rounded, to copy.
+template <typename T, typename F>
+__device__ __forceinline__ void write_rows(T* p, __nv_bfloat16* copy, int64_t pitch, int some,
+                                           float keep, F value) {
+  constexpr int kAtOnce = 16;
+  for (int i0 = 0; i0 < some; i0 += kAtOnce) {
+    T old[kAtOnce];                       // all on their way before the first is used
+    if (p != nullptr)
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (i0 + i < some) old[i] = p[(i0 + i) * pitch];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if (i0 + i < some) {
+        float w = value(i0 + i);
+        if (p != nullptr) {
+          w = fmaf(to_float(old[i]), keep, w);
+          from_float(w, p + (i0 + i) * pitch);
+        }
+        if (copy != nullptr) from_float(w, copy + (i0 + i) * pitch);
+      }
+  }
+}
+
+// 32 x 32 values in rows of 128 bytes, 16 rows in `low`, 16 in `high`; their 16-byte parts change
+// places with the row.
+__device__ __forceinline__ float4* swapped_part(uint16_t* low, uint16_t* high, int i, int k) {
+  return reinterpret_cast<float4*>(i < 16 ? low : high) + (i & 15) * 8 + (k ^ (i & 7));
+}
+// Those of them that exist to the weights (or out), a value a lane: where sizes or alignment do
+// not allow four.
+__device__ __forceinline__ void finish_ragged(void* param, int param_type, __nv_bfloat16* copy,
+                                           int64_t pitch, int some, float keep, float step,
+                                           uint16_t* low, uint16_t* high) {
+  const int lane = threadIdx.x & 31;
+  const auto value = [&](int i) {
+    return reinterpret_cast<const float*>(swapped_part(low, high, i, lane >> 2))[lane & 3] * step;
+  };
+  if (param == nullptr || param_type == DORA_F32)
+    write_rows(static_cast<float*>(param), copy, pitch, some, keep, value);
+  else if (param_type == DORA_BF16)
+    write_rows(static_cast<__nv_bfloat16*>(param), copy, pitch, some, keep, value);
+  else
+    write_rows(static_cast<__half*>(param), copy, pitch, some, keep, value);
+}
+
 // 32 x 32 new values of X (scaled; a row a lane) to where the caller wants them, lanes along
 // what is contiguous there: four values each, where sizes and alignment allow, after they have
-// changed places in shared memory, 16 rows in `low`, 16 in `high`.
+// changed places in shared memory, 16 rows in `low`, 16 in `high`.  kRagged: they may not allow it
+// (a kernel of its own: with both ways in one the other spills, 540 us become 586).
+template <bool kRagged>
 __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int row0, int col0,
                                             int lane, float (&x)[32], uint16_t* low,
                                             uint16_t* high) {
   const int outer = e.tall ? col0 : row0, inner = e.tall ? row0 : col0;
   const int outers = e.tall ? e.n : e.m, inners = e.tall ? e.m : e.n;
-  const bool quads = e.quads && inner + 32 <= inners && outer + 32 <= outers;
-  // where row i of what is written begins; 16-byte parts change places with the row
-  auto part = [&](int i, int k) {
-    return reinterpret_cast<float4*>(i < 16 ? low : high) + (i & 15) * 8 + (k ^ (i & 7));
-  };
+  const int some = outers - outer < 32 ? outers - outer : 32;
+  auto part = [&](int i, int k) { return swapped_part(low, high, i, k); };
   __syncwarp();                           // every lane has read its part of the piece
   if (e.tall) {
 #pragma unroll
@@ -689,16 +789,19 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
   }
   __syncwarp();
   const float step = a.muon ? -(a.lr * e.scale) * (1.f / kXScale) : 1.f / kXScale;
-  if (quads) {
+  if (!kRagged || e.quads) {
     const int k = lane & 7, i0 = lane >> 3;
+    if (inner + 4 * k >= inners) return;
     const int64_t at = static_cast<int64_t>(outer + i0) * inners + inner + 4 * k;
     const int64_t next = 4 * static_cast<int64_t>(inners);
     uint4 old[8];                         // all on their way before the first is used
     if (a.muon)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) old[u] = whole_quad(e.param, e.param_type, at + u * next);
+      for (int u = 0; u < 8; ++u)
+        if (i0 + 4 * u < some) old[u] = whole_quad(e.param, e.param_type, at + u * next);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
+      if (i0 + 4 * u >= some) continue;
       const float4 y = *part(i0 + 4 * u, k);
       float w[4] = {y.x * step, y.y * step, y.z * step, y.w * step};
       if (a.muon) {
@@ -714,24 +817,18 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
     }
   } else if (inner + lane < inners) {
     const int64_t at = static_cast<int64_t>(outer) * inners + inner + lane;
-    const int some = outers - outer < 32 ? outers - outer : 32;
-    for (int i = 0; i < some; ++i) {
-      const float y = reinterpret_cast<const float*>(part(i, lane >> 2))[lane & 3] * step;
-      const int64_t k = at + static_cast<int64_t>(i) * inners;
-      if (a.muon) {
-        const float w = fmaf(load_one(e.param, e.param_type, k), a.keep, y);
-        store_one(w, e.param, e.param_type, k);
-        if (e.copy != nullptr) store_one(w, e.copy, DORA_BF16, k);
-      } else {
-        store_one(y, e.out, DORA_BF16, k);
-      }
-    }
+    void* param = a.muon ? const_cast<char*>(static_cast<const char*>(e.param)) +
+                               at * size_of(e.param_type)
+                         : nullptr;
+    __nv_bfloat16* copy = reinterpret_cast<__nv_bfloat16*>(a.muon ? e.copy : e.out);
+    if (copy != nullptr) copy += at;
+    finish_ragged(param, e.param_type, copy, inners, some, a.keep, step, low, high);
   }
 }
 
 // What finishes 32 x 32 values of an accumulator, v, whose other inputs lie in `one`, `two`
 // and, the diagonal over its columns, `dj`.
-template <Phase kPhase>
+template <Phase kPhase, bool kRagged>
 __device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int row0, int col,
                                              bool mirrored, int lane, float own, const float* dj,
                                              const uint32_t (&v)[32], uint16_t* one,
@@ -803,10 +900,11 @@ __device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int 
         *piece_at(two, lane, k) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
       }
     }
-    if constexpr (kPhase == kLast) finish_last(e, a, row0, col, lane, x, one, two);
+    if constexpr (kPhase == kLast) finish_last<kRagged>(e, a, row0, col, lane, x, one, two);
   }
 }
 
+template <bool kRagged>
 __global__ void __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ Maps maps, List list, Args a, int steps) {
   extern __shared__ __align__(1024) uint8_t raw[];
@@ -1163,13 +1261,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         const float* dj = s.dj[place][half];
         if (phase == kGram)
-          finish_piece<kGram>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kGram, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
         else if (phase == kSquare)
-          finish_piece<kSquare>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kSquare, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
         else if (phase == kApply)
-          finish_piece<kApply>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kApply, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
         else
-          finish_piece<kLast>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kLast, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.piece_done[half][place]);
@@ -1250,45 +1348,6 @@ __device__ __forceinline__ void store_remote_part(uint4 q, uint4* to, uint32_t c
       : "memory");
 }
 
-// The gradient and momentum of eight columns from `col` of a row; what is not there is 0.
-__device__ __forceinline__ void load_update(const Entry& e, const Args& a, int row, int col,
-                                            bool quads, float* d, float* m) {
-  const int some = row < e.m ? e.n - col : 0;
-  const int64_t step = e.tall ? e.m : 1;
-  const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
-                           : static_cast<int64_t>(row) * e.n + col;
-  if (quads && some >= 8) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      unpack_quad(whole_quad(e.grad, e.grad_type, k + i), e.grad_type, d + i);
-      if (a.muon) Granule<float>::unpack(whole_quad(e.momentum, DORA_F32, k + i), m + i);
-    }
-    return;
-  }
-  if (e.grad_type == DORA_F32)
-    load_eight(static_cast<const float*>(e.grad) + k, step, some, d);
-  else if (e.grad_type == DORA_BF16)
-    load_eight(static_cast<const __nv_bfloat16*>(e.grad) + k, step, some, d);
-  else
-    load_eight(static_cast<const __half*>(e.grad) + k, step, some, d);
-  if (a.muon) load_eight(e.momentum + k, step, some, m);
-}
-__device__ __forceinline__ void store_momentum(const Entry& e, int row, int col, bool quads,
-                                               const float* m) {
-  const int some = row < e.m ? e.n - col : 0;
-  const int64_t step = e.tall ? e.m : 1;
-  const int64_t k = e.tall ? static_cast<int64_t>(col) * e.m + row
-                           : static_cast<int64_t>(row) * e.n + col;
-  if (quads && some >= 8) {
-    store_quad(m, e.momentum, DORA_F32, k);
-    store_quad(m + 4, e.momentum, DORA_F32, k + 4);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < some) e.momentum[k + i * step] = m[i];
-}
-
 __global__ void __launch_bounds__(kSmallThreads, 1)
     small_kernel(List list, Args a, int steps, int cluster) {
   extern __shared__ __align__(1024) uint8_t raw[];
@@ -1296,7 +1355,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
   const int rank = cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   pdl_wait();
-  const Entry& e = list.entries[list.count + blockIdx.x / cluster];
+  const Entry e = list.entries[list.count + blockIdx.x / cluster];   // read once
   const int parts = e.parts;
   if (skipped(a) || rank >= parts) return;  // those that have left are not waited for
   if (me == 0) {
@@ -1319,28 +1378,105 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int tile0 = rank * each, tiles = max(0, min(each, all - tile0)), col0 = 64 * tile0;
   const int halves = (e.m + 63) / 64;     // of the products over m
   const float f = factor(a);
-  const bool quads = !e.tall && (e.n & 7) == 0 && in_quads(e.grad, e.grad_type) &&
-                     (!a.muon || in_quads(e.momentum, DORA_F32));
+  const bool eights = in_eights(e, a);
 
-  // momentum and the update's norm, then the normalised update
-  auto place = [&](int w, int* r, int* k) {   // lanes along what is contiguous
-    *r = e.tall ? w % kSmallRows : w / (8 * tiles);
-    *k = e.tall ? w / kSmallRows : w % (8 * tiles);
+  // momentum and the update's norm, then the normalised update; between them the update lies
+  // in its tiles' places as fp32, 64 rows of a tile in each
+  auto raw_at = [&](int r, int k, int i) {    // values 4 i .. of part k of row r
+    uint8_t* tile = r < 64 ? s.hi[k >> 3] : s.lo[k >> 3];
+    return reinterpret_cast<uint4*>(tile + (r & 63) * 256 + (((2 * (k & 7) + i) ^ (r & 7)) << 4));
   };
   Squares sum = {0.f, -126};
-  for (int w = me; w < kSmallRows * 8 * tiles; w += kSmallThreads) {
-    int r, k;
-    place(w, &r, &k);
-    float d[8], m[8], u[8];
-    load_update(e, a, r, col0 + 8 * k, quads, d, m);
+  if (parts > 1) {                        // F has no more than the matrix' rows and columns
+    uint4* zero = reinterpret_cast<uint4*>(s.f[0]);
+    for (int i = me; i < 2 * kTileBytes / 16; i += kSmallThreads) zero[i] = make_uint4(0, 0, 0, 0);
+    if (me < kSmallRows) s.d[me] = 0.f;
+  }
+  if (eights) {
+    constexpr int kSome = 4;
+    for (int w0 = me; w0 < kSmallRows * 8 * tiles; w0 += kSome * kSmallThreads) {
+      Eight x[kSome];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      d[i] *= f;
-      if (a.muon) m[i] = fmaf(a.mu, m[i], a.omu * d[i]);
-      u[i] = update_of(a, d[i], m[i]);
+      for (int y = 0; y < kSome; ++y) {   // the count is a multiple of what all threads take
+        const int w = w0 + y * kSmallThreads;
+        x[y] = load_eight(e, a, true, w / (8 * tiles), col0 + w % (8 * tiles) * 8);
+      }
+#pragma unroll
+      for (int y = 0; y < kSome; ++y) {
+        const int w = w0 + y * kSmallThreads, r = w / (8 * tiles), k = w % (8 * tiles);
+        const bool there = r < e.m && col0 + 8 * k < e.n;
+        float d[8], m[8], u[8];
+        values_of(e, x[y], there, d, m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          d[i] *= f;
+          if (a.muon) m[i] = fmaf(a.mu, m[i], a.omu * d[i]);
+          u[i] = update_of(a, d[i], m[i]);
+        }
+        if (a.muon && there) {
+          const int64_t at = static_cast<int64_t>(r) * e.n + col0 + 8 * k;
+          store_quad(m, e.momentum, DORA_F32, at);
+          store_quad(m + 4, e.momentum, DORA_F32, at + 4);
+        }
+        sum.add(squares_of(u));
+        *raw_at(r, k, 0) = Granule<float>::pack(u);
+        *raw_at(r, k, 1) = Granule<float>::pack(u + 4);
+      }
     }
-    if (a.muon) store_momentum(e, r, col0 + 8 * k, quads, m);
-    sum.add(squares_of(u));
+  } else {
+    // by elements, lanes along what is contiguous; then zeros where there are none
+    const int cols = max(0, min(64 * tiles, e.n - col0)), count = e.m * cols;
+    const int inner = max(1, e.tall ? e.m : cols);
+    const int step_i = kSmallThreads % inner, step_o = kSmallThreads / inner;
+    constexpr int kSome = 16;
+    int i = me % inner, o = me / inner;   // of this thread's next element, without divisions
+    for (int w0 = me; w0 < count; w0 += kSome * kSmallThreads) {
+      uint32_t raw_d[kSome], raw_m[kSome];   // as they are loaded
+      float d[kSome];
+      int at[kSome], to[kSome];           // where, of at most 128 x 2048; row and column
+#pragma unroll
+      for (int y = 0; y < kSome; ++y) {
+        at[y] = e.tall ? (col0 + o) * e.m + i : o * e.n + col0 + i;
+        to[y] = e.tall ? i << 16 | o : o << 16 | i;
+        raw_d[y] = raw_m[y] = 0u;
+        if (w0 + y * kSmallThreads < count) {
+          raw_d[y] = e.grad_type == DORA_F32 ? static_cast<const uint32_t*>(e.grad)[at[y]]
+                                             : static_cast<const uint16_t*>(e.grad)[at[y]];
+          if (a.muon) raw_m[y] = reinterpret_cast<const uint32_t*>(e.momentum)[at[y]];
+        }
+        i += step_i;
+        o += step_o;
+        if (i >= inner) {
+          i -= inner;
+          ++o;
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kSome; ++y) {
+        float one[4];
+        unpack_quad(make_uint4(raw_d[y], 0u, 0u, 0u), e.grad_type, one);
+        d[y] = one[0] * f;
+        if (w0 + y * kSmallThreads >= count) continue;
+        float m = __uint_as_float(raw_m[y]);
+        if (a.muon) {
+          m = fmaf(a.mu, m, a.omu * d[y]);
+          e.momentum[at[y]] = m;
+        }
+        d[y] = update_of(a, d[y], m);
+        const int r = to[y] >> 16, c = to[y] & 0xFFFF;
+        reinterpret_cast<float*>(raw_at(r, c >> 3, (c >> 2) & 1))[c & 3] = d[y];
+      }
+      sum.add(squares_of(d));
+    }
+    // whole parts of eight where the matrix has no row or column; the rest by elements
+    for (int w = me; w < kSmallRows * 8 * tiles; w += kSmallThreads) {
+      const int r = w / (8 * tiles), k = w % (8 * tiles);
+      if (r < e.m && 8 * k + 8 <= cols) continue;
+      for (int c = 8 * k; c < 8 * k + 8; ++c)
+        if (r >= e.m || c >= cols)
+          reinterpret_cast<float*>(raw_at(r, k, (c >> 2) & 1))[c & 3] = 0.f;
+    }
+    __syncthreads();                      // an element is another thread's from here on
   }
   sum = block_squares(sum, s.scratch);
   if (me == 0)
@@ -1357,19 +1493,26 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   for (int c = 1; c < parts; ++c) sum.add(s.sums[c]);
   const float inv = (sum.sum == 0.f ? 0.f : (isfinite(sum.sum) ? 1.f / sqrtf(sum.sum) : NAN)),
               near1 = __uint_as_float(static_cast<uint32_t>(127 - sum.k) << 23);
-  for (int w = me; w < kSmallRows * 8 * tiles; w += kSmallThreads) {
-    int r, k;
-    place(w, &r, &k);
-    float d[8], m[8], v[8];
-    load_update(e, a, r, col0 + 8 * k, quads, d, m);
+  for (int t = 0; t < tiles; ++t) {
+    constexpr int kMine = kSmallRows * 8 / kSmallThreads;
+    uint4 h[kMine], l[kMine];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      v[i] = update_of(a, d[i] * f, a.muon ? m[i] : 0.f) * near1 * inv *
-             kXScale;
-    uint4 h, l;
-    split(v, &h, &l);
-    *tile_part(s.hi[k >> 3], r, k & 7) = h;
-    *tile_part(s.lo[k >> 3], r, k & 7) = l;
+    for (int y = 0; y < kMine; ++y) {
+      const int w = me + y * kSmallThreads, r = w >> 3, k = 8 * t + (w & 7);
+      float v[8];
+      Granule<float>::unpack(*raw_at(r, k, 0), v);
+      Granule<float>::unpack(*raw_at(r, k, 1), v + 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = v[i] * near1 * inv * kXScale;
+      split(v, &h[y], &l[y]);
+    }
+    __syncthreads();                      // the tile's values have been read
+#pragma unroll
+    for (int y = 0; y < kMine; ++y) {
+      const int w = me + y * kSmallThreads, r = w >> 3, k = w & 7;
+      *tile_part(s.hi[t], r, k) = h[y];
+      *tile_part(s.lo[t], r, k) = l[y];
+    }
   }
 
   const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
@@ -1443,34 +1586,38 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     }
     if (parts > 1) {
       cluster_sync();                     // all parts of A are there
-      const int rows = kSmallRows / parts, per_row = kSmallThreads / rows, some = 128 / per_row;
-      const int r = rank * rows + me / per_row, first = me % per_row * some;
-      for (int c = first; c < first + some; c += 8) {
-        float x[8];
+      // an equal share of the rows and columns that there are for each, eight columns at a time;
+      // a thread adds up to 64 values, all on their way before the first is added
+      const int log = parts == 2 ? 1 : (parts == 4 ? 2 : 3);
+      const int eighths = (e.m + 7) / 8, groups = 8 * eighths * eighths;
+      const int share = (groups + parts - 1) >> log, end = min((rank + 1) * share, groups);
+      const int group = rank * share + me;
+      uint4 in[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        uint4 part[kMaxParts][2];         // all on their way before the first is added
+      for (int i = 0; i < 16; ++i) {      // of the i-th pair: eight columns, a part of A
+        const int pair = i >> 1, g = group + (pair >> log) * kSmallThreads;
+        in[i] = g < end ? load_remote(wide_part(s.g[0], g / eighths, 2 * (g % eighths) + (i & 1)),
+                                      pair & (parts - 1))
+                        : make_uint4(0, 0, 0, 0);
+      }
+      float x[8];
 #pragma unroll
-        for (int p = 0; p < kMaxParts; ++p)
-          if (p < parts) {
-            part[p][0] = load_remote(wide_part(s.g[0], r, c >> 2), p);
-            part[p][1] = load_remote(wide_part(s.g[0], r, (c >> 2) + 1), p);
-          }
+      for (int pair = 0; pair < 8; ++pair) {
+        float y[8];
+        Granule<float>::unpack(in[2 * pair], y);
+        Granule<float>::unpack(in[2 * pair + 1], y + 4);
+        const int p = pair & (parts - 1);
 #pragma unroll
-        for (int p = 0; p < kMaxParts; ++p)
-          if (p < parts) {
-            float y[8];
-            Granule<float>::unpack(part[p][0], y);
-            Granule<float>::unpack(part[p][1], y + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += y[i];
-          }
+        for (int i = 0; i < 8; ++i) x[i] = p == 0 ? y[i] : x[i] + y[i];
+        const int g = group + (pair >> log) * kSmallThreads;
+        if (p != parts - 1 || g >= end) continue;
+        const int r = g / eighths, c8 = g % eighths;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= kFScale / (kXScale * kXScale);
-        keep(r, c >> 3, x, [&](float own, bool diagonal, uint4 h) {
-          for (int p = 0; p < parts; ++p) {
-            if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), p);
-            store_remote_part(h, tile_part(s.f[c >> 6], r, (c >> 3) & 7), p);
+        keep(r, c8, x, [&](float own, bool diagonal, uint4 h) {
+          for (int c = 0; c < parts; ++c) {
+            if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), c);
+            store_remote_part(h, tile_part(s.f[c8 >> 3], r, c8 & 7), c);
           }
         });
       }
@@ -1553,7 +1700,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       }
       if (last) {
         uint16_t* scratch = reinterpret_cast<uint16_t*>(s.extra[0]) + warp * 2 * kPiece;
-        finish_last(e, a, q * 32, col0 + 32 * p, lane, x, scratch, scratch + kPiece);
+        finish_last<true>(e, a, q * 32, col0 + 32 * p, lane, x, scratch, scratch + kPiece);
       }
     }
   }
@@ -1586,6 +1733,10 @@ bool aligned_to(const void* p, int32_t dtype) {
 }
 bool in_quads(const void* p, int32_t dtype) {
   return (reinterpret_cast<uintptr_t>(p) & (dtype == DORA_F32 ? 15u : 7u)) == 0;
+}
+bool written_in_quads(const dora_matrix& t) {
+  return (t.cols & 3) == 0 && in_quads(t.param, t.param_dtype) && in_quads(t.copy, DORA_BF16) &&
+         in_quads(t.out, DORA_BF16);
 }
 bool known_type(int32_t t) { return t >= DORA_BF16 && t <= DORA_F32; }
 
@@ -1627,7 +1778,7 @@ struct Sizes {
   int64_t chunks = 0, x_tiles = 0, sym = 0, all = 0, tiles = 0, diag = 0;
   int narrow_sym = 0, narrow_all = 0;     // 1: tiles of 128 columns
   int32_t large = 0, parts = 1;           // matrices that are not small; most CTAs of a small one
-  bool has_params = true, has_outs = true;
+  bool has_params = true, has_outs = true, ragged = false;   // ragged: among the large ones
 };
 
 bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
@@ -1658,6 +1809,7 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
     z.tiles += 3 * s.x_tiles + 2 * s.f_tiles;
     z.diag += s.diag;
     z.large += s.parts == 0;
+    z.ragged |= s.parts == 0 && !written_in_quads(t);
     if (s.parts > z.parts) z.parts = s.parts;
     if (t.param == nullptr) z.has_params = false;
     if (t.out == nullptr) z.has_outs = false;
@@ -1727,9 +1879,9 @@ bool valid_list(const dora_matrix_list* l) {
 }
 
 int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::Args& a, int steps,
-                    cudaStream_t stream) {
+                    bool ragged, cudaStream_t stream) {
   constexpr int smem = sizeof(ortho::Smem);
-  auto kern = ortho::product_kernel;
+  const auto kern = ragged ? ortho::product_kernel<true> : ortho::product_kernel<false>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return launched(e);
   const int tiles = l.n_sym > l.n_all ? l.n_sym : l.n_all, pairs = num_sms() / 2;
@@ -1792,7 +1944,7 @@ int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaS
     if (e == DORA_OK)
       e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
                               dim3(ortho::kRowThreads), 0, stream, l, a));
-    if (e == DORA_OK) e = launch_products(maps, l, a, steps, stream);
+    if (e == DORA_OK) e = launch_products(maps, l, a, steps, list->ragged != 0, stream);
   }
   if (e == DORA_OK && list->count > list->large)
     e = launch_small(l, a, steps, list->count - list->large, list->parts, stream);
@@ -1831,6 +1983,7 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
   l.count = count;
   l.large = z.large;
   l.parts = z.parts;
+  l.ragged = z.ragged;
   l.has_params = z.has_params;
   l.has_outs = z.has_outs;
   // all tiles as one tall matrix of 64 columns
@@ -1871,8 +2024,7 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.m = s.m;
       e.n = s.n;
       e.tall = t.rows > t.cols;
-      e.quads = (t.cols & 3) == 0 && in_quads(t.param, t.param_dtype) && in_quads(t.copy, DORA_BF16) &&
-                in_quads(t.out, DORA_BF16);
+      e.quads = written_in_quads(t);
       e.mb = s.mb;
       e.nb = s.nb;
       e.x[0] = tile;
