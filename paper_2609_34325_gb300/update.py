@@ -1,16 +1,19 @@
 """The policy update of the actor's two heads, from a rollout's actions to
 changed weights (App. D.2: clipped PPO, a few epochs a rollout; Table 4: Adam).
 
-    python -m paper_2609_34325_gb300.update [--updates 60] [--images 256] [--tokens 196]
+    python -m paper_2609_34325_gb300.update [--updates 60] [--images 256] [--tokens 196] [--muon]
 
 ``HeadUpdate`` holds a linear budget head and a linear selector on the
 encoder's features (Z_CLS [B, f] and the tokens' Z [T, f] of a packed batch):
 fp32 master weights, their Adam moments and the bf16 copies that the forward
 reads.  ``act`` samples a budget and an ordered removal sequence for every
-image; ``update`` runs the epochs: forward of the heads, the clipped losses with
-their gradients (dora_policy_loss, dora_pl_policy_loss), the weights' gradients,
-their global norm (dora_grad_norm) and an Adam step on the clipped gradients
-(dora_adam_step).  Nothing in it waits for the device.
+image, with their log-probabilities, the budgets' entropies and what else they
+could have been (dora_token_logprob); ``update`` runs the epochs: forward of the
+heads, the clipped losses with their gradients (dora_policy_loss,
+dora_pl_policy_loss), the weights' gradients, their global norm (dora_grad_norm)
+and an Adam step on the clipped gradients (dora_adam_step), or, with ``muon``, a
+Muon step on the budget head's matrix (dora_muon_step) and Adam on the vectors.
+Nothing in it waits for the device.
 
 Run as a command it learns a synthetic task (random features, a hidden
 importance of every token; an action is worth the tokens it removes less the
@@ -22,8 +25,9 @@ import argparse
 
 import torch
 
-from . import (ParamList, alloc_adam_state, alloc_policy_workspace, dora_adam_step,
-               dora_grad_norm, dora_pl_policy_loss, dora_pl_sample, dora_policy_loss)
+from . import (MatrixList, ParamList, alloc_adam_state, alloc_policy_workspace, dora_adam_step,
+               dora_grad_norm, dora_muon_step, dora_pl_policy_loss, dora_pl_sample,
+               dora_policy_loss, dora_token_logprob)
 
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
@@ -35,12 +39,18 @@ def _gumbel(shape, generator, device):
 
 class Rollout:
     """What a rollout leaves for its update: features, boundaries, the actions
-    taken and their log-probabilities when they were taken."""
+    taken and their log-probabilities when they were taken; the budgets' entropies,
+    and the most probable budgets [B, ALTERNATIVES] with their log-probabilities."""
 
-    def __init__(self, z_cls, z_tok, cu, budgets, legal, k, order, budget_logp, order_logp):
+    def __init__(self, z_cls, z_tok, cu, budgets, legal, k, order, budget_logp, order_logp,
+                 entropy=None, top_budgets=None, top_logp=None):
         self.z_cls, self.z_tok, self.cu = z_cls, z_tok, cu
         self.budgets, self.legal, self.k, self.order = budgets, legal, k, order
         self.budget_logp, self.order_logp = budget_logp, order_logp
+        self.entropy, self.top_budgets, self.top_logp = entropy, top_budgets, top_logp
+
+
+ALTERNATIVES = 3
 
 
 class HeadUpdate:
@@ -50,7 +60,7 @@ class HeadUpdate:
 
     def __init__(self, features: int, budgets: int, device, seed: int = 0, lr: float = 1e-2,
                  clip: float = 0.2, entropy_coef: float = 0.01, max_norm: float = 0.5,
-                 epochs: int = 3):
+                 epochs: int = 3, muon: bool = False):
         g = torch.Generator(device=device).manual_seed(seed)
         self.features, self.budgets = features, budgets
         self.lr, self.clip, self.entropy_coef = lr, clip, entropy_coef
@@ -62,6 +72,15 @@ class HeadUpdate:
         self.moments = [[torch.zeros(s, device=device) for s in shapes] for _ in range(2)]
         self.list = ParamList(self.grads, params=self.weights, exp_avg=self.moments[0],
                               exp_avg_sq=self.moments[1], copies=self.copies)
+        # Muon for the matrix, then Adam for the vectors alone; the norm is over all of them
+        self.matrices, self.adam_list = None, self.list
+        if muon:
+            self.matrices = MatrixList(self.grads[:1], params=self.weights[:1],
+                                       momentum=self.moments[0][:1], copies=self.copies[:1],
+                                       scales=[0.2 * max(shapes[0]) ** 0.5])
+            self.adam_list = ParamList(self.grads[1:], params=self.weights[1:],
+                                       exp_avg=self.moments[0][1:], exp_avg_sq=self.moments[1][1:],
+                                       copies=self.copies[1:])
         self.adam = alloc_adam_state(device)
         self.norm = torch.zeros(2, device=device)
         self.workspace = alloc_policy_workspace(device)
@@ -90,10 +109,14 @@ class HeadUpdate:
                        status=self.status)
         none = torch.zeros(batch, device=dev)
         budget_logp, order_logp = torch.empty(batch, device=dev), torch.empty(batch, device=dev)
-        dora_policy_loss(logits, budgets, none, none, budget_logp, legal=legal,
-                         status=self.status)
+        entropy = torch.empty(batch, device=dev)
+        top_logp = torch.empty(batch, ALTERNATIVES, device=dev)
+        top_budgets = torch.empty(batch, ALTERNATIVES, dtype=_I32, device=dev)
+        dora_token_logprob(logits, budgets, budget_logp, legal=legal, entropy=entropy,
+                           top_logp=top_logp, top_tokens=top_budgets, status=self.status)
         dora_pl_policy_loss(scores, cu, k, order, none, none, order_logp, status=self.status)
-        return Rollout(z_cls, z_tok, cu, budgets, legal, k, order, budget_logp, order_logp)
+        return Rollout(z_cls, z_tok, cu, budgets, legal, k, order, budget_logp, order_logp,
+                       entropy, top_budgets, top_logp)
 
     def losses(self, r: Rollout, budget_adv, order_adv):
         """One forward and backward of both heads: ``grads`` of the weights from
@@ -121,7 +144,9 @@ class HeadUpdate:
         for _ in range(self.epochs):
             self.losses(r, budget_adv, order_adv)
             dora_grad_norm(self.list, self.max_norm, self.norm)
-            dora_adam_step(self.list, self.adam, self.lr, clip=self.norm)
+            if self.matrices is not None:
+                dora_muon_step(self.matrices, self.lr, clip=self.norm, status=self.status)
+            dora_adam_step(self.adam_list, self.adam, self.lr, clip=self.norm)
 
 
 def normalised(x):
@@ -167,10 +192,11 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=196)
     ap.add_argument("--features", type=int, default=128)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--muon", action="store_true", help="Muon for the budget head's matrix")
     a = ap.parse_args(argv)
     dev = torch.device("cuda:0")
     torch.cuda.set_device(dev)
-    heads = HeadUpdate(a.features, (a.tokens - 4) // 2, dev, seed=a.seed)
+    heads = HeadUpdate(a.features, (a.tokens - 4) // 2, dev, seed=a.seed, muon=a.muon)
     task = RemovalTask(a.images, a.tokens, a.features, dev, seed=a.seed + 1)
     history = []
     for u in range(a.updates):
