@@ -699,6 +699,13 @@ __device__ __forceinline__ void prefetch_weights(const Entry& e, int block, int 
                                                         size_of(e.param_type)));
 }
 
+// The pieces of a warp's half of a tile, 32 columns each; none in the second of a pair of block
+// rows where the matrix ends with the first: what lies there is not defined, and no other row is
+// made of it.
+__device__ __forceinline__ int pieces_of(const Task& t, int block) {
+  return block < t.e.mb ? t.width >> 6 : 0;
+}
+
 // Two values of a 16-byte part, as a pair of fp32.
 __device__ __forceinline__ uint64_t halves(uint32_t w) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -1117,8 +1124,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Task* at = task(n);
       if (!__all_sync(0xffffffffu, at != nullptr)) break;
       const Entry& e = at->e;
-      const int phase = at->phase, half = at->width >> 1, pieces = at->width >> 6;
+      const int phase = at->phase, half = at->width >> 1;
       const int first_col = at->j * kBlock, block = 2 * at->i + rank;
+      const int pieces = pieces_of(*at, block);
       const int64_t one = (phase == kSquare ? e.f : e.x[at->from]) +
                           static_cast<int64_t>(block) * 2 * (phase == kSquare ? e.mb : e.nb);
       const int64_t two = e.lo + static_cast<int64_t>(block) * 2 * e.nb;
@@ -1175,13 +1183,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Task* at = task(n);
         if (at == nullptr) break;
         const Entry& e = at->e;
-        const int phase = at->phase, half = at->width >> 1, pieces = at->width >> 6;
+        const int phase = at->phase, half = at->width >> 1;
         const int first_col = at->j * kBlock, block = 2 * at->i + rank, mb = e.mb;
+        const int pieces = pieces_of(*at, block);
+        if (pieces == 0) {
+          // Nothing to copy, but no report before the matrix' phase has begun: it would be
+          // counted for the one before.
+          if (unsaid != nullptr) report(true);
+          if (!wait_done(e.done, at->need, abort, list.header)) break;
+        }
         const int row_tiles = phase == kApply ? 2 * e.nb : 2 * mb;
         const int64_t to = phase == kGram ? e.f : (phase == kSquare ? e.g : e.x[at->from ^ 1]);
         const int64_t one = to + static_cast<int64_t>(block) * row_tiles;
         const int64_t two = e.lo + static_cast<int64_t>(block) * row_tiles;
-        const bool mirrored = phase < kApply && at->j >= 2 * at->i + 2 && block < mb;
+        const bool mirrored = phase < kApply && at->j >= 2 * at->i + 2;
         for (int c = 0; ok && c < pieces; ++c, ++done) {
           const int i = done % kPlaces;
           for (int h = 0; h < 2; ++h) {
@@ -1227,7 +1242,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Task& t = s.task[slot];
       if (t.matrix < 0) break;
       const Entry& e = t.e;
-      const int phase = t.phase, pieces = t.width >> 6;
+      const int phase = t.phase, pieces = pieces_of(t, 2 * t.i + rank);
       const int row0 = (2 * t.i + rank) * kBlock + q * 32;
       const int col0 = t.j * kBlock + half * (t.width >> 1);
       const bool mirrored = t.j >= 2 * t.i + 2;
@@ -1236,7 +1251,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
                             half * (t.width >> 1);
       uint32_t next[32];
-      tmem_ld32(from, next);
+      if (pieces > 0) {
+        tmem_ld32(from, next);
+      } else {                            // nothing of the accumulator is wanted
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
+      }
       float own = 0.f;                    // of the lane's row: d, or a + e
       if (phase == kSquare) own = __ldcg(&e.d[row0 + lane]);
       if (phase >= kApply) own = kA + __ldcg(&e.e[row0 + lane]);
