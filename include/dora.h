@@ -788,7 +788,7 @@ int dora_pl_policy_loss(const float* scores, const int32_t* cu, int32_t batch, i
  *            part but those with n_r = 0.  A token at or past n_r, or n_r outside
  *            [0, classes], gives NaN outputs (alternatives NaN, -1) and
  *            DORA_ERR_DEVICE_BAD_COUNT.
- * temperature  finite and above 0, as is one over it.
+ * temperature  from 1e-18 to 1e18.
  * top        alternatives for every row, 0 to 32: top_logp fp32 and top_tokens
  *            int32 [rows, top], most probable first, equal logits by the lower
  *            index (-0 equals 0).  Logits of -inf are no alternatives; where a row
@@ -907,8 +907,9 @@ int dora_adam_step(const dora_param_list* list, void* state, double lr, double b
  *   scale            of the matrix's update in dora_muon_step (e.g.
  *                    sqrt(max(1, rows / cols)), or 0.2 sqrt(max(rows, cols)) for
  *                    updates as large as Adam's).
- * The shorter side is at most 16384, and there are at most 2^32 elements.  Pointers are
- * aligned to their elements; 16-byte alignment is faster.  No two buffers overlap.
+ * The shorter side is at most 16384, the longer one 262144.  Pointers are
+ * aligned to their elements; 16-byte alignment is faster.  Buffers that are written
+ * overlap no other (prepare refuses them).
  * dora_matrix_list_prepare writes the list into `data` (device,
  * dora_matrix_list_size bytes, 256-byte aligned) and fills the host handle *list, which
  * the calls below take; done once for a set of buffers.  The list's memory also holds the
@@ -947,7 +948,8 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
  * which brings all singular values near 1 (five steps: those above a hundredth of
  * the norm to 0.7 .. 1.2).  A matrix of zeros stays one; one that holds a value that is
  * not finite becomes NaN.  fp16 products added in fp32, X carried in 22 bits: 1.2e-3 off
- * at most (2-norm), less than the rounding of `out`.  Same inputs, same bits.
+ * at most (2-norm), a longer side n above 65536 adds up to n 2^-26: no more than the rounding
+ * of `out`.  Same inputs, same bits.
  * status     nullable device int32: DORA_ERR_TIMEOUT should a bounded wait run out,
  *            which leaves `out` unfinished.
  */
@@ -963,7 +965,7 @@ int dora_orthogonalize(const dora_matrix_list* list, int32_t steps, int32_t* sta
  * NS as in dora_orthogonalize, mu in [0, 1).  clip nullable: the norm fp32 [2] of
  * dora_grad_norm; f = clip[1], and a norm that is not finite skips the step (nothing
  * changes).  NULL: f = 1.  A wait that runs out (status) leaves the weights of the
- * matrices concerned as they were, or partly updated.
+ * matrices concerned as they were, or partly updated, their momentum updated.
  */
 int dora_muon_step(const dora_matrix_list* list, double lr, double momentum, int32_t nesterov,
                    double weight_decay, int32_t steps, const float* clip, int32_t* status,

@@ -27,8 +27,8 @@ __all__ = [
     "dora_classifier_head", "dora_classifier_head_lc1", "dora_fold_layerscale",
     "dora_pl_sample", "dora_pl_logprob", "dora_branch", "dora_kd_cost", "dora_step_rewards",
     "dora_policy_loss", "dora_pl_policy_loss", "dora_policy_workspace_size",
-    "alloc_policy_workspace", "dora_token_logprob", "dora_token_logprob_grad", "ParamList", "dora_grad_norm", "dora_clip_grads",
-    "dora_adam_step", "dora_adam_init", "alloc_adam_state", "MatrixList", "dora_orthogonalize",
+    "alloc_policy_workspace", "dora_token_logprob", "dora_token_logprob_grad",
+    "ParamList", "dora_grad_norm", "dora_clip_grads", "dora_adam_step", "dora_adam_init", "alloc_adam_state", "MatrixList", "dora_orthogonalize",
     "dora_muon_step",
 ]
 
@@ -183,6 +183,13 @@ def _stream(stream):
     if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
         return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
+
+
+def _on_current(device, name):
+    """The device's index, where kernels are launched on it."""
+    if device != (_raw_device or torch.cuda.current_device)():
+        raise ValueError(f"{name} must be on the current device")
+    return device
 
 
 def _req(t, dtype, name, optional=False):
@@ -1015,7 +1022,7 @@ def _logit_rows(logits, classes):
         raise ValueError("classes must be in [1, logits.shape[1]]")
     if rows > _I32_MAX or classes > _I32_MAX:
         _in_32_bits(rows, classes)
-    return logits.data_ptr(), dt, rows, classes, ld, logits.get_device()
+    return logits.data_ptr(), dt, rows, classes, ld, _on_current(logits.get_device(), "logits")
 
 
 def _rows(t, dtype, n, device, name):
@@ -1296,6 +1303,7 @@ class MatrixList:
         if scales is None:
             scales = [max(1.0, t.size(0) / max(1, t.size(1))) ** 0.5 for t in self.grads]
         self.scales = [float(x) for x in scales]
+        self.device = _on_current(g0.get_device(), "the matrices")
         c = (_MatrixC * n)()
         for at, t, scale, row in zip(c, self.grads, self.scales, zip(*columns)):
             _in_32_bits(*t.shape)
@@ -1306,8 +1314,8 @@ class MatrixList:
             at.param_dtype = _DTYPES[t.dtype]
         size = int(load_library().dora_matrix_list_size(c, n))
         if size == 0:
-            raise ValueError("a matrix is empty, has a shorter side above 16384 or more than "
-                             "2^32 elements, or its scale is not finite")
+            raise ValueError("a matrix is empty, has a shorter side above 16384 or a longer one "
+                             "above 262144, or its scale is not finite, or buffers overlap")
         self.data = _bytes_on(size, device, stream)
         self.c = _MatrixListC()
         self.ref = ctypes.byref(self.c)
@@ -1319,6 +1327,7 @@ class MatrixList:
 def _matrices(mlist):
     if not isinstance(mlist, MatrixList):
         raise TypeError("a MatrixList is required")
+    _on_current(mlist.device, "the matrices")
     return mlist.ref
 
 

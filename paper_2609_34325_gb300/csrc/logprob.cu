@@ -7,8 +7,8 @@
 //   l = (z_a - m) / T - ln s,   H = ln s - t / (T s),   p_j = e^{d_j / T - ln s};
 // and from dl = d loss / d l and dH = d loss / d H, with (m, ln s, H) of the forward:
 //   d loss / d z_j = [dl (1(j = a) - p_j) - dH p_j (ln p_j + H)] / T
-//                  = p_j (A + B d_j) + 1(j = a) dl / T,
-//   A = (-dl - dH (H - ln s)) / T,   B = -dH / T^2.
+//                  = p_j (A + B d_j / T) + 1(j = a) dl / T,
+//   A = (-dl - dH (H - ln s)) / T,   B = -dH / T.
 // Both are bound by memory: the forward reads the legal logits once, the gradient reads
 // them once and writes as many.
 #include <cuda_bf16.h>
@@ -308,9 +308,8 @@ __global__ void __launch_bounds__(kThreads) logprob_warp_kernel(Batch<T> b, Outp
   }
 }
 
-// Longer rows: a CTA a row, or a cluster of kCtas, an equal part of its granules each, dealt
-// out to the threads in turn.  The next granules are on their way while some are added, and a
-// row's first while the one before is put in order.
+// Longer rows: a CTA for each, or a cluster of kCtas, an equal part of its granules each, dealt
+// out to the threads in turn; the next granules are on their way while some are added.
 template <typename T, int kBlock, int kCtas>
 __global__ void __launch_bounds__(kBlock, 1024 / kBlock)
     logprob_cta_kernel(Batch<T> b, Outputs o) {
@@ -324,169 +323,149 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock)
   const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
   const int rank = kCtas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const float scale = b.inv_t * policy::kLog2e;
-  const int step = gridDim.x / kCtas;
+  const int row = blockIdx.x / kCtas;
   if (me == 0) n_hits = n_keys = 0;
   if (kCtas > 1) cluster_sync();          // the others are there to be written to
   pdl_wait();
-
-  RowUse use = {kNone, -1, 0};
+  const RowUse use = row_use(b, row);
+  if (use.kind != kComputed) {
+    if (rank == 0) fill_row(o, row, use.kind == kNone ? 0.f : NAN, me, kBlock, b.status);
+    return;
+  }
+  const int n = use.n;
+  const RowPtr<T> z(b.logits + row * b.ld, n);
+  const int each = (z.some_hi + kCtas - 1) / kCtas;
+  const int lo = rank * each, hi = min(lo + each, z.some_hi);
+  const auto load = [&](int i) { return z.load(i < hi ? i : z.some_hi, n); };
   uint4 q[kU];
-  // a row and its first granules
-  auto begin = [&](int row) {
-    use = row < b.rows ? row_use(b, row) : RowUse{kNone, -1, 0};
-    if (use.kind != kComputed) return;
-    const RowPtr<T> z(b.logits + row * b.ld, use.n);
-    const int each = (z.some_hi + kCtas - 1) / kCtas, hi = min((rank + 1) * each, z.some_hi);
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int i = rank * each + me + u * kBlock;
-      q[u] = z.load(i < hi ? i : z.some_hi, use.n);
-    }
-  };
-  int row = blockIdx.x / kCtas;
-  begin(row);
-  for (; row < b.rows; row += step) {
-    const RowUse now = use;
-    if (now.kind != kComputed) {
-      if (rank == 0)
-        fill_row(o, row, now.kind == kNone ? 0.f : NAN, me, kBlock, b.status);
-      begin(row + step);
-      continue;
-    }
-    const int n = now.n;
-    const RowPtr<T> z(b.logits + row * b.ld, n);
-    const int each = (z.some_hi + kCtas - 1) / kCtas;
-    const int lo = rank * each, hi = min(lo + each, z.some_hi);
-    float za = 0.f;
-    if (me == 0 && now.token >= 0) za = to_float(z.z[now.token]);
-    RowSum x;
-    x.clear();
-    // the largest logit of every kU << shift of a thread's granules to a slot of its own
-    int shift = 0, batch = 0;
-    while (((each + kU * kBlock - 1) / (kU * kBlock) - 1) >> shift >= kSlots) ++shift;
-    float largest = -INFINITY;
-    for (int i = lo + me; i < hi; i += kU * kBlock, ++batch) {
-      uint4 next[kU];
+  for (int u = 0; u < kU; ++u) q[u] = load(lo + me + u * kBlock);
+  float za = 0.f;
+  if (me == 0 && use.token >= 0) za = to_float(z.z[use.token]);
+  RowSum x;
+  x.clear();
+  // the largest logit of every kU << shift of a thread's granules to a slot of its own
+  int shift = 0, batch = 0;
+  while (((each + kU * kBlock - 1) / (kU * kBlock) - 1) >> shift >= kSlots) ++shift;
+  float largest = -INFINITY;
+  for (int i = lo + me; i < hi; i += kU * kBlock, ++batch) {
+    uint4 next[kU];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int k = i + (kU + u) * kBlock;
-        next[u] = z.load(k < hi ? k : z.some_hi, n);
-      }
-      x.add<T>(q, scale);
-      if (o.top > 0) {
-#pragma unroll
-        for (int u = 0; u < kU; ++u) largest = fmaxf(largest, Granule<T>::largest(q[u]));
-        some[batch >> shift][me] = largest;
-        if (((batch + 1) & ((1 << shift) - 1)) == 0) largest = -INFINITY;
-      }
-#pragma unroll
-      for (int u = 0; u < kU; ++u) q[u] = next[u];
-    }
-    begin(row + step);
-    Part part = x.over(32, scale);
-    if (lane == 0) slots[warp] = part;
-    maxima[me] = x.m;
-    __syncthreads();
-    part = policy::join_parts<kW>(slots, scale);
-    if (kCtas > 1) {
-      if (me < kCtas) policy::store_part_remote(part, &parts[rank], me);
-    }
-    const int64_t at = static_cast<int64_t>(row) * o.top;
+    for (int u = 0; u < kU; ++u) next[u] = load(i + (kU + u) * kBlock);
+    x.add<T>(q, scale);
     if (o.top > 0) {
-      if (warp == 0) {
-        float m[kW];
 #pragma unroll
-        for (int i = 0; i < kW; ++i) m[i] = maxima[lane + 32 * i];
-        const float t = threshold<kW>(m, o.top);
-        if (lane == 0) tau_at = t;
-      }
-      __syncthreads();
-      const float tau = tau_at;
-      if (x.m >= tau && x.m > -INFINITY)
-        for (int k = 0; k << shift < batch; ++k)
-          if (some[k][me] >= tau) {
-            const int h = atomicAdd(&n_hits, 1);
-            if (h < kHits) hits[h] = k * kBlock + me;
-          }
-      __syncthreads();
-      const int n_hit = n_hits, log = 2 + shift;   // granules of a hit
-      static_assert(kU == 4, "two bits of an index into them");
-      if (n_hit <= kHits)
-        for (int w = me; w < n_hit << log; w += kBlock) {
-          const int hit = hits[w >> log], in = w & ((1 << log) - 1);
-          const int i = lo + hit % kBlock + ((hit / kBlock << log) + in) * kBlock;
-          if (i < hi)
-            for_candidates<T>(z.load(i, n), i * kE - z.mis, tau, [&](uint64_t key) {
-              const int c = atomicAdd(&n_keys, 1);
-              if (c < kKeys) keys[rank * kKeys + c] = key;
-            });
-        }
-      __syncthreads();
-      int found = n_keys;
-      if (found > kKeys || n_hit > kHits) {   // many equal logits: one by one
-        uint64_t last = ~0ull;
-        __syncthreads();
-        for (found = 0; found < o.top; ++found) {
-          uint64_t mine = 0;
-          for (int i = lo + me; i < hi; i += kBlock)
-            mine = largest_below<T>(z.load(i, n), i * kE - z.mis, last, mine);
-          mine = warp_largest(mine);
-          if (lane == 0) best[warp] = mine;
-          __syncthreads();
-          last = best[0];
-#pragma unroll
-          for (int w = 1; w < kW; ++w) last = best[w] > last ? best[w] : last;
-          __syncthreads();
-          if (last == 0) break;
-          if (me == 0) keys[rank * kKeys + found] = last;
-        }
-        __syncthreads();
-      }
-      if (kCtas > 1) {                    // to the first CTA
-        if (rank != 0)
-          for (int i = me; i < found; i += kBlock)
-            store_key_remote(keys[rank * kKeys + i], &keys[rank * kKeys + i], 0);
-        if (me == 0) store_remote(found, &found_in[rank], 0);
-      } else if (me == 0) {
-        found_in[0] = found;
-      }
+      for (int u = 0; u < kU; ++u) largest = fmaxf(largest, Granule<T>::largest(q[u]));
+      some[batch >> shift][me] = largest;
+      if (((batch + 1) & ((1 << shift) - 1)) == 0) largest = -INFINITY;
     }
-    if (kCtas > 1) cluster_sync();        // the parts and the keys have arrived
-    else if (o.top > 0) __syncthreads();
-    if (me == 0) n_hits = n_keys = 0;
-    if (rank == 0) {
-      if (kCtas > 1) part = policy::join_parts<kCtas>(parts, scale);
-      const float ls = write_row(o, row, part, za, now.token >= 0, b.inv_t, me == 0);
-      if (o.top > 0) {
-        if (!isfinite(ls)) {
-          write_no_top(o, at, me, kBlock);
-        } else {
-          int found = found_in[0];
-          if (kCtas > 1) {                // close the gaps between the CTAs' keys
-            found = 0;
-            for (int c = 0; c < kCtas; ++c) {
-              const int some = found_in[c];
-              uint64_t key = 0;
-              if (me < some) key = keys[c * kKeys + me];
-              __syncthreads();
-              if (me < some) keys[found + me] = key;
-              found += some;
-            }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) q[u] = next[u];
+  }
+  Part part = x.over(32, scale);
+  if (lane == 0) slots[warp] = part;
+  maxima[me] = x.m;
+  __syncthreads();
+  part = policy::join_parts<kW>(slots, scale);
+  if (kCtas > 1) {
+    if (me < kCtas) policy::store_part_remote(part, &parts[rank], me);
+  }
+  const int64_t at = static_cast<int64_t>(row) * o.top;
+  if (o.top > 0) {
+    if (warp == 0) {
+      float m[kW];
+#pragma unroll
+      for (int i = 0; i < kW; ++i) m[i] = maxima[lane + 32 * i];
+      const float t = threshold<kW>(m, o.top);
+      if (lane == 0) tau_at = t;
+    }
+    __syncthreads();
+    const float tau = tau_at;
+    if (x.m >= tau && x.m > -INFINITY)
+      for (int k = 0; k << shift < batch; ++k)
+        if (some[k][me] >= tau) {
+          const int h = atomicAdd(&n_hits, 1);
+          if (h < kHits) hits[h] = k * kBlock + me;
+        }
+    __syncthreads();
+    const int n_hit = n_hits, log = 2 + shift;   // granules of a hit
+    static_assert(kU == 4, "two bits of an index into them");
+    if (n_hit <= kHits)
+      for (int w = me; w < n_hit << log; w += kBlock) {
+        const int hit = hits[w >> log], in = w & ((1 << log) - 1);
+        const int i = lo + hit % kBlock + ((hit / kBlock << log) + in) * kBlock;
+        if (i < hi)
+          for_candidates<T>(z.load(i, n), i * kE - z.mis, tau, [&](uint64_t key) {
+            const int c = atomicAdd(&n_keys, 1);
+            if (c < kKeys) keys[rank * kKeys + c] = key;
+          });
+      }
+    __syncthreads();
+    int found = n_keys;
+    if (found > kKeys || n_hit > kHits) {   // many equal logits: one by one
+      uint64_t last = ~0ull;
+      __syncthreads();
+      for (found = 0; found < o.top; ++found) {
+        uint64_t mine = 0;
+        for (int i = lo + me; i < hi; i += kBlock)
+          mine = largest_below<T>(z.load(i, n), i * kE - z.mis, last, mine);
+        mine = warp_largest(mine);
+        if (lane == 0) best[warp] = mine;
+        __syncthreads();
+        last = best[0];
+#pragma unroll
+        for (int w = 1; w < kW; ++w) last = best[w] > last ? best[w] : last;
+        __syncthreads();
+        if (last == 0) break;
+        if (me == 0) keys[rank * kKeys + found] = last;
+      }
+      __syncthreads();
+    }
+    if (kCtas > 1) {                    // to the first CTA
+      if (rank != 0)
+        for (int i = me; i < found; i += kBlock)
+          store_key_remote(keys[rank * kKeys + i], &keys[rank * kKeys + i], 0);
+      if (me == 0) store_remote(found, &found_in[rank], 0);
+    } else if (me == 0) {
+      found_in[0] = found;
+    }
+  }
+  if (kCtas > 1) cluster_sync();        // the parts and the keys have arrived
+  else if (o.top > 0) __syncthreads();
+  if (rank == 0) {
+    if (kCtas > 1) part = policy::join_parts<kCtas>(parts, scale);
+    const float ls = write_row(o, row, part, za, use.token >= 0, b.inv_t, me == 0);
+    if (o.top > 0) {
+      if (!isfinite(ls)) {
+        write_no_top(o, at, me, kBlock);
+      } else {
+        int found = found_in[0];
+        if (kCtas > 1) {                // close the gaps between the CTAs' keys
+          found = 0;
+          for (int c = 0; c < kCtas; ++c) {
+            const int some = found_in[c];
+            uint64_t key = 0;
+            if (me < some) key = keys[c * kKeys + me];
             __syncthreads();
+            if (me < some) keys[found + me] = key;
+            found += some;
           }
-          write_top(o, at, keys, found, me, kBlock, part.m, b.inv_t, ls);
+          __syncthreads();
         }
+        write_top(o, at, keys, found, me, kBlock, part.m, b.inv_t, ls);
       }
     }
-    // the shared places are free for the next row
-    if (kCtas > 1) cluster_sync();
-    else __syncthreads();
   }
 }
 
 // ---------------------------------------------------------------------------
 // The gradient: one look at every granule, nothing to wait for.
 // ---------------------------------------------------------------------------
+constexpr float kLn2 = 0.6931471805599453f;
+// At or below this power of two, whatever the row (its shift is 0 or more), p is 0, and so are
+// p a and p b y, with no infinity to make a NaN of them.
+constexpr float kLeast = -512.f;
+
 template <typename T>
 struct GradIn {
   const float* norm;                      // [rows, 2]
@@ -497,7 +476,7 @@ struct GradIn {
 };
 
 struct RowGrad {
-  float m, shift, a, b, at_token;         // e^{scale d - shift} (a + b d) (+ at_token)
+  float m, shift, a, b, at_token;         // 2^{y - shift} (a + b y) (+ at_token), y = scale d
 };
 
 template <typename T>
@@ -509,7 +488,7 @@ __device__ __forceinline__ RowGrad row_grad(const Batch<T>& b, const GradIn<T>& 
     dh = g.dentropy[row];
     a = fmaf(-dh, g.entropy[row] - norm.y, a);
   }
-  return {norm.x, norm.y * policy::kLog2e, a * b.inv_t, -dh * b.inv_t * b.inv_t, dl * b.inv_t};
+  return {norm.x, norm.y * policy::kLog2e, a * b.inv_t, -dh * b.inv_t * kLn2, dl * b.inv_t};
 }
 
 template <typename T>
@@ -519,8 +498,8 @@ __device__ __forceinline__ uint4 grad_granule(uint4 q, const RowGrad& k, float s
   policy::differences<T>(q, -k.m, d);
 #pragma unroll
   for (int e = 0; e < kE; ++e) {
-    const float p = policy::ex2(fmaf(d[e], scale, -k.shift));
-    float v = p * fmaf(k.b, fmaxf(d[e], policy::kFloor), k.a);
+    const float y = fmaxf(d[e] * scale, kLeast);
+    float v = policy::ex2(y - k.shift) * fmaf(k.b, y, k.a);
     if (e == token) v += k.at_token;
     d[e] = v;
   }
@@ -603,7 +582,9 @@ bool valid_batch(const void* logits, int32_t dtype, int32_t rows, int32_t classe
   if (rows < 0 || rows > (1 << 30) || classes < 1 || classes > (1 << 30) || ld < classes ||
       dtype < DORA_BF16 || dtype > DORA_F32)
     return false;
-  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return false;
+  // Below 1e18 a difference at policy::kFloor, which stands for all larger ones, has an
+  // exponential of 0; above 1e-18 one over the temperature leaves room for the gradients.
+  if (!(temperature >= 1e-18f && temperature <= 1e18f)) return false;
   return rows == 0 || (logits != nullptr && (reinterpret_cast<uintptr_t>(logits) &
                                              (dtype == DORA_F32 ? 3u : 1u)) == 0);
 }

@@ -227,7 +227,7 @@ def test_rows_that_are_not_valid(classes):
     assert np.isfinite(_np(grad)[0]).all() and np.isfinite(_np(o["logp"])[0])
 
 
-def _grad_check(z, tokens, legal, temperature, dl, dh, got, o):
+def _grad_check(z, tokens, legal, temperature, dl, dh, got, o, flush=0.0):
     zz, dtype = _np(z), z.dtype
     tk = None if tokens is None else tokens.cpu().numpy()
     lg = None if legal is None else legal.cpu().numpy()
@@ -249,7 +249,11 @@ def _grad_check(z, tokens, legal, temperature, dl, dh, got, o):
     if dln is not None:
         rows = np.flatnonzero(tk >= 0)
         size[rows, tk[rows]] += np.abs(dln)[rows] * 0.5
+    # flush: probabilities that 32 bits hold as 0
+    size_0 = (0 if dln is None else np.abs(dln)[:, None]) + (
+        0 if dhn is None else np.abs(dhn)[:, None] * (100 + np.abs(ls) + np.abs(h)))
     r, a = ROUND[dtype]
+    a = a + flush * size_0 / temperature
     tol = r * np.abs(ref) + a + (1 + r) * e * size / temperature
     assert np.all(np.abs(_np(got) - ref) <= tol), np.max(np.abs(_np(got) - ref) / tol)
 
@@ -360,6 +364,40 @@ def test_same_bits_streams_and_graphs(rows, classes):
     for k, v in first.items():
         assert torch.equal(v, second[k]) and torch.equal(v, third[k])
     assert torch.equal(grads[0], grads[1])
+
+
+@pytest.mark.parametrize("classes", [20, 900, 6000, 40000])
+@pytest.mark.parametrize("temperature", [1e-18, 1e-6, 1e-3, 30.0, 1e6, 1e18])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_extreme_temperatures(classes, temperature, dtype):
+    z = _logits(4, classes, dtype, 16)
+    z[0, ::3] = float("-inf")
+    z[1, ::2] = torch.finfo(dtype).min
+    z[2, 1:5] = z[2, :4].clone()
+    legal = torch.tensor([classes, classes, classes, classes - 3], dtype=I32, device=dev())
+    tokens = torch.tensor([1, 1, 0, 5], dtype=I32, device=dev())
+    o = _forward(z, tokens, legal, temperature, top=3)
+    dl = torch.tensor([1.0, -2.0, 0.5, 1.0], device=dev())
+    dh = torch.tensor([0.5, 1.0, -1.0, 2.0], device=dev())
+    grad = torch.full_like(z, 7.0)
+    P.dora_token_logprob_grad(z, tokens, o["norm"], grad, dlogp=dl, dentropy=dh,
+                              entropy=o["entropy"], legal=legal, temperature=temperature)
+    torch.cuda.synchronize()
+    # the temperature itself and one over it are rounded: an exponent is 2^-22 of itself off at most
+    t = float(np.float32(temperature))
+    _check(z, tokens, o, legal, t)
+    assert bool(torch.isfinite(grad).all())
+    _grad_check(z, tokens, legal, t, dl, dh, grad, o, flush=2.0 ** -126)
+
+
+def test_another_current_device_is_refused(monkeypatch):
+    z = torch.zeros(4, 6, device=dev())
+    tokens, f = torch.zeros(4, dtype=I32, device=dev()), torch.zeros(4, device=dev())
+    monkeypatch.setattr(P, "_raw_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        P.dora_token_logprob(z, tokens, f)
+    with pytest.raises(ValueError, match="current device"):
+        P.dora_token_logprob_grad(z, tokens, torch.zeros(4, 2, device=dev()), z, dlogp=f)
 
 
 def test_empty_batches_and_refusals():

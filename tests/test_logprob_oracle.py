@@ -84,7 +84,7 @@ def test_host_checks(lib):
     assert forward(rows=-1) == 1 and forward(rows=(1 << 30) + 1) == 1
     assert forward(classes=0) == 1 and forward(ld=7) == 1
     assert forward(tokens=None) == 1 and forward(logp=None) == 1
-    for t in (0.0, -1.0, float("inf"), float("nan"), 1e-39):
+    for t in (0.0, -1.0, float("inf"), float("nan"), 1e-39, 9e-19, 1.1e18):
         assert forward(t=t) == 1
     assert forward(top=33, top_logp=16, top_tokens=16) == 1 and forward(top=-1) == 1
     assert forward(top=2, top_logp=16) == 1 and forward(top=2, top_tokens=16) == 1
