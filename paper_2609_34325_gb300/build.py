@@ -18,17 +18,18 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libdora.so")
 # The timeout-path test library: the same objects, except that the bounded waits of
-# the attention and policy loss kernels give up after 5 ms and their first CTA
-# withholds its first K/V load, or its second row, so a wait runs out
-# (tests/test_gpu_timeout.py, tests/test_gpu_policy_timeout.py).
+# the attention, policy loss and orthogonalising kernels give up after 5 ms and their
+# first CTA (or pair) withholds its first K/V load, its second row, or its first operands
+# or product, so a wait runs out (tests/test_gpu_timeout.py,
+# tests/test_gpu_policy_timeout.py, tests/test_gpu_ortho_timeout.py).
 TIMEOUT_TEST_LIB_PATH = os.path.join(HERE, "libdora_timeout_test.so")
 TIMEOUT_TEST_FLAGS = ["-DDORA_TEST_WITHHOLD_KV_LOAD", "-DDORA_TEST_WITHHOLD_ROW_LOAD",
-                      "-DDORA_TEST_WAIT_LIMIT_NS=5000000ull"]
+                      "-DDORA_TEST_WITHHOLD_TILE_LOAD", "-DDORA_TEST_WAIT_LIMIT_NS=5000000ull"]
 SOURCES = ["token_ops.cu", "gemm_tcgen05.cu", "attn_tcgen05.cu", "api.cu", "noalloc.cu",
            "actor.cu", "actor_front.cu", "actor_tail.cu", "embed_head.cu", "training.cu",
            "policy.cu", "logprob.cu", "optim.cu", "ortho.cu"]
 # the translation units rebuilt with the test flags for the timeout-path library
-TIMEOUT_TEST_SOURCES = ("attn_tcgen05.cu", "policy.cu")
+TIMEOUT_TEST_SOURCES = ("attn_tcgen05.cu", "policy.cu", "ortho.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

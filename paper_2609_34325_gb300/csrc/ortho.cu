@@ -31,7 +31,10 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
 #include <string.h>
+
+#include <algorithm>
 
 #include "dora.h"
 #include "dora_ptx.cuh"
@@ -51,8 +54,11 @@ constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
 constexpr int kRowThreads = 256, kRowCtas = 4;
-constexpr int kMaxShort = 16384;
-constexpr int64_t kMaxElements = int64_t{1} << 32;   // a phase of one takes 50 ms, far from a wait's limit
+// Largest sides.  A's sums of n products are added 16 at a time into 32 bits, each time cut off
+// rather than rounded, which makes A too small by up to n 2^-28 of itself: with the longest n the
+// result is up to 4e-3 off for it.  A phase of the largest matrix takes 50 ms, far from a wait's
+// limit.
+constexpr int kMaxShort = 16384, kMaxLong = 262144;
 
 struct Squares;
 
@@ -185,16 +191,6 @@ __global__ void fill_tiles_kernel(List list) {
 }
 
 __device__ __forceinline__ int size_of(int type) { return type == DORA_F32 ? 4 : 2; }
-__device__ __forceinline__ float load_one(const void* p, int type, int64_t i) {
-  if (type == DORA_F32) return static_cast<const float*>(p)[i];
-  if (type == DORA_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[i]);
-  return to_float(static_cast<const __half*>(p)[i]);
-}
-__device__ __forceinline__ void store_one(float v, void* p, int type, int64_t i) {
-  if (type == DORA_F32) static_cast<float*>(p)[i] = v;
-  else if (type == DORA_BF16) from_float(v, static_cast<__nv_bfloat16*>(p) + i);
-  else from_float(v, static_cast<__half*>(p) + i);
-}
 
 // Four elements from the k-th, zeros past the last: 16 bytes of fp32, 8 (in x and y) of the
 // others, at once where `quads` says that they are aligned to that.
@@ -1008,6 +1004,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = false;
             break;
           }
+#ifdef DORA_TEST_WITHHOLD_TILE_LOAD
+          // timeout-path test library only: the first pair never loads its first stage nor
+          // expects its bytes, so that the wait for it runs out with no copy of it in flight
+          if (blockIdx.x < 2 && it == 0) continue;
+#endif
           // the bytes of both CTAs are counted on the first one's barrier
           if (rank == 0)
             mbar_arrive_expect_tx(&s.full[st], 2 * (kTileBytes + (wide ? kTileBytes : kHalfTile)));
@@ -1306,9 +1307,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) {
       list.header->abort = 1;
       record_status(a.status, DORA_ERR_TIMEOUT);
-      if (rank == 0)                      // loads that were issued but never consumed land first
+      // Loads that were issued but never consumed land first.  Those of the second CTA are counted
+      // by the first, which need not have asked for as many: time for them instead.
+      if (rank == 0)
         for (int it = s.consumed; it < s.issued; ++it)
-          mbar_wait_limited(&s.full[it % kStages], (it / kStages) & 1, 100ull * 1000 * 1000);
+          mbar_wait_limited(&s.full[it % kStages], (it / kStages) & 1, 10ull * 1000 * 1000);
+      const uint64_t t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 1000ull * 1000) __nanosleep(1000);
     }
     __syncthreads();
   }
@@ -1335,7 +1340,7 @@ struct SmallSmem {
   uint8_t f[2][kTileBytes], g[2][kTileBytes], extra[2][kTileBytes];
   float d[kSmallRows], e[kSmallRows];
   Squares sums[kMaxParts], scratch[kSmallThreads / 32];
-  uint64_t done;                          // the MMAs of a product
+  uint64_t done, drain;                   // the MMAs of a product; all, after an abort
   uint32_t tmem;
   int abort, bad[kMaxParts];
 };
@@ -1381,6 +1386,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   if (skipped(a) || rank >= parts) return;  // those that have left are not waited for
   if (me == 0) {
     mbar_init(&s.done, 1);
+    mbar_init(&s.drain, 1);
     s.abort = 0;
     fence_barrier_init();
   }
@@ -1548,6 +1554,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     tc_fence_after();
     if (warp == 0 && elect_one()) {
       issue();
+#ifdef DORA_TEST_WITHHOLD_TILE_LOAD
+      // timeout-path test library only: the first CTA never says that its first product is done
+      if (blockIdx.x != 0 || products != 0)
+#endif
       mma_commit(&s.done);
     }
     __syncwarp();
@@ -1725,8 +1735,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       }
     }
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (*abort && warp == 0) {              // MMAs that were not waited for end first
+    if (elect_one()) {
+      mma_commit(&s.drain);
+      mbar_wait_limited(&s.drain, 0, kWaitLimitNs);
+    }
+    __syncwarp();
+  }
   if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -1802,6 +1820,41 @@ struct Sizes {
   bool has_params = true, has_outs = true, ragged = false;   // ragged: among the large ones
 };
 
+// A buffer of a list: [from, to), written by the calls or only read.
+struct Extent {
+  uintptr_t from, to;
+  bool written;
+};
+// Whether a buffer that is written overlaps any other.
+bool overlapping(const dora_matrix* ms, int32_t count) {
+  Extent* all = static_cast<Extent*>(malloc(sizeof(Extent) * 5 * static_cast<size_t>(count)));
+  if (all == nullptr) return true;
+  size_t n = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    const dora_matrix& t = ms[i];
+    const uint64_t elements = static_cast<uint64_t>(t.rows) * static_cast<uint64_t>(t.cols);
+    const auto add = [&](const void* p, int32_t dtype, bool written) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+      if (p != nullptr) all[n++] = {at, at + elements * (dtype == DORA_F32 ? 4 : 2), written};
+    };
+    add(t.grad, t.grad_dtype, false);
+    add(t.param, t.param_dtype, true);
+    add(t.momentum, DORA_F32, true);
+    add(t.copy, DORA_BF16, true);
+    add(t.out, DORA_BF16, true);
+  }
+  std::sort(all, all + n, [](const Extent& a, const Extent& b) { return a.from < b.from; });
+  uintptr_t read_to = 0, written_to = 0;  // ends of the buffers so far
+  bool overlap = false;
+  for (size_t i = 0; i < n; ++i) {
+    overlap |= all[i].from < written_to || (all[i].written && all[i].from < read_to);
+    uintptr_t& to = all[i].written ? written_to : read_to;
+    if (all[i].to > to) to = all[i].to;
+  }
+  free(all);
+  return overlap;
+}
+
 bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
   Sizes z;
   int64_t sym[2] = {0, 0}, all[2] = {0, 0};
@@ -1819,8 +1872,7 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
         !aligned_to(t.out, DORA_BF16))
       return false;
     const Shape s = shape_of(t);
-    if (s.m > ortho::kMaxShort || static_cast<int64_t>(s.m) * s.n > ortho::kMaxElements)
-      return false;
+    if (s.m > ortho::kMaxShort || s.n > ortho::kMaxLong) return false;
     z.chunks += s.chunks;
     z.x_tiles += s.x_tiles;
     for (int k = 0; k < 2; ++k) {
@@ -1837,6 +1889,7 @@ bool count_all(const dora_matrix* ms, int32_t count, Sizes* out) {
     // counted in 32 bits, the tiles' rows among them
     if (z.tiles > (1 << 23) || z.chunks > (1 << 30)) return false;
   }
+  if (overlapping(ms, count)) return false;
   // Narrow tiles where wide ones would leave pairs of SMs without any.
   z.narrow_sym = sym[0] < kFewTiles;
   z.narrow_all = all[0] < kFewTiles;

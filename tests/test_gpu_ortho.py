@@ -286,6 +286,51 @@ def test_what_lies_beside_the_matrices_stays():
     assert not bool((out == 7.0).any())
 
 
+def test_another_current_device_is_refused(monkeypatch):
+    (x,) = _random([(8, 12)], F32, 72)
+    lst = P.MatrixList([x], params=[x.clone()], momentum=[x.clone()], outs=[x.to(BF16)])
+    monkeypatch.setattr(P, "_raw_device", lambda: 1)
+    for call in (lambda: P.MatrixList([x], outs=[x.to(BF16)]), lambda: P.dora_orthogonalize(lst),
+                 lambda: P.dora_muon_step(lst, 0.1)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
+# The longest side; and more than 2^31 elements.  An X X^T of n columns is added up in n / 16
+# steps, each cut off to 32 bits, half of 2^-23 of what there is on average: n 2^-28 of itself at
+# most, of which the iterations, |b s^2 + 2 c s^4| <= 1.8 each, make less than n 2^-26.
+@pytest.mark.parametrize("m,n", [(130, 1 << 18), (8200, 1 << 18)])
+def test_long_matrices(m, n):
+    # What the iteration makes of X0 is M X0, with M a polynomial of A = X0 X0^T, here from fp32
+    # products of few columns added in 64 bits
+    x = torch.empty(m, n, dtype=BF16, device=dev())
+    for r in range(m):
+        x[r].normal_(generator=torch.Generator(device=dev()).manual_seed(r))
+    x[:60] += x[60:120]
+    before = torch.backends.cuda.matmul.allow_tf32
+    torch.backends.cuda.matmul.allow_tf32 = False
+    gram = torch.zeros(m, m, dtype=torch.float64, device=dev())
+    for c in range(0, n, 4096):
+        y = x[:, c:c + 4096].float()
+        gram += (y @ y.t()).double()
+    size = torch.trace(gram).sqrt()
+    gram = (gram / (size * size)).float()
+    a, b, c = O.NS_COEF
+    eye = torch.eye(m, device=dev())
+    poly = eye
+    for _ in range(5):
+        p = poly @ gram @ poly.t()
+        poly = (a * eye + b * p + c * p @ p) @ poly
+    out = torch.empty_like(x)
+    P.dora_orthogonalize(P.MatrixList([x], outs=[out]))
+    torch.cuda.synchronize()
+    for c in (0, n // 2, n - 1000):
+        want = poly @ x[:, c:c + 1000].float() / size.float()
+        off = float((out[:, c:c + 1000].float() - want).norm() / want.norm())
+        assert off <= _bound(m * 1000) + n * 2.0 ** -26 + 2.0 ** -8, (c, off)
+    torch.backends.cuda.matmul.allow_tf32 = before
+
+
 def test_refusals():
     (x,) = _random([(8, 12)], F32, 71)
     bf = x.to(BF16)
@@ -297,6 +342,10 @@ def test_refusals():
                 dict(grads=[x[:0]], outs=[bf[:0]]), dict(grads=[x, x], outs=[bf])):
         with pytest.raises((TypeError, ValueError)):
             P.MatrixList(**bad)
+    with pytest.raises(ValueError):          # buffers that overlap
+        P.MatrixList([x], params=[x], momentum=[x.clone()])
+    with pytest.raises(ValueError):
+        P.MatrixList([x, x], outs=[bf, bf])
     only_outs = P.MatrixList([x], outs=[bf.clone()])
     only_params = P.MatrixList([x], params=[x.clone()], momentum=[x.clone()])
     with pytest.raises(P.DoraError):

@@ -67,9 +67,12 @@ def lib():
     return P.load_library()
 
 
+FAR = 1 << 40                        # between buffers
+
+
 def _matrix(**more):
-    a = dict(grad=256, param=256, momentum=256, copy=256, out=256, rows=5, cols=7, grad_dtype=0,
-             param_dtype=2, scale=1.0)
+    a = dict(grad=FAR, param=2 * FAR, momentum=3 * FAR, copy=4 * FAR, out=5 * FAR, rows=5, cols=7,
+             grad_dtype=0, param_dtype=2, scale=1.0)
     a.update(more)
     return P._MatrixC(**{k: v or 0 if isinstance(v, (int, float)) else v for k, v in a.items()})
 
@@ -89,8 +92,9 @@ def test_list_host_checks(lib):
                 dict(grad_dtype=3), dict(grad_dtype=2, grad=258), dict(momentum=0),
                 dict(param=0, momentum=0), dict(param=0), dict(param_dtype=-1), dict(param=258),
                 dict(momentum=258), dict(copy=257), dict(out=257), dict(scale=float("nan")),
+                dict(out=FAR), dict(momentum=2 * FAR + 136), dict(copy=5 * FAR - 2),
                 dict(scale=float("inf")), dict(rows=16385, cols=16385),
-                dict(rows=1 << 20, cols=4097)):
+                dict(rows=1, cols=262145), dict(rows=262145, cols=300)):
         assert size(**bad) == 0, bad
     assert lib.dora_matrix_list_size(None, 1) == 0
     assert lib.dora_matrix_list_size(ctypes.byref(_matrix()), 0) == 0
@@ -101,6 +105,19 @@ def test_list_host_checks(lib):
     assert prepare(ctypes.byref(m), 1, 300, one, ctypes.byref(l), None) == 1
     assert prepare(ctypes.byref(m), 1, 256, one - 1, ctypes.byref(l), None) == 1
     assert prepare(ctypes.byref(m), 1, 256, one, None, None) == 1
+    # an array of two: the same gradient twice may be read, nothing may be written twice
+    apart = {k: 7 * FAR + i * 256 for i, k in enumerate(("param", "momentum", "copy", "out"))}
+
+    def both(**more):
+        pair = (P._MatrixC * 2)(_matrix(), _matrix(**{**apart, **more}))
+        return lib.dora_matrix_list_size(pair, 2)
+
+    assert both() > one and both(grad=FAR + 70) > one and both(param=2 * FAR + 140) > one
+    for bad in (dict(param=2 * FAR), dict(momentum=3 * FAR + 136), dict(copy=4 * FAR + 68),
+                dict(out=FAR + 68), dict(grad=5 * FAR + 68), dict(grad=2 * FAR - 2)):
+        assert both(**bad) == 0, bad
+    assert prepare((P._MatrixC * 2)(_matrix(), _matrix()), 2, 256, 1 << 30, ctypes.byref(l),
+                   None) == 1
 
 
 def test_call_host_checks(lib):
