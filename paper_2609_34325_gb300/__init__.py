@@ -28,8 +28,8 @@ __all__ = [
     "dora_pl_sample", "dora_pl_logprob", "dora_branch", "dora_kd_cost", "dora_step_rewards",
     "dora_policy_loss", "dora_pl_policy_loss", "dora_policy_workspace_size",
     "alloc_policy_workspace", "dora_token_logprob", "dora_token_logprob_grad",
-    "ParamList", "dora_grad_norm", "dora_clip_grads", "dora_adam_step", "dora_adam_init", "alloc_adam_state", "MatrixList", "dora_orthogonalize",
-    "dora_muon_step",
+    "ParamList", "dora_grad_norm", "dora_clip_grads", "dora_adam_step", "dora_adam_init",
+    "alloc_adam_state", "MatrixList", "dora_orthogonalize", "dora_muon_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))

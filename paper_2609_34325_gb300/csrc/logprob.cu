@@ -9,8 +9,12 @@
 //   d loss / d z_j = [dl (1(j = a) - p_j) - dH p_j (ln p_j + H)] / T
 //                  = p_j (A + B d_j / T) + 1(j = a) dl / T,
 //   A = (-dl - dH (H - ln s)) / T,   B = -dH / T.
-// Both are bound by memory: the forward reads the legal logits once, the gradient reads
-// them once and writes as many.
+// The forward reads the legal logits once, the gradient reads them once and writes as many.
+// Measured, against what that takes of memory: 2048 x 32000 bf16 with 8 alternatives (15% of the
+// rows idle) 32 us of 16, its gradient 43 of 36; 4095 x 50001 fp16 with 5 81 of 57 and 133 of
+// 118.  The gradient is memory's.  The forward is bound by what it executes (two
+// operations of a pair and an exponential an element) and by the ends of its rows:
+// 2048 x 32000 takes 26 us without alternatives.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -233,7 +237,8 @@ __device__ __forceinline__ uint64_t largest_below(uint4 q, int first, uint64_t l
   return best;
 }
 
-// Short rows: a warp holds one, kHeld granules a lane.
+// Short rows: a warp holds one, kHeld granules a lane; no barrier.  256 rows of 96 fp32 logits
+// take 9 us in a call, the host's time.
 template <typename T, int kHeld>
 __global__ void __launch_bounds__(kThreads) logprob_warp_kernel(Batch<T> b, Outputs o) {
   constexpr int kE = Granule<T>::kElems, kKeys = 128;
@@ -459,7 +464,7 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock)
 }
 
 // ---------------------------------------------------------------------------
-// The gradient: one look at every granule, nothing to wait for.
+// The gradient: one look at every granule, nothing to wait for; memory (6.0 TB/s of a copy's 6.8).
 // ---------------------------------------------------------------------------
 constexpr float kLn2 = 0.6931471805599453f;
 // At or below this power of two, whatever the row (its shift is 0 or more), p is 0, and so are

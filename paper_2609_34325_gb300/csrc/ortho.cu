@@ -8,8 +8,8 @@
 // symmetric ones by half: 3 m^2 n + m^3 operations.
 //
 // Precision.  The products take fp16 operands (11 bits; with bf16's 8 the result is 1 to
-// 20% off) and add in fp32.  Two things keep the rounding small where it counts: X itself is carried
-// as hi + lo, two fp16 values of 22 bits, of which only hi goes into the products; and
+// 20% off) and add in fp32.  Two things keep the rounding small where it counts: X itself is
+// carried as hi + lo, two fp16 values of 22 bits, of which only hi goes into the products; and
 // the diagonals of A and of B = b A + c A^2, which hold most of both once the singular
 // values are near 1, stay out of the products, in fp32.  With A = D + F and B = E + G (D, E
 // diagonal, F, G without one):
@@ -17,14 +17,21 @@
 //   E = b D + c (D^2 + diag(F F)),  G = b F + c (D F + F D + F F) off the diagonal,
 //   X <- (a + E) X + G X_hi,
 // so that what is rounded is multiplied by the small G rather than by B, whose product with
-// X nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
-// step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the iteration in 64 bits
-// (relative 2-norm), half the rounding of a bf16 output.
+// nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
+// step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the
+// iteration in 64 bits (relative 2-norm), half the rounding of a bf16 output.
 //
 // Layout.  X hi, X lo, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
-// bytes), padded with zeros: whatever the matrices' sizes, one tensor map describes all
-// of them.  A tile is an operand either way: K-major (rows of X for X X^T) or MN-major (rows
-// of X as the K of G X).
+// bytes): whatever the matrices' sizes, one tensor map describes all of them.  The first block
+// of rows past a matrix' end is filled up with zeros; the second of a last pair is not
+// defined, and nothing that is kept is made of it.  A tile is an operand either way: K-major
+// (rows of X for X X^T) or MN-major (rows of X as the K of G X).
+//
+// Measured (five iterations with momentum and weights): 96 matrices of 1024 x 1024 and 48 of
+// 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.95 ms, of which the two passes before
+// the products 1.15; at the products' 5.4e12 operations that is 1.0 PFLOP/s of 1.94.  72 of
+// 384 x 384 to 1536 x 384 0.53 ms, one of 4096 x 1024 and its like (4) 0.44, the actor's twelve
+// small ones 65 to 70 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -49,7 +56,10 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 // Factors of X and F in fp16, whose values stay below 1.21 and 1.5; G has none.
 constexpr float kXScale = 32768.f, kFScale = 256.f;
 constexpr int kMaxSteps = 32;
-constexpr int64_t kGroup = 64 << 20;      // elements of a group of matrices, about
+// Elements of a group of matrices, about.  A larger group hides the waits between a matrix'
+// phases, a smaller one keeps X in L2; 96 of 1024 x 1024 and 48 of 4096 x 1024: 6 M elements
+// 13.9 ms, 18 M 7.6, 32 M 7.2, 48 M 7.06, 80 M 6.99.
+constexpr int64_t kGroup = 64 << 20;
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
@@ -214,7 +224,8 @@ __device__ __forceinline__ uint4 load_quad(const void* p, int type, int64_t k, i
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (k + j < total)
-        w[j >> 1] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[k + j]) << (16 * (j & 1));
+        w[j >> 1] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[k + j])
+                     << (16 * (j & 1));
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -262,9 +273,10 @@ __device__ __forceinline__ float update_of(const Args& a, float d, float m) {
 }
 
 // ---------------------------------------------------------------------------
-// Momentum, and the update's norm.  A CTA takes a run of chunks, a matrix's one after the
-// other.  A thread sums its squares in fp32; where that leaves the middle of the range, it sums
-// those of u 2^-k, with k the exponent of its largest |u|, so that no finite update
+// Momentum, and the update's norm: memory (21 M elements of bf16 gradients 48 us, 4.4 TB/s; the
+// loads of a chunk are all on their way before the first is used, a chunk's squares are joined
+// behind a barrier).  A CTA takes a run of chunks, a matrix's one after the other.  A thread
+// sums its squares in fp32; where that leaves the middle of the range, it sums those of u 2^-k, with k the exponent of its largest |u|, so that no finite update
 // overflows or vanishes.  The chunks are joined in their order by the CTA that is last
 // of the matrix.
 // ---------------------------------------------------------------------------
@@ -498,7 +510,9 @@ __device__ __forceinline__ void split(const float* v, uint4* hi, uint4* lo) {
   *lo = Granule<__half>::pack(rest);
 }
 
-// The normalised update into its tiles; a CTA takes a run of them.
+// The normalised update into its tiles; a CTA takes a run of them.  Memory: 54 us where the
+// momentum took 48; the norm must be known first, so that gradient and momentum are read a
+// second time (the update in a buffer of its own, instead, would be written and read).
 __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List list, Args a) {
   pdl_wait();
   if (skipped(a)) return;
@@ -563,7 +577,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
 // ---------------------------------------------------------------------------
 // The products, all iterations of all matrices in one launch.  The work is a list of
 // output tiles (256 rows, 256 or 128 columns) in an order in which each depends on
-// earlier ones only: the matrices in groups that fit L2, of a group one phase of all its
+// earlier ones only: the matrices in groups, of a group one phase of all its
 // matrices after the other.  CTA pairs take the tiles as they get done with others
 // (a counter), and a tile waits until its matrix has finished the phase before (a counter
 // a matrix).  Whoever holds a tile runs, and the earliest unfinished one waits for
@@ -576,10 +590,14 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
 // copies ahead of them, into three places for each, where it is written over, and from where
 // another one copies it out and reports the tile.  The second CTA's idle MMA warp fetches
 // the tiles.
+//
+// What bounds it: with many stages of K a tile, the operands' way from L2, 64 KB a stage and
+// pair (large backbone's list: 930 cycles a stage on 76 pairs, 512 alone); with few, the
+// epilogues and X's traffic; with few tiles, the chain of phases.
 // ---------------------------------------------------------------------------
 enum Phase { kGram, kSquare, kApply, kLast };
 
-constexpr int kStages = 4;
+constexpr int kStages = 4;                // large list: 3 7.36 ms, 4 6.94, 5 (two places) 6.95
 constexpr int kBlock = 128;               // rows of a CTA's part of an output tile
 constexpr int kWide = 256;                // columns of one
 constexpr int kK = 64;                    // of a stage
@@ -978,14 +996,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int64_t left = gram ? e.x[t.from] : (sym ? e.f : e.g);
         const bool wide = t.width == kWide;
         const int nb = e.nb;
-        const int32_t ya =
-            static_cast<int32_t>((left + static_cast<int64_t>(2 * t.i + rank) * row_tiles) * kTileRows);
+        const int32_t ya = static_cast<int32_t>(
+            (left + static_cast<int64_t>(2 * t.i + rank) * row_tiles) * kTileRows);
         // symmetric: rows of the left operand, 128 or 64 for each CTA; else 64 rows of X, two
         // column tiles or one for each CTA
         int32_t yb;
         if (sym)
-          yb = static_cast<int32_t>((left + static_cast<int64_t>(t.j + (wide ? rank : 0)) * row_tiles) *
-                                    kTileRows) + (wide ? 0 : rank * 64);
+          yb = static_cast<int32_t>(
+                   (left + static_cast<int64_t>(t.j + (wide ? rank : 0)) * row_tiles) * kTileRows) +
+               (wide ? 0 : rank * 64);
         else
           yb = static_cast<int32_t>((e.x[t.from] + 2 * t.j + (wide ? 2 * rank : rank)) * kTileRows);
         for (int k = 0; k < count; ++k, ++it) {
@@ -1134,7 +1153,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool there = true;
       if (lane == 0) there = wait_done(e.done, at->need, abort, list.header);
       if (!__all_sync(0xffffffffu, there)) break;
-      if (phase == kLast && e.param != nullptr) prefetch_weights(e, block, first_col, at->width, lane);
+      if (phase == kLast && e.param != nullptr)
+        prefetch_weights(e, block, first_col, at->width, lane);
       for (int c = 0; ok && c < pieces; ++c, ++loads) {
         const int i = loads % kPlaces;
         for (int h = 0; ok && h < 2; ++h) {
@@ -1329,8 +1349,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // or 8, holds one, 256 columns of X each, in shared memory; A, B and what they are made of are
 // 128 x 128.  Where there are several CTAs each adds up its rows of X X^T over all of them and
 // sends every one its rows of F.  What bounds it is the chain of three products an iteration,
-// each with its reading of tensor memory: the twelve matrices of the actor took 126 us of
-// hand-offs between CTAs in the kernel above.
+// each with its reading of tensor memory, 8 to 9 thousand cycles in one CTA, 16 to 17 in four
+// (128 x 128 and 64 x 787); the first pass and the last take as long as one or two.  The actor's
+// twelve matrices take 65 us (a step 70), with the kernel above 90 and 143.
 // ---------------------------------------------------------------------------
 constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
 constexpr int kSmallThreads = 256;
@@ -1812,6 +1833,8 @@ Shape shape_of(const dora_matrix& t) {
   s.all[1] = pairs * s.nb;
   return s;
 }
+// A list of fewer wide tiles than pairs of SMs is cut into narrow ones: four matrices of
+// 4096 x 1024 and its transpose 432 us, with wide ones 468.
 constexpr int64_t kFewTiles = 76;
 struct Sizes {
   int64_t chunks = 0, x_tiles = 0, sym = 0, all = 0, tiles = 0, diag = 0;
