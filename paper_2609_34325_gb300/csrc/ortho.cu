@@ -276,7 +276,8 @@ __device__ __forceinline__ float update_of(const Args& a, float d, float m) {
 // Momentum, and the update's norm: memory (21 M elements of bf16 gradients 48 us, 4.4 TB/s; the
 // loads of a chunk are all on their way before the first is used, a chunk's squares are joined
 // behind a barrier).  A CTA takes a run of chunks, a matrix's one after the other.  A thread
-// sums its squares in fp32; where that leaves the middle of the range, it sums those of u 2^-k, with k the exponent of its largest |u|, so that no finite update
+// sums its squares in fp32; where that leaves the middle of the range, it sums those of u 2^-k,
+// with k the exponent of its largest |u|, so that no finite update
 // overflows or vanishes.  The chunks are joined in their order by the CTA that is last
 // of the matrix.
 // ---------------------------------------------------------------------------
