@@ -28,10 +28,10 @@
 // (rows of X for X X^T) or MN-major (rows of X as the K of G X).
 //
 // Measured (five iterations with momentum and weights): 96 matrices of 1024 x 1024 and 48 of
-// 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.95 ms, of which the two passes before
-// the products 1.15; at the products' 5.4e12 operations that is 1.0 PFLOP/s of 1.94.  72 of
-// 384 x 384 to 1536 x 384 0.53 ms, one of 4096 x 1024 and its like (4) 0.44, the actor's twelve
-// small ones 65 to 70 us.
+// 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.7 to 6.85 ms, of which the two passes
+// before the products 0.92; at their 5.4e12 operations the products run at 1.0 PFLOP/s of 1.94.
+// 72 of 384 x 384 to 1536 x 384 0.50 ms, four of 4096 x 1024 and its transpose 0.42, the actor's
+// twelve small ones 65 to 71 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -63,7 +63,7 @@ constexpr int64_t kGroup = 64 << 20;
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
-constexpr int kRowThreads = 256, kRowCtas = 4;
+constexpr int kRowThreads = 256, kRowCtas = 4, kMomentumCtas = 3;
 // Largest sides.  A's sums of n products are added 16 at a time into 32 bits, each time cut off
 // rather than rounded, which makes A too small by up to n 2^-28 of itself: with the longest n the
 // result is up to 4e-3 off for it.  A phase of the largest matrix takes 50 ms, far from a wait's
@@ -273,10 +273,12 @@ __device__ __forceinline__ float update_of(const Args& a, float d, float m) {
 }
 
 // ---------------------------------------------------------------------------
-// Momentum, and the update's norm: memory (21 M elements of bf16 gradients 48 us, 4.4 TB/s; the
-// loads of a chunk are all on their way before the first is used, a chunk's squares are joined
-// behind a barrier).  A CTA takes a run of chunks, a matrix's one after the other.  A thread
-// sums its squares in fp32; where that leaves the middle of the range, it sums those of u 2^-k,
+// Momentum, and the update's norm: memory (201 M elements of bf16 gradients 452 us, 4.5 TB/s).
+// The loads of a chunk are all on their way while the one before is joined behind a barrier, and
+// a CTA says once a matrix what it has done (for every chunk, with its fence: 584 us; three CTAs
+// an SM, whose registers are enough, 452, four 492).  A CTA takes a run of chunks, a matrix's one
+// after the other.  A thread sums its squares in fp32; where that leaves the middle of the range,
+// it sums those of u 2^-k,
 // with k the exponent of its largest |u|, so that no finite update
 // overflows or vanishes.  The chunks are joined in their order by the CTA that is last
 // of the matrix.
@@ -332,7 +334,7 @@ __device__ __forceinline__ Squares squares_of(const float (&u)[kN]) {
   return {sum, k};
 }
 
-__global__ void __launch_bounds__(kRowThreads, kRowCtas) momentum_kernel(List list, Args a) {
+__global__ void __launch_bounds__(kRowThreads, kMomentumCtas) momentum_kernel(List list, Args a) {
   constexpr int kPer = kChunk / kRowThreads;
   __shared__ Squares scratch[kRowThreads / 32];
   __shared__ bool last;
@@ -350,33 +352,49 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) momentum_kernel(List li
   const int end = static_cast<int>(static_cast<int64_t>(list.n_chunks) * (blockIdx.x + 1) /
                                    gridDim.x);
   const Entry* at = list.entries + (c < end ? list.chunk_of[c] : 0);
-  for (; c < end; ++c) {
-    if (c - at->first_chunk >= at->chunks) ++at;
-    const Entry& e = *at;
-    const int64_t total = static_cast<int64_t>(e.m) * e.n;
-    const int64_t from = static_cast<int64_t>(c - e.first_chunk) * kChunk;
-    // quads of elements, all on their way before the first is looked at
-    const bool quads = in_quads(e.grad, e.grad_type) && (!a.muon || in_quads(e.momentum, DORA_F32));
-    uint4 qg[kPer / 4], qm[kPer / 4];
-    if (quads && from + kChunk <= total) {
+  uint4 qg[kPer / 4], qm[kPer / 4];
+  // quads of a chunk's elements, all on their way before the first is looked at
+  auto quads_of = [&](const Entry& e) {
+    return in_quads(e.grad, e.grad_type) && (!a.muon || in_quads(e.momentum, DORA_F32));
+  };
+  auto elements = [&](const Entry& e, int64_t from) {
+    const int64_t left = static_cast<int64_t>(e.m) * e.n - from;
+    return left < kChunk ? static_cast<int>(left) : kChunk;
+  };
+  auto load = [&](const Entry& e, int chunk) {
+    const int64_t from = static_cast<int64_t>(chunk - e.first_chunk) * kChunk;
+    const int some = elements(e, from);
+    const bool quads = quads_of(e);
+    const char* g = static_cast<const char*>(e.grad) + from * size_of(e.grad_type);
+    const float* m = e.momentum + from;
+    if (quads && some == kChunk) {
 #pragma unroll
       for (int i = 0; i < kPer / 4; ++i) {
-        const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
-        qg[i] = whole_quad(e.grad, e.grad_type, k);
-        qm[i] = a.muon ? whole_quad(e.momentum, DORA_F32, k) : make_uint4(0, 0, 0, 0);
+        const int k = 4 * (threadIdx.x + i * kRowThreads);
+        qg[i] = whole_quad(g, e.grad_type, k);
+        qm[i] = a.muon ? whole_quad(m, DORA_F32, k) : make_uint4(0, 0, 0, 0);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kPer / 4; ++i) {
-        const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
-        qg[i] = load_quad(e.grad, e.grad_type, k, total, quads);
-        qm[i] = a.muon ? load_quad(e.momentum, DORA_F32, k, total, quads) : make_uint4(0, 0, 0, 0);
+        const int k = 4 * (threadIdx.x + i * kRowThreads);
+        qg[i] = load_quad(g, e.grad_type, k, some, quads);
+        qm[i] = a.muon ? load_quad(m, DORA_F32, k, some, quads) : make_uint4(0, 0, 0, 0);
       }
     }
+  };
+  unsigned chunks = 0;                    // of the matrix, by this CTA
+  if (c < end) load(*at, c);
+  for (; c < end; ++c) {
+    const Entry& e = *at;
+    const int64_t from = static_cast<int64_t>(c - e.first_chunk) * kChunk;
+    const int some = elements(e, from);
+    const bool quads = quads_of(e);
+    float* momentum = e.momentum + from;
     float u[kPer];
 #pragma unroll
     for (int i = 0; i < kPer / 4; ++i) {
-      const int64_t k = from + 4 * (threadIdx.x + i * kRowThreads);
+      const int k = 4 * (threadIdx.x + i * kRowThreads);
       float d[4], m[4];
       unpack_quad(qg[i], e.grad_type, d);
       Granule<float>::unpack(qm[i], m);
@@ -387,19 +405,27 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) momentum_kernel(List li
         u[4 * i + j] = update_of(a, d[j], m[j]);
       }
       if (!a.muon) continue;
-      if (quads && k + 4 <= total) {
-        *reinterpret_cast<uint4*>(e.momentum + k) = Granule<float>::pack(m);
+      if (quads && k + 4 <= some) {
+        *reinterpret_cast<uint4*>(momentum + k) = Granule<float>::pack(m);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (k + j < total) e.momentum[k + j] = m[j];
+          if (k + j < some) momentum[k + j] = m[j];
       }
     }
-    const Squares sum = block_squares(squares_of(u), scratch);
-    if (threadIdx.x == 0) {
-      e.partial[c - e.first_chunk] = sum;
-      last = take_ticket(e.ticket) == static_cast<unsigned>(e.chunks) - 1;
-    }
+    Squares sum = squares_of(u);
+    // the next chunk's are on their way while this one's squares are joined
+    const bool more = c + 1 < end && c + 1 - e.first_chunk < e.chunks;
+    if (c + 1 - e.first_chunk >= e.chunks) ++at;
+    if (c + 1 < end) load(*at, c + 1);
+    sum = block_squares(sum, scratch);
+    if (threadIdx.x == 0) e.partial[c - e.first_chunk] = sum;
+    ++chunks;
+    if (more) continue;
+    // the matrix' last chunk here: one fence and one count for all of them
+    if (threadIdx.x == 0)
+      last = take_tickets(e.ticket, chunks) == static_cast<unsigned>(e.chunks) - chunks;
+    chunks = 0;
     __syncthreads();
     if (!last) continue;
     Squares all = {0.f, -126};
@@ -511,17 +537,37 @@ __device__ __forceinline__ void split(const float* v, uint4* hi, uint4* lo) {
   *lo = Granule<__half>::pack(rest);
 }
 
-// The normalised update into its tiles; a CTA takes a run of them.  Memory: 54 us where the
-// momentum took 48; the norm must be known first, so that gradient and momentum are read a
-// second time (the update in a buffer of its own, instead, would be written and read).
+// Eight rows of a column of X, contiguous where X is the transpose.
+__device__ __forceinline__ Eight load_down(const Entry& e, const Args& a, int row, int col) {
+  Eight x = {};
+  if (row >= e.m || col >= e.n) return x;   // a multiple of eight rows: all of them
+  const int64_t k = static_cast<int64_t>(col) * e.m + row;
+  const uint4* g = reinterpret_cast<const uint4*>(static_cast<const char*>(e.grad) +
+                                                  k * size_of(e.grad_type));
+  put(x.g, g[0]);
+  if (e.grad_type == DORA_F32) put(x.g + 4, g[1]);
+  if (a.muon) {
+    put(x.m, reinterpret_cast<const uint4*>(e.momentum + k)[0]);
+    put(x.m + 4, reinterpret_cast<const uint4*>(e.momentum + k)[1]);
+  }
+  return x;
+}
+
+// The normalised update into its tiles, two that lie side by side at a time; a CTA takes a run of
+// them.  Memory (201 M elements 463 us, 4.3 TB/s): the norm must be known first, so that gradient
+// and momentum are read a second time (the update in a buffer of its own, instead, would be
+// written and read).  Where X is the transpose, eight of its rows are loaded at once and change
+// places in shared memory (one by one, and a tile at a time: 572 us).
 __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List list, Args a) {
+  __shared__ __align__(16) uint16_t turned[2][kTileRows * kTileCols];   // hi, lo
   pdl_wait();
   if (skipped(a)) return;
   const float f = factor(a);
-  int t = static_cast<int>(static_cast<int64_t>(list.n_x) * blockIdx.x / gridDim.x);
-  const int end = static_cast<int>(static_cast<int64_t>(list.n_x) * (blockIdx.x + 1) / gridDim.x);
+  const int pairs = list.n_x / 2;
+  int t = static_cast<int>(static_cast<int64_t>(pairs) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<int64_t>(pairs) * (blockIdx.x + 1) / gridDim.x);
   if (t >= end) return;
-  const Tile first = list.x[t];
+  const Tile first = list.x[2 * t];
   int matrix = first.matrix, ti = first.i, tj = first.j;
   for (; t < end; ++t) {
     const Entry& e = list.entries[matrix];
@@ -529,43 +575,96 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
     const int64_t at = static_cast<int64_t>(ti) * (2 * e.nb) + tj;
     char* hi = tile_at(list, e.x[0] + at);
     char* lo = tile_at(list, e.lo + at);
-    const bool eights = in_eights(e, a);
-    constexpr int kItems = kTileRows * 8 / kRowThreads;
-    // pieces of eight columns, the lanes along what is contiguous in the matrix
-    auto place = [&](int y, int* r, int* piece) {
-      const int w = threadIdx.x + y * kRowThreads;
-      *r = e.tall ? w % kTileRows : w / 8;
-      *piece = e.tall ? w / kTileRows : w % 8;
+    constexpr int kSome = 2;              // eights of a thread on their way at once
+    // hi and lo of eight values
+    auto finish = [&](const Eight& x, bool packed, uint4* h, uint4* l) {
+      float d[8], m[8], v[8];
+      values_of(e, x, packed, d, m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        v[i] = update_of(a, d[i] * f, a.muon ? m[i] : 0.f) * norm.y * norm.x * kXScale;
+      split(v, h, l);
     };
-    constexpr int kSome = 2;
+    if (e.tall && (e.m & 7) == 0 && aligned16(e.grad) && (!a.muon || aligned16(e.momentum))) {
+      const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int y0 = 0; y0 < kItems; y0 += kSome) {
-      Eight x[kSome];
+      for (int side = 0; side < 2; ++side) {
+        // a warp takes 64 rows of four columns; 16-byte parts of a row change places with its
+        // eights of rows
+        auto place = [&](int y, int* r, int* c) {
+          const int w = warp + y * (kRowThreads / 32);
+          *r = 64 * (w & 1) + 8 * (lane & 7);
+          *c = 4 * (w >> 1) + (lane >> 3);
+        };
+#pragma unroll 1
+        for (int y0 = 0; y0 < 4; y0 += kSome) {
+          Eight x[kSome];
 #pragma unroll
-      for (int y = 0; y < kSome; ++y) {
-        int r, piece;
-        place(y0 + y, &r, &piece);
-        x[y] = load_eight(e, a, eights, ti * kTileRows + r, tj * kTileCols + piece * 8);
+          for (int y = 0; y < kSome; ++y) {
+            int r, c;
+            place(y0 + y, &r, &c);
+            x[y] = load_down(e, a, ti * kTileRows + r, (tj + side) * kTileCols + c);
+          }
+#pragma unroll
+          for (int y = 0; y < kSome; ++y) {
+            int r, c;
+            place(y0 + y, &r, &c);
+            uint4 h, l;
+            finish(x[y], true, &h, &l);
+            const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
+            const int to = r * kTileCols + (((c >> 3) ^ ((r >> 3) & 7)) << 3) + (c & 7);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              turned[0][to + i * kTileCols] = static_cast<uint16_t>(hs[i >> 1] >> (16 * (i & 1)));
+              turned[1][to + i * kTileCols] = static_cast<uint16_t>(ls[i >> 1] >> (16 * (i & 1)));
+            }
+          }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < kTileRows * 8 / kRowThreads; ++y) {
+          const int w = threadIdx.x + y * kRowThreads, r = w >> 3, k = w & 7;
+          const int from = r * kTileCols + ((k ^ ((r >> 3) & 7)) << 3);
+          const uint32_t to = tile_offset(r, 8 * k) + side * kTileBytes;
+          *reinterpret_cast<uint4*>(hi + to) = *reinterpret_cast<const uint4*>(&turned[0][from]);
+          *reinterpret_cast<uint4*>(lo + to) = *reinterpret_cast<const uint4*>(&turned[1][from]);
+        }
+        __syncthreads();
       }
+    } else {
+      const bool eights = in_eights(e, a);
+      // pieces of eight columns, the lanes along what is contiguous in the matrix
+      auto place = [&](int y, int* r, int* piece) {
+        const int w = threadIdx.x + y * kRowThreads;
+        *r = e.tall ? w % kTileRows : w / 16;
+        *piece = e.tall ? w / kTileRows : w % 16;
+      };
+#pragma unroll 1
+      for (int y0 = 0; y0 < kTileRows * 16 / kRowThreads; y0 += kSome) {
+        Eight x[kSome];
 #pragma unroll
-      for (int y = 0; y < kSome; ++y) {
-        int r, piece;
-        place(y0 + y, &r, &piece);
-        // a row or columns past the end were loaded one by one
-        const bool packed = eights && ti * kTileRows + r < e.m && tj * kTileCols + piece * 8 < e.n;
-        float d[8], m[8], v[8];
-        values_of(e, x[y], packed, d, m);
+        for (int y = 0; y < kSome; ++y) {
+          int r, piece;
+          place(y0 + y, &r, &piece);
+          x[y] = load_eight(e, a, eights, ti * kTileRows + r, tj * kTileCols + piece * 8);
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          v[i] = update_of(a, d[i] * f, a.muon ? m[i] : 0.f) * norm.y * norm.x * kXScale;
-        uint4 h, l;
-        split(v, &h, &l);
-        const uint32_t to = tile_offset(r, piece * 8);
-        *reinterpret_cast<uint4*>(hi + to) = h;
-        *reinterpret_cast<uint4*>(lo + to) = l;
+        for (int y = 0; y < kSome; ++y) {
+          int r, piece;
+          place(y0 + y, &r, &piece);
+          // a row or columns past the end were loaded one by one
+          const bool packed = eights && ti * kTileRows + r < e.m &&
+                              tj * kTileCols + piece * 8 < e.n;
+          uint4 h, l;
+          finish(x[y], packed, &h, &l);
+          const uint32_t to = tile_offset(r, piece % 8 * 8) + piece / 8 * kTileBytes;
+          *reinterpret_cast<uint4*>(hi + to) = h;
+          *reinterpret_cast<uint4*>(lo + to) = l;
+        }
       }
     }
-    if (++tj == 2 * e.nb) {
+    tj += 2;
+    if (tj == 2 * e.nb) {
       tj = 0;
       if (++ti == 2 * ((e.mb + 1) / 2)) {
         ti = 0;
@@ -673,6 +772,12 @@ __device__ __forceinline__ unsigned load_relaxed(const unsigned* p) {
 // Wait until at most one bulk group of this thread has not completed.
 __device__ __forceinline__ void bulk_wait_group1() {
   asm volatile("cp.async.bulk.wait_group 1;" ::: "memory");
+}
+// A tile to L2.
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x),
+               "r"(y)
+               : "memory");
 }
 // Waits until `need` arrivals were counted; the limit runs anew with each that comes.
 __device__ __forceinline__ bool wait_done(const unsigned* done, unsigned need, volatile int* abort,
@@ -849,19 +954,20 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
 }
 
 // What finishes 32 x 32 values of an accumulator, v, whose other inputs lie in `one`, `two`
-// and, the diagonal over its columns, `dj`.
-template <Phase kPhase, bool kRagged>
+// and, the diagonal over its columns, `dj`.  `reload` brings the next values to v, as soon as
+// these have been used.
+template <Phase kPhase, bool kRagged, typename F>
 __device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int row0, int col,
                                              bool mirrored, int lane, float own, const float* dj,
                                              const uint32_t (&v)[32], uint16_t* one,
-                                             uint16_t* two) {
+                                             uint16_t* two, F reload) {
   const int row = row0 + lane;
   if constexpr (kPhase == kGram || kPhase == kSquare) {
     const bool diagonal = col == row0;    // pieces hold it or nothing of it
     const uint64_t base = twice(fmaf(kC, own, kB) * (1.f / kFScale));
+    uint32_t words[16];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      uint32_t words[4];
       const uint4 f = kPhase == kSquare ? *piece_at(one, lane, k) : make_uint4(0, 0, 0, 0);
       const uint32_t old[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
@@ -891,38 +997,50 @@ __device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int 
           f2_unpack(x, d0, d1);
           x = f2_pack(lane == c ? 0.f : d0, lane == c + 1 ? 0.f : d1);
         }
-        words[i] = to_halves(x);
+        words[4 * k + i] = to_halves(x);
       }
-      const uint4 h = make_uint4(words[0], words[1], words[2], words[3]);
+    }
+    reload();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint4 h = make_uint4(words[4 * k], words[4 * k + 1], words[4 * k + 2],
+                                 words[4 * k + 3]);
       *piece_at(one, lane, k) = h;
       if (mirrored) mirror(two, 8 * k, lane, h);
     }
   } else {
-    float x[32];
+    float x[kPhase == kLast ? 32 : 1];
+    uint32_t nh[kPhase == kApply ? 16 : 1], nl[kPhase == kApply ? 16 : 1];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const uint4 h = *piece_at(one, lane, k), l = *piece_at(two, lane, k);
       const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
-      uint32_t nh[4], nl[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = 8 * k + 2 * i;
         // (a + E) X + G X_hi
         const uint64_t y = f2_fma(twice(own), f2_add(halves(hs[i]), halves(ls[i])),
                                   f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])));
-        if (kPhase == kApply) {
-          nh[i] = to_halves(y);
-          nl[i] = to_halves(f2_fma(halves(nh[i]), twice(-1.f), y));
+        if constexpr (kPhase == kApply) {
+          nh[4 * k + i] = to_halves(y);
+          nl[4 * k + i] = to_halves(f2_fma(halves(nh[4 * k + i]), twice(-1.f), y));
         } else {
           f2_unpack(y, x[c], x[c + 1]);
         }
       }
-      if (kPhase == kApply) {
-        *piece_at(one, lane, k) = make_uint4(nh[0], nh[1], nh[2], nh[3]);
-        *piece_at(two, lane, k) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
-      }
     }
-    if constexpr (kPhase == kLast) finish_last<kRagged>(e, a, row0, col, lane, x, one, two);
+    reload();
+    if constexpr (kPhase == kApply) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        *piece_at(one, lane, k) = make_uint4(nh[4 * k], nh[4 * k + 1], nh[4 * k + 2],
+                                             nh[4 * k + 3]);
+        *piece_at(two, lane, k) = make_uint4(nl[4 * k], nl[4 * k + 1], nl[4 * k + 2],
+                                             nl[4 * k + 3]);
+      }
+    } else {
+      finish_last<kRagged>(e, a, row0, col, lane, x, one, two);
+    }
   }
 }
 
@@ -1152,6 +1270,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                           static_cast<int64_t>(block) * 2 * (phase == kSquare ? e.mb : e.nb);
       const int64_t two = e.lo + static_cast<int64_t>(block) * 2 * e.nb;
       bool there = true;
+      // what has not been read for an iteration; it may still be written, by copies through L2
+      // (72 matrices of 384 x 384 to 1536 x 384: 504 us, without 511)
+      if (phase >= kApply && lane < pieces)
+        tma_prefetch_2d(&maps.tile, 0, static_cast<int32_t>(
+            (two + (first_col >> 6) + lane) * kTileRows));
       if (lane == 0) there = wait_done(e.done, at->need, abort, list.header);
       if (!__all_sync(0xffffffffu, there)) break;
       if (phase == kLast && e.param != nullptr)
@@ -1272,9 +1395,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
                             half * (t.width >> 1);
-      uint32_t next[32];
+      uint32_t v[32];
       if (pieces > 0) {
-        tmem_ld32(from, next);
+        tmem_ld32(from, v);
       } else {                            // nothing of the accumulator is wanted
         tc_fence_before();
         __syncwarp();
@@ -1286,31 +1409,34 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int c = 0; c < pieces; ++c, ++done) {
         const int col = col0 + 32 * c, place = done % kPlaces;
         uint16_t *one = s.piece[place][0][half][q], *two = s.piece[place][1][half][q];
+        const bool there = mbar_wait_warp(&s.piece_full[half][place], (done / kPlaces) & 1, abort);
         tmem_ld_wait();
-        uint32_t v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = next[i];
-        if (c + 1 < pieces) {
-          tmem_ld32(from + 32 * (c + 1), next);
-        } else {                          // this warp is done with the accumulator
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
-        }
-        if (!mbar_wait_warp(&s.piece_full[half][place], (done / kPlaces) & 1, abort)) {
-          tmem_ld_wait();
+        if (!there) {
           ok = false;
           break;
         }
         const float* dj = s.dj[place][half];
+        auto reload = [&] {
+          if (c + 1 < pieces) {
+            tmem_ld32(from + 32 * (c + 1), v);
+          } else {                        // this warp is done with the accumulator
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(&s.acc_empty[acc], 0);
+          }
+        };
         if (phase == kGram)
-          finish_piece<kGram, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kGram, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
+                                       reload);
         else if (phase == kSquare)
-          finish_piece<kSquare, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kSquare, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
+                                         reload);
         else if (phase == kApply)
-          finish_piece<kApply, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kApply, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
+                                        reload);
         else
-          finish_piece<kLast, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two);
+          finish_piece<kLast, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
+                                       reload);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.piece_done[half][place]);
@@ -2034,13 +2160,13 @@ int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaS
   ortho::Maps maps;
   static_assert(sizeof(maps) == sizeof(list->map), "the maps' size is part of the interface");
   memcpy(&maps, list->map, sizeof(maps));
-  const int most = num_sms() * ortho::kRowCtas;
+  const int most = num_sms() * ortho::kRowCtas, some = num_sms() * ortho::kMomentumCtas;
   int e = DORA_OK;
   if (l.count > 0) {
-    e = launched(launch_pdl(ortho::momentum_kernel, dim3(l.n_chunks < most ? l.n_chunks : most),
+    e = launched(launch_pdl(ortho::momentum_kernel, dim3(l.n_chunks < some ? l.n_chunks : some),
                             dim3(ortho::kRowThreads), 0, stream, l, a));
     if (e == DORA_OK)
-      e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x < most ? l.n_x : most),
+      e = launched(launch_pdl(ortho::normalise_kernel, dim3(l.n_x / 2 < most ? l.n_x / 2 : most),
                               dim3(ortho::kRowThreads), 0, stream, l, a));
     if (e == DORA_OK) e = launch_products(maps, l, a, steps, list->ragged != 0, stream);
   }

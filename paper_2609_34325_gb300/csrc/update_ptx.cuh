@@ -45,10 +45,16 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
 
 // One more CTA is done: its number, from 0.  What the thread wrote before is visible to
 // the one that gets the last number, and to what follows a barrier of its CTA.
-__device__ __forceinline__ unsigned take_ticket(unsigned* ticket) {
+__device__ __forceinline__ unsigned take_tickets(unsigned* ticket, unsigned some) {
   unsigned n;
-  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(n) : "l"(ticket) : "memory");
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;"
+               : "=r"(n)
+               : "l"(ticket), "r"(some)
+               : "memory");
   return n;
+}
+__device__ __forceinline__ unsigned take_ticket(unsigned* ticket) {
+  return take_tickets(ticket, 1u);
 }
 
 // A word into CTA `cta` of the cluster.
