@@ -31,7 +31,7 @@
 // 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.7 to 6.85 ms, of which the two passes
 // before the products 0.92; at their 5.4e12 operations the products run at 1.0 PFLOP/s of 1.94.
 // 72 of 384 x 384 to 1536 x 384 0.50 ms, four of 4096 x 1024 and its transpose 0.42, the actor's
-// twelve small ones 65 to 71 us.
+// twelve small ones 65, with momentum and weights 68 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -847,11 +847,11 @@ __device__ __forceinline__ void mirror(uint16_t* piece, int first, int lane, uin
 }
 
 // One value a lane in each of `some` rows: keep times the weight at p (none: 0) plus value(row),
-// to p and, rounded, to copy.
-template <typename T, typename F>
+// to p and, rounded, to copy; kAtOnce weights are loaded at a time (a small matrix' 32 rows at
+// once: the actor's step 70.4 -> 68.3 us; the product kernel has no registers for more than 16).
+template <int kAtOnce, typename T, typename F>
 __device__ __forceinline__ void write_rows(T* p, __nv_bfloat16* copy, int64_t pitch, int some,
                                            float keep, F value) {
-  constexpr int kAtOnce = 16;
   for (int i0 = 0; i0 < some; i0 += kAtOnce) {
     T old[kAtOnce];                       // all on their way before the first is used
     if (p != nullptr)
@@ -878,6 +878,7 @@ __device__ __forceinline__ float4* swapped_part(uint16_t* low, uint16_t* high, i
 }
 // Those of them that exist to the weights (or out), a value a lane: where sizes or alignment do
 // not allow four.
+template <int kAtOnce>
 __device__ __forceinline__ void finish_ragged(void* param, int param_type, __nv_bfloat16* copy,
                                            int64_t pitch, int some, float keep, float step,
                                            uint16_t* low, uint16_t* high) {
@@ -886,18 +887,18 @@ __device__ __forceinline__ void finish_ragged(void* param, int param_type, __nv_
     return reinterpret_cast<const float*>(swapped_part(low, high, i, lane >> 2))[lane & 3] * step;
   };
   if (param == nullptr || param_type == DORA_F32)
-    write_rows(static_cast<float*>(param), copy, pitch, some, keep, value);
+    write_rows<kAtOnce>(static_cast<float*>(param), copy, pitch, some, keep, value);
   else if (param_type == DORA_BF16)
-    write_rows(static_cast<__nv_bfloat16*>(param), copy, pitch, some, keep, value);
+    write_rows<kAtOnce>(static_cast<__nv_bfloat16*>(param), copy, pitch, some, keep, value);
   else
-    write_rows(static_cast<__half*>(param), copy, pitch, some, keep, value);
+    write_rows<kAtOnce>(static_cast<__half*>(param), copy, pitch, some, keep, value);
 }
 
 // 32 x 32 new values of X (scaled; a row a lane) to where the caller wants them, lanes along
 // what is contiguous there: four values each, where sizes and alignment allow, after they have
 // changed places in shared memory, 16 rows in `low`, 16 in `high`.  kRagged: they may not allow it
 // (a kernel of its own: with both ways in one the other spills, 540 us become 586).
-template <bool kRagged>
+template <bool kRagged, int kAtOnce = 16>
 __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int row0, int col0,
                                             int lane, float (&x)[32], uint16_t* low,
                                             uint16_t* high) {
@@ -949,7 +950,7 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
                          : nullptr;
     __nv_bfloat16* copy = reinterpret_cast<__nv_bfloat16*>(a.muon ? e.copy : e.out);
     if (copy != nullptr) copy += at;
-    finish_ragged(param, e.param_type, copy, inners, some, a.keep, step, low, high);
+    finish_ragged<kAtOnce>(param, e.param_type, copy, inners, some, a.keep, step, low, high);
   }
 }
 
@@ -1478,7 +1479,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // sends every one its rows of F.  What bounds it is the chain of three products an iteration,
 // each with its reading of tensor memory, 8 to 9 thousand cycles in one CTA, 16 to 17 in four
 // (128 x 128 and 64 x 787); the first pass and the last take as long as one or two.  The actor's
-// twelve matrices take 65 us (a step 70), with the kernel above 90 and 143.
+// twelve matrices take 65 us (a step 68), with the kernel above 90 and 143.
 // ---------------------------------------------------------------------------
 constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
 constexpr int kSmallThreads = 256;
@@ -1879,7 +1880,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       }
       if (last) {
         uint16_t* scratch = reinterpret_cast<uint16_t*>(s.extra[0]) + warp * 2 * kPiece;
-        finish_last<true>(e, a, q * 32, col0 + 32 * p, lane, x, scratch, scratch + kPiece);
+        finish_last<true, 32>(e, a, q * 32, col0 + 32 * p, lane, x, scratch, scratch + kPiece);
       }
     }
   }
