@@ -1049,7 +1049,6 @@ template <bool kRagged>
 __global__ void __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ Maps maps, List list, Args a, int steps) {
   extern __shared__ __align__(1024) uint8_t raw[];
-  pdl_trigger();
   Smem& s = *reinterpret_cast<Smem*>(raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = static_cast<int>(cluster_ctarank());
@@ -1084,6 +1083,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();
   tc_fence_after();
   pdl_wait();
+  pdl_trigger();                          // all that came before the call is complete: small_kernel
   const bool none = skipped(a);
   const uint32_t tmem = s.tmem;
   volatile int* abort = &s.abort;
@@ -1480,6 +1480,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 // each with its reading of tensor memory, 8 to 9 thousand cycles in one CTA, 16 to 17 in four
 // (128 x 128 and 64 x 787); the first pass and the last take as long as one or two.  The actor's
 // twelve matrices take 65 us (a step 68), with the kernel above 90 and 143.
+//
+// In a list of both kinds it runs beside the products, on the SMs that they leave (`beside`): it
+// needs nothing of theirs, and they start it when all work before the call is complete.  One CTA
+// waits for them at its end, so that whatever follows waits for both.
 // ---------------------------------------------------------------------------
 constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
 constexpr int kSmallThreads = 256;
@@ -1524,15 +1528,20 @@ __device__ __forceinline__ void store_remote_part(uint4 q, uint4* to, uint32_t c
 }
 
 __global__ void __launch_bounds__(kSmallThreads, 1)
-    small_kernel(List list, Args a, int steps, int cluster) {
+    small_kernel(List list, Args a, int steps, int cluster, bool beside) {
   extern __shared__ __align__(1024) uint8_t raw[];
   SmallSmem& s = *reinterpret_cast<SmallSmem*>(raw);
   const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
   const int rank = cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  pdl_wait();
+  if (!beside) pdl_wait();
   const Entry e = list.entries[list.count + blockIdx.x / cluster];   // read once
   const int parts = e.parts;
-  if (skipped(a) || rank >= parts) return;  // those that have left are not waited for
+  const bool waits = beside && blockIdx.x == 0;   // at the end, for the products
+  if (skipped(a)) {
+    if (waits) pdl_wait();
+    return;
+  }
+  if (rank >= parts) return;              // those that have left are not waited for
   if (me == 0) {
     mbar_init(&s.done, 1);
     mbar_init(&s.drain, 1);
@@ -1898,6 +1907,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (waits) pdl_wait();
 }
 
 }  // namespace ortho
@@ -2127,7 +2137,7 @@ int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::
 }
 
 int launch_small(const ortho::List& l, const ortho::Args& a, int steps, int matrices, int parts,
-                 cudaStream_t stream) {
+                 bool beside, cudaStream_t stream) {
   constexpr int smem = sizeof(ortho::SmallSmem);
   const cudaError_t e = cudaFuncSetAttribute(
       ortho::small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -2151,7 +2161,7 @@ int launch_small(const ortho::List& l, const ortho::Args& a, int steps, int matr
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return launched(cudaLaunchKernelEx(&cfg, ortho::small_kernel, l, a, steps, parts));
+  return launched(cudaLaunchKernelEx(&cfg, ortho::small_kernel, l, a, steps, parts, beside));
 }
 
 int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaStream_t stream) {
@@ -2172,7 +2182,7 @@ int run(const dora_matrix_list* list, int32_t steps, const ortho::Args& a, cudaS
     if (e == DORA_OK) e = launch_products(maps, l, a, steps, list->ragged != 0, stream);
   }
   if (e == DORA_OK && list->count > list->large)
-    e = launch_small(l, a, steps, list->count - list->large, list->parts, stream);
+    e = launch_small(l, a, steps, list->count - list->large, list->parts, l.count > 0, stream);
   return e;
 }
 }  // namespace

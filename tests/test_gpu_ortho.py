@@ -276,6 +276,33 @@ def test_a_matrix_does_not_depend_on_its_list():
         assert torch.equal(alone, o)
 
 
+@pytest.mark.parametrize("small,large", [(6, 2), (200, 1), (40, 30)])
+def test_small_matrices_beside_large_ones(small, large):
+    # both kinds in a list run at the same time; steps one behind the other, and what reads the
+    # weights after them, wait for both
+    shapes = [(100, 37), (64, 787), (9, 1500), (128, 128)] * small + [(640, 700), (257, 511)] * large
+    shapes = shapes[:small] + shapes[4 * small:]
+
+    def steps(lists):
+        g, m, p = _muon(shapes, BF16, F32, 43)
+        seen = []
+        made = [P.MatrixList([g[i] for i in k], params=[p[i] for i in k],
+                             momentum=[m[i] for i in k]) for k in lists]
+        for _ in range(4):
+            for lst in made:
+                P.dora_muon_step(lst, 1e-2)
+            seen.append([x.clone() for x in p])
+            for x, y in zip(g, p):                 # gradients of the new weights
+                x.copy_(y * 0.1 + x * 0.9)
+        torch.cuda.synchronize()
+        return [x for r in seen for x in r] + m
+
+    every = range(len(shapes))
+    together = steps([every])
+    apart = steps([[i for i in every if i < small], [i for i in every if i >= small]])
+    assert all(torch.equal(a, b) for a, b in zip(together, apart))
+
+
 def test_what_lies_beside_the_matrices_stays():
     flat = torch.full((4000,), 7.0, dtype=BF16, device=dev())
     out = flat[101:101 + 33 * 65].view(33, 65)
