@@ -19,7 +19,8 @@
 // so that what is rounded is multiplied by the small G rather than by B, whose product with
 // nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
 // step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the
-// iteration in 64 bits (relative 2-norm), half the rounding of a bf16 output.
+// iteration in 64 bits (relative 2-norm), half the rounding of a bf16 output; up to 32 rows it
+// would be more, and F and G are split as X is (kFineRows).
 //
 // Layout.  X hi, X lo, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
 // bytes): whatever the matrices' sizes, one tensor map describes all of them.  The first block
@@ -1489,6 +1490,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------
 constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
 constexpr int kSmallThreads = 256;
+// Up to so many rows F and G are carried as hi + lo too, in the tiles that their second 64 columns
+// would take, and all products take both halves: the roundings of few values do not average
+// out (random matrices of 1 to 16 rows: 4e-4 to 7e-3 off without, 1e-5 at most with).
+constexpr int kFineRows = 32;
 
 struct SmallSmem {
   uint8_t hi[kSmallTiles][kTileBytes], lo[kSmallTiles][kTileBytes];
@@ -1564,6 +1569,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int all = (e.n + 63) / 64, each = (all + parts - 1) / parts;
   const int tile0 = rank * each, tiles = max(0, min(each, all - tile0)), col0 = 64 * tile0;
   const int halves = (e.m + 63) / 64;     // of the products over m
+  const bool fine = e.m <= kFineRows;
   const float f = factor(a);
   const bool eights = in_eights(e, a);
 
@@ -1728,9 +1734,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     product([&] {
       for (int t = 0; t < tiles; ++t) {
         const uint64_t x = sdesc_sw128(smem_u32(s.hi[t]), 16, 1024);
+        const uint64_t y = sdesc_sw128(smem_u32(s.lo[t]), 16, 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ss(tmem, x + 2 * k, x + 2 * k, idesc_f16(128, 128, false), (t | k) != 0);
+        for (int k = 0; k < 4; ++k) {
+          constexpr uint32_t idesc = idesc_f16(128, 128, false);
+          mma_bf16_ss(tmem, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
+          if (!fine) continue;
+          mma_bf16_ss(tmem, x + 2 * k, y + 2 * k, idesc, 1u);
+          mma_bf16_ss(tmem, y + 2 * k, x + 2 * k, idesc, 1u);
+        }
       }
     });
     // F and d, from A
@@ -1743,9 +1755,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             own = x[i] * (1.f / kFScale);
             x[i] = 0.f;
           }
-        store(own, true, Granule<__half>::pack(x));
+        store(own, true, x);
       } else {
-        store(0.f, false, Granule<__half>::pack(x));
+        store(0.f, false, x);
       }
     };
 #pragma unroll
@@ -1768,9 +1780,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             x[i] = __uint_as_float(v[8 * k + i]) * (kFScale / (kXScale * kXScale));
-          keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, uint4 h) {
+          keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, const float* y) {
             if (diagonal) s.d[row] = own;
-            *tile_part(s.f[half], row, 4 * c + k) = h;
+            if (!fine) {
+              *tile_part(s.f[half], row, 4 * c + k) = Granule<__half>::pack(y);
+            } else if (half == 0) {
+              uint4 h, l;
+              split(y, &h, &l);
+              *tile_part(s.f[0], row, 4 * c + k) = h;
+              *tile_part(s.f[1], row, 4 * c + k) = l;
+            }
           });
         }
       }
@@ -1805,10 +1824,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         const int r = g / eighths, c8 = g % eighths;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= kFScale / (kXScale * kXScale);
-        keep(r, c8, x, [&](float own, bool diagonal, uint4 h) {
+        keep(r, c8, x, [&](float own, bool diagonal, const float* y) {
+          uint4 h, l;
+          split(y, &h, &l);
           for (int c = 0; c < parts; ++c) {
             if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), c);
             store_remote_part(h, tile_part(s.f[c8 >> 3], r, c8 & 7), c);
+            if (fine) store_remote_part(l, tile_part(s.f[1], r, c8 & 7), c);
           }
         });
       }
@@ -1817,9 +1839,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     product([&] {
       for (int t = 0; t < halves; ++t) {
         const uint64_t x = sdesc_sw128(smem_u32(s.f[t]), 16, 1024);
+        const uint64_t y = sdesc_sw128(smem_u32(s.f[1]), 16, 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ss(tmem + 128, x + 2 * k, x + 2 * k, idesc_f16(128, 128, false), (t | k) != 0);
+        for (int k = 0; k < 4; ++k) {
+          constexpr uint32_t idesc = idesc_f16(128, 128, false);
+          mma_bf16_ss(tmem + 128, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
+          if (!fine) continue;
+          mma_bf16_ss(tmem + 128, x + 2 * k, y + 2 * k, idesc, 1u);
+          mma_bf16_ss(tmem + 128, y + 2 * k, x + 2 * k, idesc, 1u);
+        }
       }
     });
     const float di = s.d[row], base = fmaf(kC, di, kB) * (1.f / kFScale);
@@ -1832,7 +1860,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       for (int k = 0; k < 4; ++k) {
         const int col = 64 * half + 32 * c + 8 * k;
         float x[8], off[8];
-        Granule<__half>::unpack(*tile_part(s.f[half], row, 4 * c + k), off);
+        Granule<__half>::unpack(*tile_part(s.f[fine ? 0 : half], row, 4 * c + k), off);
+        if (fine) {
+          float rest[8];
+          Granule<__half>::unpack(*tile_part(s.f[1], row, 4 * c + k), rest);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) off[i] += rest[i];
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float ff = __uint_as_float(v[8 * k + i]) * (kC / (kFScale * kFScale));
@@ -1842,7 +1876,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             x[i] = 0.f;
           }
         }
-        *tile_part(s.g[half], row, 4 * c + k) = Granule<__half>::pack(x);
+        if (!fine) {
+          *tile_part(s.g[half], row, 4 * c + k) = Granule<__half>::pack(x);
+        } else if (half == 0) {
+          uint4 h, l;
+          split(x, &h, &l);
+          *tile_part(s.g[0], row, 4 * c + k) = h;
+          *tile_part(s.g[1], row, 4 * c + k) = l;
+        }
       }
     }
     product([&] {
@@ -1851,9 +1892,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       for (int t = 0; t < halves; ++t) {
         const uint64_t x = sdesc_sw128(smem_u32(s.g[t]), 16, 1024);
         const uint64_t y = sdesc_sw128(smem_u32(s.hi[0]) + t * kHalfTile, kTileBytes, 1024);
+        const uint64_t xl = sdesc_sw128(smem_u32(s.g[1]), 16, 1024);
+        const uint64_t yl = sdesc_sw128(smem_u32(s.lo[0]), kTileBytes, 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
           mma_bf16_ss(tmem + 256, x + 2 * k, y + 128 * k, idesc, (t | k) != 0);
+          if (!fine) continue;
+          mma_bf16_ss(tmem + 256, x + 2 * k, yl + 128 * k, idesc, 1u);
+          mma_bf16_ss(tmem + 256, xl + 2 * k, y + 128 * k, idesc, 1u);
+        }
       }
     });
     const bool last = step + 1 == steps;

@@ -131,6 +131,23 @@ def test_zeros_and_what_is_not_finite():
         assert _off(_np(outs[i]), O.newton_schulz(_np(grads[i]))) <= _bound(4096) + 2.0 ** -8
 
 
+# Up to 32 rows or columns X, F and G have 22 bits: an iteration's four roundings of 2^-22 (the
+# sums' among them) grow by 3.4445 at most in each of those that follow: 4 2^-22 (1 + 3.4 + .. +
+# 3.4445^4) = 1.9e-4.  Weights of 0, a rate of 1 and no momentum show the result in 32 bits.
+@pytest.mark.parametrize("shape", [(1, 1), (1, 2), (2, 1), (1, 40), (2, 2), (2, 5), (3, 3), (50, 3),
+                                   (5, 5), (8, 9), (16, 16), (32, 32), (32, 33), (20, 700),
+                                   (700, 12), (32, 2048), (1500, 17)])
+def test_few_rows_are_exact(shape):
+    grads = _random([shape] * 20, F32, 81)
+    params = [torch.zeros_like(x) for x in grads]
+    lst = P.MatrixList(grads, params=params, momentum=[torch.zeros_like(x) for x in grads],
+                       scales=[1.0] * 20)
+    P.dora_muon_step(lst, 1.0, momentum=0.0)
+    torch.cuda.synchronize()
+    for x, p in zip(grads, params):
+        assert _off(-_np(p), O.newton_schulz(_np(x))) <= 2e-4
+
+
 def test_low_rank_updates():
     g = torch.Generator(device=dev()).manual_seed(7)
     for r, c, k in ((200, 300, 1), (300, 200, 5), (128, 640, 2)):
