@@ -32,7 +32,7 @@
 // 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.7 to 6.85 ms, of which the two passes
 // before the products 0.92; at their 5.4e12 operations the products run at 1.0 PFLOP/s of 1.94.
 // 72 of 384 x 384 to 1536 x 384 0.50 ms, four of 4096 x 1024 and its transpose 0.42, the actor's
-// twelve small ones 65, with momentum and weights 68 us.
+// twelve small ones 67, with momentum and weights 70 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1482,7 +1482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // sends every one its rows of F.  What bounds it is the chain of three products an iteration,
 // each with its reading of tensor memory, 8 to 9 thousand cycles in one CTA, 16 to 17 in four
 // (128 x 128 and 64 x 787); the first pass and the last take as long as one or two.  The actor's
-// twelve matrices take 65 us (a step 68), with the kernel above 90 and 143.
+// twelve matrices take 67 us (a step 70), with the kernel above 90 and 143.
 //
 // In a list of both kinds it runs beside the products, on the SMs that they leave (`beside`): it
 // needs nothing of theirs, and they start it when all work before the call is complete.  One CTA
@@ -1534,21 +1534,11 @@ __device__ __forceinline__ void store_remote_part(uint4 q, uint4* to, uint32_t c
       : "memory");
 }
 
-__global__ void __launch_bounds__(kSmallThreads, 1)
-    small_kernel(List list, Args a, int steps, int cluster, bool beside) {
-  extern __shared__ __align__(1024) uint8_t raw[];
-  SmallSmem& s = *reinterpret_cast<SmallSmem*>(raw);
-  const int me = threadIdx.x, warp = me >> 5, lane = me & 31;
-  const int rank = cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  if (!beside) pdl_wait();
-  const Entry e = list.entries[list.count + blockIdx.x / cluster];   // read once
-  const int parts = e.parts;
-  const bool waits = beside && blockIdx.x == 0;   // at the end, for the products
-  if (skipped(a)) {
-    if (waits) pdl_wait();
-    return;
-  }
-  if (rank >= parts) return;              // those that have left are not waited for
+// The matrix of a CTA, or its part of one.
+template <bool kFine>
+__device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int steps, int rank,
+                                             SmallSmem& s) {
+  const int me = threadIdx.x, warp = me >> 5, lane = me & 31, parts = e.parts;
   if (me == 0) {
     mbar_init(&s.done, 1);
     mbar_init(&s.drain, 1);
@@ -1569,7 +1559,6 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int all = (e.n + 63) / 64, each = (all + parts - 1) / parts;
   const int tile0 = rank * each, tiles = max(0, min(each, all - tile0)), col0 = 64 * tile0;
   const int halves = (e.m + 63) / 64;     // of the products over m
-  const bool fine = e.m <= kFineRows;
   const float f = factor(a);
   const bool eights = in_eights(e, a);
 
@@ -1739,7 +1728,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         for (int k = 0; k < 4; ++k) {
           constexpr uint32_t idesc = idesc_f16(128, 128, false);
           mma_bf16_ss(tmem, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
-          if (!fine) continue;
+          if (!kFine) continue;
           mma_bf16_ss(tmem, x + 2 * k, y + 2 * k, idesc, 1u);
           mma_bf16_ss(tmem, y + 2 * k, x + 2 * k, idesc, 1u);
         }
@@ -1782,7 +1771,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             x[i] = __uint_as_float(v[8 * k + i]) * (kFScale / (kXScale * kXScale));
           keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, const float* y) {
             if (diagonal) s.d[row] = own;
-            if (!fine) {
+            if (!kFine) {
               *tile_part(s.f[half], row, 4 * c + k) = Granule<__half>::pack(y);
             } else if (half == 0) {
               uint4 h, l;
@@ -1830,7 +1819,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
           for (int c = 0; c < parts; ++c) {
             if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), c);
             store_remote_part(h, tile_part(s.f[c8 >> 3], r, c8 & 7), c);
-            if (fine) store_remote_part(l, tile_part(s.f[1], r, c8 & 7), c);
+            if (kFine) store_remote_part(l, tile_part(s.f[1], r, c8 & 7), c);
           }
         });
       }
@@ -1844,7 +1833,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         for (int k = 0; k < 4; ++k) {
           constexpr uint32_t idesc = idesc_f16(128, 128, false);
           mma_bf16_ss(tmem + 128, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
-          if (!fine) continue;
+          if (!kFine) continue;
           mma_bf16_ss(tmem + 128, x + 2 * k, y + 2 * k, idesc, 1u);
           mma_bf16_ss(tmem + 128, y + 2 * k, x + 2 * k, idesc, 1u);
         }
@@ -1860,8 +1849,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       for (int k = 0; k < 4; ++k) {
         const int col = 64 * half + 32 * c + 8 * k;
         float x[8], off[8];
-        Granule<__half>::unpack(*tile_part(s.f[fine ? 0 : half], row, 4 * c + k), off);
-        if (fine) {
+        Granule<__half>::unpack(*tile_part(s.f[kFine ? 0 : half], row, 4 * c + k), off);
+        if (kFine) {
           float rest[8];
           Granule<__half>::unpack(*tile_part(s.f[1], row, 4 * c + k), rest);
 #pragma unroll
@@ -1876,7 +1865,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             x[i] = 0.f;
           }
         }
-        if (!fine) {
+        if (!kFine) {
           *tile_part(s.g[half], row, 4 * c + k) = Granule<__half>::pack(x);
         } else if (half == 0) {
           uint4 h, l;
@@ -1897,7 +1886,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           mma_bf16_ss(tmem + 256, x + 2 * k, y + 128 * k, idesc, (t | k) != 0);
-          if (!fine) continue;
+          if (!kFine) continue;
           mma_bf16_ss(tmem + 256, x + 2 * k, yl + 128 * k, idesc, 1u);
           mma_bf16_ss(tmem + 256, xl + 2 * k, y + 128 * k, idesc, 1u);
         }
@@ -1956,7 +1945,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  if (waits) pdl_wait();
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1)
+    small_kernel(List list, Args a, int steps, int cluster, bool beside) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  SmallSmem& s = *reinterpret_cast<SmallSmem*>(raw);
+  const int rank = cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  if (!beside) pdl_wait();
+  const Entry e = list.entries[list.count + blockIdx.x / cluster];   // read once
+  // those of a cluster that have no part leave, and are not waited for
+  if (!skipped(a) && rank < e.parts) {
+    if (e.m <= kFineRows) small_matrix<true>(e, a, steps, rank, s);
+    else small_matrix<false>(e, a, steps, rank, s);   // apart: the actor's 67 us, in one 72
+  }
+  if (beside && blockIdx.x == 0) pdl_wait();   // for the products
 }
 
 }  // namespace ortho
