@@ -948,9 +948,10 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
  * which brings all singular values near 1 (five steps: those above a hundredth of
  * the norm to 0.7 .. 1.2).  A matrix of zeros stays one; one that holds a value that is
  * not finite becomes NaN.  fp16 products added in fp32, X carried in 22 bits: 1.2e-3 off
- * at most (2-norm), a longer side n above 65536 adds up to n 2^-26: no more than the rounding
- * of `out`.  All operands have 22 bits where the shorter side is at most 32 and the longer one
- * 2048: 2e-4 at most.  Same inputs, same bits.
+ * at most (2-norm) for matrices of noise, a longer side n above 65536 adds up to n 2^-26.
+ * All operands have 22 bits where the shorter side is at most 128 and the longer one 2048: 3e-4 at
+ * most after five steps, also where few directions hold most of a matrix.  Same inputs, same
+ * bits.
  * status     nullable device int32: DORA_ERR_TIMEOUT should a bounded wait run out,
  *            which leaves `out` unfinished.
  */

@@ -19,8 +19,9 @@
 // so that what is rounded is multiplied by the small G rather than by B, whose product with
 // nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
 // step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the
-// iteration in 64 bits (relative 2-norm), half the rounding of a bf16 output; up to 32 rows it
-// would be more, and F and G are split as X is (kFineRows).
+// iteration in 64 bits (relative 2-norm) for matrices of noise.  Where few directions hold most of
+// a matrix it would be up to 3e-2: what lies beside them is raised by 3.4 an iteration, and with
+// it the rounding of X_hi.  Small matrices therefore take F, G and X as hi + lo in all products.
 //
 // Layout.  X hi, X lo, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
 // bytes): whatever the matrices' sizes, one tensor map describes all of them.  The first block
@@ -32,7 +33,7 @@
 // 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.7 to 6.85 ms, of which the two passes
 // before the products 0.92; at their 5.4e12 operations the products run at 1.0 PFLOP/s of 1.94.
 // 72 of 384 x 384 to 1536 x 384 0.50 ms, four of 4096 x 1024 and its transpose 0.42, the actor's
-// twelve small ones 67, with momentum and weights 70 us.
+// twelve small ones 85, with momentum and weights 88 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1480,9 +1481,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 // or 8, holds one, 256 columns of X each, in shared memory; A, B and what they are made of are
 // 128 x 128.  Where there are several CTAs each adds up its rows of X X^T over all of them and
 // sends every one its rows of F.  What bounds it is the chain of three products an iteration,
-// each with its reading of tensor memory, 8 to 9 thousand cycles in one CTA, 16 to 17 in four
-// (128 x 128 and 64 x 787); the first pass and the last take as long as one or two.  The actor's
-// twelve matrices take 67 us (a step 70), with the kernel above 90 and 143.
+// each with its reading of tensor memory; the first pass and the last take as long as one or two.
+//
+// X, F and G are hi + lo, 22 bits, and every product adds hi hi, hi lo and lo hi.  With 11 bits of
+// F and G, and of X in G X, the actor's twelve matrices took 67 us instead of 85 (a step 70
+// instead of 88), but a matrix of few directions came out wrong by up to 3e-2 (64 x 512 of two rows
+// that are not zero, nearly along one direction), with 22 bits by 2e-5.
 //
 // In a list of both kinds it runs beside the products, on the SMs that they leave (`beside`): it
 // needs nothing of theirs, and they start it when all work before the call is complete.  One CTA
@@ -1490,14 +1494,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------
 constexpr int kSmallRows = 128, kSmallTiles = 4, kMaxParts = 8;
 constexpr int kSmallThreads = 256;
-// Up to so many rows F and G are carried as hi + lo too, in the tiles that their second 64 columns
-// would take, and all products take both halves: the roundings of few values do not average
-// out (random matrices of 1 to 16 rows: 4e-4 to 7e-3 off without, 1e-5 at most with).
-constexpr int kFineRows = 32;
 
 struct SmallSmem {
   uint8_t hi[kSmallTiles][kTileBytes], lo[kSmallTiles][kTileBytes];
-  uint8_t f[2][kTileBytes], g[2][kTileBytes], extra[2][kTileBytes];
+  uint8_t f[4][kTileBytes];               // F, then G in its place: hi of 64 columns each, then lo
+  uint8_t extra[2][kTileBytes];
   float d[kSmallRows], e[kSmallRows];
   Squares sums[kMaxParts], scratch[kSmallThreads / 32];
   uint64_t done, drain;                   // the MMAs of a product; all, after an abort
@@ -1510,9 +1511,9 @@ static_assert(sizeof(SmallSmem) <= 227 * 1024, "shared memory");
 __device__ __forceinline__ uint4* tile_part(uint8_t* tile, int r, int k) {
   return reinterpret_cast<uint4*>(tile + r * 128 + ((k ^ (r & 7)) << 4));
 }
-// Part k of row r of a 128 x 128 matrix of fp32 values.
-__device__ __forceinline__ uint4* wide_part(uint8_t* matrix, int r, int k) {
-  return reinterpret_cast<uint4*>(matrix + r * 512 + ((k ^ (r & 31)) << 4));
+// Part k of row r of a matrix of fp32 values of `cols` columns, 64 or 128.
+__device__ __forceinline__ uint4* wide_part(uint8_t* matrix, int cols, int r, int k) {
+  return reinterpret_cast<uint4*>(matrix + r * cols * 4 + ((k ^ (r & (cols / 4 - 1))) << 4));
 }
 __device__ __forceinline__ uint4 load_remote(const uint4* from, uint32_t cta) {
   uint4 q;
@@ -1535,7 +1536,6 @@ __device__ __forceinline__ void store_remote_part(uint4 q, uint4* to, uint32_t c
 }
 
 // The matrix of a CTA, or its part of one.
-template <bool kFine>
 __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int steps, int rank,
                                              SmallSmem& s) {
   const int me = threadIdx.x, warp = me >> 5, lane = me & 31, parts = e.parts;
@@ -1559,6 +1559,10 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
   const int all = (e.n + 63) / 64, each = (all + parts - 1) / parts;
   const int tile0 = rank * each, tiles = max(0, min(each, all - tile0)), col0 = 64 * tile0;
   const int halves = (e.m + 63) / 64;     // of the products over m
+  const int wide = 64 * halves;           // rows and columns of A that are looked at
+  // a CTA's part of A, for the others: beside F where it is small, else in F's place, so that all
+  // have read it before F is written
+  uint8_t* part_of_a = halves == 1 ? s.extra[0] : s.f[0];
   const float f = factor(a);
   const bool eights = in_eights(e, a);
 
@@ -1571,7 +1575,7 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
   Squares sum = {0.f, -126};
   if (parts > 1) {                        // F has no more than the matrix' rows and columns
     uint4* zero = reinterpret_cast<uint4*>(s.f[0]);
-    for (int i = me; i < 2 * kTileBytes / 16; i += kSmallThreads) zero[i] = make_uint4(0, 0, 0, 0);
+    for (int i = me; i < 4 * kTileBytes / 16; i += kSmallThreads) zero[i] = make_uint4(0, 0, 0, 0);
     if (me < kSmallRows) s.d[me] = 0.f;
   }
   if (eights) {
@@ -1699,6 +1703,7 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
 
   const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(q * 32) << 16;
+  const bool has_rows = q * 32 < wide, has_part = has_rows && half < halves;
   int products = 0;
   // What the threads wrote to shared memory is there for the tensor cores; one thread issues the
   // MMAs of a product, all wait for it.
@@ -1728,7 +1733,6 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
         for (int k = 0; k < 4; ++k) {
           constexpr uint32_t idesc = idesc_f16(128, 128, false);
           mma_bf16_ss(tmem, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
-          if (!kFine) continue;
           mma_bf16_ss(tmem, x + 2 * k, y + 2 * k, idesc, 1u);
           mma_bf16_ss(tmem, y + 2 * k, x + 2 * k, idesc, 1u);
         }
@@ -1749,56 +1753,55 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
         store(0.f, false, x);
       }
     };
+    if (has_part)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {         // 32 columns at a time
-      uint32_t v[32];
-      tmem_ld32(tmem + lanes + 64 * half + 32 * c, v);
-      tmem_ld_wait();
-      if (tiles == 0)
+      for (int c = 0; c < 2; ++c) {       // 32 columns at a time
+        uint32_t v[32];
+        tmem_ld32(tmem + lanes + 64 * half + 32 * c, v);
+        tmem_ld_wait();
+        if (tiles == 0)
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = 0u;
-      if (parts > 1) {
+          for (int i = 0; i < 32; ++i) v[i] = 0u;
+        if (parts > 1) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          *wide_part(s.g[0], row, 16 * half + 8 * c + k) =
-              make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-      } else {
+          for (int k = 0; k < 8; ++k)
+            *wide_part(part_of_a, wide, row, 16 * half + 8 * c + k) =
+                make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float x[8];
+          for (int k = 0; k < 4; ++k) {
+            float x[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            x[i] = __uint_as_float(v[8 * k + i]) * (kFScale / (kXScale * kXScale));
-          keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, const float* y) {
-            if (diagonal) s.d[row] = own;
-            if (!kFine) {
-              *tile_part(s.f[half], row, 4 * c + k) = Granule<__half>::pack(y);
-            } else if (half == 0) {
+            for (int i = 0; i < 8; ++i)
+              x[i] = __uint_as_float(v[8 * k + i]) * (kFScale / (kXScale * kXScale));
+            keep(row, 8 * half + 4 * c + k, x, [&](float own, bool diagonal, const float* y) {
+              if (diagonal) s.d[row] = own;
               uint4 h, l;
               split(y, &h, &l);
-              *tile_part(s.f[0], row, 4 * c + k) = h;
-              *tile_part(s.f[1], row, 4 * c + k) = l;
-            }
-          });
+              *tile_part(s.f[half], row, 4 * c + k) = h;
+              *tile_part(s.f[2 + half], row, 4 * c + k) = l;
+            });
+          }
         }
       }
-    }
     if (parts > 1) {
       cluster_sync();                     // all parts of A are there
-      // an equal share of the rows and columns that there are for each, eight columns at a time;
-      // a thread adds up to 64 values, all on their way before the first is added
+      // an equal share of the rows and columns that there are (in F's place: of all) for each,
+      // eight columns at a time; a thread adds up to 64 values, all on their way before the first
+      // is added
       const int log = parts == 2 ? 1 : (parts == 4 ? 2 : 3);
-      const int eighths = (e.m + 7) / 8, groups = 8 * eighths * eighths;
+      const int eighths = halves == 1 ? (e.m + 7) / 8 : wide / 8, groups = 8 * eighths * eighths;
       const int share = (groups + parts - 1) >> log, end = min((rank + 1) * share, groups);
       const int group = rank * share + me;
       uint4 in[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {      // of the i-th pair: eight columns, a part of A
         const int pair = i >> 1, g = group + (pair >> log) * kSmallThreads;
-        in[i] = g < end ? load_remote(wide_part(s.g[0], g / eighths, 2 * (g % eighths) + (i & 1)),
-                                      pair & (parts - 1))
+        in[i] = g < end ? load_remote(wide_part(part_of_a, wide, g / eighths,
+                                                2 * (g % eighths) + (i & 1)), pair & (parts - 1))
                         : make_uint4(0, 0, 0, 0);
       }
+      if (halves == 2) cluster_sync();    // all have read them
       float x[8];
 #pragma unroll
       for (int pair = 0; pair < 8; ++pair) {
@@ -1819,7 +1822,7 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
           for (int c = 0; c < parts; ++c) {
             if (diagonal) store_remote(__float_as_int(own), reinterpret_cast<int*>(&s.d[r]), c);
             store_remote_part(h, tile_part(s.f[c8 >> 3], r, c8 & 7), c);
-            if (kFine) store_remote_part(l, tile_part(s.f[1], r, c8 & 7), c);
+            store_remote_part(l, tile_part(s.f[2 + (c8 >> 3)], r, c8 & 7), c);
           }
         });
       }
@@ -1828,65 +1831,54 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
     product([&] {
       for (int t = 0; t < halves; ++t) {
         const uint64_t x = sdesc_sw128(smem_u32(s.f[t]), 16, 1024);
-        const uint64_t y = sdesc_sw128(smem_u32(s.f[1]), 16, 1024);
+        const uint64_t y = sdesc_sw128(smem_u32(s.f[2 + t]), 16, 1024);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           constexpr uint32_t idesc = idesc_f16(128, 128, false);
           mma_bf16_ss(tmem + 128, x + 2 * k, x + 2 * k, idesc, (t | k) != 0);
-          if (!kFine) continue;
           mma_bf16_ss(tmem + 128, x + 2 * k, y + 2 * k, idesc, 1u);
           mma_bf16_ss(tmem + 128, y + 2 * k, x + 2 * k, idesc, 1u);
         }
       }
     });
     const float di = s.d[row], base = fmaf(kC, di, kB) * (1.f / kFScale);
+    if (has_part)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      uint32_t v[32];
-      tmem_ld32(tmem + 128 + lanes + 64 * half + 32 * c, v);
-      tmem_ld_wait();
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32];
+        tmem_ld32(tmem + 128 + lanes + 64 * half + 32 * c, v);
+        tmem_ld_wait();
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int col = 64 * half + 32 * c + 8 * k;
-        float x[8], off[8];
-        Granule<__half>::unpack(*tile_part(s.f[kFine ? 0 : half], row, 4 * c + k), off);
-        if (kFine) {
-          float rest[8];
-          Granule<__half>::unpack(*tile_part(s.f[1], row, 4 * c + k), rest);
+        for (int k = 0; k < 4; ++k) {
+          const int col = 64 * half + 32 * c + 8 * k;
+          uint4 *hi = tile_part(s.f[half], row, 4 * c + k),
+                *lo = tile_part(s.f[2 + half], row, 4 * c + k);
+          float x[8], h[8], l[8];
+          Granule<__half>::unpack(*hi, h);
+          Granule<__half>::unpack(*lo, l);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) off[i] += rest[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float ff = __uint_as_float(v[8 * k + i]) * (kC / (kFScale * kFScale));
-          x[i] = fmaf(off[i], fmaf(s.d[col + i], kC / kFScale, base), ff);
-          if (row == col + i) {
-            s.e[row] = fmaf(fmaf(kC, di, kB), di, ff);
-            x[i] = 0.f;
+          for (int i = 0; i < 8; ++i) {
+            const float ff = __uint_as_float(v[8 * k + i]) * (kC / (kFScale * kFScale));
+            x[i] = fmaf(h[i] + l[i], fmaf(s.d[col + i], kC / kFScale, base), ff);
+            if (row == col + i) {
+              s.e[row] = fmaf(fmaf(kC, di, kB), di, ff);
+              x[i] = 0.f;
+            }
           }
-        }
-        if (!kFine) {
-          *tile_part(s.g[half], row, 4 * c + k) = Granule<__half>::pack(x);
-        } else if (half == 0) {
-          uint4 h, l;
-          split(x, &h, &l);
-          *tile_part(s.g[0], row, 4 * c + k) = h;
-          *tile_part(s.g[1], row, 4 * c + k) = l;
+          split(x, hi, lo);               // G, in F's place
         }
       }
-    }
     product([&] {
       if (tiles == 0) return;
       const uint32_t idesc = idesc_f16(128, 64 * tiles, true);
       for (int t = 0; t < halves; ++t) {
-        const uint64_t x = sdesc_sw128(smem_u32(s.g[t]), 16, 1024);
+        const uint64_t x = sdesc_sw128(smem_u32(s.f[t]), 16, 1024);
         const uint64_t y = sdesc_sw128(smem_u32(s.hi[0]) + t * kHalfTile, kTileBytes, 1024);
-        const uint64_t xl = sdesc_sw128(smem_u32(s.g[1]), 16, 1024);
-        const uint64_t yl = sdesc_sw128(smem_u32(s.lo[0]), kTileBytes, 1024);
+        const uint64_t xl = sdesc_sw128(smem_u32(s.f[2 + t]), 16, 1024);
+        const uint64_t yl = sdesc_sw128(smem_u32(s.lo[0]) + t * kHalfTile, kTileBytes, 1024);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           mma_bf16_ss(tmem + 256, x + 2 * k, y + 128 * k, idesc, (t | k) != 0);
-          if (!kFine) continue;
           mma_bf16_ss(tmem + 256, x + 2 * k, yl + 128 * k, idesc, 1u);
           mma_bf16_ss(tmem + 256, xl + 2 * k, y + 128 * k, idesc, 1u);
         }
@@ -1908,7 +1900,7 @@ __device__ __forceinline__ void small_matrix(const Entry& e, const Args& a, int 
       }
     }
     const float own = kA + s.e[row];
-    for (int p = half; p < 2 * tiles; p += 2) {
+    for (int p = half; has_rows && p < 2 * tiles; p += 2) {
       uint32_t v[32];
       tmem_ld32(tmem + 256 + lanes + 32 * p, v);
       tmem_ld_wait();
@@ -1955,10 +1947,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   if (!beside) pdl_wait();
   const Entry e = list.entries[list.count + blockIdx.x / cluster];   // read once
   // those of a cluster that have no part leave, and are not waited for
-  if (!skipped(a) && rank < e.parts) {
-    if (e.m <= kFineRows) small_matrix<true>(e, a, steps, rank, s);
-    else small_matrix<false>(e, a, steps, rank, s);   // apart: the actor's 67 us, in one 72
-  }
+  if (!skipped(a) && rank < e.parts) small_matrix(e, a, steps, rank, s);
   if (beside && blockIdx.x == 0) pdl_wait();   // for the products
 }
 
