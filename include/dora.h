@@ -947,11 +947,10 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
  *   A = X X^T,   X <- 3.4445 X + (-4.7750 A + 2.0315 A^2) X,
  * which brings all singular values near 1 (five steps: those above a hundredth of
  * the norm to 0.7 .. 1.2).  A matrix of zeros stays one; one that holds a value that is
- * not finite becomes NaN.  fp16 products added in fp32, X carried in 22 bits: 1.2e-3 off
- * at most (2-norm) for matrices of noise, a longer side n above 65536 adds up to n 2^-26.
- * All operands have 22 bits where the shorter side is at most 128 and the longer one 2048: 3e-4 at
- * most after five steps, also where few directions hold most of a matrix.  Same inputs, same
- * bits.
+ * not finite becomes NaN.  All operands have 22 bits (two fp16 values), added in fp32:
+ * 3e-4 off at most (2-norm, five steps, before `out` is rounded), also where few directions or few
+ * rows hold most of a matrix, and for long sums, which are cut off rather than rounded, m 2^-22
+ * and n 2^-26 more (m the shorter side, n the longer one).  Same inputs, same bits.
  * status     nullable device int32: DORA_ERR_TIMEOUT should a bounded wait run out,
  *            which leaves `out` unfinished.
  */

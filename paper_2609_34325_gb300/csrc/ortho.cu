@@ -7,33 +7,40 @@
 // values stay below 1.21).  Three products an iteration on the tensor cores, the two
 // symmetric ones by half: 3 m^2 n + m^3 operations.
 //
-// Precision.  The products take fp16 operands (11 bits; with bf16's 8 the result is 1 to
-// 20% off) and add in fp32.  Two things keep the rounding small where it counts: X itself is
-// carried as hi + lo, two fp16 values of 22 bits, of which only hi goes into the products; and
-// the diagonals of A and of B = b A + c A^2, which hold most of both once the singular
-// values are near 1, stay out of the products, in fp32.  With A = D + F and B = E + G (D, E
-// diagonal, F, G without one):
-//   A^2 = D^2 + D F + F D + F F,    B X = E X + G X_hi,
+// Precision.  What lies beside the directions that hold most of a matrix is raised by 3.4 an
+// iteration, and every error there with it, up to 140 times in five: products of fp16 operands
+// (11 bits) were up to 3e-2 off where few directions or few rows hold a gradient.  Therefore
+// every operand is hi + lo, two fp16 values of 22 bits, of which the products take hi hi, hi lo
+// and lo hi, added in fp32.  (Taking lo of X alone would leave up to 3e-3 where two rows are not
+// zero: the roundings of few values do not average out.)  The diagonals of A and of
+// B = b A + c A^2, which hold most of both once the singular values are near 1, stay out of the
+// products, in fp32.  With A = D + F and B = E + G (D, E diagonal, F, G without one):
+//   A^2 = D^2 + D F + F D + F F,    B X = E X + G X,
 //   E = b D + c (D^2 + diag(F F)),  G = b F + c (D F + F D + F F) off the diagonal,
-//   X <- (a + E) X + G X_hi,
-// so that what is rounded is multiplied by the small G rather than by B, whose product with
-// nearly cancels against a X.  (lo has no factor of its own: with X times 2^15, its smallest
-// step is 1e-9 of a normalised update's average.)  The result is 2e-4 to 1.2e-3 off the
-// iteration in 64 bits (relative 2-norm) for matrices of noise.  Where few directions hold most of
-// a matrix it would be up to 3e-2: what lies beside them is raised by 3.4 an iteration, and with
-// it the rounding of X_hi.  Small matrices therefore take F, G and X as hi + lo in all products.
+//   X <- (a + E) X + G X.
+// (lo has no factor of its own: with X times 2^15, its smallest step is 1e-9 of a normalised
+// update's average.)  Measured against the iteration in 64 bits (relative 2-norm): matrices of
+// noise 1e-6 to 2e-5 (64 x 512 to 4096 x 4096), one direction over 1e-3 of noise 5e-5 to 2.3e-4
+// (64 x 512 to 1024 x 1024), 6.6e-4 (4096 x 4096); the iteration in fp32 4e-6, 2.2e-4, 4.3e-4.
+// What is left of it is how the tensor cores add: cut off, not rounded, so that long sums are
+// too small, 7e-4 off for a side of 65536.
 //
-// Layout.  X hi, X lo, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
-// bytes): whatever the matrices' sizes, one tensor map describes all of them.  The first block
+// Layout.  X, F and G are kept in tiles of 128 x 64 fp16 values (16 KB, rows of 128
+// bytes): whatever the matrices' sizes, a few tensor maps describe all of them.  The first block
 // of rows past a matrix' end is filled up with zeros; the second of a last pair is not
 // defined, and nothing that is kept is made of it.  A tile is an operand either way: K-major
 // (rows of X for X X^T) or MN-major (rows of X as the K of G X).
+// X's halves, hi and lo, take turns in three slots (slot_tile).  F and G are symmetric: hi lies
+// above the diagonal, the mirror image of lo below it, in as much memory as one of them takes.
+// With T the matrix that is stored, F = T + T^T, in the blocks of the diagonal too; elsewhere one
+// of the two terms is hi, the other lo.
 //
 // Measured (five iterations with momentum and weights): 96 matrices of 1024 x 1024 and 48 of
-// 4096 x 1024, bf16 gradients and copies, fp32 weights: 6.7 to 6.85 ms, of which the two passes
-// before the products 0.92; at their 5.4e12 operations the products run at 1.0 PFLOP/s of 1.94.
-// 72 of 384 x 384 to 1536 x 384 0.50 ms, four of 4096 x 1024 and its transpose 0.42, the actor's
-// twelve small ones 85, with momentum and weights 88 us.
+// 4096 x 1024, bf16 gradients and copies, fp32 weights: 13.1 ms, of which the two passes
+// before the products 0.92; at three times their 5.4e12 operations the products run at 1.3
+// PFLOP/s of 1.94.  72 of 384 x 384 to 1536 x 384 0.77 ms, four of 4096 x 1024 and its transpose
+// 1.0, the actor's twelve small ones 85, with momentum and weights 88 us.  (Operands of 11 bits:
+// 6.8, 0.50, 0.42 ms, 67 and 70 us.)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -60,16 +67,16 @@ constexpr float kXScale = 32768.f, kFScale = 256.f;
 constexpr int kMaxSteps = 32;
 // Elements of a group of matrices, about.  A larger group hides the waits between a matrix'
 // phases, a smaller one keeps X in L2; 96 of 1024 x 1024 and 48 of 4096 x 1024: 6 M elements
-// 13.9 ms, 18 M 7.6, 32 M 7.2, 48 M 7.06, 80 M 6.99.
+// 32.3 ms, 18 M 15.7, 32 M 13.5, 48 M 13.1, 128 M 13.1.
 constexpr int64_t kGroup = 64 << 20;
 constexpr int kTileRows = 128, kTileCols = 64;
 constexpr int kTileBytes = kTileRows * kTileCols * 2;
 constexpr int kChunk = 4096;              // elements of a matrix that a CTA takes at once
 constexpr int kRowThreads = 256, kRowCtas = 4, kMomentumCtas = 3;
-// Largest sides.  A's sums of n products are added 16 at a time into 32 bits, each time cut off
-// rather than rounded, which makes A too small by up to n 2^-28 of itself: with the longest n the
-// result is up to 4e-3 off for it.  A phase of the largest matrix takes 50 ms, far from a wait's
-// limit.
+// Largest sides.  A's sums of n products are added 16 at a time into 32 bits, three times over,
+// each time cut off rather than rounded, which makes A too small by up to 3 n 2^-28 of itself:
+// with the longest n the result is 2.6e-3 off for it (130 x 2^18, noise).  A phase of the largest
+// matrix, 2.1e14 operations, takes 0.2 s at the large list's rate; a wait's limit is 1 s.
 constexpr int kMaxShort = 16384, kMaxLong = 262144;
 
 struct Squares;
@@ -85,14 +92,14 @@ struct Entry {
   int32_t quads;                          // what is written is aligned to four values, row by row
   int32_t mb, nb;                         // blocks of 128 rows, of 128 columns; X, F and G
                                           // have an even number of the first
-  int64_t x[2], lo, f, g;                 // first tiles of X hi (two, in turn), X lo, F, G
+  int64_t x, slot, f, g;                  // first tiles of X's three slots, tiles of each, F, G
   float *d, *e;                           // the diagonals of A and B
   Squares* partial;                       // of its chunks
   float2* norm;                           // one over the norm of u 2^-k, and 2^-k
   unsigned* ticket;                       // chunks done; zero between calls
   unsigned* done;                         // CTAs' parts of its tiles that are done, in this call
   int32_t chunks;
-  int32_t n_sym, n_all;                   // its tiles of A and B, and of X
+  int32_t n_sym, n_all;                   // its tiles of A and B, and of half of X
   int32_t sym_width, all_width;           // their columns
   int32_t parts;                          // of a small matrix: CTAs
   // first of its chunks, of its tiles of X and of its output tiles among the list's
@@ -111,8 +118,8 @@ struct Group {
   int sym0, sym1, all0, all1;
 };
 
-// One piece of work: a pair of block rows (or one) of a matrix, its first block column and
-// its columns.
+// One piece of work: a pair of block rows (or one) of a matrix, its first column, of A and B in
+// blocks, of a half of X in tiles, and its columns.
 struct Tile {
   int32_t matrix, i, j, width;
 };
@@ -165,9 +172,9 @@ __global__ void fill_tiles_kernel(List list) {
   if (t < list.n_all) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_all; });
     const Entry& e = list.entries[q];
-    const int at = static_cast<int>(t - e.first_all), each = e.all_width / 128;
+    const int at = static_cast<int>(t - e.first_all), each = e.all_width / kTileCols;
     const int w = (e.nb + each - 1) / each, j = at % w * each;
-    list.all[t] = Tile{q, at / w, j, j + each <= e.nb ? e.all_width : 128};
+    list.all[t] = Tile{q, at / w, j, (j + each <= e.nb ? each : e.nb - j) * kTileCols};
   }
   if (t < list.n_sym) {
     const int q = matrix_of(list, t, [](const Entry& e) { return e.first_sym; });
@@ -458,6 +465,20 @@ __device__ __forceinline__ char* tile_at(const List& list, int64_t tile) {
 __device__ __forceinline__ uint32_t pair_of(float a, float b) {
   return Granule<__half>::pair(a, b);
 }
+// X lies in two halves of nb columns of tiles, each hi, then lo, in two of three slots.  An
+// iteration writes the new left half to the third and the new right one over the old left one, so
+// that `turn` iterations (mod 3) later the left half is in slot -turn, the right one in the next.
+// What an iteration writes lies where the next one looks for it.
+__device__ __forceinline__ int64_t slot_tile(const Entry& e, int turn, int half) {
+  const int at = half - turn;
+  return e.x + (at < 0 ? at + 3 : at) * e.slot;
+}
+// Tile of hi (part 0) or lo (1) of a block row and a column of tiles.
+__device__ __forceinline__ int64_t x_tile(const Entry& e, int turn, int row, int col, int part) {
+  const int half = col >= e.nb ? 1 : 0;
+  return slot_tile(e, turn, half) + part * (e.slot / 2) + static_cast<int64_t>(row) * e.nb + col -
+         half * e.nb;
+}
 
 // The gradient and the momentum of eight columns from `col` of a row of X, as they are loaded:
 // nothing is made of them before all loads of a thread are on their way.  What is not there is 0.
@@ -574,9 +595,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
   for (; t < end; ++t) {
     const Entry& e = list.entries[matrix];
     const float2 norm = *e.norm;
-    const int64_t at = static_cast<int64_t>(ti) * (2 * e.nb) + tj;
-    char* hi = tile_at(list, e.x[0] + at);
-    char* lo = tile_at(list, e.lo + at);
+    // of the tile and of the one beside it
+    const auto hi = [&](int side) { return tile_at(list, x_tile(e, 0, ti, tj + side, 0)); };
+    const auto lo = [&](char* p) { return p + e.slot / 2 * kTileBytes; };
     constexpr int kSome = 2;              // eights of a thread on their way at once
     // hi and lo of eight values
     auto finish = [&](const Eight& x, bool packed, uint4* h, uint4* l) {
@@ -627,9 +648,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
         for (int y = 0; y < kTileRows * 8 / kRowThreads; ++y) {
           const int w = threadIdx.x + y * kRowThreads, r = w >> 3, k = w & 7;
           const int from = r * kTileCols + ((k ^ ((r >> 3) & 7)) << 3);
-          const uint32_t to = tile_offset(r, 8 * k) + side * kTileBytes;
-          *reinterpret_cast<uint4*>(hi + to) = *reinterpret_cast<const uint4*>(&turned[0][from]);
-          *reinterpret_cast<uint4*>(lo + to) = *reinterpret_cast<const uint4*>(&turned[1][from]);
+          char* to = hi(side) + tile_offset(r, 8 * k);
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&turned[0][from]);
+          *reinterpret_cast<uint4*>(lo(to)) = *reinterpret_cast<const uint4*>(&turned[1][from]);
         }
         __syncthreads();
       }
@@ -659,9 +680,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
                               tj * kTileCols + piece * 8 < e.n;
           uint4 h, l;
           finish(x[y], packed, &h, &l);
-          const uint32_t to = tile_offset(r, piece % 8 * 8) + piece / 8 * kTileBytes;
-          *reinterpret_cast<uint4*>(hi + to) = h;
-          *reinterpret_cast<uint4*>(lo + to) = l;
+          char* to = hi(piece >> 3) + tile_offset(r, piece % 8 * 8);
+          *reinterpret_cast<uint4*>(to) = h;
+          *reinterpret_cast<uint4*>(lo(to)) = l;
         }
       }
     }
@@ -686,20 +707,23 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) normalise_kernel(List l
 // nobody, so that there is always progress, however many CTAs are resident.
 //
 // One MMA spans a pair, each CTA holding its 128 rows of the left operand and half of the right
-// one, so that a stage is 32 KB for each.  In a CTA one warp copies operands into a ring of
-// stages, one issues the MMAs (in the first CTA) into one of two accumulators, and eight finish
-// the other one, 32 x 32 values at a time: what they read besides (F; X hi and lo) a warp
-// copies ahead of them, into three places for each, where it is written over, and from where
-// another one copies it out and reports the tile.  The second CTA's idle MMA warp fetches
-// the tiles.
+// one.  64 of K take two stages of 32 KB in each: hi of both operands, or F and G as they lie, then
+// lo, or their mirror images, MN-major; of the four products of their parts lo lo is left out, but
+// where a part is hi and lo at once (K in a block of the diagonal).  In a CTA one warp copies
+// operands into a ring of stages, one issues the MMAs (in the first CTA) into one of two
+// accumulators, and eight finish the other one, 32 x 32 values at a time: what they read besides
+// (F; X hi and lo) a warp copies ahead of them, into three places for each, where it is written
+// over, and from where another one copies it out and reports the tile.  The second CTA's idle MMA
+// warp fetches the tiles.
 //
-// What bounds it: with many stages of K a tile, the operands' way from L2, 64 KB a stage and
-// pair (large backbone's list: 930 cycles a stage on 76 pairs, 512 alone); with few, the
-// epilogues and X's traffic; with few tiles, the chain of phases.
+// What bounds it: with many stages of K a tile, the tensor cores' three products and the
+// operands' way from L2, 128 KB for 64 of K and a pair; with few, the epilogues and X's traffic;
+// with few tiles, the chain of phases.
 // ---------------------------------------------------------------------------
 enum Phase { kGram, kSquare, kApply, kLast };
 
-constexpr int kStages = 4;                // large list: 3 7.36 ms, 4 6.94, 5 (two places) 6.95
+constexpr int kStages = 4;                // 5 (two places): large list 12.8 ms instead of 13.1,
+                                          // four large matrices 1.00 instead of 0.99
 constexpr int kBlock = 128;               // rows of a CTA's part of an output tile
 constexpr int kWide = 256;                // columns of one
 constexpr int kK = 64;                    // of a stage
@@ -709,15 +733,15 @@ constexpr int kHalfTile = kTileBytes / 2; // 64 rows
 constexpr int kPlaces = 3;
 constexpr int kPiece = 32 * 32;           // values that a warp finishes at once
 constexpr int kRing = 4;                  // tiles fetched ahead (384-wide blocks' list, four large
-                                          // matrices: 2 552 and 407 us, 3 508 and 403, 4 499 and
-                                          // 418, 6 508 and 426)
+                                          // matrices: 2 782 and 919 us, 3 758 and 975, 4 769 and
+                                          // 991, 6 789 and 975)
 constexpr int kTileArrivals = 2;           // at a matrix' counter: one a CTA
 constexpr uint16_t kPairMask = 0x3;
 
 // A tile as the roles of a pair receive it, with its matrix' entry: waiting for other CTAs
 // empties the L1 cache, and every look at the list would go to L2.
 struct Task {
-  int matrix, i, j, width, phase, from, need, pad;
+  int matrix, i, j, width, phase, turn, need, half;
   Entry e;
 };
 constexpr int kTaskWords = sizeof(Task) / 4;
@@ -741,9 +765,10 @@ struct Maps {
   CUtensorMap tile, half, column, piece;
 };
 
-__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
-  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | (static_cast<uint32_t>(n >> 3) << 17) |
-         (static_cast<uint32_t>(m >> 4) << 24);
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major,
+                                                 bool a_mn_major = false) {
+  return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
+         (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
 // 16-byte part `p` of lane's row of a piece (rows of 64 bytes, as a copy swizzles them).
@@ -776,12 +801,6 @@ __device__ __forceinline__ unsigned load_relaxed(const unsigned* p) {
 // Wait until at most one bulk group of this thread has not completed.
 __device__ __forceinline__ void bulk_wait_group1() {
   asm volatile("cp.async.bulk.wait_group 1;" ::: "memory");
-}
-// A tile to L2.
-__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x),
-               "r"(y)
-               : "memory");
 }
 // Waits until `need` arrivals were counted; the limit runs anew with each that comes.
 __device__ __forceinline__ bool wait_done(const unsigned* done, unsigned need, volatile int* abort,
@@ -829,6 +848,10 @@ __device__ __forceinline__ void prefetch_weights(const Entry& e, int block, int 
 __device__ __forceinline__ int pieces_of(const Task& t, int block) {
   return block < t.e.mb ? t.width >> 6 : 0;
 }
+// A tile's first column, of A and B or of X.
+__device__ __forceinline__ int first_column(const Task& t) {
+  return t.phase < kApply ? t.j * kBlock : (t.j + t.half * t.e.nb) * kTileCols;
+}
 
 // Two values of a 16-byte part, as a pair of fp32.
 __device__ __forceinline__ uint64_t halves(uint32_t w) {
@@ -842,12 +865,17 @@ __device__ __forceinline__ uint32_t to_halves(uint64_t v) {
 }
 __device__ __forceinline__ uint64_t twice(float v) { return f2_pack(v, v); }
 
-// The mirror image of a row's 16-byte part: eight values of a column.
-__device__ __forceinline__ void mirror(uint16_t* piece, int first, int lane, uint4 q) {
-  const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    *value_in(piece, first + i, lane) = static_cast<uint16_t>(words[i >> 1] >> (16 * (i & 1)));
+__device__ __forceinline__ float half_value(uint16_t w) {
+  return __half2float(__ushort_as_half(w));
+}
+__device__ __forceinline__ uint16_t half_bits(float v) {
+  return __half_as_ushort(__float2half_rn(v));
+}
+// Where a 32 x 32 piece of F or G lies: above the diagonal, on it, or below, where it is made of
+// its mirror image.
+enum Place { kAbove, kOn, kBelow };
+__device__ __forceinline__ Place place_of(int row0, int col) {
+  return col > row0 ? kAbove : (col == row0 ? kOn : kBelow);
 }
 
 // One value a lane in each of `some` rows: keep times the weight at p (none: 0) plus value(row),
@@ -901,7 +929,7 @@ __device__ __forceinline__ void finish_ragged(void* param, int param_type, __nv_
 // 32 x 32 new values of X (scaled; a row a lane) to where the caller wants them, lanes along
 // what is contiguous there: four values each, where sizes and alignment allow, after they have
 // changed places in shared memory, 16 rows in `low`, 16 in `high`.  kRagged: they may not allow it
-// (a kernel of its own: with both ways in one the other spills, 540 us become 586).
+// (a kernel of its own: with both ways in one the other spills).
 template <bool kRagged, int kAtOnce = 16>
 __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int row0, int col0,
                                             int lane, float (&x)[32], uint16_t* low,
@@ -960,58 +988,70 @@ __device__ __forceinline__ void finish_last(const Entry& e, const Args& a, int r
 
 // What finishes 32 x 32 values of an accumulator, v, whose other inputs lie in `one`, `two`
 // and, the diagonal over its columns, `dj`.  `reload` brings the next values to v, as soon as
-// these have been used.
+// these have been used.  Of F and G, `one` is hi, `two` the mirror image of lo; on the diagonal
+// `one` is both, hi above it and lo below.
 template <Phase kPhase, bool kRagged, typename F>
 __device__ __forceinline__ void finish_piece(const Entry& e, const Args& a, int row0, int col,
-                                             bool mirrored, int lane, float own, const float* dj,
+                                             int lane, float own, const float* dj,
                                              const uint32_t (&v)[32], uint16_t* one,
                                              uint16_t* two, F reload) {
   const int row = row0 + lane;
   if constexpr (kPhase == kGram || kPhase == kSquare) {
-    const bool diagonal = col == row0;    // pieces hold it or nothing of it
-    const uint64_t base = twice(fmaf(kC, own, kB) * (1.f / kFScale));
-    uint32_t words[16];
+    const Place place = place_of(row0, col);
+    constexpr float kFactor =
+        kPhase == kGram ? kFScale / (kXScale * kXScale) : kC / (kFScale * kFScale);
+    // c F F + (b + c (d_i + d_j)) f
+    const float base = fmaf(kC, own, kB) * (1.f / kFScale);
+    if (place == kAbove) {
+      uint32_t high[16], low[16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint4 f = kPhase == kSquare ? *piece_at(one, lane, k) : make_uint4(0, 0, 0, 0);
-      const uint32_t old[4] = {f.x, f.y, f.z, f.w};
+      for (int k = 0; k < 4; ++k) {
+        const uint4 f = kPhase == kSquare ? *piece_at(one, lane, k) : make_uint4(0, 0, 0, 0);
+        const uint32_t fs[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 8 * k + 2 * i;
-        const uint64_t acc = f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-        uint64_t x;
-        float d0, d1;
-        if (kPhase == kGram) {
-          x = f2_mul(acc, twice(kFScale / (kXScale * kXScale)));
-          if (diagonal) {
-            f2_unpack(x, d0, d1);
-            if (lane == c || lane == c + 1) e.d[row] = (lane == c ? d0 : d1) * (1.f / kFScale);
+        for (int i = 0; i < 4; ++i) {
+          const int c = 8 * k + 2 * i;
+          uint64_t x = f2_mul(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])),
+                              twice(kFactor));
+          if (kPhase == kSquare) {
+            const uint64_t rest = f2_pack(half_value(*value_in(two, c, lane)),
+                                          half_value(*value_in(two, c + 1, lane)));
+            const float2 d = *reinterpret_cast<const float2*>(dj + c);
+            x = f2_fma(f2_add(halves(fs[i]), rest),
+                       f2_fma(f2_pack(d.x, d.y), twice(kC / kFScale), twice(base)), x);
           }
-        } else {
-          // c F F + (b + c (d_i + d_j)) f
-          x = f2_mul(acc, twice(kC / (kFScale * kFScale)));
-          if (diagonal) {
-            f2_unpack(x, d0, d1);
-            if (lane == c || lane == c + 1)
-              e.e[row] = fmaf(fmaf(kC, own, kB), own, lane == c ? d0 : d1);
-          }
-          const float2 d = *reinterpret_cast<const float2*>(dj + c);
-          x = f2_fma(halves(old[i]), f2_fma(f2_pack(d.x, d.y), twice(kC / kFScale), base), x);
+          high[4 * k + i] = to_halves(x);
+          low[4 * k + i] = to_halves(f2_fma(halves(high[4 * k + i]), twice(-1.f), x));
         }
-        if (diagonal) {
-          f2_unpack(x, d0, d1);
-          x = f2_pack(lane == c ? 0.f : d0, lane == c + 1 ? 0.f : d1);
-        }
-        words[4 * k + i] = to_halves(x);
       }
-    }
-    reload();
+      reload();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint4 h = make_uint4(words[4 * k], words[4 * k + 1], words[4 * k + 2],
-                                 words[4 * k + 3]);
-      *piece_at(one, lane, k) = h;
-      if (mirrored) mirror(two, 8 * k, lane, h);
+      for (int k = 0; k < 4; ++k)
+        *piece_at(one, lane, k) = make_uint4(high[4 * k], high[4 * k + 1], high[4 * k + 2],
+                                             high[4 * k + 3]);
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        *value_in(two, c, lane) = static_cast<uint16_t>(low[c >> 1] >> (16 * (c & 1)));
+    } else if (place == kOn) {
+      // a lane reads and writes its own row's values behind the diagonal and their mirror images
+#pragma unroll
+      for (int c = 0; c < 32; ++c) {
+        float x = __uint_as_float(v[c]) * kFactor;
+        if (c == lane) {
+          if (kPhase == kGram) e.d[row] = x * (1.f / kFScale);
+          else e.e[row] = fmaf(fmaf(kC, own, kB), own, x);
+          *value_in(one, lane, lane) = 0;
+        } else if (c > lane) {
+          uint16_t *high = value_in(one, lane, c), *low = value_in(one, c, lane);
+          if (kPhase == kSquare)
+            x = fmaf(half_value(*high) + half_value(*low), fmaf(dj[c], kC / kFScale, base), x);
+          *high = half_bits(x);
+          *low = half_bits(x - half_value(*high));
+        }
+      }
+      reload();
+    } else {
+      reload();
     }
   } else {
     float x[kPhase == kLast ? 32 : 1];
@@ -1115,57 +1155,80 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Entry& e = t.e;
         if (!known && !wait_done(e.done, t.need, abort, list.header)) break;
         known = false;
-        const bool gram = t.phase == kGram, sym = gram || t.phase == kSquare;
-        const int count = stages_of(e, t), row_tiles = gram ? 2 * e.nb : 2 * e.mb;
-        const int64_t left = gram ? e.x[t.from] : (sym ? e.f : e.g);
-        const bool wide = t.width == kWide;
-        const int nb = e.nb;
-        const int32_t ya = static_cast<int32_t>(
-            (left + static_cast<int64_t>(2 * t.i + rank) * row_tiles) * kTileRows);
-        // symmetric: rows of the left operand, 128 or 64 for each CTA; else 64 rows of X, two
-        // column tiles or one for each CTA
-        int32_t yb;
-        if (sym)
-          yb = static_cast<int32_t>(
-                   (left + static_cast<int64_t>(t.j + (wide ? rank : 0)) * row_tiles) * kTileRows) +
-               (wide ? 0 : rank * 64);
-        else
-          yb = static_cast<int32_t>((e.x[t.from] + 2 * t.j + (wide ? 2 * rank : rank)) * kTileRows);
-        for (int k = 0; k < count; ++k, ++it) {
-          const int st = it % kStages;
-          // a look at the next task while the stages are full anyway
-          if (k == count - 1 && k >= kStages &&
-              mbar_test(&s.task_full[(n + 1) % kRing], ((n + 1) / kRing) & 1)) {
-            const Task* next = task(n + 1);
-            if (next != nullptr &&
-                load_acquire(next->e.done) >= static_cast<unsigned>(next->need)) {
-              fence_proxy_async_all();
-              known = true;
+        const bool gram = t.phase == kGram, apply = t.phase >= kApply;
+        const int count = stages_of(e, t), mb = e.mb, nb = e.nb, block = 2 * t.i + rank;
+        const bool wide = t.width > 128;
+        const int64_t fg = apply ? e.g : e.f;
+        // columns of tiles of the right operand that this CTA holds (MN-major); those past a
+        // tile's end are the last one's again, and not looked at
+        const int first = t.j + (wide ? 2 * rank : rank), last = t.j + (t.width >> 6) - 1;
+        const int c0 = min(first, last), c1 = min(first + 1, last);
+        // two stages for 64 of K: hi of X, or F and G as they lie, then lo of X, or their mirror
+        // image
+        for (int k = 0; ok && k < count; ++k)
+          for (int part = 0; part < 2; ++part, ++it) {
+            const int st = it % kStages;
+            // a look at the next task while the stages are full anyway
+            if (part == 1 && k == count - 1 && 2 * k >= kStages &&
+                mbar_test(&s.task_full[(n + 1) % kRing], ((n + 1) / kRing) & 1)) {
+              const Task* next = task(n + 1);
+              if (next != nullptr &&
+                  load_acquire(next->e.done) >= static_cast<unsigned>(next->need)) {
+                fence_proxy_async_all();
+                known = true;
+              }
+            }
+            if (!mbar_wait(&s.empty[st], ((it / kStages) & 1) ^ 1, abort)) {
+              ok = false;
+              break;
+            }
+#ifdef DORA_TEST_WITHHOLD_TILE_LOAD
+            // timeout-path test library only: the first pair never loads its first stage nor
+            // expects its bytes, so that the wait for it runs out with no copy of it in flight
+            if (blockIdx.x < 2 && it == 0) continue;
+#endif
+            // the bytes of both CTAs are counted on the first one's barrier
+            if (rank == 0)
+              mbar_arrive_expect_tx(&s.full[st],
+                                    2 * (kTileBytes + (wide ? kTileBytes : kHalfTile)));
+            const auto load = [&](const CUtensorMap* map, void* to, int64_t tile, int row) {
+              tma_load_2d_pair(to, map, &s.full[st], 0, 0,
+                               static_cast<int32_t>(tile * kTileRows) + row);
+            };
+            uint8_t *sa = s.a[st], *sb = s.b[st];
+            const int kb = k >> 1, kr = (k & 1) * 64;   // block row of 64 of K, and row in it
+            if (gram) {
+              load(&maps.tile, sa, x_tile(e, t.turn, block, k, part), 0);
+              if (wide) load(&maps.tile, sb, x_tile(e, t.turn, t.j + rank, k, part), 0);
+              else load(&maps.half, sb, x_tile(e, t.turn, t.j, k, part), 64 * rank);
+              continue;
+            }
+            const auto straight = [&](int row) {          // 64 columns of a block row
+              return fg + static_cast<int64_t>(row) * (2 * mb) + k;
+            };
+            const auto turned = [&](int col) {            // 64 rows of a column of tiles
+              return fg + static_cast<int64_t>(kb) * (2 * mb) + col;
+            };
+            if (part == 0) {
+              load(&maps.tile, sa, straight(block), 0);
+            } else {
+              load(&maps.half, sa, turned(2 * block), kr);
+              load(&maps.half, sa + kHalfTile, turned(2 * block + 1), kr);
+            }
+            if (apply) {
+              const int64_t x = slot_tile(e, t.turn, t.half) + part * (e.slot / 2) +
+                                static_cast<int64_t>(kb) * nb;
+              load(&maps.half, sb, x + c0, kr);
+              if (wide) load(&maps.half, sb + kHalfTile, x + c1, kr);
+            } else if (part == 0) {
+              if (wide) load(&maps.tile, sb, straight(t.j + rank), 0);
+              else load(&maps.half, sb, straight(t.j), 64 * rank);
+            } else {
+              const int c = 2 * t.j + (wide ? 2 * rank : rank);
+              load(&maps.half, sb, turned(c), kr);
+              if (wide) load(&maps.half, sb + kHalfTile, turned(c + 1), kr);
             }
           }
-          if (!mbar_wait(&s.empty[st], ((it / kStages) & 1) ^ 1, abort)) {
-            ok = false;
-            break;
-          }
-#ifdef DORA_TEST_WITHHOLD_TILE_LOAD
-          // timeout-path test library only: the first pair never loads its first stage nor
-          // expects its bytes, so that the wait for it runs out with no copy of it in flight
-          if (blockIdx.x < 2 && it == 0) continue;
-#endif
-          // the bytes of both CTAs are counted on the first one's barrier
-          if (rank == 0)
-            mbar_arrive_expect_tx(&s.full[st], 2 * (kTileBytes + (wide ? kTileBytes : kHalfTile)));
-          tma_load_2d_pair(s.a[st], &maps.tile, &s.full[st], 0, 0, ya + k * kTileRows);
-          if (sym) {
-            tma_load_2d_pair(s.b[st], wide ? &maps.tile : &maps.half, &s.full[st], 0, 0,
-                             yb + k * kTileRows);
-          } else {
-            const int32_t y = yb + (k >> 1) * 2 * nb * kTileRows + (k & 1) * 64;
-            tma_load_2d_pair(s.b[st], &maps.half, &s.full[st], 0, 0, y);
-            if (wide)
-              tma_load_2d_pair(s.b[st] + kHalfTile, &maps.half, &s.full[st], 0, 0, y + kTileRows);
-          }
-        }
         task_done(n);
       }
       s.issued = it;
@@ -1176,29 +1239,57 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       const Task* at;
       for (int n = 0; ok && (at = task(n)) != nullptr; ++n) {
-        const int count = stages_of(at->e, *at);
-        const bool sym = at->phase == kGram || at->phase == kSquare;
-        const uint32_t idesc = idesc_f16(2 * kBlock, at->width, !sym);
+        const int count = stages_of(at->e, *at), phase = at->phase;
+        const int i = at->i, j = at->j, wide = at->width > 128 ? 1 : 0;
         task_done(n);
-        // 16 of K further on: 32 bytes of a row, or 16 rows
-        const uint64_t step = sym ? 2 : 128;
+        const bool gram = phase == kGram, apply = phase >= kApply;
         const int acc = n & 1;
         if (!mbar_wait(&s.acc_empty[acc], ((n >> 1) & 1) ^ 1, abort)) break;
         tc_fence_after();
         const uint32_t d = tmem + static_cast<uint32_t>(acc * kWide);
-        for (int k = 0; k < count; ++k, ++it) {
+        uint32_t more = 0;                // 0: the tile's first MMA, which adds to nothing
+        // Part p of the left operand times part q of the right one: K-major, but F and G's mirror
+        // images and the right operand of G X are MN-major.
+        const auto product = [&](int p, int q, int st) {
+          const bool a_mn = !gram && p == 1, b_mn = apply || (!gram && q == 1);
+          const int sa = p == 0 ? st : (st + 1) % kStages, sb = q == 0 ? st : (st + 1) % kStages;
+          const uint64_t ad = sdesc_sw128(smem_u32(s.a[sa]), a_mn ? kHalfTile : 16, 1024);
+          const uint64_t bd = sdesc_sw128(smem_u32(s.b[sb]), b_mn ? kHalfTile : 16, 1024);
+          // 16 of K further on: 32 bytes of a row, or 16 rows
+          const uint64_t step_a = a_mn ? 128 : 2, step_b = b_mn ? 128 : 2;
+          const uint32_t idesc = idesc_f16(2 * kBlock, wide ? 256 : 128, b_mn, a_mn);
+#pragma unroll
+          for (int c = 0; c < kK / 16; ++c) {
+            mma_bf16_ss_pair(d, ad + step_a * c, bd + step_b * c, idesc, more);
+            more = 1;
+          }
+        };
+        for (int k = 0; k < count; ++k, it += 2) {
+          // which parts are lo: their product is left out.  F and G's first part is hi behind the
+          // diagonal's blocks, lo before them, and both in them.
+          const int kb = k >> 1;
+          const int low_a = gram ? 1 : (kb >> 1 < i ? 0 : (kb >> 1 > i ? 1 : 2));
+          const int low_b = gram || apply ? 1 : (kb < j ? 0 : (kb > j + wide ? 1 : 2));
+          const auto wanted = [&](int p, int q) { return p != low_a || q != low_b; };
           const int st = it % kStages;
           if (!mbar_wait(&s.full[st], (it / kStages) & 1, abort)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint64_t ad = sdesc_sw128(smem_u32(s.a[st]), 16, 1024);
-          const uint64_t bd = sdesc_sw128(smem_u32(s.b[st]), sym ? 16 : kHalfTile, 1024);
-#pragma unroll
-          for (int q = 0; q < kK / 16; ++q)
-            mma_bf16_ss_pair(d, ad + 2 * q, bd + step * q, idesc, (k | q) != 0 ? 1u : 0u);
+          if (wanted(0, 0)) product(0, 0, st);
+          const int st1 = (it + 1) % kStages;
+          if (!mbar_wait(&s.full[st1], ((it + 1) / kStages) & 1, abort)) {
+            ++it;
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (wanted(1, 0)) product(1, 0, st);
+          if (wanted(0, 1)) product(0, 1, st);
+          if (wanted(1, 1)) product(1, 1, st);
           mma_commit_pair(&s.empty[st], kPairMask);
+          mma_commit_pair(&s.empty[st1], kPairMask);
         }
         if (ok) mma_commit_pair(&s.acc_full[acc], kPairMask);
       }
@@ -1221,19 +1312,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) w = atomicAdd(&list.header->ticket, 1u);
         w = __shfl_sync(0xffffffffu, w, 0);
         Tile x = {-1, 0, 0, 0};
-        int phase = 0, step = 0;
+        int phase = 0, step = 0, half = 0;
         unsigned before = 0;
         for (; g < n_groups; ++g) {
           const Group q = list.groups[g];
-          const unsigned sym = q.sym1 - q.sym0, all = q.all1 - q.all0, each = 2 * sym + all;
+          const unsigned sym = q.sym1 - q.sym0, all = q.all1 - q.all0, each = 2 * (sym + all);
           if (w - base >= each * steps) {
             base += each * steps;
             continue;
           }
           step = static_cast<int>((w - base) / each);
           const unsigned r = (w - base) % each;
+          half = r >= 2 * sym + all;
           x = r < 2 * sym ? list.sym[q.sym0 + (r < sym ? r : r - sym)]
-                          : list.all[q.all0 + (r - 2 * sym)];
+                          : list.all[q.all0 + (r - 2 * sym - (half ? all : 0))];
           phase = r < sym ? kGram : (r < 2 * sym ? kSquare : (step + 1 < steps ? kApply : kLast));
           break;
         }
@@ -1241,10 +1333,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         x.matrix = __shfl_sync(0xffffffffu, x.matrix, 0);
         // the entry by words, a few a lane
         const Entry* e = list.entries + (x.matrix < 0 ? 0 : x.matrix);
+        // the right half is written over the left one, where it is written
         before = phase == kGram ? 0u : (phase == kSquare ? e->n_sym : 2u * e->n_sym);
+        if (phase == kApply && half) before += e->n_all;
         const int need =
-            static_cast<int>(kTileArrivals * (step * (2u * e->n_sym + e->n_all) + before));
-        const int head[8] = {x.matrix, x.i, x.j, x.width, phase, step & 1, need, 0};
+            static_cast<int>(kTileArrivals * (2u * step * (e->n_sym + e->n_all) + before));
+        const int head[8] = {x.matrix, x.i, x.j, x.width, phase, step % 3, need, half};
         int* to = reinterpret_cast<int*>(&s.task[i]);
         for (int cta = 0; cta < 2; ++cta) {
           if (lane == 0)
@@ -1269,17 +1363,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!__all_sync(0xffffffffu, at != nullptr)) break;
       const Entry& e = at->e;
       const int phase = at->phase, half = at->width >> 1;
-      const int first_col = at->j * kBlock, block = 2 * at->i + rank;
-      const int pieces = pieces_of(*at, block);
-      const int64_t one = (phase == kSquare ? e.f : e.x[at->from]) +
-                          static_cast<int64_t>(block) * 2 * (phase == kSquare ? e.mb : e.nb);
-      const int64_t two = e.lo + static_cast<int64_t>(block) * 2 * e.nb;
+      const int block = 2 * at->i + rank, pieces = pieces_of(*at, block);
+      const int first_col = first_column(*at);
+      const int64_t x = slot_tile(e, at->turn, at->half) +
+                        static_cast<int64_t>(block) * e.nb - at->half * e.nb;
       bool there = true;
-      // what has not been read for an iteration; it may still be written, by copies through L2
-      // (72 matrices of 384 x 384 to 1536 x 384: 504 us, without 511)
-      if (phase >= kApply && lane < pieces)
-        tma_prefetch_2d(&maps.tile, 0, static_cast<int32_t>(
-            (two + (first_col >> 6) + lane) * kTileRows));
       if (lane == 0) there = wait_done(e.done, at->need, abort, list.header);
       if (!__all_sync(0xffffffffu, there)) break;
       if (phase == kLast && e.param != nullptr)
@@ -1289,19 +1377,29 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; ok && h < 2; ++h) {
           ok = mbar_wait_warp(&s.piece_empty[h][i], ((loads / kPlaces) & 1) ^ 1, abort);
           if (!ok || !elect_one()) continue;
-          const int col = first_col + h * half + 32 * c;
+          const int col = first_col + h * half + 32 * c, block_col = col >> 7;
           uint64_t* bar = &s.piece_full[h][i];
-          if (phase == kGram) {           // nothing to read: the place is free
+          // nothing to read: the place is free
+          if (phase == kGram || (phase == kSquare && block_col < block)) {
             mbar_arrive(bar);
             continue;
           }
-          mbar_arrive_expect_tx(bar, phase == kSquare ? 4 * kPiece * 2 + 128 : 8 * kPiece * 2);
-          if (phase == kSquare) bulk_load(s.dj[i][h], e.d + col, 128, bar);
-          tma_load_2d(s.piece[i][0][h], &maps.column, bar, col & 32,
-                      static_cast<int32_t>((one + (col >> 6)) * kTileRows));
-          if (phase != kSquare)
-            tma_load_2d(s.piece[i][1][h], &maps.column, bar, col & 32,
-                        static_cast<int32_t>((two + (col >> 6)) * kTileRows));
+          mbar_arrive_expect_tx(bar, 8 * kPiece * 2 + (phase == kSquare ? 128 : 0));
+          if (phase == kSquare) {
+            const int64_t f = e.f + static_cast<int64_t>(block) * (2 * e.mb) + (col >> 6);
+            bulk_load(s.dj[i][h], e.d + col, 128, bar);
+            tma_load_2d(s.piece[i][0][h], &maps.column, bar, col & 32,
+                        static_cast<int32_t>(f * kTileRows));
+            const int64_t image = e.f + static_cast<int64_t>(block_col) * (2 * e.mb) + 2 * block;
+            for (int w = 0; w < 4; ++w)
+              tma_load_2d(s.piece[i][1][h][w], &maps.piece, bar, (w & 1) * 32,
+                          static_cast<int32_t>((image + (w >> 1)) * kTileRows + (col & 127)));
+          } else {
+            for (int part = 0; part < 2; ++part)
+              tma_load_2d(s.piece[i][part][h], &maps.column, bar, col & 32,
+                          static_cast<int32_t>((x + part * (e.slot / 2) + (col >> 6)) *
+                                               kTileRows));
+          }
         }
         __syncwarp();
       }
@@ -1334,7 +1432,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (at == nullptr) break;
         const Entry& e = at->e;
         const int phase = at->phase, half = at->width >> 1;
-        const int first_col = at->j * kBlock, block = 2 * at->i + rank, mb = e.mb;
+        const int block = 2 * at->i + rank, first_col = first_column(*at);
         const int pieces = pieces_of(*at, block);
         if (pieces == 0) {
           // Nothing to copy, but no report before the matrix' phase has begun: it would be
@@ -1342,11 +1440,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (unsaid != nullptr) report(true);
           if (!wait_done(e.done, at->need, abort, list.header)) break;
         }
-        const int row_tiles = phase == kApply ? 2 * e.nb : 2 * mb;
-        const int64_t to = phase == kGram ? e.f : (phase == kSquare ? e.g : e.x[at->from ^ 1]);
-        const int64_t one = to + static_cast<int64_t>(block) * row_tiles;
-        const int64_t two = e.lo + static_cast<int64_t>(block) * row_tiles;
-        const bool mirrored = phase < kApply && at->j >= 2 * at->i + 2;
+        const int row_tiles = 2 * e.mb;
+        const int64_t to = phase == kGram ? e.f : e.g;
+        // X as it lies an iteration later
+        const int64_t x = slot_tile(e, at->turn == 2 ? 0 : at->turn + 1, at->half) +
+                          static_cast<int64_t>(block) * e.nb - at->half * e.nb;
         for (int c = 0; ok && c < pieces; ++c, ++done) {
           const int i = done % kPlaces;
           for (int h = 0; h < 2; ++h) {
@@ -1354,19 +1452,29 @@ __global__ void __launch_bounds__(kThreads, 1)
               report(true);
             ok = mbar_wait(&s.piece_done[h][i], (done / kPlaces) & 1, abort);
             if (!ok) break;
-            const int col = first_col + h * half + 32 * c;
-            if (phase != kLast)
-              tma_store_2d(&maps.column, s.piece[i][0][h], col & 32,
-                           static_cast<int32_t>((one + (col >> 6)) * kTileRows));
-            if (phase == kApply)
-              tma_store_2d(&maps.column, s.piece[i][1][h], col & 32,
-                           static_cast<int32_t>((two + (col >> 6)) * kTileRows));
-            if (mirrored)
-              for (int w = 0; w < 4; ++w)   // 32 columns of the mirror image each
+            const int col = first_col + h * half + 32 * c, block_col = col >> 7;
+            if (phase == kApply) {
+              for (int part = 0; part < 2; ++part)
+                tma_store_2d(&maps.column, s.piece[i][part][h], col & 32,
+                             static_cast<int32_t>((x + part * (e.slot / 2) + (col >> 6)) *
+                                                  kTileRows));
+            } else if (phase < kApply && block_col >= block) {
+              // hi, four warps' rows at once but in the diagonal's blocks, and 32 columns of the
+              // mirror image of lo each
+              const int64_t tile = to + static_cast<int64_t>(block) * row_tiles + (col >> 6);
+              const int64_t image = to + static_cast<int64_t>(block_col) * row_tiles + 2 * block;
+              const int above = block_col > block ? 4 : (col & 127) >> 5;
+              if (above == 4)
+                tma_store_2d(&maps.column, s.piece[i][0][h], col & 32,
+                             static_cast<int32_t>(tile * kTileRows));
+              else
+                for (int w = 0; w <= above; ++w)
+                  tma_store_2d(&maps.piece, s.piece[i][0][h][w], col & 32,
+                               static_cast<int32_t>(tile * kTileRows + 32 * w));
+              for (int w = 0; w < above; ++w)
                 tma_store_2d(&maps.piece, s.piece[i][1][h][w], (w & 1) * 32,
-                             static_cast<int32_t>(
-                                 (to + static_cast<int64_t>(col >> 7) * row_tiles + 2 * block +
-                                  (w >> 1)) * kTileRows + (col & 127)));
+                             static_cast<int32_t>((image + (w >> 1)) * kTileRows + (col & 127)));
+            }
             bulk_commit_group();          // also without any: one for every place
             bulk_wait_group_read1();
             if (place != nullptr) mbar_arrive(place);
@@ -1394,8 +1502,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Entry& e = t.e;
       const int phase = t.phase, pieces = pieces_of(t, 2 * t.i + rank);
       const int row0 = (2 * t.i + rank) * kBlock + q * 32;
-      const int col0 = t.j * kBlock + half * (t.width >> 1);
-      const bool mirrored = t.j >= 2 * t.i + 2;
+      const int col0 = first_column(t) + half * (t.width >> 1);
       if (!mbar_wait_warp(&s.acc_full[acc], (n >> 1) & 1, abort)) break;
       tc_fence_after();
       const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + acc * kWide +
@@ -1431,17 +1538,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         if (phase == kGram)
-          finish_piece<kGram, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
-                                       reload);
+          finish_piece<kGram, kRagged>(e, a, row0, col, lane, own, dj, v, one, two, reload);
         else if (phase == kSquare)
-          finish_piece<kSquare, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
-                                         reload);
+          finish_piece<kSquare, kRagged>(e, a, row0, col, lane, own, dj, v, one, two, reload);
         else if (phase == kApply)
-          finish_piece<kApply, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
-                                        reload);
+          finish_piece<kApply, kRagged>(e, a, row0, col, lane, own, dj, v, one, two, reload);
         else
-          finish_piece<kLast, kRagged>(e, a, row0, col, mirrored, lane, own, dj, v, one, two,
-                                       reload);
+          finish_piece<kLast, kRagged>(e, a, row0, col, lane, own, dj, v, one, two, reload);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.piece_done[half][place]);
@@ -1483,10 +1586,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // sends every one its rows of F.  What bounds it is the chain of three products an iteration,
 // each with its reading of tensor memory; the first pass and the last take as long as one or two.
 //
-// X, F and G are hi + lo, 22 bits, and every product adds hi hi, hi lo and lo hi.  With 11 bits of
-// F and G, and of X in G X, the actor's twelve matrices took 67 us instead of 85 (a step 70
-// instead of 88), but a matrix of few directions came out wrong by up to 3e-2 (64 x 512 of two rows
-// that are not zero, nearly along one direction), with 22 bits by 2e-5.
+// All operands are hi + lo here too.  The actor's twelve matrices take 85 us (a step 88).
 //
 // In a list of both kinds it runs beside the products, on the SMs that they leave (`beside`): it
 // needs nothing of theirs, and they start it when all work before the call is complete.  One CTA
@@ -2005,15 +2105,16 @@ Shape shape_of(const dora_matrix& t) {
   s.x_tiles = pairs * 2 * 2 * s.nb;
   s.f_tiles = pairs * 2 * 2 * s.mb;
   s.diag = pairs * 2;
-  // of 256 columns, and of 128
+  // of 256 columns, and of 128; of X in each of its halves
   s.sym[0] = pairs * (pairs + 1) / 2;
-  s.all[0] = pairs * ((s.nb + 1) / 2);
+  s.all[0] = pairs * ((s.nb + 3) / 4);
   s.sym[1] = pairs * s.mb - pairs * (pairs - 1);
-  s.all[1] = pairs * s.nb;
+  s.all[1] = pairs * ((s.nb + 1) / 2);
   return s;
 }
 // A list of fewer wide tiles than pairs of SMs is cut into narrow ones: four matrices of
-// 4096 x 1024 and its transpose 432 us, with wide ones 468.
+// 4096 x 1024 and its transpose 0.99 ms, with wide ones 1.04; lists of more are slower with narrow
+// ones (384-wide blocks 886 us for 769, the large list 16.3 ms for 13.1).
 constexpr int64_t kFewTiles = 76;
 struct Sizes {
   int64_t chunks = 0, x_tiles = 0, sym = 0, all = 0, tiles = 0, diag = 0;
@@ -2160,7 +2261,7 @@ int launch_products(const ortho::Maps& maps, const ortho::List& l, const ortho::
   const auto kern = ragged ? ortho::product_kernel<true> : ortho::product_kernel<false>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return launched(e);
-  const int tiles = l.n_sym > l.n_all ? l.n_sym : l.n_all, pairs = num_sms() / 2;
+  const int tiles = l.n_sym > 2 * l.n_all ? l.n_sym : 2 * l.n_all, pairs = num_sms() / 2;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -2303,9 +2404,8 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.quads = written_in_quads(t);
       e.mb = s.mb;
       e.nb = s.nb;
-      e.x[0] = tile;
-      e.x[1] = tile + s.x_tiles;
-      e.lo = tile + 2 * s.x_tiles;
+      e.x = tile;
+      e.slot = s.x_tiles;
       e.f = tile + 3 * s.x_tiles;
       e.g = e.f + s.f_tiles;
       tile = e.g + s.f_tiles;

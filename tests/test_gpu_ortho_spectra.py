@@ -2,8 +2,8 @@
 lies beside them is raised by 3.4445 an iteration, and so is every error there.
 
 Bounds.  Operands have 22 bits.  An iteration's four roundings (of X as it is kept, of what
-X, F and G go into the products as, the sums' among them) are 2^-22 of X's Frobenius norm at most, and
-grow by 3.4445 at most in each iteration that follows:
+X, F and G go into the products as, the sums' among them) are 2^-22 of X's Frobenius norm at
+most, and grow by 3.4445 at most in each iteration that follows:
   4 2^-22 sum_k 3.4445^(4 - k) |X_k| / |X_5|,
 with the norms of the iteration itself in 64 bits.  The products' sums are cut off, not rounded, at
 each of their 16 values: 3 n 2^-28 of themselves over n of them (half of 2^-23 on average, three
@@ -96,3 +96,62 @@ def test_small_matrices_of_noise(shape):
     _check([x, np.ascontiguousarray(x.T)])
     _check([x], steps=1)
     _check([x], steps=3)
+
+
+# Matrices whose products are cut into tiles: odd and even numbers of blocks each way, few rows of
+# many columns.
+LARGE = [(2, 2049), (4, 4096), (8, 4096), (16, 3000), (129, 129), (130, 1100), (200, 300),
+         (257, 511), (300, 600), (384, 384), (390, 1000), (640, 700)]
+
+
+@pytest.mark.parametrize("shape", LARGE)
+@pytest.mark.parametrize("k,noise", [(1, 1e-2), (1, 1e-3), (3, 1e-4), (8, 1e-3)])
+def test_large_matrices_of_few_directions(shape, k, noise):
+    x = _few_directions(*shape, k, noise, 6)
+    _check([x, np.ascontiguousarray(_few_directions(*shape, k, noise, 7).T)])
+
+
+@pytest.mark.parametrize("shape", LARGE)
+@pytest.mark.parametrize("active,noise", [(1, 0.0), (2, 1.0), (2, 3e-3)])
+def test_large_matrices_of_few_rows_that_are_not_zero(shape, active, noise):
+    x = _few_directions(*shape, 1, noise, 8, active)
+    _check([x, np.ascontiguousarray(_few_directions(*shape, 1, noise, 9, active).T)])
+
+
+@pytest.mark.parametrize("shape", LARGE)
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5])
+def test_large_matrices_of_noise(shape, steps):
+    x = np.random.default_rng(10).standard_normal(shape).astype(np.float32)
+    _check([x, np.ascontiguousarray(x.T)], steps)
+
+
+def test_matrices_of_few_directions_in_a_list():
+    # wide tiles and narrow ones, small matrices beside large ones
+    shapes = [(384, 384), (1536, 384), (384, 1152), (64, 787), (2, 2049), (640, 1024)] * 5
+    _check([_few_directions(*s, 1 + i % 3, 1e-3, 11 + i) for i, s in enumerate(shapes)])
+    _check([_few_directions(1024, 1024, 1, 3e-3, 50)])
+
+
+# The sums over m, of G X, are cut off beside the strong directions too, where the iterations raise
+# what is lost: with larger m more than the term above allows.  The documented bound has m 2^-22
+# for them: 3 m / 16 additions, each short of up to 2^-23 of what there is, at random 2^-24 of it,
+# together sqrt(3 m / 16) of that, grown by up to 3.4445^4 = 141: 61 2^-24 sqrt(m), below m 2^-22
+# from 233 rows on.
+@pytest.mark.parametrize("shape", [(2048, 2048), (1024, 9000)])
+@pytest.mark.parametrize("noise", [1e-2, 1e-3, 1e-4])
+def test_long_sums_hold_the_documented_bound(shape, noise):
+    m, n = shape
+    g = torch.Generator(device=dev()).manual_seed(60)
+    x = torch.randn(m, 1, generator=g, device=dev()) @ torch.randn(1, n, generator=g, device=dev())
+    x += noise * torch.randn(m, n, generator=g, device=dev())
+    a, b, c = O.NS_COEF
+    y = x.double()
+    y /= y.norm()
+    for _ in range(5):
+        gram = y @ y.t()
+        y = a * y + (b * gram + c * gram @ gram) @ y
+    p = torch.zeros_like(x)
+    P.dora_muon_step(P.MatrixList([x], params=[p], momentum=[torch.zeros_like(x)], scales=[1.0]),
+                     1.0, momentum=0.0)
+    torch.cuda.synchronize()
+    assert float((-p.double() - y).norm() / y.norm()) <= 3e-4 + m * 2.0 ** -22 + n * 2.0 ** -26
