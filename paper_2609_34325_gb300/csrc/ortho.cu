@@ -86,7 +86,7 @@ struct Entry {
   void* param;
   float* momentum;
   uint16_t *copy, *out;                   // bf16
-  int32_t rows, cols, grad_type, param_type;
+  int32_t grad_type, param_type;
   float scale;
   int32_t m, n, tall;                     // X is m x n; tall: X = U^T
   int32_t quads;                          // what is written is aligned to four values, row by row
@@ -2393,8 +2393,6 @@ int dora_matrix_list_prepare(const dora_matrix* matrices, int32_t count, void* d
       e.momentum = t.momentum;
       e.copy = t.copy;
       e.out = t.out;
-      e.rows = t.rows;
-      e.cols = t.cols;
       e.grad_type = t.grad_dtype;
       e.param_type = t.param_dtype;
       e.scale = t.scale;

@@ -98,6 +98,18 @@ def test_small_matrices_of_noise(shape):
     _check([x], steps=3)
 
 
+# Columns go to the CTAs of a cluster by 64, an equal share each, rounded up: nine 64s to four CTAs
+# as 3, 3, 3 and 0, eighteen to eight as 3 each to the first six.
+@pytest.mark.parametrize("shape", [(64, 520), (100, 520), (20, 576), (1, 513), (128, 1100),
+                                   (33, 1344), (128, 1025)])
+def test_clusters_whose_last_ctas_have_no_columns(shape):
+    x = np.random.default_rng(12).standard_normal(shape).astype(np.float32)
+    _check([x, np.ascontiguousarray(x.T)] * 3)
+    if shape[0] > 1:
+        x = _few_directions(*shape, 1, 1e-3, 13)
+        _check([x, np.ascontiguousarray(x.T)], steps=4)
+
+
 # Matrices whose products are cut into tiles: odd and even numbers of blocks each way, few rows of
 # many columns.
 LARGE = [(2, 2049), (4, 4096), (8, 4096), (16, 3000), (129, 129), (130, 1100), (200, 300),
