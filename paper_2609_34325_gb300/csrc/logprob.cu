@@ -88,12 +88,17 @@ struct Outputs {
   int32_t* top_tokens;
 };
 
+// (z - m) / T - ln s.  By halves: two finite logits may be further apart than 32 bits hold.
+__device__ __forceinline__ float log_prob(float z, float m, float inv_t, float ls) {
+  return fmaf(0.5f * z - 0.5f * m, 2.f * inv_t, -ls);
+}
+
 // The scalars of a row; returns ln s.
 __device__ __forceinline__ float write_row(const Outputs& o, int row, const Part& x, float za,
                                            bool has_token, float inv_t, bool leader) {
   const float ls = logf(x.s);
   if (leader) {
-    if (o.logp != nullptr) o.logp[row] = has_token ? fmaf(za - x.m, inv_t, -ls) : 0.f;
+    if (o.logp != nullptr) o.logp[row] = has_token ? log_prob(za, x.m, inv_t, ls) : 0.f;
     if (o.entropy != nullptr) o.entropy[row] = fmaf(-x.t / x.s, inv_t, ls);
     if (o.norm != nullptr) {
       const bool fine = isfinite(ls);     // not where all logits are -inf, or one is NaN or +inf
@@ -192,7 +197,7 @@ __device__ __forceinline__ void write_top(const Outputs& o, int64_t at, const ui
     int before = 0;
     for (int c = 0; c < found; ++c) before += keys[c] > key;
     if (before < o.top) {
-      o.top_logp[at + before] = fmaf(value_of(key) - m, inv_t, -ls);
+      o.top_logp[at + before] = log_prob(value_of(key), m, inv_t, ls);
       o.top_tokens[at + before] = index_of(key);
     }
   }

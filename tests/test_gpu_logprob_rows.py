@@ -254,3 +254,20 @@ def test_tokens_outside_their_rows_are_not_valid():
             assert np.isnan(_np(o["logp"])[r]) and np.isnan(_np(o["norm"])[r]).all()
             assert o["top_tokens"][r].tolist() == [-1, -1]
         assert np.isfinite(_np(o["logp"])[[0, 5, 15]]).all()
+
+
+@pytest.mark.parametrize("rows,classes", [(3, 60), (3, 700), (3, 5000), (2, 70000), (1500, 3000)])
+def test_logits_further_apart_than_32_bits_hold(rows, classes):
+    # -3e38 lies 6e38 below 3e38: with temperature 1e10 6e28, of which a float is 2^-22 off at most
+    z = torch.zeros(rows, classes, device=dev())
+    z[:, 0], z[:, 1], z[:, 2] = 3e38, -3e38, float("-inf")
+    for token, want in ((1, 6e28), (3, 3e28)):
+        tokens = torch.full((rows,), token, dtype=I32, device=dev())
+        logp, top_logp = torch.zeros(rows, device=dev()), torch.zeros(rows, 32, device=dev())
+        top_tokens = torch.zeros(rows, 32, dtype=I32, device=dev())
+        P.dora_token_logprob(z, tokens, logp, temperature=1e10, top_logp=top_logp,
+                             top_tokens=top_tokens)
+        torch.cuda.synchronize()
+        assert np.all(np.abs(_np(logp) + want) <= want * 2.0 ** -22)
+        assert bool((top_tokens[:, 0] == 0).all()) and not top_logp[:, 0].any()
+        assert np.all(np.abs(_np(top_logp[:, 1:]) + 3e28) <= 3e28 * 2.0 ** -22)
