@@ -2458,9 +2458,9 @@ int dora_muon_step(const dora_matrix_list* list, double lr, double momentum, int
                    double weight_decay, int32_t steps, const float* clip, int32_t* status,
                    dora_stream_t stream) {
   if (!valid_list(list) || !list->has_params || steps < 1 || steps > ortho::kMaxSteps ||
-      !isfinite(lr) || !(momentum >= 0. && momentum < 1.) || !(weight_decay >= 0.) ||
-      !isfinite(weight_decay))
-    return DORA_ERR_INVALID_ARG;
+      !isfinite(static_cast<float>(lr)) || !(momentum >= 0. && momentum < 1.) ||
+      !(weight_decay >= 0.) || !isfinite(static_cast<float>(1. - lr * weight_decay)))
+    return DORA_ERR_INVALID_ARG;          // the kernels take them in 32 bits
   ortho::Args a = {};
   a.clip = clip;
   a.muon = 1;
