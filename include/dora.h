@@ -963,11 +963,10 @@ int dora_orthogonalize(const dora_matrix_list* list, int32_t steps, int32_t* sta
  *   momentum  m <- mu m + (1 - mu) d
  *   update    u = (1 - mu) d + mu m (nesterov != 0), or m
  *   param     p <- p (1 - lr weight_decay) - lr scale NS(u)
- * NS as in dora_orthogonalize, mu in [0, 1), lr and 1 - lr weight_decay finite in 32 bits.  clip
- * nullable: the norm fp32 [2] of
- * dora_grad_norm; f = clip[1], and a norm that is not finite skips the step (nothing
- * changes).  NULL: f = 1.  A wait that runs out (status) leaves the weights of the
- * matrices concerned as they were, or partly updated, their momentum updated.
+ * NS as in dora_orthogonalize, mu in [0, 1), lr and 1 - lr weight_decay finite in 32 bits.
+ * clip nullable: the norm fp32 [2] of dora_grad_norm; f = clip[1], and a norm that is not
+ * finite skips the step (nothing changes).  NULL: f = 1.  A wait that runs out (status) leaves
+ * the weights of the matrices concerned as they were, or partly updated, their momentum updated.
  */
 int dora_muon_step(const dora_matrix_list* list, double lr, double momentum, int32_t nesterov,
                    double weight_decay, int32_t steps, const float* clip, int32_t* status,

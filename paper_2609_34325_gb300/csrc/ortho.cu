@@ -3,9 +3,9 @@
 //
 // With X the update U (or U^T, so that X is m x n with m <= n) over its Frobenius norm,
 //   A = X X^T,   X <- a X + (b A + c A^2) X
-// brings every singular value near 1 (the quintic of coefficients a, b, c below, whose
-// values stay below 1.21).  Three products an iteration on the tensor cores, the two
-// symmetric ones by half: 3 m^2 n + m^3 operations.
+// brings every singular value near 1 (the quintic that K. Jordan et al. published with Muon, 2024,
+// of coefficients a, b, c below, whose values stay below 1.21).  Three products an iteration on
+// the tensor cores, the two symmetric ones by half: 3 m^2 n + m^3 operations.
 //
 // Precision.  What lies beside the directions that hold most of a matrix is raised by 3.4 an
 // iteration, and every error there with it, up to 140 times in five: products of fp16 operands
@@ -880,7 +880,7 @@ __device__ __forceinline__ Place place_of(int row0, int col) {
 
 // One value a lane in each of `some` rows: keep times the weight at p (none: 0) plus value(row),
 // to p and, rounded, to copy; kAtOnce weights are loaded at a time (a small matrix' 32 rows at
-// once: the actor's step 70.4 -> 68.3 us; the product kernel has no registers for more than 16).
+// once: 2 us of the actor's step less; the product kernel has no registers for more than 16).
 template <int kAtOnce, typename T, typename F>
 __device__ __forceinline__ void write_rows(T* p, __nv_bfloat16* copy, int64_t pitch, int some,
                                            float keep, F value) {
