@@ -462,9 +462,6 @@ __device__ __forceinline__ uint32_t tile_offset(int r, int c) {
 __device__ __forceinline__ char* tile_at(const List& list, int64_t tile) {
   return list.tiles + tile * kTileBytes;
 }
-__device__ __forceinline__ uint32_t pair_of(float a, float b) {
-  return Granule<__half>::pair(a, b);
-}
 // X lies in two halves of nb columns of tiles, each hi, then lo, in two of three slots.  An
 // iteration writes the new left half to the third and the new right one over the old left one, so
 // that `turn` iterations (mod 3) later the left half is in slot -turn, the right one in the next.
